@@ -246,7 +246,7 @@ def _plain_plan(s):
     held, want = (length + page - 1) // page, (length + new + page - 1) // page
     need = torch.where(fits, want - held, torch.zeros_like(held))
     upto = need.cumsum(0)
-    served = fits & (upto <= avail)
+    served = fits & ((upto <= avail) | (need == 0))
     taken = torch.where(upto <= avail, upto, torch.zeros_like(upto)).max()
     given = torch.where(count < 0, held, torch.zeros_like(held))
     given_before = given.cumsum(0) - given
@@ -469,7 +469,7 @@ def _exact_plan(s):
             continue
         need = -(-(n + c) // page) - held
         wanted += need
-        if wanted > avail:
+        if need and wanted > avail:
             out.append(n)
             continue
         for j in range(need):
