@@ -56,7 +56,8 @@ typedef enum relation_status {
   RELATION_ERR_ALIGNMENT = 3,   /* pointer or stride alignment rule broken               */
   RELATION_ERR_WORKSPACE = 4,   /* workspace missing or smaller than the size query      */
   RELATION_ERR_CUDA = 5,        /* a CUDA runtime call failed (launch, attribute, ...)   */
-  RELATION_ERR_TIMEOUT = 6      /* written to *dev_status by a kernel whose wait expired */
+  RELATION_ERR_TIMEOUT = 6,     /* written to *dev_status by a kernel whose wait expired */
+  RELATION_ERR_CAPACITY = 7     /* written to *dev_status: no page or table entry is left  */
 } relation_status;
 
 typedef enum relation_dtype { RELATION_F32 = 0, RELATION_BF16 = 1 } relation_dtype;
@@ -258,6 +259,146 @@ relation_status relation_decode(const void* q, const void* k_cache, const void* 
                                 float tau_s, relation_shape cache, long long q_sB, long long q_sH,
                                 relation_dtype dt, void* workspace, size_t ws_bytes,
                                 int* dev_status, relation_stream_t stream);
+
+/*
+ * Serving from a paged cache.  A request's keys and values lie in pages of `page_size` rows that
+ * need not follow each other: row r of request b is row r % page_size of page
+ * block_table[b][r / page_size].  A step is
+ *   relation_page_plan     the pages, slots and positions of the step's new tokens,
+ *   relation_cache_append  their rows, rotated and mixed, into those slots,
+ *   relation_paged_decode  the Relation row of every request's last token over its pages,
+ *   relation_sample        the next tokens from their logits;
+ * none of them needs a length on the host, so that a step can be captured in a CUDA graph.
+ *
+ * relation_page_plan: from the requests' lengths and counts,
+ *   lengths     device int[B]: rows of request b in the cache before this step.
+ *   counts      device int[B]: its new tokens, >= 0; negative: the request has ended and its
+ *               pages go back to the ring of free pages.
+ *   block_table device int[B][cols], row stride table_stride: entries 0 .. ceil(len / page_size) - 1
+ *               are read; the entries of the new tokens' pages are written, no others.
+ *   free_pages  device int[n_pages]: a ring of page ids; free_state device int[2]: {head, count},
+ *               entries head .. head + count - 1 (modulo n_pages) are free.  New pages are taken
+ *               from the head in the order of the requests; pages that come back in this call are
+ *               written behind the end, in the same order, and can be taken from the next call on.
+ *   free_state_out  device int[2]: the ring's state after the step.
+ *   lengths_out device int[B]: the lengths after it (0 for an ended request).
+ *   starts      device int[B + 1]: exclusive sums of the counts: request b's tokens are
+ *               starts[b] .. starts[b + 1] - 1 of the step (sums past 2^31 - 1 read 2^31 - 1).
+ *   slots       device long long[n_tokens]: page id * page_size + row of every token, and
+ *   positions   device int[n_tokens]: its zero-based position; -1 for the buffer's padding and
+ *               for the tokens of a request that is not served.
+ * A request is not served, and keeps its length, where its rows would exceed the table row
+ * (cols * page_size), its tokens the buffer (n_tokens) or its new pages the free ones; once the
+ * free pages are exceeded no later request gets any in this call.  dev_status (if given) receives
+ * RELATION_ERR_CAPACITY then, and RELATION_ERR_INVALID_ARG for a length outside
+ * [0, cols * page_size] (not served), a state outside the ring (read as empty) or more pages
+ * coming back than were taken (the excess is dropped).
+ * The outputs must not overlap the inputs: free_state_out and lengths_out are buffers of their
+ * own.  cols * page_size and B * cols are at most 2^31 - 1 (else RELATION_ERR_UNSUPPORTED); 4-byte
+ * alignment (slots: 8).  Asynchronous on `stream`; one launch; nothing is allocated.
+ */
+relation_status relation_page_plan(const int* lengths, const int* counts, int B, int page_size,
+                                   int* block_table, int cols, long long table_stride,
+                                   int* free_pages, int n_pages, const int* free_state,
+                                   int* free_state_out, int* lengths_out, int* starts,
+                                   long long* slots, int* positions, int n_tokens,
+                                   int* dev_status, relation_stream_t stream);
+
+/* A paged cache's layout: one for the keys' and the values' pages. */
+typedef struct relation_pages {
+  int n_pages;    /* pages                                                     */
+  int page_size;  /* rows of a page                                            */
+  int H;          /* key/value heads                                           */
+  int d_h;        /* head width                                                */
+  long long sP;   /* element stride between pages                              */
+  long long sR;   /* element stride between the rows of a page                 */
+  long long sH;   /* element stride between heads; d_h is contiguous           */
+} relation_pages;
+
+/*
+ * relation_cache_append: the layer's transforms of N new tokens at their own positions, their
+ * keys and values written into a paged cache (relation_layer_prep with positions and slots):
+ *   q[t] = RoPE(p1[t]),  K[slot_t] = RoPE(p2[t]),  V[slot_t] = Givens(info[t]),
+ * with channel pair (2c, 2c + 1) of a token at position m turned by m * rope_base^(-2c/d_h) and the
+ * head pairs of `pairing` mixed by theta, both as in relation_layer_prep.
+ *   p1, p2, info : [N][H][d_h] in dt, element strides sT, sH; q has the same layout and may
+ *                  alias p1.  p1 and q may both be null (no queries).
+ *   theta        : device float[H/2]; null: V[slot_t] = info[t].
+ *   rope_base    : > 0, or 0 for coordinates that are rotated already.
+ *   positions    : device int[N]; may be null where rope_base is 0.
+ *   slots        : device long long[N] as relation_page_plan writes them; a token with a negative
+ *                  slot is padding: its query is zero and no cache row is written.  Two tokens of
+ *                  a call must not share a slot.
+ *   k_pages, v_pages : [n_pages][page_size][H][d_h] in dt with the strides of `cache` (whose H and
+ *                  d_h are the tokens').
+ * fp32 or bf16 (arithmetic in fp32), d_h up to 256, even where rope_base > 0, H even where theta is
+ * given (else RELATION_ERR_UNSUPPORTED).  Rows whose pointers and strides are multiples of 16 bytes,
+ * with d_h a multiple of 8, move in 16-byte groups, any others element by element.  A slot past
+ * the last page is padding and reported to dev_status (if given) as RELATION_ERR_INVALID_ARG.
+ * Asynchronous on `stream`; one launch; nothing is allocated.
+ */
+relation_status relation_cache_append(const void* p1, const void* p2, const void* info,
+                                      const float* theta, int pairing, float rope_base,
+                                      const int* positions, const long long* slots, void* q,
+                                      int N, long long sT, long long sH, void* k_pages,
+                                      void* v_pages, relation_pages cache, relation_dtype dt,
+                                      int* dev_status, relation_stream_t stream);
+
+/*
+ * relation_paged_decode: relation_decode over a paged cache: Y and logZ of the last row of every
+ * request (row lengths[b] - 1, at one-based position lengths[b]) against its rows before it.
+ *   q           [B][H][d_h] queries, element strides q_sB, q_sH (d_h contiguous); o likewise.
+ *               H is a multiple of cache.H: query heads h G .. h G + G - 1 share key/value head h,
+ *               G = H / cache.H.
+ *   k_pages, v_pages : [n_pages][page_size][cache.H][d_h] with the strides of `cache`.
+ *   block_table device int[B][cols], row stride table_stride: entries up to
+ *               ceil(lengths[b] / page_size) are read.
+ *   lengths     device int[B], 0 <= len_b <= cols * page_size.  A request of length 0 is idle: its
+ *               Y is zero and its logZ -inf.
+ *   logz        [B][H] fp32 output: log of the row's normaliser.
+ *   workspace   device scratch of relation_paged_decode_workspace_size(H, cache, dt) bytes, 16-byte
+ *               aligned; it does not grow with the batch or the cache.
+ * fp32 or bf16 with any 1 <= d_h <= 128; pages whose pointers and strides are multiples of 16 bytes,
+ * with d_h a multiple of 16 bytes, are read in 16-byte groups, any others element by element.  A
+ * length outside its range makes the request idle, a page id outside [0, n_pages) reads page 0 (the
+ * request's result is then undefined); both are reported to dev_status (if given) as
+ * RELATION_ERR_INVALID_ARG.  Asynchronous on `stream`; nothing is allocated.
+ */
+size_t relation_paged_decode_workspace_size(int H, relation_pages cache, relation_dtype dt);
+relation_status relation_paged_decode(const void* q, const void* k_pages, const void* v_pages,
+                                      const int* block_table, int cols, long long table_stride,
+                                      const int* lengths, void* o, float* logz, float lambda,
+                                      float tau_s, int B, int H, relation_pages cache,
+                                      long long q_sB, long long q_sH, relation_dtype dt,
+                                      void* workspace, size_t ws_bytes, int* dev_status,
+                                      relation_stream_t stream);
+
+/*
+ * relation_sample: the next token of every row of logits from a given uniform number.
+ *   logits      [R][V] in dt, row stride s_row (element alignment), V <= 327552 (else
+ *               RELATION_ERR_UNSUPPORTED).  -inf masks a token.
+ *   u           device float[R] in [0, 1].
+ *   temperature, top_k, top_p, min_p : device float / int / float / float [R], each may be null
+ *               (1, none, none, none).  temperature 0 takes the largest logit, the lowest index
+ *               of equal ones.  top_k <= 0 or >= V, top_p >= 1 and min_p <= 0 keep every token.
+ * Token j weighs w_j = exp((x_j - max x) / temperature) in fp32, summed as the whole number
+ * floor(2^40 w_j), so that the result is the same for any batch.  Tokens are ordered by descending
+ * w_j, equal ones by index; the first top_k are kept, of these the shortest beginning that holds
+ * floor(top_p * their sum) (at least one), of these the ones with w_j >= min_p (of the largest
+ * weight).  The token is the first, in the order of the indices, whose running sum over the kept
+ * tokens exceeds floor(u * the kept sum).
+ *   token       device int[R]; logprob device float[R]: log of its probability among the kept;
+ *   logz        device float[R]: log of the sum of exp(x_j / temperature) over the kept.
+ * A row without an unmasked token gets token -1 and logprob = logz = -inf; one with a NaN, or
+ * with a temperature that is negative or not finite or a u outside [0, 1] (reported to dev_status,
+ * if given, as RELATION_ERR_INVALID_ARG), token -1 and logprob = logz = NaN.  Logits of +inf share
+ * the probability among them.  Asynchronous on `stream`; one launch; nothing is allocated.
+ */
+relation_status relation_sample(const void* logits, int R, int V, long long s_row,
+                                relation_dtype dt, const float* u, const float* temperature,
+                                const int* top_k, const float* top_p, const float* min_p,
+                                int* token, float* logprob, float* logz, int* dev_status,
+                                relation_stream_t stream);
 
 /*
  * Context parallelism (sequence sharding) of the forward.  The Exchange summary of a query

@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import os
 import threading
+from typing import NamedTuple
 
 import torch
 
@@ -20,7 +21,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "_build", "librelation.so")
 
 # relation_status
-OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT = range(7)
+OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA, ERR_TIMEOUT, \
+    ERR_CAPACITY = range(8)
 # relation_dtype
 F32, BF16 = 0, 1
 # relation_kernel
@@ -36,7 +38,9 @@ EXPORTED = ("relation_fwd", "relation_fwd_ex", "relation_bwd", "relation_bwd_ex"
             "relation_linear_fwd_workspace_size",
             "relation_linear_bwd", "relation_linear_bwd_workspace_size",
             "relation_linear_bwd_ex", "relation_linear_bwd_ex_workspace_size", "relation_layer_prep",
-            "relation_layer_grad", "relation_layer_grad_workspace_size")
+            "relation_layer_grad", "relation_layer_grad_workspace_size", "relation_page_plan",
+            "relation_cache_append", "relation_paged_decode",
+            "relation_paged_decode_workspace_size", "relation_sample")
 
 
 class RelationLibraryMissing(RuntimeError):
@@ -55,6 +59,12 @@ class RelationError(RuntimeError):
 class Shape(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int), ("T", ctypes.c_int), ("H", ctypes.c_int),
                 ("d_h", ctypes.c_int), ("sB", ctypes.c_longlong), ("sT", ctypes.c_longlong),
+                ("sH", ctypes.c_longlong)]
+
+
+class Pages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("H", ctypes.c_int),
+                ("d_h", ctypes.c_int), ("sP", ctypes.c_longlong), ("sR", ctypes.c_longlong),
                 ("sH", ctypes.c_longlong)]
 
 
@@ -105,6 +115,15 @@ def load(path: str | None = None):
                                             vp, sz, vp]
         lib.relation_layer_grad_workspace_size.argtypes = [Shape, i]
         lib.relation_layer_grad_workspace_size.restype = sz
+        lib.relation_page_plan.argtypes = [vp, vp, i, i, vp, i, ll, vp, i, vp, vp, vp, vp, vp, vp, i,
+                                           ip, vp]
+        lib.relation_cache_append.argtypes = [vp, vp, vp, vp, i, f, vp, vp, vp, i, ll, ll, vp, vp,
+                                              Pages, i, ip, vp]
+        lib.relation_paged_decode.argtypes = [vp, vp, vp, vp, i, ll, vp, vp, vp, f, f, i, i, Pages, ll,
+                                              ll, i, vp, sz, ip, vp]
+        lib.relation_paged_decode_workspace_size.argtypes = [i, Pages, i]
+        lib.relation_paged_decode_workspace_size.restype = sz
+        lib.relation_sample.argtypes = [vp, i, i, ll, i, vp, vp, vp, vp, vp, vp, vp, vp, ip, vp]
         lib.relation_linear_bwd_workspace_size.restype = ctypes.c_size_t
         lib.relation_decode_workspace_size.restype = ctypes.c_size_t
         lib.relation_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, f, f, Shape, i, vp,
@@ -473,6 +492,193 @@ def decode(q, k_cache, v_cache, lengths, lam: float, tau_s: float = 2.0, *, out=
     if rc != OK:
         raise RelationError(rc, "relation_decode")
     return out, logz
+
+
+class PagePlan(NamedTuple):
+    """What page_plan returns; the block table and the free pages are updated in place."""
+    slots: torch.Tensor       # int64 [n_tokens]: page * page_size + row, -1 for padding
+    positions: torch.Tensor   # int32 [n_tokens]: zero-based position, -1 for padding
+    starts: torch.Tensor      # int32 [B + 1]: request b's tokens are starts[b] .. starts[b + 1] - 1
+    lengths: torch.Tensor     # int32 [B]: rows in the cache after the step
+    free_state: torch.Tensor  # int32 [2]: head and count of the ring of free pages after it
+
+
+def _int32(name, t, device, shape=None):
+    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != device or not t.is_cuda:
+        raise ValueError(f"{name} must be a contiguous int32 tensor on the operands' CUDA device")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} must have shape {tuple(shape)}")
+
+
+def page_plan(lengths, counts, block_table, free_pages, free_state, page_size: int, n_tokens: int,
+              *, out: PagePlan | None = None, dev_status=None, stream=None) -> PagePlan:
+    """Pages, slots and positions of one step's new tokens: lengths and counts int32 [B] (count
+    < 0: the request has ended), block_table int32 [B, cols] (rows may be strided) and the ring
+    free_pages int32 [n_pages], both updated in place, free_state int32 [2] = (head, count).
+    ``n_tokens`` is the size of the step's token buffer.  See relation_page_plan."""
+    dev, B = lengths.device, lengths.numel()
+    _int32("lengths", lengths, dev)
+    _int32("counts", counts, dev, lengths.shape)
+    _int32("free_pages", free_pages, dev)
+    _int32("free_state", free_state, dev, (2,))
+    if block_table.dim() != 2 or block_table.shape[0] != B or block_table.dtype != torch.int32 or \
+            block_table.stride(1) != 1 or block_table.device != dev:
+        raise ValueError("block_table must be an int32 [B, cols] tensor with contiguous rows on "
+                         "the operands' device")
+    if out is None:
+        # one allocation, the slots first: a step's call is bound by the host
+        words = 3 * int(n_tokens) + 2 * B + 3
+        buf = torch.empty(words, dtype=torch.int32, device=dev)
+        n = int(n_tokens)
+        slots, positions, starts, new, state = buf.split((2 * n, n, B + 1, B, 2))
+        out = PagePlan(slots.view(torch.int64), positions, starts, new, state)
+    else:
+        if out.slots.dtype != torch.int64 or out.slots.numel() != n_tokens or \
+                not out.slots.is_contiguous() or out.slots.device != dev:
+            raise ValueError("out.slots must be a contiguous int64 [n_tokens] tensor")
+        _int32("out.positions", out.positions, dev, (n_tokens,))
+        _int32("out.starts", out.starts, dev, (B + 1,))
+        _int32("out.lengths", out.lengths, dev, (B,))
+        _int32("out.free_state", out.free_state, dev, (2,))
+    rc = load().relation_page_plan(_ptr(lengths), _ptr(counts), B, int(page_size),
+                                   _ptr(block_table), block_table.shape[1], block_table.stride(0),
+                                   _ptr(free_pages), free_pages.numel(), _ptr(free_state),
+                                   _ptr(out.free_state), _ptr(out.lengths), _ptr(out.starts),
+                                   _ptr(out.slots), _ptr(out.positions), int(n_tokens),
+                                   _ptr(dev_status), _stream(stream))
+    if rc != OK:
+        raise RelationError(rc, "relation_page_plan")
+    return out
+
+
+def pages_of(k_pages, v_pages) -> Pages:
+    """relation_pages of a pair of [n_pages, page_size, H, d] tensors with d contiguous."""
+    _same_layout(k_pages, v_pages)
+    st = k_pages.stride()
+    if len(st) != 4 or st[3] != 1:
+        raise ValueError("pages must be [n_pages, page_size, H, d] tensors with d contiguous")
+    return Pages(*k_pages.shape, *st[:3])
+
+
+def cache_append(p1, p2, info, theta, positions, slots, k_pages, v_pages, pairing: int = 0,
+                 rope_base: float = 1.0e4, *, out=None, dev_status=None, stream=None):
+    """The layer's transforms of N new tokens at their positions, written into the pages:
+    k_pages[slot] = RoPE(p2), v_pages[slot] = Givens(info); returns q = RoPE(p1) (None where p1 is
+    None).  p1, p2, info [N, H, d] of one layout, theta fp32 [H/2] or None (no mixing), positions
+    int32 [N] (unused with rope_base 0: no rotation), slots int64 [N], negative for padding."""
+    if p1 is None:
+        _same_layout(p2, info)
+    else:
+        _same_layout(p2, p1, info)
+    pages = pages_of(k_pages, v_pages)
+    if p2.dim() != 3 or p2.stride(2) != 1 or p2.dtype != k_pages.dtype or \
+            p2.device != k_pages.device or p2.shape[1:] != k_pages.shape[2:]:
+        raise ValueError("tokens must be [N, H, d] with d contiguous, of the pages' H, d, dtype "
+                         "and device")
+    N, dev = p2.shape[0], p2.device
+    if slots.dtype != torch.int64 or slots.shape != (N,) or not slots.is_contiguous() or \
+            slots.device != dev:
+        raise ValueError("slots must be a contiguous int64 tensor of N entries")
+    if positions is not None:
+        _int32("positions", positions, dev, (N,))
+    if theta is not None and (theta.dtype != torch.float32 or theta.device != dev or
+                              theta.numel() != p2.shape[1] // 2 or not theta.is_contiguous()):
+        raise ValueError("theta must be contiguous fp32 [H/2] on the inputs' device")
+    if p1 is None:
+        out = None
+    elif out is None:
+        out = _like(p1)
+    else:
+        _same_layout(p1, out)
+    st = p2.stride()
+    rc = load().relation_cache_append(_ptr(p1), _ptr(p2), _ptr(info), _ptr(theta), int(pairing),
+                                      float(rope_base), _ptr(positions), _ptr(slots), _ptr(out), N,
+                                      st[0], st[1], _ptr(k_pages), _ptr(v_pages), pages,
+                                      _dtype_code(p2), _ptr(dev_status), _stream(stream))
+    if rc != OK:
+        raise RelationError(rc, "relation_cache_append")
+    return out
+
+
+def paged_decode_workspace_size(q, k_pages) -> int:
+    """Device bytes paged_decode needs for queries [B, H, d] over these pages."""
+    return int(load().relation_paged_decode_workspace_size(q.shape[1], pages_of(k_pages, k_pages),
+                                                           _dtype_code(k_pages)))
+
+
+def paged_decode(q, k_pages, v_pages, block_table, lengths, lam: float, tau_s: float = 2.0, *,
+                 out=None, logz=None, workspace=None, dev_status=None, stream=None):
+    """One new token per request over [n_pages, page_size, Hk, d] pages: q [B, H, d] with H a
+    multiple of Hk, block_table int32 [B, cols] (rows may be strided), lengths int32 [B] counting
+    the new token (0: idle).  Returns (Y [B, H, d], logZ [B, H])."""
+    pages = pages_of(k_pages, v_pages)
+    dev = k_pages.device
+    if q.dim() != 3 or q.shape[2] != pages.d_h or q.stride(2) != 1 or \
+            q.dtype != k_pages.dtype or q.device != dev:
+        raise ValueError("q must be [B, H, d] with d contiguous, of the pages' d, dtype and device")
+    B, H = q.shape[:2]
+    _int32("lengths", lengths, dev, (B,))
+    if block_table.dim() != 2 or block_table.shape[0] != B or block_table.dtype != torch.int32 or \
+            block_table.stride(1) != 1 or block_table.device != dev:
+        raise ValueError("block_table must be an int32 [B, cols] tensor with contiguous rows on "
+                         "the pages' device")
+    if out is None:
+        out = _like(q)
+    elif out.shape != q.shape or out.stride() != q.stride() or out.dtype != q.dtype or \
+            out.device != dev:
+        raise ValueError("out must have q's layout")
+    if logz is None:
+        logz = torch.empty((B, H), device=dev, dtype=torch.float32)
+    elif logz.shape != (B, H) or logz.dtype != torch.float32 or not logz.is_contiguous():
+        raise ValueError("logz must be a dense fp32 [B, H] tensor")
+    lib, dt = load(), _dtype_code(q)
+    if workspace is None:
+        workspace = torch.empty(lib.relation_paged_decode_workspace_size(H, pages, dt), device=dev,
+                                dtype=torch.uint8)
+    st = q.stride()
+    rc = lib.relation_paged_decode(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(block_table),
+                                   block_table.shape[1], block_table.stride(0), _ptr(lengths),
+                                   _ptr(out), _ptr(logz), float(lam), float(tau_s), B, H, pages,
+                                   st[0], st[1], dt, _ptr(workspace),
+                                   workspace.numel() * workspace.element_size(), _ptr(dev_status),
+                                   _stream(stream))
+    if rc != OK:
+        raise RelationError(rc, "relation_paged_decode")
+    return out, logz
+
+
+def _rows(name, t, R, dtype, device):
+    if t is not None and (t.dtype != dtype or t.shape != (R,) or not t.is_contiguous() or
+                          t.device != device):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of one entry per row on the "
+                         "logits' device")
+    return _ptr(t)
+
+
+def sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None,
+           dev_status=None, stream=None):
+    """The next token of every row of logits [R, V] (fp32 or bf16, rows may be strided) from
+    uniform numbers u fp32 [R]; temperature, top_p, min_p fp32 [R] and top_k int32 [R], each
+    optional.  Returns (token int32 [R], logprob fp32 [R], logz fp32 [R]); see relation_sample."""
+    if logits.dim() != 2 or logits.stride(1) != 1 or not logits.is_cuda:
+        raise ValueError("logits must be a CUDA [R, V] tensor with contiguous rows")
+    (R, V), dev, f4 = logits.shape, logits.device, torch.float32
+    dt = _dtype_code(logits)
+    args = [_rows("u", u, R, f4, dev), _rows("temperature", temperature, R, f4, dev),
+            _rows("top_k", top_k, R, torch.int32, dev), _rows("top_p", top_p, R, f4, dev),
+            _rows("min_p", min_p, R, f4, dev)]
+    if out is None:
+        both = torch.empty((2, R), dtype=f4, device=dev)
+        out = (torch.empty(R, dtype=torch.int32, device=dev), both[0], both[1])
+    token, logprob, logz = out
+    _rows("token", token, R, torch.int32, dev)
+    _rows("logprob", logprob, R, f4, dev)
+    _rows("logz", logz, R, f4, dev)
+    rc = load().relation_sample(_ptr(logits), R, V, logits.stride(0), dt, *args, _ptr(token),
+                                _ptr(logprob), _ptr(logz), _ptr(dev_status), _stream(stream))
+    if rc != OK:
+        raise RelationError(rc, "relation_sample")
+    return out
 
 
 BWD_PREPARE, BWD_TILES, BWD_FINALIZE, BWD_ALL = 1, 2, 4, 7

@@ -224,6 +224,83 @@ int decode_chunks(int t_max);
 size_t decode_workspace_bytes(int B, int H, int t_max);
 cudaError_t launch_decode(const DecodeProblem& p, void* workspace, cudaStream_t s);
 
+// Pages of the requests' cache rows (relation_plan.cu): relation_page_plan's arguments.
+struct PlanProblem {
+  const int* lengths;   // [B] rows in the cache
+  const int* counts;    // [B] new tokens; < 0: the request has ended
+  int* table;           // [B][cols] page ids, row stride t_stride
+  int* ring;            // [n_pages] free pages
+  const int* state;     // {head, count} of the ring
+  int* state_out;
+  int* lengths_out;     // [B]
+  int* starts;          // [B + 1]
+  long long* slots;     // [n_tokens]
+  int* positions;       // [n_tokens]
+  int* dev_status;      // nullable
+  long long t_stride;
+  int B, page, cols, n_pages, n_tokens;
+};
+cudaError_t launch_plan(const PlanProblem& p, cudaStream_t s);
+
+// New tokens into a paged cache (relation_append.cu): relation_cache_append's arguments.
+struct AppendProblem {
+  const void* p1;       // [N][H][d] (element strides sT, sH); null with q
+  const void* p2;
+  const void* info;
+  const float* theta;   // [H/2]; null: no mixing
+  const int* positions; // [N]
+  const long long* slots;
+  void* q;              // like p1
+  void* k;              // pages [n_pages][page][H][d] (element strides sP, sR, sC)
+  void* v;
+  int* dev_status;
+  int pairing;
+  float rope_base;      // 0: no rotation
+  int N, H, d, n_pages, page;
+  long long sT, sH, sP, sR, sC;
+  relation_dtype dtype;
+};
+cudaError_t launch_append(const AppendProblem& p, cudaStream_t s);
+
+// One new token per request over a paged cache (relation_paged.cu): relation_paged_decode's
+// arguments.
+struct PagedProblem {
+  const void* q;        // [B][H][d] (element strides qsB, qsH)
+  const void* k;        // pages [n_pages][page][Hk][d] (element strides sP, sR, sC)
+  const void* v;
+  const int* table;     // [B][cols] page ids, row stride t_stride
+  const int* lengths;   // [B]
+  void* out;            // like q
+  float* logz;          // [B][H]
+  int* dev_status;
+  float lambda, tau_s, inv_sqrt_d;
+  int B, H, Hk, d, cols, n_pages, page;
+  int HG;               // groups of query heads that are taken together (set by the launcher)
+  long long t_stride, sP, sR, sC, qsB, qsH;
+  relation_dtype dtype;
+};
+size_t paged_workspace_bytes(int H, int Hk);
+cudaError_t launch_paged(const PagedProblem& p, void* workspace, cudaStream_t s);
+
+// The next token of every row (relation_sample.cu): relation_sample's arguments.
+struct SampleProblem {
+  const void* logits;        // [R][V], row stride s_row
+  const float* u;            // [R] in [0, 1]
+  const float* temperature;  // [R] each, nullable
+  const int* top_k;
+  const float* top_p;
+  const float* min_p;
+  int* token;                // [R]
+  float* logprob;
+  float* logz;
+  int* dev_status;
+  int R, V;
+  long long s_row;
+  relation_dtype dtype;
+};
+int sample_max_vocabulary();
+cudaError_t launch_sample(const SampleProblem& p, cudaStream_t s);
+
 cudaError_t launch_selftest_wait(int* dev_status, int timeout_us, cudaStream_t s);
 
 // Where the last failing CUDA step of this thread happened (reported by

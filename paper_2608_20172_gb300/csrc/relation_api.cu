@@ -453,6 +453,141 @@ relation_status relation_decode(const void* q, const void* k_cache, const void* 
   return from_cuda(rel::launch_decode(p, workspace, reinterpret_cast<cudaStream_t>(stream)));
 }
 
+relation_status relation_page_plan(const int* lengths, const int* counts, int B, int page_size,
+                                   int* block_table, int cols, long long table_stride,
+                                   int* free_pages, int n_pages, const int* free_state,
+                                   int* free_state_out, int* lengths_out, int* starts,
+                                   long long* slots, int* positions, int n_tokens,
+                                   int* dev_status, relation_stream_t stream) {
+  if (B < 1 || page_size < 1 || cols < 1 || n_pages < 1 || n_tokens < 1 || table_stride < cols)
+    return RELATION_ERR_INVALID_ARG;
+  if ((long long)cols * page_size > 0x7fffffffLL || (long long)B * cols > 0x7fffffffLL)
+    return RELATION_ERR_UNSUPPORTED;
+  for (const void* x : {(const void*)lengths, (const void*)counts, (const void*)block_table,
+                        (const void*)free_pages, (const void*)free_state,
+                        (const void*)free_state_out, (const void*)lengths_out,
+                        (const void*)starts, (const void*)slots, (const void*)positions}) {
+    if (!x) return RELATION_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(x) & (x == slots ? 7u : 3u)) return RELATION_ERR_ALIGNMENT;
+  }
+  if (lengths_out == lengths || lengths_out == counts || free_state_out == free_state)
+    return RELATION_ERR_INVALID_ARG;
+  if (reinterpret_cast<uintptr_t>(dev_status) & 3u) return RELATION_ERR_ALIGNMENT;
+  rel::PlanProblem p{};
+  p.lengths = lengths; p.counts = counts; p.table = block_table; p.ring = free_pages;
+  p.state = free_state; p.state_out = free_state_out; p.lengths_out = lengths_out;
+  p.starts = starts; p.slots = slots; p.positions = positions; p.dev_status = dev_status;
+  p.t_stride = table_stride; p.B = B; p.page = page_size; p.cols = cols; p.n_pages = n_pages;
+  p.n_tokens = n_tokens;
+  return from_cuda(rel::launch_plan(p, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+
+relation_status check_pages(const relation_pages& c, relation_dtype dt) {
+  if (dt != RELATION_F32 && dt != RELATION_BF16) return RELATION_ERR_INVALID_ARG;
+  if (c.n_pages < 1 || c.page_size < 1 || c.H < 1 || c.d_h < 1) return RELATION_ERR_INVALID_ARG;
+  if (c.sP < 1 || c.sR < 1 || c.sH < 1) return RELATION_ERR_INVALID_ARG;
+  return RELATION_OK;
+}
+
+// Null or not a multiple of the element size
+relation_status check_elements(std::initializer_list<const void*> ptrs, size_t size) {
+  for (const void* p : ptrs) {
+    if (!p) return RELATION_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(p) % size) return RELATION_ERR_ALIGNMENT;
+  }
+  return RELATION_OK;
+}
+
+}  // namespace
+
+relation_status relation_cache_append(const void* p1, const void* p2, const void* info,
+                                      const float* theta, int pairing, float rope_base,
+                                      const int* positions, const long long* slots, void* q,
+                                      int N, long long sT, long long sH, void* k_pages,
+                                      void* v_pages, relation_pages cache, relation_dtype dt,
+                                      int* dev_status, relation_stream_t stream) {
+  relation_status st;
+  if ((st = check_pages(cache, dt)) != RELATION_OK) return st;
+  if (N < 1 || sT < 1 || sH < 1 || (pairing != 0 && pairing != 1)) return RELATION_ERR_INVALID_ARG;
+  if (!isfinite(rope_base) || rope_base < 0.0f) return RELATION_ERR_INVALID_ARG;
+  if ((p1 == nullptr) != (q == nullptr)) return RELATION_ERR_INVALID_ARG;
+  if (rope_base > 0.0f && !positions) return RELATION_ERR_INVALID_ARG;
+  if ((st = check_elements({p2, info, k_pages, v_pages}, elem_size(dt))) != RELATION_OK) return st;
+  if (p1 && (st = check_elements({p1, q}, elem_size(dt))) != RELATION_OK) return st;
+  if ((st = check_elements({slots}, 8)) != RELATION_OK) return st;
+  for (const void* x : {(const void*)theta, (const void*)positions, (const void*)dev_status})
+    if (reinterpret_cast<uintptr_t>(x) & 3u) return RELATION_ERR_ALIGNMENT;
+  if (cache.d_h > 256 || (rope_base > 0.0f && cache.d_h % 2) || (theta && cache.H % 2))
+    return RELATION_ERR_UNSUPPORTED;
+  if (N > 0x3fffffff || (long long)cache.H * cache.d_h > (1 << 24)) return RELATION_ERR_UNSUPPORTED;
+  rel::AppendProblem p{};
+  p.p1 = p1; p.p2 = p2; p.info = info; p.theta = theta; p.positions = positions; p.slots = slots;
+  p.q = q; p.k = k_pages; p.v = v_pages; p.dev_status = dev_status;
+  p.pairing = pairing; p.rope_base = rope_base;
+  p.N = N; p.H = cache.H; p.d = cache.d_h; p.n_pages = cache.n_pages; p.page = cache.page_size;
+  p.sT = sT; p.sH = sH; p.sP = cache.sP; p.sR = cache.sR; p.sC = cache.sH;
+  p.dtype = dt;
+  return from_cuda(rel::launch_append(p, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t relation_paged_decode_workspace_size(int H, relation_pages cache, relation_dtype dt) {
+  if (check_pages(cache, dt) != RELATION_OK || cache.d_h > 128 || H < 1 || H % cache.H) return 0;
+  return rel::paged_workspace_bytes(H, cache.H);
+}
+
+relation_status relation_paged_decode(const void* q, const void* k_pages, const void* v_pages,
+                                      const int* block_table, int cols, long long table_stride,
+                                      const int* lengths, void* o, float* logz, float lambda,
+                                      float tau_s, int B, int H, relation_pages cache,
+                                      long long q_sB, long long q_sH, relation_dtype dt,
+                                      void* workspace, size_t ws_bytes, int* dev_status,
+                                      relation_stream_t stream) {
+  relation_status st;
+  if ((st = check_pages(cache, dt)) != RELATION_OK) return st;
+  if (B < 1 || H < 1 || H % cache.H || cols < 1 || table_stride < cols || q_sB < 1 || q_sH < 1)
+    return RELATION_ERR_INVALID_ARG;
+  if ((st = check_scalars(lambda, tau_s)) != RELATION_OK) return st;
+  if (cache.d_h > 128) return RELATION_ERR_UNSUPPORTED;
+  if ((long long)B * H > 0x7fffffffLL || (long long)cols * cache.page_size > 0x7fffffffLL)
+    return RELATION_ERR_UNSUPPORTED;
+  if ((st = check_elements({q, k_pages, v_pages, o}, elem_size(dt))) != RELATION_OK) return st;
+  if ((st = check_elements({block_table, lengths, logz}, 4)) != RELATION_OK) return st;
+  if (reinterpret_cast<uintptr_t>(dev_status) & 3u) return RELATION_ERR_ALIGNMENT;
+  if (!workspace || ws_bytes < rel::paged_workspace_bytes(H, cache.H)) return RELATION_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return RELATION_ERR_ALIGNMENT;
+  rel::PagedProblem p{};
+  p.q = q; p.k = k_pages; p.v = v_pages; p.table = block_table; p.lengths = lengths;
+  p.out = o; p.logz = logz; p.dev_status = dev_status;
+  p.lambda = lambda; p.tau_s = tau_s; p.inv_sqrt_d = 1.0f / sqrtf((float)cache.d_h);
+  p.B = B; p.H = H; p.Hk = cache.H; p.d = cache.d_h; p.cols = cols; p.n_pages = cache.n_pages;
+  p.page = cache.page_size; p.t_stride = table_stride; p.sP = cache.sP; p.sR = cache.sR;
+  p.sC = cache.sH; p.qsB = q_sB; p.qsH = q_sH; p.dtype = dt;
+  return from_cuda(rel::launch_paged(p, workspace, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+relation_status relation_sample(const void* logits, int R, int V, long long s_row,
+                                relation_dtype dt, const float* u, const float* temperature,
+                                const int* top_k, const float* top_p, const float* min_p,
+                                int* token, float* logprob, float* logz, int* dev_status,
+                                relation_stream_t stream) {
+  relation_status st;
+  if (dt != RELATION_F32 && dt != RELATION_BF16) return RELATION_ERR_INVALID_ARG;
+  if (R < 1 || V < 1 || (R > 1 && s_row < V)) return RELATION_ERR_INVALID_ARG;
+  if ((st = check_elements({logits}, elem_size(dt))) != RELATION_OK) return st;
+  if ((st = check_elements({u, token, logprob, logz}, 4)) != RELATION_OK) return st;
+  for (const void* x : {(const void*)temperature, (const void*)top_k, (const void*)top_p,
+                        (const void*)min_p, (const void*)dev_status})
+    if (reinterpret_cast<uintptr_t>(x) & 3u) return RELATION_ERR_ALIGNMENT;
+  if (V > rel::sample_max_vocabulary() || R > (1 << 27)) return RELATION_ERR_UNSUPPORTED;
+  rel::SampleProblem p{};
+  p.logits = logits; p.u = u; p.temperature = temperature; p.top_k = top_k; p.top_p = top_p;
+  p.min_p = min_p; p.token = token; p.logprob = logprob; p.logz = logz; p.dev_status = dev_status;
+  p.R = R; p.V = V; p.s_row = s_row; p.dtype = dt;
+  return from_cuda(rel::launch_sample(p, reinterpret_cast<cudaStream_t>(stream)));
+}
+
 size_t relation_bwd_workspace_size(relation_shape shp, relation_dtype dt) {
   if (check_shape(shp, dt) != RELATION_OK) return 0;
   return rel::bwd_workspace_bytes(shp.B, shp.H, shp.T, shp.d_h);
@@ -519,6 +654,7 @@ const char* relation_status_string(relation_status s) {
     case RELATION_ERR_WORKSPACE: return "RELATION_ERR_WORKSPACE";
     case RELATION_ERR_CUDA: return "RELATION_ERR_CUDA";
     case RELATION_ERR_TIMEOUT: return "RELATION_ERR_TIMEOUT";
+    case RELATION_ERR_CAPACITY: return "RELATION_ERR_CAPACITY";
   }
   return "RELATION_ERR_UNKNOWN";
 }
