@@ -375,7 +375,7 @@ relation_status relation_paged_decode(const void* q, const void* k_pages, const 
 
 /*
  * relation_sample: the next token of every row of logits from a given uniform number.
- *   logits      [R][V] in dt, row stride s_row (element alignment), V <= 327552 (else
+ *   logits      [R][V] in dt, row stride s_row (element alignment), V <= 262144 (else
  *               RELATION_ERR_UNSUPPORTED).  -inf masks a token.
  *   u           device float[R] in [0, 1].
  *   temperature, top_k, top_p, min_p : device float / int / float / float [R], each may be null

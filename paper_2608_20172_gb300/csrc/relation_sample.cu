@@ -13,9 +13,11 @@
 // temperature 0 takes the largest logit (w_j = 1 there and 0 elsewhere, k = 1).
 //
 // A cluster of CTAs shares a row: each holds its slice of the weights in shared memory, so that the
-// logits are read once.  The cuts are found by a radix search over the composite key (w_j, index),
-// which no two tokens share: per digit a histogram of counts and masses of the tokens that agree with
-// the digits found so far, summed over the cluster through distributed shared memory.
+// logits are read once.  A cut is found from above: a histogram of the weights' leading bits, of
+// which every bin knows its count and its exact mass, names the bin in which the cut lies; while that
+// bin holds more than kList tokens, further digits of the key (w_j, index), which no two tokens
+// share, narrow it; then its tokens are ranked against each other.  What the CTAs have to know of
+// each other goes through distributed shared memory.
 #include <cooperative_groups.h>
 #include <math.h>
 
@@ -31,23 +33,33 @@ using u64 = unsigned long long;
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kMaxSlice = 40 * 1024;  // tokens of a CTA (with Smem 221 of its 227 KB)
-constexpr int kIndexBits = 22;        // of the composite key: 30 bits of w, then the index
-constexpr int kKeyBits = 30 + kIndexBits;
-constexpr int kDigit = 11, kBins = 1 << kDigit;
-constexpr int kSlots = 3;             // a mass in 14-bit parts, whose sums stay below 2^32
+constexpr int kMaxSlice = 32 * 1024;  // tokens of a CTA
+constexpr int kIndexBits = 22;        // of the key: 30 bits of w, then the index from the top down
+constexpr int kFirst = 87;            // the exponent of 2^-40, below which a weight is 0
+constexpr int kDigit = 8;             // further digits
+constexpr int kList = 512;            // tokens that are ranked against each other
 
+// A slice of at most 2^(32 - LOW) tokens: its bins' sums of LOW-bit numbers stay below 2^32.
+constexpr int low_bits(bool wide) { return wide ? 17 : 18; }
+constexpr int bins_of(int low) { return ((127 - kFirst) << (23 - low)) + 1; }
+
+template <int LOW>
 struct Smem {
-  unsigned hist[1 + kSlots][kBins];  // this CTA's: counts, parts of the masses
-  unsigned count[kBins];             // the cluster's
+  static constexpr int kBins = bins_of(LOW);
+  unsigned hist[2][kBins];      // this CTA's bins: tokens, sums of the low bits
+  unsigned count[kBins];        // the cluster's: tokens and masses
   u64 mass[kBins];
-  u64 scan[2][kWarps];
-  u64 warp_sum[kWarps], total;
-  float red[kWarps];
-  float max;
-  int nan;
-  u64 above_count, above_mass;       // of the digit that was found,
-  unsigned digit;                    // and the digit
+  unsigned part[4][1 << kDigit];  // a digit's histogram: tokens, the masses in 14-bit parts;
+  unsigned d_count[1 << kDigit];  // the cluster's
+  u64 d_mass[1 << kDigit];
+  u64 list[kList];              // keys of the tokens in the cut's bin: this CTA's,
+  u64 all[kList];               // the cluster's
+  u64 scan[2][kWarps], total, kept;
+  float red[kWarps], max;
+  int nan, n_list;
+  // what the threads tell each other
+  unsigned bin, inside;
+  u64 above_count, above_mass, key;
 };
 
 __device__ __forceinline__ u64 fixed_of(float w) {
@@ -56,122 +68,251 @@ __device__ __forceinline__ u64 fixed_of(float w) {
 __device__ __forceinline__ u64 key_of(float w, int j) {
   return (u64)__float_as_uint(w) << kIndexBits | (u64)((1 << kIndexBits) - 1 - j);
 }
-
-__device__ __forceinline__ u64 warp_sum(u64 x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-  return x;
+__device__ __forceinline__ u64 weight_of_key(u64 key) {
+  return fixed_of(__uint_as_float((unsigned)(key >> kIndexBits)));
 }
 
-// The digit at `shift` of the boundary's key among this row's tokens with key >= least whose higher
-// digits are `prefix`: the boundary is the first token in descending order at which the running
-// count (by_mass: mass), beginning with `above`, reaches `want`.
-__device__ __forceinline__ void find_digit(cg::cluster_group& cl, Smem& sm, const float* w, int n,
-                                           int j0, u64 least, u64 prefix, int shift, int bits,
-                                           bool by_mass, u64 want, u64 above_count,
-                                           u64 above_mass) {
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  for (int i = tid; i < (1 + kSlots) * kBins; i += kThreads) (&sm.hist[0][0])[i] = 0;
-  __syncthreads();
-  for (int i = tid; i < n; i += kThreads) {
-    const float x = w[i];
-    const u64 key = key_of(x, j0 + i);
-    if (key < least || key >> (shift + bits) != prefix) continue;
-    const unsigned d = (unsigned)(key >> shift) & ((1u << bits) - 1);
-    const u64 q = fixed_of(x);
-    atomicAdd(&sm.hist[0][d], 1u);
-    atomicAdd(&sm.hist[1][d], (unsigned)q & 0x3fff);
-    atomicAdd(&sm.hist[2][d], (unsigned)(q >> 14) & 0x3fff);
-    atomicAdd(&sm.hist[3][d], (unsigned)(q >> 28));
-  }
-  cl.sync();
-  // each CTA adds up its share of the bins and hands them to all
-  const int C = (int)cl.num_blocks(), share = kBins / C, b0 = (int)cl.block_rank() * share;
-  for (int i = tid; i < share; i += kThreads) {
-    unsigned c = 0;
-    u64 m = 0;
-    for (int r = 0; r < C; ++r) {
-      const Smem* o = cl.map_shared_rank(&sm, r);
-      c += o->hist[0][b0 + i];
-      m += (u64)o->hist[1][b0 + i] + ((u64)o->hist[2][b0 + i] << 14) + ((u64)o->hist[3][b0 + i] << 28);
-    }
-    for (int r = 0; r < C; ++r) {
-      Smem* o = cl.map_shared_rank(&sm, r);
-      o->count[b0 + i] = c;
-      o->mass[b0 + i] = m;
-    }
-  }
-  cl.sync();
-  // from the highest bin down: thread t holds bins kBins - 1 - t per .. 
-  constexpr int per = kBins / kThreads;
-  u64 c = 0, m = 0;
-#pragma unroll
-  for (int i = 0; i < per; ++i) {
-    const int d = kBins - 1 - (tid * per + i);
-    c += sm.count[d];
-    m += sm.mass[d];
-  }
-  u64 cs = c, ms = m;
+// A bin is the weights that agree in all but their LOW last bits, w = 2^(E - 150) (top + low) with
+// the leading one in top.  In units of 2^-40, rounded down, that is
+// top << (E - 110) + low << (E - 110), or for E < 110 (top >> (110 - E)) + (low >> (110 - E)): top
+// ends in LOW zeros, and a low that is shifted past them adds nothing.
+template <int LOW>
+__device__ __forceinline__ unsigned low_part(unsigned bits) {
+  const int right = 110 - (int)(bits >> 23);
+  const unsigned low = bits & ((1u << LOW) - 1);
+  return right > 0 ? low >> right : low;
+}
+template <int LOW>
+__device__ __forceinline__ u64 mass_of(int bin, unsigned count, u64 low) {
+  const unsigned bits = ((unsigned)bin << LOW) + ((unsigned)kFirst << 23);
+  const int right = 110 - (int)(bits >> 23);
+  const unsigned top = (bits & 0x7fffffu) | 0x800000u;
+  return right > 0 ? (u64)count * (top >> right) + low : ((u64)count * top + low) << -right;
+}
+
+// This thread's exclusive sums over the block.
+__device__ __forceinline__ void block_scan(u64 (*part)[kWarps], u64& a, u64& b) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  u64 as = a, bs = b;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const u64 a = __shfl_up_sync(0xffffffffu, cs, o), b = __shfl_up_sync(0xffffffffu, ms, o);
+    const u64 x = __shfl_up_sync(0xffffffffu, as, o), y = __shfl_up_sync(0xffffffffu, bs, o);
     if (lane >= o) {
-      cs += a;
-      ms += b;
+      as += x;
+      bs += y;
     }
   }
+  __syncthreads();  // part is free
   if (lane == 31) {
-    sm.scan[0][warp] = cs;
-    sm.scan[1][warp] = ms;
+    part[0][warp] = as;
+    part[1][warp] = bs;
   }
   __syncthreads();
-  u64 ca = above_count + cs - c, ma = above_mass + ms - m;  // above this thread's bins
+  a = as - a;
+  b = bs - b;
   for (int i = 0; i < warp; ++i) {
-    ca += sm.scan[0][i];
-    ma += sm.scan[1][i];
+    a += part[0][i];
+    b += part[1][i];
   }
-#pragma unroll
-  for (int i = 0; i < per; ++i) {
-    const int d = kBins - 1 - (tid * per + i);
-    const u64 before = by_mass ? ma : ca, own = by_mass ? sm.mass[d] : sm.count[d];
-    if (before < want && want <= before + own) {
-      sm.digit = d;
-      sm.above_count = ca;
-      sm.above_mass = ma;
-    }
-    ca += sm.count[d];
-    ma += sm.mass[d];
-  }
-  __syncthreads();
 }
 
-// The boundary's key; *mass = the sum of the weights down to and with it.
-__device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem& sm, const float* w, int n,
-                                        int j0, u64 least, bool by_mass, u64 want, u64* mass) {
-  u64 prefix = 0, above_count = 0, above_mass = 0;
-  int shift = kKeyBits;
-  while (shift > 0) {
+// A histogram's bins from the highest down, a run of them per thread, and the sums above this
+// thread's.
+struct Bins {
+  const unsigned* count;
+  const u64* mass;
+  int first, last;  // from, and down to but without
+  u64 c, m;
+  __device__ __forceinline__ Bins(const unsigned* count, const u64* mass, int bins, u64 above_count,
+                                  u64 above_mass, u64 (*part)[kWarps], u64* total)
+      : count(count), mass(mass), c(0), m(0) {
+    const int per = (bins + kThreads - 1) / kThreads;
+    first = bins - 1 - (int)threadIdx.x * per;
+    last = max(first - per, -1);
+    for (int d = first; d > last; --d) {
+      c += count[d];
+      m += mass[d];
+    }
+    const u64 own = m;
+    block_scan(part, c, m);
+    if (total && threadIdx.x == kThreads - 1) *total = m + own;
+    c += above_count;
+    m += above_mass;
+  }
+  // The bin in which the running count (by_mass: mass) reaches `want`, into sm.bin, sm.inside (its
+  // tokens) and sm.above_*; sm.inside 0: in none.
+  template <typename S>
+  __device__ __forceinline__ void find(S& sm, bool by_mass, u64 want) const {
+    if (threadIdx.x == 0) sm.inside = 0;
+    __syncthreads();
+    u64 ca = c, ma = m;
+    for (int d = first; d > last; --d) {
+      const u64 before = by_mass ? ma : ca, own = by_mass ? mass[d] : count[d];
+      if (before < want && want <= before + own) {
+        sm.bin = d;
+        sm.inside = count[d];
+        sm.above_count = ca;
+        sm.above_mass = ma;
+      }
+      ca += count[d];
+      ma += mass[d];
+    }
+    __syncthreads();
+  }
+};
+
+// Sum the CTAs' bins: each CTA adds up its share of them and hands it to all.
+template <typename S, typename F>
+__device__ __forceinline__ void add_bins(cg::cluster_group& cl, S& sm, unsigned* count, u64* mass,
+                                         int bins, F own) {
+  const int C = (int)cl.num_blocks(), share = (bins + C - 1) / C, b0 = (int)cl.block_rank() * share;
+  cl.sync();
+  for (int i = b0 + (int)threadIdx.x; i < min(bins, b0 + share); i += kThreads) {
+    unsigned c = 0;
+    u64 m = 0;
+    own(i, c, m);
+    for (int r = 0; r < C; ++r) {
+      cl.map_shared_rank(count, r)[i] = c;
+      cl.map_shared_rank(mass, r)[i] = m;
+    }
+  }
+  cl.sync();
+}
+
+// The key of the cut that lies in sm.bin, among sm.inside tokens, and the mass down to and with it.
+template <int LOW>
+__device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, const float* w, int n,
+                                        int j0, bool by_mass, u64 want, u64* mass) {
+  const int tid = threadIdx.x, C = (int)cl.num_blocks();
+  u64 prefix = sm.bin + ((u64)kFirst << (23 - LOW));  // the key's bits from `shift` up
+  int shift = kIndexBits + LOW;
+  u64 above_count = sm.above_count, above_mass = sm.above_mass;
+  while (sm.inside > kList) {
     const int bits = min(kDigit, shift);
     shift -= bits;
-    find_digit(cl, sm, w, n, j0, least, prefix, shift, bits, by_mass, want, above_count, above_mass);
-    prefix = prefix << bits | sm.digit;
+    for (int i = tid; i < 4 << kDigit; i += kThreads) (&sm.part[0][0])[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < n; i += kThreads) {
+      const u64 key = key_of(w[i], j0 + i);
+      if (key >> (shift + bits) != prefix) continue;
+      const unsigned d = (unsigned)(key >> shift) & ((1u << bits) - 1);
+      const u64 q = fixed_of(w[i]);
+      atomicAdd(&sm.part[0][d], 1u);
+      atomicAdd(&sm.part[1][d], (unsigned)q & 0x3fff);
+      atomicAdd(&sm.part[2][d], (unsigned)(q >> 14) & 0x3fff);
+      atomicAdd(&sm.part[3][d], (unsigned)(q >> 28));
+    }
+    add_bins(cl, sm, sm.d_count, sm.d_mass, 1 << kDigit, [&](int i, unsigned& c, u64& m) {
+      for (int r = 0; r < C; ++r) {
+        const Smem<LOW>* o = cl.map_shared_rank(&sm, r);
+        c += o->part[0][i];
+        m += (u64)o->part[1][i] + ((u64)o->part[2][i] << 14) + ((u64)o->part[3][i] << 28);
+      }
+    });
+    Bins(sm.d_count, sm.d_mass, 1 << kDigit, above_count, above_mass, sm.scan, nullptr)
+        .find(sm, by_mass, want);
+    prefix = prefix << bits | sm.bin;
     above_count = sm.above_count;
     above_mass = sm.above_mass;
   }
-  *mass = above_mass + sm.mass[sm.digit];
-  return prefix;
+  // the tokens of the bin, of all CTAs
+  if (tid == 0) sm.n_list = 0;
+  __syncthreads();
+  for (int i = tid; i < n; i += kThreads) {
+    const u64 key = key_of(w[i], j0 + i);
+    if (key >> shift == prefix) sm.list[atomicAdd(&sm.n_list, 1)] = key;
+  }
+  cl.sync();
+  int total = 0, at = -1;
+  const u64* from = nullptr;
+  for (int r = 0; r < C; ++r) {
+    const Smem<LOW>* o = cl.map_shared_rank(&sm, r);
+    const int m = o->n_list;
+    if (tid >= total && tid < total + m) {
+      from = o->list;
+      at = tid - total;
+    }
+    total += m;
+  }
+  const u64 key = from ? from[at] : 0;
+  if (from) sm.all[tid] = key;
+  __syncthreads();
+  if (from) {  // (total <= kList = kThreads)
+    u64 c = above_count, m = above_mass;
+    for (int i = 0; i < total; ++i) {
+      const u64 other = sm.all[i];
+      if (other > key) {
+        ++c;
+        m += weight_of_key(other);
+      }
+    }
+    const u64 q = weight_of_key(key);
+    if (by_mass ? m < want && want <= m + q : c + 1 == want) {
+      sm.key = key;
+      sm.above_mass = m + q;
+    }
+  }
+  __syncthreads();
+  *mass = sm.above_mass;
+  const u64 found = sm.key;
+  cl.sync();  // the lists have been read
+  return found;
 }
 
+// The slice into shared memory as fp32; its largest, and whether it holds a NaN.  16-byte groups
+// between the first and the last boundary; `w` starts where such a group falls on one, too.
 template <typename TI>
-__device__ __forceinline__ float value(const TI* p) {
-  return (float)*p;
+__device__ __forceinline__ void load_slice(const TI* x, int n, float* w, float& mx, bool& bad) {
+  constexpr int G = 16 / (int)sizeof(TI);
+  const int tid = threadIdx.x;
+  const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15u)) % 16 / sizeof(TI)));
+  const int groups = (n - head) / G;
+  auto take = [&](float v) {
+    mx = fmaxf(mx, v);
+    bad |= v != v;
+  };
+  for (int i = tid; i < head; i += kThreads) take(w[i] = (float)x[i]);
+  for (int i = head + groups * G + tid; i < n; i += kThreads) take(w[i] = (float)x[i]);
+  const uint4* xs = reinterpret_cast<const uint4*>(x + head);
+  float* ws = w + head;
+  constexpr int kAhead = 4;
+  for (int g0 = tid; g0 < groups; g0 += kAhead * kThreads) {
+    uint4 r[kAhead];
+#pragma unroll
+    for (int t = 0; t < kAhead; ++t)
+      if (g0 + t * kThreads < groups) r[t] = __ldg(xs + g0 + t * kThreads);
+#pragma unroll
+    for (int t = 0; t < kAhead; ++t) {
+      const int g = g0 + t * kThreads;
+      if (g >= groups) break;
+      const uint32_t u[4] = {r[t].x, r[t].y, r[t].z, r[t].w};
+      float v[G];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (sizeof(TI) == 4) {
+          v[e] = __uint_as_float(u[e]);
+        } else {
+          v[2 * e] = __uint_as_float(u[e] << 16);
+          v[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < G; e += 4) {
+        *reinterpret_cast<float4*>(ws + g * G + e) = make_float4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        take(v[e]);
+        take(v[e + 1]);
+        take(v[e + 2]);
+        take(v[e + 3]);
+      }
+    }
+  }
 }
 
-template <typename TI>
+template <typename TI, int LOW>
 __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int slice) {
+  using S = Smem<LOW>;
   extern __shared__ __align__(16) unsigned char raw[];
-  Smem& sm = *reinterpret_cast<Smem*>(raw);
-  float* w = reinterpret_cast<float*>(raw + sizeof(Smem));
+  S& sm = *reinterpret_cast<S*>(raw);
   cg::cluster_group cl = cg::this_cluster();
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   const int row = (int)blockIdx.x / C, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -180,20 +321,20 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
   const float temperature = p.temperature ? p.temperature[row] : 1.f, u = p.u[row];
   const bool greedy = temperature == 0.f;
   const float scale = greedy ? 1.f : __fdiv_rn(1.f, temperature);
-  int k = greedy ? 1 : p.top_k ? p.top_k[row] : 0;
+  const int k = greedy ? 1 : p.top_k ? p.top_k[row] : 0;
   const float top_p = p.top_p ? p.top_p[row] : 1.f;
   const float min_p = p.min_p ? fminf(p.min_p[row], 1.f) : 0.f;
   const bool valid = temperature >= 0.f && temperature < INFINITY && u >= 0.f && u <= 1.f;
+  const bool by_k = k > 0 && k < p.V, by_p = top_p < 1.f;
   // the slice, and the row's largest logit
   const TI* x = reinterpret_cast<const TI*>(p.logits) + (long long)row * p.s_row + j0;
+  float* w = reinterpret_cast<float*>(raw + (sizeof(S) + 15) / 16 * 16);
+  w += (4 - (16 - (reinterpret_cast<uintptr_t>(x) & 15u)) % 16 / sizeof(TI) % 4) % 4;
   float mx = -INFINITY;
   bool bad = false;
-  for (int i = tid; i < n; i += kThreads) {
-    const float v = value(x + i);
-    w[i] = v;
-    mx = fmaxf(mx, v);
-    bad |= v != v;
-  }
+  load_slice<TI>(x, n, w, mx, bad);
+  if (by_k || by_p)
+    for (int i = tid; i < 2 * S::kBins; i += kThreads) (&sm.hist[0][0])[i] = 0;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   if (lane == 0) sm.red[warp] = mx;
@@ -207,7 +348,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
   float M = -INFINITY;
   bool nan = false;
   for (int r = 0; r < C; ++r) {
-    const Smem* o = cl.map_shared_rank(&sm, r);
+    const S* o = cl.map_shared_rank(&sm, r);
     M = fmaxf(M, o->max);
     nan |= o->nan != 0;
   }
@@ -221,97 +362,109 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
     cl.sync();  // sm.max has been read
     return;
   }
-  for (int i = tid; i < n; i += kThreads) {
+  // the weights.  Every thread takes a run of the slice of odd length, so that neither the lanes'
+  // accesses collide nor the index order is lost.
+  const int len = (slice + kThreads - 1) / kThreads | 1, i0 = min(n, tid * len), i1 = min(n, i0 + len);
+  u64 sum = 0;
+  for (int i = i0; i < i1; ++i) {
     const float v = w[i];
-    w[i] = v == M ? 1.f : greedy ? 0.f : expf(__fmul_rn(__fsub_rn(v, M), scale));
-  }
-  __syncthreads();
-  u64 least = 0, mass = ~0ull;
-  if (k > 0 && k < p.V) least = find_key(cl, sm, w, n, j0, 0, false, (u64)k, &mass);
-  if (top_p < 1.f) {
-    if (mass == ~0ull) {  // of all tokens
-      u64 s = 0;
-      for (int i = tid; i < n; i += kThreads) s += fixed_of(w[i]);
-      s = warp_sum(s);
-      if (lane == 0) sm.warp_sum[warp] = s;
-      __syncthreads();
-      if (tid == 0) {
-        for (int i = 1; i < kWarps; ++i) s += sm.warp_sum[i];
-        sm.total = s;
+    const float e = v == M ? 1.f : greedy ? 0.f : expf(__fmul_rn(__fsub_rn(v, M), scale));
+    w[i] = e;
+    if (by_k || by_p) {
+      const unsigned bits = __float_as_uint(e);
+      const int bin = (int)(bits >> LOW) - (kFirst << (23 - LOW));
+      if (bin >= 0) {
+        atomicAdd(&sm.hist[0][bin], 1u);
+        atomicAdd(&sm.hist[1][bin], low_part<LOW>(bits));
       }
-      cl.sync();
-      mass = 0;
-      for (int r = 0; r < C; ++r) mass += cl.map_shared_rank(&sm, r)->total;
-      cl.sync();  // sm.total has been read
+    } else if (!(e < min_p)) {
+      sum += fixed_of(e);
     }
-    const long long want = (long long)floor((double)top_p * (double)(long long)mass);
-    least = find_key(cl, sm, w, n, j0, least, true, (u64)max(want, 1LL), &mass);
   }
-  // kept weights of every warp's stretch, then of every CTA
-  const int seg = (slice / kWarps + 31) / 32 * 32 + 32, i0 = min(n, warp * seg), i1 = min(n, i0 + seg);
+  u64 least = 0;
+  if (by_k || by_p) {
+    add_bins(cl, sm, sm.count, sm.mass, S::kBins, [&](int i, unsigned& c, u64& m) {
+      u64 low = 0;
+      for (int r = 0; r < C; ++r) {
+        const S* o = cl.map_shared_rank(&sm, r);
+        c += o->hist[0][i];
+        low += o->hist[1][i];
+      }
+      m = mass_of<LOW>(i, c, low);
+    });
+    const Bins bins(sm.count, sm.mass, S::kBins, 0, 0, sm.scan, &sm.total);
+    __syncthreads();
+    u64 mass = sm.total;
+    if (by_k) {
+      bins.find(sm, false, (u64)k);
+      if (sm.inside) least = find_key<LOW>(cl, sm, w, n, j0, false, (u64)k, &mass);
+    }
+    if (by_p) {
+      const long long want = (long long)floor((double)top_p * (double)(long long)mass);
+      bins.find(sm, true, (u64)max(want, 1LL));
+      least = find_key<LOW>(cl, sm, w, n, j0, true, (u64)max(want, 1LL), &mass);
+    }
+  }
+  // the kept weights of this thread's run, in the order of the indices
+  const unsigned least_w = (unsigned)(least >> kIndexBits);
+  const int last_j = (1 << kIndexBits) - 1 - (int)(least & ((1 << kIndexBits) - 1));
   auto weight = [&](int i) -> u64 {
-    const float v = w[i];
-    return key_of(v, j0 + i) >= least && !(v < min_p) ? fixed_of(v) : 0;
+    const unsigned bits = __float_as_uint(w[i]);
+    const bool in = bits > least_w || (bits == least_w && j0 + i <= last_j);
+    return in && !(w[i] < min_p) ? fixed_of(w[i]) : 0;
   };
-  u64 s = 0;
-  for (int i = i0 + lane; i < i1; i += 32) s += weight(i);
-  s = warp_sum(s);
-  if (lane == 0) sm.warp_sum[warp] = s;
-  __syncthreads();
-  if (tid == 0) {
-    u64 t = 0;
-    for (int i = 0; i < kWarps; ++i) t += sm.warp_sum[i];
-    sm.total = t;
-  }
+  if (by_k || by_p)
+    for (int i = i0; i < i1; ++i) sum += weight(i);
+  u64 before = sum, none = 0;
+  block_scan(sm.scan, before, none);
+  if (tid == kThreads - 1) sm.kept = before + sum;
   cl.sync();
-  u64 total = 0, before = 0;
+  u64 total = 0;
   for (int r = 0; r < C; ++r) {
-    const u64 t = cl.map_shared_rank(&sm, r)->total;
+    const u64 t = cl.map_shared_rank(&sm, r)->kept;
     if (r < rank) before += t;
     total += t;
   }
   const u64 target =
       (u64)min((long long)floor((double)u * (double)(long long)total), (long long)total - 1);
-  for (int i = 0; i < warp; ++i) before += sm.warp_sum[i];
-  if (before <= target && target < before + s) {  // this warp's stretch
-    for (int i = i0; i < i1; i += 32) {
-      const u64 own = i + lane < i1 ? weight(i + lane) : 0;
-      u64 run = own;
-#pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const u64 t = __shfl_up_sync(0xffffffffu, run, o);
-        if (lane >= o) run += t;
-      }
-      if (before + run - own <= target && target < before + run) {
-        const float sum = logf(__fmul_rn((float)(long long)total, 1.f / 1099511627776.f));
-        p.token[row] = j0 + i + lane;
-        p.logprob[row] = logf(w[i + lane]) - sum;
-        p.logz[row] = __fadd_rn(__fmul_rn(M, scale), sum);
-      }
-      before += __shfl_sync(0xffffffffu, run, 31);
+  if (before <= target && target < before + sum) {  // this thread's run
+    int i = i0;
+    for (;; ++i) {
+      before += weight(i);
       if (before > target) break;
     }
+    const float log_sum = logf(__fmul_rn((float)(long long)total, 1.f / 1099511627776.f));
+    p.token[row] = j0 + i;
+    p.logprob[row] = logf(w[i]) - log_sum;
+    p.logz[row] = __fadd_rn(__fmul_rn(M, scale), log_sum);
   }
   cl.sync();  // the other CTAs' shared memory has been read
+}
+
+template <typename TI, int LOW>
+cudaError_t launch_low(const SampleProblem& p, int cluster, int slice, cudaStream_t s) {
+  const int smem = ((int)sizeof(Smem<LOW>) + 15) / 16 * 16 + (slice + 4) * (int)sizeof(float);
+  cudaError_t e = cudaFuncSetAttribute(sample_kernel<TI, LOW>,
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e != cudaSuccess) { note_failure("sample: shared memory"); return e; }
+  e = launch_pdl(sample_kernel<TI, LOW>, dim3((unsigned)p.R * cluster), kThreads, smem, s, cluster, p,
+                 slice);
+  if (e != cudaSuccess) note_failure("sample: launch");
+  return e;
 }
 
 template <typename TI>
 cudaError_t launch_t(const SampleProblem& p, cudaStream_t s) {
   int cluster = 1;  // at least 4096 tokens per CTA
   while (cluster < kMaxCluster && p.V > 4096 * cluster) cluster *= 2;
-  const int slice = (p.V / cluster + 7) / 8 * 8 + 8;
-  const int smem = (int)sizeof(Smem) + slice * (int)sizeof(float);
-  cudaError_t e = cudaFuncSetAttribute(sample_kernel<TI>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                       smem);
-  if (e != cudaSuccess) { note_failure("sample: shared memory"); return e; }
-  e = launch_pdl(sample_kernel<TI>, dim3((unsigned)p.R * cluster), kThreads, smem, s, cluster, p, slice);
-  if (e != cudaSuccess) note_failure("sample: launch");
-  return e;
+  const int slice = ((p.V + cluster - 1) / cluster + 7) / 8 * 8;
+  if (slice <= 1 << (32 - low_bits(false))) return launch_low<TI, low_bits(false)>(p, cluster, slice, s);
+  return launch_low<TI, low_bits(true)>(p, cluster, slice, s);
 }
 
 }  // namespace sample
 
-int sample_max_vocabulary() { return sample::kMaxCluster * (sample::kMaxSlice - 16); }
+int sample_max_vocabulary() { return sample::kMaxCluster * sample::kMaxSlice; }
 
 cudaError_t launch_sample(const SampleProblem& p, cudaStream_t s) {
   if (p.dtype == RELATION_F32) return sample::launch_t<float>(p, s);
