@@ -37,7 +37,8 @@ constexpr int kMaxSlice = 32 * 1024;  // tokens of a CTA
 constexpr int kIndexBits = 22;        // of the key: 30 bits of w, then the index from the top down
 constexpr int kFirst = 87;            // the exponent of 2^-40, below which a weight is 0
 constexpr int kDigit = 8;             // further digits
-constexpr int kList = 512;            // tokens that are ranked against each other
+constexpr int kList = 768;            // tokens that are ranked against each other
+constexpr int kAlone = 128;           // so few that every CTA ranks them all
 
 // A slice of at most 2^(32 - LOW) tokens: its bins' sums of LOW-bit numbers stay below 2^32.
 constexpr int low_bits(bool wide) { return wide ? 17 : 18; }
@@ -46,24 +47,38 @@ constexpr int bins_of(int low) { return ((127 - kFirst) << (23 - low)) + 1; }
 template <int LOW>
 struct Smem {
   static constexpr int kBins = bins_of(LOW);
-  unsigned hist[2][kBins];      // this CTA's bins: tokens, sums of the low bits
-  unsigned count[kBins];        // the cluster's: tokens and masses
+  union {
+    unsigned hist[2][kBins];          // this CTA's bins: tokens, sums of the low bits
+    struct {                          // later:
+      unsigned part[4][1 << kDigit];  // a digit's histogram: tokens, the masses in 14-bit parts,
+      unsigned d_count[1 << kDigit];  // the cluster's
+      u64 d_mass[1 << kDigit];
+    };
+    struct {                          // and in turn:
+      u64 all[kList];                 // keys of the cluster's tokens in the cut's bin
+      u64 extra[kThreads];            // kept mass of every run that lies in that bin
+    };
+  };
+  unsigned count[kBins];              // the cluster's bins: tokens and masses
   u64 mass[kBins];
-  unsigned part[4][1 << kDigit];  // a digit's histogram: tokens, the masses in 14-bit parts;
-  unsigned d_count[1 << kDigit];  // the cluster's
-  u64 d_mass[1 << kDigit];
-  u64 list[kList];              // keys of the tokens in the cut's bin: this CTA's,
-  u64 all[kList];               // the cluster's
-  u64 scan[2][kWarps], total, kept;
-  float red[kWarps], max;
-  int nan, n_list;
+  u64 list[2][kList];                 // this CTA's tokens in the cut's bin, of the first and second cut
+  int sizes[2][kMaxCluster], n_list;  // every CTA's number of them
+  u64 scan[2][kWarps], total;
+  u64 kept[kMaxCluster];              // of every CTA: its kept mass,
+  float max[kMaxCluster];             // its largest logit (NaN: it has one)
+  float red[kWarps];
   // what the threads tell each other
   unsigned bin, inside;
-  u64 above_count, above_mass, key;
+  u64 above_count, above_mass, key, key_mass;
 };
 
+// floor(2^40 w) for 0 <= w <= 1 from the bits of w.  (The conversion instruction to 64 bits bounds a
+// pass over the weights: 64 rows of 131072 take 35 us with it.)
 __device__ __forceinline__ u64 fixed_of(float w) {
-  return __float2ull_rz(w * 1099511627776.f);  // 2^40 w: the product is exact
+  const unsigned bits = __float_as_uint(w);
+  const int left = (int)(bits >> 23) - 110;
+  const unsigned top = (bits & 0x7fffffu) | 0x800000u;
+  return left >= 0 ? (u64)top << left : (u64)(top >> min(-left, 31));
 }
 __device__ __forceinline__ u64 key_of(float w, int j) {
   return (u64)__float_as_uint(w) << kIndexBits | (u64)((1 << kIndexBits) - 1 - j);
@@ -110,9 +125,11 @@ __device__ __forceinline__ void block_scan(u64 (*part)[kWarps], u64& a, u64& b) 
   __syncthreads();
   a = as - a;
   b = bs - b;
-  for (int i = 0; i < warp; ++i) {
-    a += part[0][i];
-    b += part[1][i];
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) {
+    const u64 x = part[0][i], y = part[1][i];
+    a += i < warp ? x : 0;
+    b += i < warp ? y : 0;
   }
 }
 
@@ -179,20 +196,28 @@ __device__ __forceinline__ void add_bins(cg::cluster_group& cl, S& sm, unsigned*
   cl.sync();
 }
 
+// A thread's run of the slice, w[i0 .. i1).
+struct Run {
+  int i0, i1, len;
+};
+
 // The key of the cut that lies in sm.bin, among sm.inside tokens, and the mass down to and with it.
+// *above (if set) gets the mass of this thread's run down to the cut, without weights below min_p.
 template <int LOW>
-__device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, const float* w, int n,
-                                        int j0, bool by_mass, u64 want, u64* mass) {
-  const int tid = threadIdx.x, C = (int)cl.num_blocks();
+__device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, const float* w,
+                                        const Run& run, int j0, int which, bool by_mass, u64 want,
+                                        float min_p, u64* mass, u64* above) {
+  const int tid = threadIdx.x, C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   u64 prefix = sm.bin + ((u64)kFirst << (23 - LOW));  // the key's bits from `shift` up
   int shift = kIndexBits + LOW;
   u64 above_count = sm.above_count, above_mass = sm.above_mass;
   while (sm.inside > kList) {
     const int bits = min(kDigit, shift);
     shift -= bits;
+    __syncthreads();
     for (int i = tid; i < 4 << kDigit; i += kThreads) (&sm.part[0][0])[i] = 0;
     __syncthreads();
-    for (int i = tid; i < n; i += kThreads) {
+    for (int i = run.i0; i < run.i1; ++i) {
       const u64 key = key_of(w[i], j0 + i);
       if (key >> (shift + bits) != prefix) continue;
       const unsigned d = (unsigned)(key >> shift) & ((1u << bits) - 1);
@@ -203,7 +228,9 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
       atomicAdd(&sm.part[3][d], (unsigned)(q >> 28));
     }
     add_bins(cl, sm, sm.d_count, sm.d_mass, 1 << kDigit, [&](int i, unsigned& c, u64& m) {
-      for (int r = 0; r < C; ++r) {
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        if (r >= C) break;
         const Smem<LOW>* o = cl.map_shared_rank(&sm, r);
         c += o->part[0][i];
         m += (u64)o->part[1][i] + ((u64)o->part[2][i] << 14) + ((u64)o->part[3][i] << 28);
@@ -215,62 +242,118 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
     above_count = sm.above_count;
     above_mass = sm.above_mass;
   }
-  // the tokens of the bin, of all CTAs
+  // The bin's tokens, of all CTAs, and the run's mass above it.  (Mostly the weight's bits alone
+  // tell where a token lies.)
   if (tid == 0) sm.n_list = 0;
   __syncthreads();
-  for (int i = tid; i < n; i += kThreads) {
-    const u64 key = key_of(w[i], j0 + i);
-    if (key >> shift == prefix) sm.list[atomicAdd(&sm.n_list, 1)] = key;
-  }
-  cl.sync();
-  int total = 0, at = -1;
-  const u64* from = nullptr;
-  for (int r = 0; r < C; ++r) {
-    const Smem<LOW>* o = cl.map_shared_rank(&sm, r);
-    const int m = o->n_list;
-    if (tid >= total && tid < total + m) {
-      from = o->list;
-      at = tid - total;
+  u64* list = sm.list[which];
+  u64 sum = 0;
+  const unsigned high = shift >= kIndexBits ? (unsigned)prefix : 0;
+#pragma unroll 4
+  for (int i = run.i0; i < run.i1; ++i) {
+    const float x = w[i];
+    bool in, over;
+    if (shift >= kIndexBits) {
+      const unsigned bits = __float_as_uint(x) >> (shift - kIndexBits);
+      in = bits == high;
+      over = bits > high;
+    } else {
+      const u64 key = key_of(x, j0 + i) >> shift;
+      in = key == prefix;
+      over = key > prefix;
     }
+    if (in) list[atomicAdd(&sm.n_list, 1)] = key_of(x, j0 + i);
+    if (over && !(x < min_p)) sum += fixed_of(x);
+  }
+  __syncthreads();
+  const int mine = sm.n_list;
+  if (tid < C) cl.map_shared_rank(&sm, tid)->sizes[which][rank] = mine;
+  cl.sync();
+  int total = 0;  // <= kList
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) {
+    if (r >= C) break;
+    const int m = sm.sizes[which][r];
+    const u64* from = cl.map_shared_rank(list, r);
+    for (int i = tid; i < m; i += kThreads) sm.all[total + i] = from[i];
     total += m;
   }
-  const u64 key = from ? from[at] : 0;
-  if (from) sm.all[tid] = key;
+  sm.extra[tid] = 0;
   __syncthreads();
-  if (from) {  // (total <= kList = kThreads)
-    u64 c = above_count, m = above_mass;
-    for (int i = 0; i < total; ++i) {
+  // Few tokens: every CTA ranks them all.  More: its own, and tells the others of the cut.
+  const bool alone = total <= kAlone;
+  const u64* ranked = alone ? sm.all : list;
+  const int n_ranked = alone ? total : mine;
+  int group = 32;  // threads of a token
+  while (group > 1 && n_ranked * group > kThreads) group >>= 1;
+  const int sub = tid % group;
+  for (int g0 = 0; g0 < n_ranked; g0 += kThreads / group) {
+    const int g = g0 + tid / group;
+    const u64 key = g < n_ranked ? ranked[g] : ~0ull;
+    u64 c = 0, m = 0;
+#pragma unroll 4
+    for (int i = sub; i < total; i += group) {
       const u64 other = sm.all[i];
       if (other > key) {
         ++c;
         m += weight_of_key(other);
       }
     }
-    const u64 q = weight_of_key(key);
-    if (by_mass ? m < want && want <= m + q : c + 1 == want) {
-      sm.key = key;
-      sm.above_mass = m + q;
+    for (int o = group >> 1; o > 0; o >>= 1) {
+      c += __shfl_xor_sync(0xffffffffu, c, o);
+      m += __shfl_xor_sync(0xffffffffu, m, o);
+    }
+    if (g < n_ranked && sub == 0) {
+      c += above_count;
+      m += above_mass;
+      const u64 q = weight_of_key(key);
+      if (by_mass ? m < want && want <= m + q : c + 1 == want) {
+        for (int r = 0; r < C; ++r) {
+          Smem<LOW>* o = alone ? &sm : cl.map_shared_rank(&sm, r);
+          o->key = key;
+          o->key_mass = m + q;
+          if (alone) break;
+        }
+      }
     }
   }
-  __syncthreads();
-  *mass = sm.above_mass;
+  if (alone)
+    __syncthreads();
+  else
+    cl.sync();
   const u64 found = sm.key;
-  cl.sync();  // the lists have been read
+  *mass = sm.key_mass;
+  if (above) {
+    for (int i = tid; i < mine; i += kThreads) {
+      const u64 key = list[i];
+      const int at = (1 << kIndexBits) - 1 - (int)(key & ((1 << kIndexBits) - 1)) - j0;
+      if (key >= found && !(__uint_as_float((unsigned)(key >> kIndexBits)) < min_p))
+        atomicAdd(&sm.extra[at / run.len], weight_of_key(key));
+    }
+    __syncthreads();
+    *above = sum + sm.extra[tid];
+  }
+  __syncthreads();  // (sm.key and the lists' neighbours are written again)
   return found;
 }
 
-// The slice into shared memory as fp32; its largest, and whether it holds a NaN.  16-byte groups
+// The larger of two, NaN if one is
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+
+// The slice into shared memory as fp32, and its largest (NaN if it holds one).  16-byte groups
 // between the first and the last boundary; `w` starts where such a group falls on one, too.
 template <typename TI>
-__device__ __forceinline__ void load_slice(const TI* x, int n, float* w, float& mx, bool& bad) {
+__device__ __forceinline__ float load_slice(const TI* x, int n, float* w) {
   constexpr int G = 16 / (int)sizeof(TI);
   const int tid = threadIdx.x;
   const int head = min(n, (int)((16 - (reinterpret_cast<uintptr_t>(x) & 15u)) % 16 / sizeof(TI)));
   const int groups = (n - head) / G;
-  auto take = [&](float v) {
-    mx = fmaxf(mx, v);
-    bad |= v != v;
-  };
+  float mx = -INFINITY;
+  auto take = [&](float v) { mx = max_nan(mx, v); };
   for (int i = tid; i < head; i += kThreads) take(w[i] = (float)x[i]);
   for (int i = head + groups * G + tid; i < n; i += kThreads) take(w[i] = (float)x[i]);
   const uint4* xs = reinterpret_cast<const uint4*>(x + head);
@@ -306,6 +389,7 @@ __device__ __forceinline__ void load_slice(const TI* x, int n, float* w, float& 
       }
     }
   }
+  return mx;
 }
 
 template <typename TI, int LOW>
@@ -330,28 +414,22 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
   const TI* x = reinterpret_cast<const TI*>(p.logits) + (long long)row * p.s_row + j0;
   float* w = reinterpret_cast<float*>(raw + (sizeof(S) + 15) / 16 * 16);
   w += (4 - (16 - (reinterpret_cast<uintptr_t>(x) & 15u)) % 16 / sizeof(TI) % 4) % 4;
-  float mx = -INFINITY;
-  bool bad = false;
-  load_slice<TI>(x, n, w, mx, bad);
+  float mx = load_slice<TI>(x, n, w);
   if (by_k || by_p)
     for (int i = tid; i < 2 * S::kBins; i += kThreads) (&sm.hist[0][0])[i] = 0;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+  for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   if (lane == 0) sm.red[warp] = mx;
-  bad = __syncthreads_or(bad);
-  if (tid == 0) {
-    for (int i = 1; i < kWarps; ++i) mx = fmaxf(mx, sm.red[i]);
-    sm.max = mx;
-    sm.nan = bad;
+  __syncthreads();
+  if (tid < C) {  // to every CTA
+#pragma unroll
+    for (int i = 0; i < kWarps; ++i) mx = max_nan(mx, sm.red[i]);
+    cl.map_shared_rank(&sm, tid)->max[rank] = mx;
   }
   cl.sync();
   float M = -INFINITY;
-  bool nan = false;
-  for (int r = 0; r < C; ++r) {
-    const S* o = cl.map_shared_rank(&sm, r);
-    M = fmaxf(M, o->max);
-    nan |= o->nan != 0;
-  }
+  for (int r = 0; r < C; ++r) M = max_nan(M, sm.max[r]);
+  const bool nan = M != M;
   if (!valid || nan || M == -INFINITY) {  // (the same in every CTA of the cluster)
     if (rank == 0 && tid == 0) {
       p.token[row] = -1;
@@ -359,16 +437,19 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
       p.logz[row] = valid && !nan ? -INFINITY : NAN;
       if (!valid && p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
     }
-    cl.sync();  // sm.max has been read
     return;
   }
   // the weights.  Every thread takes a run of the slice of odd length, so that neither the lanes'
   // accesses collide nor the index order is lost.
   const int len = (slice + kThreads - 1) / kThreads | 1, i0 = min(n, tid * len), i1 = min(n, i0 + len);
+  const Run run{i0, i1, len};
+  // (greedy: a difference times infinity)
+  const float slope = greedy ? INFINITY : scale;
   u64 sum = 0;
+#pragma unroll 4
   for (int i = i0; i < i1; ++i) {
     const float v = w[i];
-    const float e = v == M ? 1.f : greedy ? 0.f : expf(__fmul_rn(__fsub_rn(v, M), scale));
+    const float e = v == M ? 1.f : expf(__fmul_rn(__fsub_rn(v, M), slope));
     w[i] = e;
     if (by_k || by_p) {
       const unsigned bits = __float_as_uint(e);
@@ -384,28 +465,42 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
   u64 least = 0;
   if (by_k || by_p) {
     add_bins(cl, sm, sm.count, sm.mass, S::kBins, [&](int i, unsigned& c, u64& m) {
+      unsigned cs[kMaxCluster], ls[kMaxCluster];  // (all in flight)
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        const S* o = cl.map_shared_rank(&sm, min(r, C - 1));
+        cs[r] = o->hist[0][i];
+        ls[r] = o->hist[1][i];
+      }
       u64 low = 0;
-      for (int r = 0; r < C; ++r) {
-        const S* o = cl.map_shared_rank(&sm, r);
-        c += o->hist[0][i];
-        low += o->hist[1][i];
+#pragma unroll
+      for (int r = 0; r < kMaxCluster; ++r) {
+        c += r < C ? cs[r] : 0;
+        low += r < C ? ls[r] : 0;
       }
       m = mass_of<LOW>(i, c, low);
     });
     const Bins bins(sm.count, sm.mass, S::kBins, 0, 0, sm.scan, &sm.total);
     __syncthreads();
     u64 mass = sm.total;
+    bool summed = false;
     if (by_k) {
       bins.find(sm, false, (u64)k);
-      if (sm.inside) least = find_key<LOW>(cl, sm, w, n, j0, false, (u64)k, &mass);
+      if (sm.inside) {
+        least = find_key<LOW>(cl, sm, w, run, j0, 0, false, (u64)k, min_p, &mass, by_p ? nullptr : &sum);
+        summed = !by_p;
+      }
     }
     if (by_p) {
       const long long want = (long long)floor((double)top_p * (double)(long long)mass);
       bins.find(sm, true, (u64)max(want, 1LL));
-      least = find_key<LOW>(cl, sm, w, n, j0, true, (u64)max(want, 1LL), &mass);
+      least = find_key<LOW>(cl, sm, w, run, j0, 1, true, (u64)max(want, 1LL), min_p, &mass, &sum);
+      summed = true;
     }
+    if (!summed)  // fewer than k tokens with a weight
+      for (int i = i0; i < i1; ++i) sum += w[i] < min_p ? 0 : fixed_of(w[i]);
   }
-  // the kept weights of this thread's run, in the order of the indices
+  // the kept weights in the order of the indices
   const unsigned least_w = (unsigned)(least >> kIndexBits);
   const int last_j = (1 << kIndexBits) - 1 - (int)(least & ((1 << kIndexBits) - 1));
   auto weight = [&](int i) -> u64 {
@@ -413,32 +508,41 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
     const bool in = bits > least_w || (bits == least_w && j0 + i <= last_j);
     return in && !(w[i] < min_p) ? fixed_of(w[i]) : 0;
   };
-  if (by_k || by_p)
-    for (int i = i0; i < i1; ++i) sum += weight(i);
   u64 before = sum, none = 0;
   block_scan(sm.scan, before, none);
-  if (tid == kThreads - 1) sm.kept = before + sum;
-  cl.sync();
+  if (tid == kThreads - 1) sm.total = before + sum;
+  __syncthreads();
+  if (tid < C) cl.map_shared_rank(&sm, tid)->kept[rank] = sm.total;
+  cl.sync();  // (the last access to another CTA's shared memory)
   u64 total = 0;
   for (int r = 0; r < C; ++r) {
-    const u64 t = cl.map_shared_rank(&sm, r)->kept;
-    if (r < rank) before += t;
-    total += t;
+    if (r < rank) before += sm.kept[r];
+    total += sm.kept[r];
   }
   const u64 target =
       (u64)min((long long)floor((double)u * (double)(long long)total), (long long)total - 1);
-  if (before <= target && target < before + sum) {  // this thread's run
-    int i = i0;
-    for (;; ++i) {
-      before += weight(i);
-      if (before > target) break;
+  const unsigned hit = __ballot_sync(0xffffffffu, before <= target && target < before + sum);
+  if (!hit) return;
+  // the warp goes through the run that was hit
+  const int owner = __ffs(hit) - 1, stop = __shfl_sync(0xffffffffu, i1, owner);
+  before = __shfl_sync(0xffffffffu, before, owner);
+  for (int i = __shfl_sync(0xffffffffu, i0, owner); i < stop; i += 32) {
+    const u64 own = i + lane < stop ? weight(i + lane) : 0;
+    u64 upto = own;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const u64 t = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += t;
     }
-    const float log_sum = logf(__fmul_rn((float)(long long)total, 1.f / 1099511627776.f));
-    p.token[row] = j0 + i;
-    p.logprob[row] = logf(w[i]) - log_sum;
-    p.logz[row] = __fadd_rn(__fmul_rn(M, scale), log_sum);
+    if (before + upto - own <= target && target < before + upto) {
+      const float log_sum = logf(__fmul_rn((float)(long long)total, 1.f / 1099511627776.f));
+      p.token[row] = j0 + i + lane;
+      p.logprob[row] = logf(w[i + lane]) - log_sum;
+      p.logz[row] = __fadd_rn(__fmul_rn(M, scale), log_sum);
+    }
+    before += __shfl_sync(0xffffffffu, upto, 31);
+    if (before > target) break;
   }
-  cl.sync();  // the other CTAs' shared memory has been read
 }
 
 template <typename TI, int LOW>
