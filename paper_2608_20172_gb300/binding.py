@@ -494,6 +494,11 @@ def decode(q, k_cache, v_cache, lengths, lam: float, tau_s: float = 2.0, *, out=
     return out, logz
 
 
+# The calls of a serving step are short, so that the host's time counts: one expression checks what
+# a call needs, and the reason is looked for only where it fails.
+_I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
+
+
 class PagePlan(NamedTuple):
     """What page_plan returns; the block table and the free pages are updated in place."""
     slots: torch.Tensor       # int64 [n_tokens]: page * page_size + row, -1 for padding
@@ -503,11 +508,17 @@ class PagePlan(NamedTuple):
     free_state: torch.Tensor  # int32 [2]: head and count of the ring of free pages after it
 
 
-def _int32(name, t, device, shape=None):
-    if t.dtype != torch.int32 or not t.is_contiguous() or t.device != device or not t.is_cuda:
-        raise ValueError(f"{name} must be a contiguous int32 tensor on the operands' CUDA device")
-    if shape is not None and t.shape != shape:
-        raise ValueError(f"{name} must have shape {tuple(shape)}")
+def _need(name, t, device, dtype, count):
+    """Raise unless t is a contiguous CUDA tensor of `count` entries of this dtype on the device."""
+    if t.dtype is not dtype or not t.is_contiguous() or t.numel() != count or \
+            t.get_device() != device or device < 0:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of {count} entries on the "
+                         "operands' CUDA device")
+
+
+def _is_table(t, B, device):
+    return t.dtype is _I32 and t.dim() == 2 and t.shape[0] == B and t.stride(1) == 1 and \
+        t.get_device() == device
 
 
 def page_plan(lengths, counts, block_table, free_pages, free_state, page_size: int, n_tokens: int,
@@ -516,35 +527,30 @@ def page_plan(lengths, counts, block_table, free_pages, free_state, page_size: i
     < 0: the request has ended), block_table int32 [B, cols] (rows may be strided) and the ring
     free_pages int32 [n_pages], both updated in place, free_state int32 [2] = (head, count).
     ``n_tokens`` is the size of the step's token buffer.  See relation_page_plan."""
-    dev, B = lengths.device, lengths.numel()
-    _int32("lengths", lengths, dev)
-    _int32("counts", counts, dev, lengths.shape)
-    _int32("free_pages", free_pages, dev)
-    _int32("free_state", free_state, dev, (2,))
-    if block_table.dim() != 2 or block_table.shape[0] != B or block_table.dtype != torch.int32 or \
-            block_table.stride(1) != 1 or block_table.device != dev:
+    dev, B, n, n_pages = lengths.get_device(), lengths.numel(), int(n_tokens), free_pages.numel()
+    _need("lengths", lengths, dev, _I32, B)
+    _need("counts", counts, dev, _I32, B)
+    _need("free_pages", free_pages, dev, _I32, n_pages)
+    _need("free_state", free_state, dev, _I32, 2)
+    if not _is_table(block_table, B, dev):
         raise ValueError("block_table must be an int32 [B, cols] tensor with contiguous rows on "
                          "the operands' device")
-    if out is None:
-        # one allocation, the slots first: a step's call is bound by the host
-        words = 3 * int(n_tokens) + 2 * B + 3
-        buf = torch.empty(words, dtype=torch.int32, device=dev)
-        n = int(n_tokens)
-        slots, positions, starts, new, state = buf.split((2 * n, n, B + 1, B, 2))
-        out = PagePlan(slots.view(torch.int64), positions, starts, new, state)
+    if out is None:  # one allocation, the slots first
+        slots, positions, starts, new, state = torch.empty(
+            3 * n + 2 * B + 3, dtype=_I32, device=lengths.device).split((2 * n, n, B + 1, B, 2))
+        out = PagePlan(slots.view(_I64), positions, starts, new, state)
     else:
-        if out.slots.dtype != torch.int64 or out.slots.numel() != n_tokens or \
-                not out.slots.is_contiguous() or out.slots.device != dev:
-            raise ValueError("out.slots must be a contiguous int64 [n_tokens] tensor")
-        _int32("out.positions", out.positions, dev, (n_tokens,))
-        _int32("out.starts", out.starts, dev, (B + 1,))
-        _int32("out.lengths", out.lengths, dev, (B,))
-        _int32("out.free_state", out.free_state, dev, (2,))
-    rc = load().relation_page_plan(_ptr(lengths), _ptr(counts), B, int(page_size),
-                                   _ptr(block_table), block_table.shape[1], block_table.stride(0),
-                                   _ptr(free_pages), free_pages.numel(), _ptr(free_state),
-                                   _ptr(out.free_state), _ptr(out.lengths), _ptr(out.starts),
-                                   _ptr(out.slots), _ptr(out.positions), int(n_tokens),
+        slots, positions, starts, new, state = out
+        _need("out.slots", slots, dev, _I64, n)
+        _need("out.positions", positions, dev, _I32, n)
+        _need("out.starts", starts, dev, _I32, B + 1)
+        _need("out.lengths", new, dev, _I32, B)
+        _need("out.free_state", state, dev, _I32, 2)
+    rc = load().relation_page_plan(lengths.data_ptr(), counts.data_ptr(), B, int(page_size),
+                                   block_table.data_ptr(), block_table.shape[1],
+                                   block_table.stride(0), free_pages.data_ptr(), n_pages,
+                                   free_state.data_ptr(), state.data_ptr(), new.data_ptr(),
+                                   starts.data_ptr(), slots.data_ptr(), positions.data_ptr(), n,
                                    _ptr(dev_status), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_page_plan")
@@ -553,11 +559,15 @@ def page_plan(lengths, counts, block_table, free_pages, free_state, page_size: i
 
 def pages_of(k_pages, v_pages) -> Pages:
     """relation_pages of a pair of [n_pages, page_size, H, d] tensors with d contiguous."""
-    _same_layout(k_pages, v_pages)
-    st = k_pages.stride()
-    if len(st) != 4 or st[3] != 1:
-        raise ValueError("pages must be [n_pages, page_size, H, d] tensors with d contiguous")
-    return Pages(*k_pages.shape, *st[:3])
+    shape, st = k_pages.shape, k_pages.stride()
+    if v_pages is not k_pages and (v_pages.shape != shape or v_pages.stride() != st or
+                                   v_pages.dtype is not k_pages.dtype or
+                                   v_pages.get_device() != k_pages.get_device()):
+        raise ValueError("the keys' and the values' pages need the same shape, strides, dtype and "
+                         "device")
+    if len(st) != 4 or st[3] != 1 or k_pages.get_device() < 0:
+        raise ValueError("pages must be CUDA [n_pages, page_size, H, d] tensors with d contiguous")
+    return Pages(*shape, *st[:3])
 
 
 def cache_append(p1, p2, info, theta, positions, slots, k_pages, v_pages, pairing: int = 0,
@@ -566,34 +576,28 @@ def cache_append(p1, p2, info, theta, positions, slots, k_pages, v_pages, pairin
     k_pages[slot] = RoPE(p2), v_pages[slot] = Givens(info); returns q = RoPE(p1) (None where p1 is
     None).  p1, p2, info [N, H, d] of one layout, theta fp32 [H/2] or None (no mixing), positions
     int32 [N] (unused with rope_base 0: no rotation), slots int64 [N], negative for padding."""
-    if p1 is None:
-        _same_layout(p2, info)
-    else:
-        _same_layout(p2, p1, info)
     pages = pages_of(k_pages, v_pages)
-    if p2.dim() != 3 or p2.stride(2) != 1 or p2.dtype != k_pages.dtype or \
-            p2.device != k_pages.device or p2.shape[1:] != k_pages.shape[2:]:
-        raise ValueError("tokens must be [N, H, d] with d contiguous, of the pages' H, d, dtype "
-                         "and device")
-    N, dev = p2.shape[0], p2.device
-    if slots.dtype != torch.int64 or slots.shape != (N,) or not slots.is_contiguous() or \
-            slots.device != dev:
-        raise ValueError("slots must be a contiguous int64 tensor of N entries")
-    if positions is not None:
-        _int32("positions", positions, dev, (N,))
-    if theta is not None and (theta.dtype != torch.float32 or theta.device != dev or
-                              theta.numel() != p2.shape[1] // 2 or not theta.is_contiguous()):
-        raise ValueError("theta must be contiguous fp32 [H/2] on the inputs' device")
+    dev, dtype, shape, st = k_pages.get_device(), k_pages.dtype, p2.shape, p2.stride()
     if p1 is None:
         out = None
     elif out is None:
         out = _like(p1)
-    else:
-        _same_layout(p1, out)
-    st = p2.stride()
-    rc = load().relation_cache_append(_ptr(p1), _ptr(p2), _ptr(info), _ptr(theta), int(pairing),
-                                      float(rope_base), _ptr(positions), _ptr(slots), _ptr(out), N,
-                                      st[0], st[1], _ptr(k_pages), _ptr(v_pages), pages,
+    for t in (p2, info) if p1 is None else (p2, info, p1, out):
+        if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or t.stride() != st:
+            raise ValueError("p1, p2, info and out need the same shape and strides and the pages' "
+                             "dtype and device")
+    if len(shape) != 3 or st[2] != 1 or shape[1] != pages.H or shape[2] != pages.d_h:
+        raise ValueError("tokens must be [N, H, d] with d contiguous, of the pages' H and d")
+    N = shape[0]
+    _need("slots", slots, dev, _I64, N)
+    if positions is not None:
+        _need("positions", positions, dev, _I32, N)
+    if theta is not None:
+        _need("theta", theta, dev, _F32, shape[1] // 2)
+    rc = load().relation_cache_append(_ptr(p1), p2.data_ptr(), info.data_ptr(), _ptr(theta),
+                                      int(pairing), float(rope_base), _ptr(positions),
+                                      slots.data_ptr(), _ptr(out), N, st[0], st[1],
+                                      k_pages.data_ptr(), v_pages.data_ptr(), pages,
                                       _dtype_code(p2), _ptr(dev_status), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_cache_append")
@@ -612,34 +616,33 @@ def paged_decode(q, k_pages, v_pages, block_table, lengths, lam: float, tau_s: f
     multiple of Hk, block_table int32 [B, cols] (rows may be strided), lengths int32 [B] counting
     the new token (0: idle).  Returns (Y [B, H, d], logZ [B, H])."""
     pages = pages_of(k_pages, v_pages)
-    dev = k_pages.device
-    if q.dim() != 3 or q.shape[2] != pages.d_h or q.stride(2) != 1 or \
-            q.dtype != k_pages.dtype or q.device != dev:
+    dev, shape, st = k_pages.get_device(), q.shape, q.stride()
+    if len(shape) != 3 or shape[2] != pages.d_h or st[2] != 1 or \
+            q.dtype is not k_pages.dtype or q.get_device() != dev:
         raise ValueError("q must be [B, H, d] with d contiguous, of the pages' d, dtype and device")
-    B, H = q.shape[:2]
-    _int32("lengths", lengths, dev, (B,))
-    if block_table.dim() != 2 or block_table.shape[0] != B or block_table.dtype != torch.int32 or \
-            block_table.stride(1) != 1 or block_table.device != dev:
+    B, H, _ = shape
+    _need("lengths", lengths, dev, _I32, B)
+    if not _is_table(block_table, B, dev):
         raise ValueError("block_table must be an int32 [B, cols] tensor with contiguous rows on "
                          "the pages' device")
     if out is None:
         out = _like(q)
-    elif out.shape != q.shape or out.stride() != q.stride() or out.dtype != q.dtype or \
-            out.device != dev:
+    elif out.shape != shape or out.stride() != st or out.dtype is not q.dtype or \
+            out.get_device() != dev:
         raise ValueError("out must have q's layout")
     if logz is None:
-        logz = torch.empty((B, H), device=dev, dtype=torch.float32)
-    elif logz.shape != (B, H) or logz.dtype != torch.float32 or not logz.is_contiguous():
-        raise ValueError("logz must be a dense fp32 [B, H] tensor")
+        logz = torch.empty((B, H), device=q.device, dtype=_F32)
+    else:
+        _need("logz", logz, dev, _F32, B * H)
     lib, dt = load(), _dtype_code(q)
     if workspace is None:
-        workspace = torch.empty(lib.relation_paged_decode_workspace_size(H, pages, dt), device=dev,
-                                dtype=torch.uint8)
-    st = q.stride()
-    rc = lib.relation_paged_decode(_ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(block_table),
-                                   block_table.shape[1], block_table.stride(0), _ptr(lengths),
-                                   _ptr(out), _ptr(logz), float(lam), float(tau_s), B, H, pages,
-                                   st[0], st[1], dt, _ptr(workspace),
+        workspace = torch.empty(lib.relation_paged_decode_workspace_size(H, pages, dt),
+                                device=q.device, dtype=torch.uint8)
+    rc = lib.relation_paged_decode(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                                   block_table.data_ptr(), block_table.shape[1],
+                                   block_table.stride(0), lengths.data_ptr(), out.data_ptr(),
+                                   logz.data_ptr(), float(lam), float(tau_s), B, H, pages, st[0],
+                                   st[1], dt, workspace.data_ptr(),
                                    workspace.numel() * workspace.element_size(), _ptr(dev_status),
                                    _stream(stream))
     if rc != OK:
@@ -647,35 +650,36 @@ def paged_decode(q, k_pages, v_pages, block_table, lengths, lam: float, tau_s: f
     return out, logz
 
 
-def _rows(name, t, R, dtype, device):
-    if t is not None and (t.dtype != dtype or t.shape != (R,) or not t.is_contiguous() or
-                          t.device != device):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor of one entry per row on the "
-                         "logits' device")
-    return _ptr(t)
-
-
 def sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, out=None,
            dev_status=None, stream=None):
     """The next token of every row of logits [R, V] (fp32 or bf16, rows may be strided) from
     uniform numbers u fp32 [R]; temperature, top_p, min_p fp32 [R] and top_k int32 [R], each
     optional.  Returns (token int32 [R], logprob fp32 [R], logz fp32 [R]); see relation_sample."""
-    if logits.dim() != 2 or logits.stride(1) != 1 or not logits.is_cuda:
+    dev, dt, st = logits.get_device(), _dtype_code(logits), logits.stride()
+    if len(st) != 2 or st[1] != 1 or dev < 0:
         raise ValueError("logits must be a CUDA [R, V] tensor with contiguous rows")
-    (R, V), dev, f4 = logits.shape, logits.device, torch.float32
-    dt = _dtype_code(logits)
-    args = [_rows("u", u, R, f4, dev), _rows("temperature", temperature, R, f4, dev),
-            _rows("top_k", top_k, R, torch.int32, dev), _rows("top_p", top_p, R, f4, dev),
-            _rows("min_p", min_p, R, f4, dev)]
+    R, V = logits.shape
+    _need("u", u, dev, _F32, R)
+    if temperature is not None:
+        _need("temperature", temperature, dev, _F32, R)
+    if top_k is not None:
+        _need("top_k", top_k, dev, _I32, R)
+    if top_p is not None:
+        _need("top_p", top_p, dev, _F32, R)
+    if min_p is not None:
+        _need("min_p", min_p, dev, _F32, R)
     if out is None:
-        both = torch.empty((2, R), dtype=f4, device=dev)
-        out = (torch.empty(R, dtype=torch.int32, device=dev), both[0], both[1])
-    token, logprob, logz = out
-    _rows("token", token, R, torch.int32, dev)
-    _rows("logprob", logprob, R, f4, dev)
-    _rows("logz", logz, R, f4, dev)
-    rc = load().relation_sample(_ptr(logits), R, V, logits.stride(0), dt, *args, _ptr(token),
-                                _ptr(logprob), _ptr(logz), _ptr(dev_status), _stream(stream))
+        out = (torch.empty(R, dtype=_I32, device=u.device), torch.empty_like(u), torch.empty_like(u))
+        token, logprob, logz = out
+    else:
+        token, logprob, logz = out
+        _need("token", token, dev, _I32, R)
+        _need("logprob", logprob, dev, _F32, R)
+        _need("logz", logz, dev, _F32, R)
+    rc = load().relation_sample(logits.data_ptr(), R, V, st[0], dt, u.data_ptr(),
+                                _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
+                                token.data_ptr(), logprob.data_ptr(), logz.data_ptr(),
+                                _ptr(dev_status), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_sample")
     return out
