@@ -275,7 +275,9 @@ struct PagedProblem {
   int* dev_status;
   float lambda, tau_s, inv_sqrt_d;
   int B, H, Hk, d, cols, n_pages, page;
-  int HG;               // groups of query heads that are taken together (set by the launcher)
+  int GG, HG;           // query heads taken together, and groups of them (set by the launcher,
+  unsigned page_mul;    // as are these: a row's page by multiplication)
+  int page_shift;
   long long t_stride, sP, sR, sC, qsB, qsH;
   relation_dtype dtype;
 };

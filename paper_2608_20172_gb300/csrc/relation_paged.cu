@@ -83,7 +83,26 @@ __device__ __forceinline__ uint4 load_group(const TI* row, int c, int d) {
   }
 }
 
-__device__ __forceinline__ float silu(float u) { return u / (1.0f + expf(-u)); }
+// 2^x by the special function unit (2 ulp), and through it e^x, whose argument's rounding adds
+// |x| 2^-24: the weights e^{E - m} are at most 1 and lose what is far below the largest.
+__device__ __forceinline__ float fast_exp(float x) { return ex2_approx(x * 1.4426950408889634f); }
+// (a denominator past 2^126 gives 0 in place of at most 1e-36)
+// 16 bytes to shared memory, zeros if not ok
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
+               "r"(ok ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ float silu(float u) { return __fdividef(u, 1.0f + fast_exp(-u)); }
+// The running maximum is raised only where a score exceeds it by more than this: weights up to
+// e^kSlack are as exact as those below 1, and a raise touches every accumulator.
+constexpr float kSlack = 6.f;
 
 __device__ __forceinline__ float warp_max(float x) {
 #pragma unroll
@@ -108,9 +127,14 @@ __device__ __forceinline__ int units_of(int len) {
   return len > 1 ? (len - 2) / kUnit + 1 : 1;
 }
 
+// r / page for 0 <= r < 2^31: with l = ceil(log2 page) >= 1 and M = floor(2^(31 + l) / page) + 1 the
+// product r M is off by less than 2^(31 + l) from r 2^(31 + l) / page (launch_t)
+__device__ __forceinline__ int page_of(const PagedProblem& p, int r) {
+  return p.page == 1 ? r : (int)(__umulhi((unsigned)r, p.page_mul) >> p.page_shift);
+}
 // Element offset of row r of request b's head 0
 __device__ __forceinline__ long long row_at(const PagedProblem& p, int b, int r) {
-  const int j = r / p.page;
+  const int j = page_of(p, r);
   int id = __ldg(p.table + (long long)b * p.t_stride + j);
   if (id < 0 || id >= p.n_pages) {  // reported, and read as page 0
     if (p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
@@ -196,27 +220,319 @@ __device__ __forceinline__ float self_dot(const PagedProblem& p, const TI* q, co
   return warp_sum(s);
 }
 
+// The warps' results of a head's part of a run, for up to GG query heads.
 template <int GG>
 struct Smem {
   float z[kWarps][GG][kMaxD], m[kWarps][GG], l[kWarps][GG];
   float self[GG];
 };
 
-constexpr int ctas_per_sm(int GG) { return GG == 1 ? 4 : GG == 2 ? 3 : 2; }
-
-// LPR lanes per row, 32 / LPR rows per load, GG query heads at once.
-template <typename TI, int LPR, int GG, bool VEC>
-__global__ void __launch_bounds__(kThreads, ctas_per_sm(GG))
-    run_kernel(PagedProblem p, float* part) {
-  constexpr int VE = Vec<TI>::N, RPL = 32 / LPR;
-  constexpr int NI = LPR == 4 ? 4 : 8;  // loads of a tile's keys
-  constexpr int R = RPL * NI;           // rows of a tile
-  constexpr int DUP = LPR > NI ? LPR / NI : 1;  // lanes that end up with the same row's score
+// The rows that a warp takes, as (m, l, z) of GG query heads, on the CUDA cores.  LPR lanes per row,
+// 32 / LPR rows per load; scores are summed over a row's lanes with half the rows handed over at
+// every step, so that a lane ends up with one row's.  Any type, head size and alignment.
+template <typename TI, int LPR, int GG_, bool VEC>
+struct Lanes {
+  using T = TI;
+  static constexpr int GG = GG_;
+  static constexpr int kCtas = GG == 1 ? 4 : GG == 2 ? 3 : 2;  // per SM, by the registers
+  static constexpr int VE = Vec<TI>::N, RPL = 32 / LPR;
+  static constexpr int NI = LPR == 4 ? 4 : 8;  // loads of a tile's keys
+  static constexpr int R = RPL * NI;           // rows of a tile
+  static constexpr int DUP = LPR > NI ? LPR / NI : 1;  // lanes that end up with the same row's score
+  static constexpr int kRing = 0;  // bytes of a CTA's ring
   static_assert(R <= 32, "a lane per row");
-  __shared__ Smem<GG> sm;
+  float q[GG][VE], z[GG][VE], m[GG], l[GG];
+
+  __device__ __forceinline__ void start(const PagedProblem& p, const TI* qb, int ng, int lane) {
+    const int c0 = (lane % LPR) * VE;
+#pragma unroll
+    for (int g = 0; g < GG; ++g) {
+      m[g] = -INFINITY;
+      l[g] = 0.f;
+#pragma unroll
+      for (int i = 0; i < VE; ++i) {
+        q[g][i] = g < ng && c0 + i < p.d ? ldf(qb + (long long)g * p.qsH + c0 + i) * p.inv_sqrt_d : 0.f;
+        z[g][i] = 0.f;
+      }
+    }
+  }
+  // rows j .. min(j + R, rb) - 1 of request b
+  __device__ __forceinline__ void tile(const PagedProblem& p, int b, const TI* kb, const TI* vb, int j,
+                                       int rb, int lane) {
+    const int group = lane / LPR, c0 = (lane % LPR) * VE;
+    const int my = (lane % LPR) / DUP * RPL + group;  // the tile's row whose score this lane gets
+    // rows past the end read the last one, and are left out below
+    const long long mine = row_at(p, b, min(j + lane % R, rb - 1));
+    uint4 kr[NI], vr[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const long long off = __shfl_sync(0xffffffffu, mine, i * RPL + group);
+      kr[i] = load_group<TI, VEC>(kb + off, c0, p.d);
+      vr[i] = load_group<TI, VEC>(vb + off, c0, p.d);
+    }
+    float P[GG];
+#pragma unroll
+    for (int g = 0; g < GG; ++g) {
+      float s[NI];
+#pragma unroll
+      for (int i = 0; i < NI; ++i) {
+        float x[VE];
+        Vec<TI>::unpack(kr[i], x);
+        s[i] = 0.f;
+#pragma unroll
+        for (int t = 0; t < VE; ++t) s[i] = fmaf(q[g][t], x[t], s[i]);
+      }
+      int cnt = NI;
+#pragma unroll
+      for (int o = LPR / 2; o > 0; o >>= 1) {
+        if (cnt > 1) {
+          cnt >>= 1;
+#pragma unroll
+          for (int i = 0; i < NI / 2; ++i) {
+            if (i >= cnt) break;
+            const bool up = lane & o;
+            const float give = up ? s[i] : s[i + cnt], keep = up ? s[i + cnt] : s[i];
+            s[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+          }
+        } else {
+          s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
+        }
+      }
+      const bool in = j + my < rb;
+      const float E = silu(s[0]), mx = in ? E : -INFINITY;
+      if (__any_sync(0xffffffffu, mx > m[g] + kSlack)) {
+        const float mn = fmaxf(m[g], warp_max(mx)), sc = m[g] == -INFINITY ? 0.f : expf(m[g] - mn);
+        m[g] = mn;
+        l[g] *= sc;
+#pragma unroll
+        for (int t = 0; t < VE; ++t) z[g][t] *= sc;
+      }
+      P[g] = in ? fast_exp(E - m[g]) : 0.f;
+      if (lane % DUP == 0) l[g] += P[g];
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      float x[VE];
+      Vec<TI>::unpack(vr[i], x);
+#pragma unroll
+      for (int g = 0; g < GG; ++g) {
+        const float w = __shfl_sync(0xffffffffu, P[g], group * LPR + i * DUP);
+#pragma unroll
+        for (int t = 0; t < VE; ++t) z[g][t] = fmaf(w, x[t], z[g][t]);
+      }
+    }
+  }
+  // this warp's tiles of rows ra .. rb - 1
+  __device__ __forceinline__ void run(const PagedProblem& p, int b, const TI* kb, const TI* vb, int ra,
+                                      int rb, uint4*, int warp, int lane) {
+    for (int j = ra + warp * R; j < rb; j += kWarps * R) tile(p, b, kb, vb, j, rb, lane);
+  }
+  __device__ __forceinline__ void finish(const PagedProblem& p, Smem<GG>& sm, int warp, int lane) {
+    const int group = lane / LPR, c0 = (lane % LPR) * VE;
+#pragma unroll
+    for (int g = 0; g < GG; ++g) {
+      l[g] = warp_sum(l[g]);
+#pragma unroll
+      for (int t = 0; t < VE; ++t) {
+#pragma unroll
+        for (int o = LPR; o < 32; o <<= 1) z[g][t] += __shfl_xor_sync(0xffffffffu, z[g][t], o);
+        if (group == 0 && c0 + t < p.d) sm.z[warp][g][c0 + t] = z[g][t];
+      }
+      if (lane == 0) {
+        sm.m[warp][g] = m[g];
+        sm.l[warp][g] = l[g];
+      }
+    }
+  }
+};
+
+// D += A B on the tensor core: A 16 x 16 by rows, B 16 x 8 by columns, bf16; D 16 x 8 fp32.  With
+// r = lane / 4, t = lane % 4 a lane holds A[r][2t, 2t + 1], A[r + 8][..], A[r][2t + 8, 2t + 9],
+// A[r + 8][..]; B[2t, 2t + 1][r], B[2t + 8, 2t + 9][r]; D[r][2t, 2t + 1], D[r + 8][..].
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3,
+                                    uint32_t b0, uint32_t b1) {
+  asm volatile(
+      "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, "
+      "{%0,%1,%2,%3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// The same for 2 to 8 query heads that share bf16 keys (16-byte groups), on the tensor core, 16 rows
+// at a time.  What the products sum over and what they leave in a column may be permuted freely, so
+// that the keys and values go from memory to the products in the registers they were loaded to:
+//   scores  A = Q (head r), B = K^T: row r of 8, channels: lane t's 16-byte groups t, t + 4, .. of
+//           the row, 4 elements of a group per product, the same elements of Q's row in A;
+//   Y       A = P (head r), B = V: rows 2t, 2t + 1, 2t + 8, 2t + 9, column r of product (i, e) is
+//           channel 8 (r + 8 i) + e, element e of the group that lane r loaded; two rows' elements
+//           are brought into one register by a byte permutation.
+// (tcgen05 products have at least 64 rows, of which 8 would be used, and read their operands from
+// shared memory; the reading of K and V bounds this, not the products.)  A's rows 8 to 15 hold what
+// the rounding of P to bf16 drops, itself rounded to bf16: P has 16 bits, and both parts of Y are
+// summed in fp32.
+template <int D>
+struct Tensor {
+  using T = __nv_bfloat16;
+  static constexpr int GG = 8, R = 16;
+  static constexpr int S = 2, kSlots = D / 8;  // stages, a lane's 16-byte slots of one
+  static constexpr int kRing = kWarps * S * kSlots * 512;
+  static constexpr int kCtas = D == 64 ? 4 : 3;
+  uint32_t q[D / 32][4];  // the lane's groups of head r's query
+  float z[D / 64][8][4], m, l;
+
+  __device__ __forceinline__ void start(const PagedProblem& p, const T* qb, int ng, int lane) {
+    const int r = lane >> 2, t = lane & 3;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int c = 8 * (t + 4 * i) + 2 * e;
+        const T* x = qb + (long long)r * p.qsH + c;  // (d is a multiple of 8)
+        const bool in = r < ng && c < p.d;
+        const unsigned lo = in ? __bfloat16_as_ushort(x[0]) : 0, hi = in ? __bfloat16_as_ushort(x[1]) : 0;
+        q[i][e] = lo | hi << 16;
+      }
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) z[i][e][k] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+  }
+  // Rows off of a tile (lane l: its row l % 16) into a stage of the lane's slots.
+  __device__ __forceinline__ void fetch(const PagedProblem& p, const T* kb, const T* vb, long long off,
+                                        uint4* stage, int lane) {
+    const int r = lane >> 2, t = lane & 3;
+    uint32_t dst = smem_u32(stage);
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const T* row = kb + __shfl_sync(0xffffffffu, off, 8 * n + r);
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i, dst += 512) {
+        const int c = 8 * (t + 4 * i);
+        cp16(dst, row + (c < p.d ? c : 0), c < p.d);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const T* row = vb + __shfl_sync(0xffffffffu, off, 2 * t + (k & 1) + 8 * (k >> 1));
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i, dst += 512) {
+        const int c = 8 * (r + 8 * i);
+        cp16(dst, row + (c < p.d ? c : 0), c < p.d);
+      }
+    }
+  }
+  __device__ __forceinline__ void run(const PagedProblem& p, int b, const T* kb, const T* vb, int ra,
+                                      int rb, uint4* ring, int warp, int lane) {
+    constexpr int step = kWarps * R;
+    uint4* mine = ring + warp * S * kSlots * 32 + lane;
+    int j = ra + warp * R;
+    // rows past the end read the last one, and are left out of the tile
+    auto row = [&](int at) { return at < rb ? row_at(p, b, min(at + (lane & 15), rb - 1)) : 0; };
+#pragma unroll
+    for (int st = 0; st < S; ++st) {
+      if (j + st * step < rb) fetch(p, kb, vb, row(j + st * step), mine + st * kSlots * 32, lane);
+      cp_commit();
+    }
+    long long next = row(j + S * step);
+    for (int st = 0; j < rb; j += step, st = st + 1 == S ? 0 : st + 1) {
+      cp_wait<S - 1>();
+      uint4* stage = mine + st * kSlots * 32;
+      tile(p, stage, j, rb, lane);
+      if (j + S * step < rb) fetch(p, kb, vb, next, stage, lane);
+      cp_commit();
+      next = row(j + (S + 1) * step);
+    }
+    cp_wait<0>();
+  }
+  __device__ __forceinline__ void tile(const PagedProblem& p, const uint4* stage, int j, int rb,
+                                       int lane) {
+    const int t = lane & 3;
+    float E[4], mx = -INFINITY;
+    bool in[4];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i) {
+        const uint4 k = stage[(n * (D / 32) + i) * 32];
+        mma(s, q[i][0], 0, q[i][1], 0, k.x, k.y);
+        mma(s, q[i][2], 0, q[i][3], 0, k.z, k.w);
+      }
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        in[2 * n + k] = j + 8 * n + 2 * t + k < rb;
+        E[2 * n + k] = silu(s[k] * p.inv_sqrt_d);
+        if (in[2 * n + k]) mx = fmaxf(mx, E[2 * n + k]);
+      }
+    }
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+    mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+    if (__any_sync(0xffffffffu, mx > m + kSlack)) {
+      const float mn = fmaxf(m, mx), sc = m == -INFINITY ? 0.f : expf(m - mn);
+      m = mn;
+      l *= sc;
+#pragma unroll
+      for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) z[i][e][k] *= sc;
+    }
+    uint32_t hi[2], lo[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+      const float a = in[2 * n] ? fast_exp(E[2 * n] - m) : 0.f;
+      const float c = in[2 * n + 1] ? fast_exp(E[2 * n + 1] - m) : 0.f;
+      l += a + c;
+      hi[n] = pack_bf16x2(a, c);
+      lo[n] = pack_bf16x2(a - __uint_as_float(hi[n] << 16), c - __uint_as_float(hi[n] & 0xffff0000u));
+    }
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      uint32_t v[4][4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint4 x = stage[(D / 16 + k * (D / 64) + i) * 32];
+        v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w;
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int sel = e & 1 ? 0x7632 : 0x5410;
+        mma(z[i][e], hi[0], lo[0], hi[1], lo[1], __byte_perm(v[0][e / 2], v[1][e / 2], sel),
+            __byte_perm(v[2][e / 2], v[3][e / 2], sel));
+      }
+    }
+  }
+  __device__ __forceinline__ void finish(const PagedProblem& p, Smem<GG>& sm, int warp, int lane) {
+    const int r = lane >> 2, t = lane & 3;
+    l += __shfl_xor_sync(0xffffffffu, l, 1);
+    l += __shfl_xor_sync(0xffffffffu, l, 2);
+    if (t == 0) {
+      sm.m[warp][r] = m;
+      sm.l[warp][r] = l;
+    }
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+          sm.z[warp][r][8 * (2 * t + k + 8 * i) + e] = z[i][e][k] + z[i][e][k + 2];
+  }
+};
+
+template <typename Core>
+__global__ void __launch_bounds__(kThreads, Core::kCtas)
+    run_kernel(PagedProblem p, float* part) {
+  using TI = typename Core::T;
+  // the ring, and then in its place the results
+  extern __shared__ uint4 ring[];
+  Smem<Core::GG>& sm = *reinterpret_cast<Smem<Core::GG>*>(ring);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int group = lane / LPR, c0 = (lane % LPR) * VE;
-  const int my = (lane % LPR) / DUP * RPL + group;  // the tile's row whose score this lane gets
   pdl_wait();
   const Sums at = scan_requests(p, blockIdx.x, -1, blockIdx.x == 0);
   // as many runs as CTAs, or one for each unit where there are fewer of these
@@ -234,8 +550,8 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(GG))
       len = length_of(p, b, false);
       n_u = units_of(len);
     }
-    const int hg = (int)((u - base) / n_u), kh = hg / groups, g0 = hg % groups * GG;
-    const int ng = min(GG, heads - g0);
+    const int hg = (int)((u - base) / n_u), kh = hg / groups, g0 = hg % groups * p.GG;
+    const int ng = min(p.GG, heads - g0);
     const long long s0 = base + (long long)hg * n_u, s1 = s0 + n_u;  // the head's units
     const long long e = min(r1, s1);
     const int ra = (int)(u - s0) * kUnit, rb = min((int)(e - s0) * kUnit, max(len - 1, 0));
@@ -244,95 +560,11 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(GG))
     const TI* vb = reinterpret_cast<const TI*>(p.v) + (long long)kh * p.sC;
     const int h0 = kh * heads + g0;
     const TI* qb = reinterpret_cast<const TI*>(p.q) + (long long)b * p.qsB + (long long)h0 * p.qsH;
-    float q[GG][VE], z[GG][VE], m[GG], l[GG];
-#pragma unroll
-    for (int g = 0; g < GG; ++g) {
-      m[g] = -INFINITY;
-      l[g] = 0.f;
-#pragma unroll
-      for (int i = 0; i < VE; ++i) {
-        q[g][i] = g < ng && c0 + i < p.d ? ldf(qb + (long long)g * p.qsH + c0 + i) * p.inv_sqrt_d : 0.f;
-        z[g][i] = 0.f;
-      }
-    }
-    for (int j = ra + warp * R; j < rb; j += kWarps * R) {
-      // rows past the end read the last one, and are left out below
-      const long long mine = row_at(p, b, min(j + lane % R, rb - 1));
-      uint4 kr[NI], vr[NI];
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        const long long off = __shfl_sync(0xffffffffu, mine, i * RPL + group);
-        kr[i] = load_group<TI, VEC>(kb + off, c0, p.d);
-        vr[i] = load_group<TI, VEC>(vb + off, c0, p.d);
-      }
-      float P[GG];
-#pragma unroll
-      for (int g = 0; g < GG; ++g) {
-        float s[NI];
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          float x[VE];
-          Vec<TI>::unpack(kr[i], x);
-          s[i] = 0.f;
-#pragma unroll
-          for (int t = 0; t < VE; ++t) s[i] = fmaf(q[g][t], x[t], s[i]);
-        }
-        // the sums over a row's lanes, halving the rows per lane while there are any
-        int cnt = NI;
-#pragma unroll
-        for (int o = LPR / 2; o > 0; o >>= 1) {
-          if (cnt > 1) {
-            cnt >>= 1;
-#pragma unroll
-            for (int i = 0; i < NI / 2; ++i) {
-              if (i >= cnt) break;
-              const bool up = lane & o;
-              const float give = up ? s[i] : s[i + cnt], keep = up ? s[i + cnt] : s[i];
-              s[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
-            }
-          } else {
-            s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
-          }
-        }
-        const bool in = j + my < rb;
-        const float E = silu(s[0]), mx = in ? E : -INFINITY;
-        if (__any_sync(0xffffffffu, mx > m[g])) {
-          const float mn = fmaxf(m[g], warp_max(mx)), sc = m[g] == -INFINITY ? 0.f : expf(m[g] - mn);
-          m[g] = mn;
-          l[g] *= sc;
-#pragma unroll
-          for (int t = 0; t < VE; ++t) z[g][t] *= sc;
-        }
-        P[g] = in ? expf(E - m[g]) : 0.f;
-        if (lane % DUP == 0) l[g] += P[g];
-      }
-#pragma unroll
-      for (int i = 0; i < NI; ++i) {
-        float x[VE];
-        Vec<TI>::unpack(vr[i], x);
-#pragma unroll
-        for (int g = 0; g < GG; ++g) {
-          const float w = __shfl_sync(0xffffffffu, P[g], group * LPR + i * DUP);
-#pragma unroll
-          for (int t = 0; t < VE; ++t) z[g][t] = fmaf(w, x[t], z[g][t]);
-        }
-      }
-    }
-    // the warp's row groups, then the warps
-#pragma unroll
-    for (int g = 0; g < GG; ++g) {
-      l[g] = warp_sum(l[g]);
-#pragma unroll
-      for (int t = 0; t < VE; ++t) {
-#pragma unroll
-        for (int o = LPR; o < 32; o <<= 1) z[g][t] += __shfl_xor_sync(0xffffffffu, z[g][t], o);
-        if (group == 0 && c0 + t < p.d) sm.z[warp][g][c0 + t] = z[g][t];
-      }
-      if (lane == 0) {
-        sm.m[warp][g] = m[g];
-        sm.l[warp][g] = l[g];
-      }
-    }
+    Core core;
+    core.start(p, qb, ng, lane);
+    core.run(p, b, kb, vb, ra, rb, ring, warp, lane);
+    if (Core::kRing > 0) __syncthreads();
+    core.finish(p, sm, warp, lane);
     long long self = 0;
     if (whole && len > 0) {
       self = row_at(p, b, len - 1);
@@ -358,7 +590,7 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(GG))
         if (whole) {
           epilogue<TI>(p, b, h0 + g, len, len > 0 ? sm.self[g] : 0.f, M, L, Z, c, vi);
         } else {  // slot 0: the run's first head (begun before it), 1: its last
-          float* o = part + (((long long)blockIdx.x * 2 + (u == s0)) * GG + g) * kPart;
+          float* o = part + (((long long)blockIdx.x * 2 + (u == s0)) * p.GG + g) * kPart;
           if (c == 0) {
             o[0] = M;
             o[1] = L;
@@ -372,14 +604,16 @@ __global__ void __launch_bounds__(kThreads, ctas_per_sm(GG))
   }
 }
 
-// Heads that several runs share: a CTA per (request, query head).
+// Heads that several runs share: a CTA per (request, query head).  The runs' weights a thread each,
+// then their z with kAhead loads in flight.
 template <typename TI>
-__global__ void __launch_bounds__(kThreads) join_kernel(PagedProblem p, const float* part, int most,
-                                                        int GG) {
-  __shared__ float self;
+__global__ void __launch_bounds__(kThreads) join_kernel(PagedProblem p, const float* part, int most) {
+  constexpr int kAhead = 16;
+  __shared__ float self, red[kWarps], w[kThreads], lw[kThreads];
   const int b = blockIdx.x / p.H, h = blockIdx.x % p.H, c = threadIdx.x;
+  const int warp = c >> 5, lane = c & 31;
   const int heads = p.H / p.Hk, groups = p.HG / p.Hk;
-  const int kh = h / heads, hg = kh * groups + (h - kh * heads) / GG, g = (h - kh * heads) % GG;
+  const int kh = h / heads, hg = kh * groups + (h - kh * heads) / p.GG, g = (h - kh * heads) % p.GG;
   pdl_wait_and_launch();
   const Sums at = scan_requests(p, 0, b, false);
   const int len = length_of(p, b, false);
@@ -389,32 +623,53 @@ __global__ void __launch_bounds__(kThreads) join_kernel(PagedProblem p, const fl
   const int k0 = (int)(((s0 + 1) * runs - 1) / U), k1 = (int)(((s0 + n_u) * runs - 1) / U);
   if (k0 == k1) return;  // (finished there)
   const long long row = row_at(p, b, len - 1) + (long long)kh * p.sC;
-  if (c < 32) {
+  const float vi = c < p.d ? ldf(reinterpret_cast<const TI*>(p.v) + row + c) : 0.f;
+  if (warp == kWarps - 1) {
     const float s = self_dot<TI>(p, reinterpret_cast<const TI*>(p.q) + (long long)b * p.qsB +
                                         (long long)h * p.qsH,
-                                 reinterpret_cast<const TI*>(p.k) + row, c);
-    if (c == 0) self = s;
+                                 reinterpret_cast<const TI*>(p.k) + row, lane);
+    if (lane == 0) self = s;
   }
+  // the first of them begins the head (its second slot), the others begin with it
+  const long long step = 2LL * p.GG * kPart;
+  const float* first = part + (long long)k0 * step + g * kPart;
+  const float* begun = first + (long long)p.GG * kPart;
+  auto at_run = [&](int i) { return i == 0 ? begun : first + i * step; };
+  const int n = k1 - k0 + 1;
+  float M = -INFINITY;
+  for (int i = c; i < n; i += kThreads) M = fmaxf(M, at_run(i)[0]);
+  M = warp_max(M);
+  if (lane == 0) red[warp] = M;
   __syncthreads();
-  if (c >= p.d) return;
-  const float vi = ldf(reinterpret_cast<const TI*>(p.v) + row + c);
-  auto at_run = [&](int k) {
-    const bool begun = (long long)k * U / runs > s0;  // before the run
-    return part + (((long long)k * 2 + !begun) * GG + g) * kPart;
-  };
-  float M = -INFINITY, L = 0.f, Z = 0.f;
-  for (int k = k0; k <= k1; ++k) M = fmaxf(M, at_run(k)[0]);
-  for (int k = k0; k <= k1; ++k) {
-    const float* x = at_run(k);
-    const float a = x[1] == 0.f ? 0.f : expf(x[0] - M);
-    L = fmaf(a, x[1], L);
-    Z = fmaf(a, x[2 + c], Z);
+#pragma unroll
+  for (int i = 0; i < kWarps; ++i) M = fmaxf(M, red[i]);
+  float L = 0.f, Z = 0.f;
+  for (int i0 = 0; i0 < n; i0 += kThreads) {  // kThreads runs' weights at a time
+    if (i0 > 0) __syncthreads();
+    if (i0 + c < n) {
+      const float* x = at_run(i0 + c);
+      w[c] = x[1] == 0.f ? 0.f : expf(x[0] - M);
+      lw[c] = x[1];
+    }
+    __syncthreads();
+    const int m = min(kThreads, n - i0);
+    for (int i = 0; i < m; i += kAhead) {
+      float zk[kAhead];
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) zk[e] = i + e < m && c < p.d ? at_run(i0 + i + e)[2 + c] : 0.f;
+#pragma unroll
+      for (int e = 0; e < kAhead; ++e) {
+        if (i + e >= m) break;
+        L = fmaf(w[i + e], lw[i + e], L);
+        Z = fmaf(w[i + e], zk[e], Z);
+      }
+    }
   }
-  epilogue<TI>(p, b, h, len, self, M, L, Z, c, vi);
+  if (c < p.d) epilogue<TI>(p, b, h, len, self, M, L, Z, c, vi);
 }
 
-template <typename TI, int LPR, int GG, bool VEC>
-cudaError_t launch_k(const PagedProblem& p, float* part, cudaStream_t s) {
+template <typename Core>
+cudaError_t launch_core(const PagedProblem& p, float* part, cudaStream_t s) {
   int dev = 0, nsm = 0;
   cudaError_t e;
   if ((e = cudaGetDevice(&dev)) != cudaSuccess ||
@@ -422,11 +677,18 @@ cudaError_t launch_k(const PagedProblem& p, float* part, cudaStream_t s) {
     note_failure("paged decode: device attributes");
     return e;
   }
-  const int per = ctas_per_sm(GG), runs = nsm * per < kMaxCtas ? nsm * per : kMaxCtas;
-  e = launch_pdl(run_kernel<TI, LPR, GG, VEC>, dim3(runs), kThreads, 0, s, 1, p, part);
+  constexpr int smem = Core::kRing > (int)sizeof(Smem<Core::GG>) ? Core::kRing : (int)sizeof(Smem<Core::GG>);
+  if (smem > 48 * 1024 &&
+      (e = cudaFuncSetAttribute(run_kernel<Core>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) !=
+          cudaSuccess) {
+    note_failure("paged decode: shared memory");
+    return e;
+  }
+  const int runs = nsm * Core::kCtas < kMaxCtas ? nsm * Core::kCtas : kMaxCtas;
+  e = launch_pdl(run_kernel<Core>, dim3(runs), kThreads, smem, s, 1, p, part);
   if (e != cudaSuccess) { note_failure("paged decode: launch"); return e; }
-  e = launch_pdl(join_kernel<TI>, dim3((unsigned)p.B * p.H), kThreads, 0, s, 1, p,
-                 (const float*)part, runs, GG);
+  e = launch_pdl(join_kernel<typename Core::T>, dim3((unsigned)p.B * p.H), kThreads, 0, s, 1, p,
+                 (const float*)part, runs);
   if (e != cudaSuccess) note_failure("paged decode: join launch");
   return e;
 }
@@ -434,36 +696,40 @@ cudaError_t launch_k(const PagedProblem& p, float* part, cudaStream_t s) {
 // Query heads taken together: the group rounded up to a power of two, at most 8
 int heads_at_once(int G) { return G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : 8; }
 
-template <typename TI, int LPR>
-cudaError_t launch_lpr(PagedProblem p, bool vec, float* part, cudaStream_t s) {
-  const int G = p.H / p.Hk, gg = heads_at_once(G);
-  p.HG = p.Hk * ((G + gg - 1) / gg);
-  if (vec) {
-    switch (gg) {
-      case 1: return launch_k<TI, LPR, 1, true>(p, part, s);
-      case 2: return launch_k<TI, LPR, 2, true>(p, part, s);
-      case 4: return launch_k<TI, LPR, 4, true>(p, part, s);
-      default: return launch_k<TI, LPR, 8, true>(p, part, s);
-    }
-  }
-  switch (gg) {
-    case 1: return launch_k<TI, LPR, 1, false>(p, part, s);
-    case 2: return launch_k<TI, LPR, 2, false>(p, part, s);
-    case 4: return launch_k<TI, LPR, 4, false>(p, part, s);
-    default: return launch_k<TI, LPR, 8, false>(p, part, s);
+template <typename TI, int LPR, bool VEC>
+cudaError_t launch_lanes(const PagedProblem& p, float* part, cudaStream_t s) {
+  switch (p.GG) {
+    case 1: return launch_core<Lanes<TI, LPR, 1, VEC>>(p, part, s);
+    case 2: return launch_core<Lanes<TI, LPR, 2, VEC>>(p, part, s);
+    case 4: return launch_core<Lanes<TI, LPR, 4, VEC>>(p, part, s);
+    default: return launch_core<Lanes<TI, LPR, 8, VEC>>(p, part, s);
   }
 }
 
 template <typename TI>
-cudaError_t launch_t(const PagedProblem& p, float* part, cudaStream_t s) {
+cudaError_t launch_t(PagedProblem p, float* part, cudaStream_t s) {
   constexpr int VE = Vec<TI>::N, most = kMaxD / VE;
+  const int G = p.H / p.Hk, n = (p.d + VE - 1) / VE;
+  p.GG = heads_at_once(G);
+  p.HG = p.Hk * ((G + p.GG - 1) / p.GG);
+  int l = 1;
+  while (l < 31 && (1 << l) < p.page) ++l;
+  p.page_mul = p.page > 1 ? (unsigned)((1ull << (31 + l)) / p.page + 1) : 0;
+  p.page_shift = l - 1;
   uintptr_t low = reinterpret_cast<uintptr_t>(p.k) | reinterpret_cast<uintptr_t>(p.v);
   for (long long x : {p.sP, p.sR, p.sC}) low |= (uintptr_t)(x * (long long)sizeof(TI));
-  const bool vec = low % 16 == 0 && p.d % VE == 0;
-  const int n = (p.d + VE - 1) / VE;
-  if (n <= most / 4) return launch_lpr<TI, most / 4>(p, vec, part, s);
-  if (n <= most / 2) return launch_lpr<TI, most / 2>(p, vec, part, s);
-  return launch_lpr<TI, most>(p, vec, part, s);
+  if (low % 16 == 0 && p.d % VE == 0) {
+    if constexpr (sizeof(TI) == 2) {
+      if (G > 1 && p.d <= 64) return launch_core<Tensor<64>>(p, part, s);
+      if (G > 1) return launch_core<Tensor<128>>(p, part, s);
+    }
+    if (n <= most / 4) return launch_lanes<TI, most / 4, true>(p, part, s);
+    if (n <= most / 2) return launch_lanes<TI, most / 2, true>(p, part, s);
+    return launch_lanes<TI, most, true>(p, part, s);
+  }
+  if (n <= most / 4) return launch_lanes<TI, most / 4, false>(p, part, s);
+  if (n <= most / 2) return launch_lanes<TI, most / 2, false>(p, part, s);
+  return launch_lanes<TI, most, false>(p, part, s);
 }
 
 }  // namespace paged
