@@ -87,11 +87,8 @@ __device__ __forceinline__ uint4 load_group(const TI* row, int c, int d) {
 // |x| 2^-24: the weights e^{E - m} are at most 1 and lose what is far below the largest.
 __device__ __forceinline__ float fast_exp(float x) { return ex2_approx(x * 1.4426950408889634f); }
 // (a denominator past 2^126 gives 0 in place of at most 1e-36)
-// 16 bytes to shared memory, zeros if not ok
-__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool ok) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src),
-               "r"(ok ? 16 : 0)
-               : "memory");
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -132,26 +129,55 @@ __device__ __forceinline__ int units_of(int len) {
 __device__ __forceinline__ int page_of(const PagedProblem& p, int r) {
   return p.page == 1 ? r : (int)(__umulhi((unsigned)r, p.page_mul) >> p.page_shift);
 }
-// Element offset of row r of request b's head 0
-__device__ __forceinline__ long long row_at(const PagedProblem& p, int b, int r) {
-  const int j = page_of(p, r);
-  int id = __ldg(p.table + (long long)b * p.t_stride + j);
+// The page id of row r of request b, and with it the element offset of the row's head 0.  In two
+// steps, so that a loop can ask for an id a tile before it uses it.
+__device__ __forceinline__ int id_at(const PagedProblem& p, int b, int r) {
+  return __ldg(p.table + (long long)b * p.t_stride + page_of(p, r));
+}
+__device__ __forceinline__ long long row_of(const PagedProblem& p, int id, int r) {
   if (id < 0 || id >= p.n_pages) {  // reported, and read as page 0
     if (p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
     id = 0;
   }
-  return (long long)id * p.sP + (long long)(r - j * p.page) * p.sR;
+  return (long long)id * p.sP + (long long)(r - page_of(p, r) * p.page) * p.sR;
+}
+__device__ __forceinline__ long long row_at(const PagedProblem& p, int b, int r) {
+  return row_of(p, id_at(p, b, r), r);
 }
 
-// Units per head of all requests, and of those before request b: b_stop, or (b_stop < 0) the one
-// that holds the first unit of run `at`.
-struct Sums {
-  long long before, all;
-  int b;
+// a / b for a, b >= 0 (b > 0): in 32 bits where both fit
+__device__ __forceinline__ long long quotient(long long a, long long b) {
+  if (((a | b) >> 32) == 0) return (unsigned)a / (unsigned)b;
+  return a / b;
+}
+
+// The units of all heads, U = all * HG, cut into `runs` runs: the first `more` of them hold one unit
+// more than the others.
+struct Cut {
+  long long U, each;
+  int runs, more;
+  __device__ __forceinline__ Cut(long long U, int ctas) : U(U) {
+    runs = (int)min((long long)ctas, U);
+    each = quotient(U, runs);
+    more = (int)(U - each * runs);
+  }
+  __device__ __forceinline__ long long begin(int k) const { return k * each + min(k, more); }
+  __device__ __forceinline__ int owner(long long u) const {
+    const long long big = more * (each + 1);
+    return (int)(u < big ? quotient(u, each + 1) : more + quotient(u - big, each));
+  }
 };
-__device__ __forceinline__ Sums scan_requests(const PagedProblem& p, long long at, int b_stop,
-                                              bool report) {
-  __shared__ long long part[kWarps], found[2];
+
+// Where a CTA begins: a request and the units (per head) before it; and the cut.
+struct Place {
+  int b;
+  long long before;
+  Cut cut;
+};
+// b_stop >= 0: that request; else the one that holds the first unit of run `run` of `ctas`.
+__device__ __forceinline__ Place find_place(const PagedProblem& p, int run, int ctas, int b_stop,
+                                            bool report) {
+  __shared__ long long part[kWarps], found;
   __shared__ int found_b;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int per = (p.B + kThreads - 1) / kThreads;
@@ -172,44 +198,41 @@ __device__ __forceinline__ Sums scan_requests(const PagedProblem& p, long long a
     if (w < warp) before += part[w];
     all += part[w];
   }
-  if (b_stop >= 0) {  // by request
+  const Cut cut(all * p.HG, ctas);
+  if (b_stop >= 0) {
     if (lo <= b_stop && b_stop < hi) {
       for (int b = lo; b < b_stop; ++b) before += units_of(length_of(p, b, false));
-      found[0] = before;
+      found = before;
       found_b = b_stop;
     }
-  } else {  // by run: unit floor(at * U / runs) of the U units of all heads (none for an idle CTA)
-    const long long U = all * p.HG, u = at * U / min((long long)gridDim.x, U);
-    long long n = before;
-    for (int b = lo; b < hi; ++b) {
-      const long long e = n + units_of(length_of(p, b, false));
-      if (n * p.HG <= u && u < e * p.HG) {
-        found[0] = n;
-        found_b = b;
+  } else if (run < cut.runs) {
+    const long long u = cut.begin(run);
+    if (before * p.HG <= u && u < (before + x) * p.HG) {  // (one thread's requests hold it)
+      int b = lo;
+      for (; b < hi - 1; ++b) {
+        const int n = units_of(length_of(p, b, false));
+        if (u < (before + n) * p.HG) break;
+        before += n;
       }
-      n = e;
+      found = before;
+      found_b = b;
     }
   }
   __syncthreads();
-  return {found[0], all, found_b};
+  return {found_b, found, cut};
 }
 
-// Column c of a finished row
-template <typename TI>
-__device__ __forceinline__ void epilogue(const PagedProblem& p, int b, int h, int len, float qk,
-                                         float M, float L, float Z, int c, float vi) {
+// A row's gate g and logZ from q . k_self and the history's M and L
+struct Gate {
+  float g, lz;
+};
+__device__ __forceinline__ Gate gate_of(const PagedProblem& p, int len, float qk, float M, float L) {
   const float S = 1.0f / (1.0f + expf(-(qk * p.inv_sqrt_d) / p.tau_s));
-  float g = 0.f, lz = S, fz = 0.f;
-  if (len > 1) {
-    const float A = M + logf(L) - p.lambda * logf((float)len);
-    g = 1.0f / (1.0f + expf(S - A));
-    lz = A > S ? A + log1pf(expf(S - A)) : S + log1pf(expf(A - S));  // NaN stays NaN
-    fz = Z / L;
-  }
-  const bool idle = len < 1;
-  reinterpret_cast<TI*>(p.out)[(long long)b * p.qsB + (long long)h * p.qsH + c] =
-      (TI)(idle ? 0.f : fmaf(g, fz - vi, vi));
-  if (c == 0) p.logz[(long long)b * p.H + h] = idle ? -INFINITY : lz;
+  if (len < 2) return {0.f, len < 1 ? -INFINITY : S};
+  const float A = M + logf(L) - p.lambda * logf((float)len);
+  // (logaddexp written so that NaN stays NaN)
+  return {1.0f / (1.0f + expf(S - A)),
+          A > S ? A + log1pf(expf(S - A)) : S + log1pf(expf(A - S))};
 }
 
 // q . k_self by one warp
@@ -256,13 +279,11 @@ struct Lanes {
       }
     }
   }
-  // rows j .. min(j + R, rb) - 1 of request b
-  __device__ __forceinline__ void tile(const PagedProblem& p, int b, const TI* kb, const TI* vb, int j,
-                                       int rb, int lane) {
+  // rows j .. min(j + R, rb) - 1, of which this lane has looked up row j + lane % R (offset mine)
+  __device__ __forceinline__ void tile(const PagedProblem& p, const TI* kb, const TI* vb,
+                                       long long mine, int j, int rb, int lane) {
     const int group = lane / LPR, c0 = (lane % LPR) * VE;
     const int my = (lane % LPR) / DUP * RPL + group;  // the tile's row whose score this lane gets
-    // rows past the end read the last one, and are left out below
-    const long long mine = row_at(p, b, min(j + lane % R, rb - 1));
     uint4 kr[NI], vr[NI];
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
@@ -325,7 +346,15 @@ struct Lanes {
   // this warp's tiles of rows ra .. rb - 1
   __device__ __forceinline__ void run(const PagedProblem& p, int b, const TI* kb, const TI* vb, int ra,
                                       int rb, uint4*, int warp, int lane) {
-    for (int j = ra + warp * R; j < rb; j += kWarps * R) tile(p, b, kb, vb, j, rb, lane);
+    // rows past the end read the last one, and are left out of the tile
+    auto row = [&](int j) { return min(j + lane % R, rb - 1); };
+    int j = ra + warp * R;
+    int id = j < rb ? id_at(p, b, row(j)) : 0;
+    for (; j < rb; j += kWarps * R) {
+      const long long mine = row_of(p, id, row(j));
+      id = j + kWarps * R < rb ? id_at(p, b, row(j + kWarps * R)) : 0;
+      tile(p, kb, vb, mine, j, rb, lane);
+    }
   }
   __device__ __forceinline__ void finish(const PagedProblem& p, Smem<GG>& sm, int warp, int lane) {
     const int group = lane / LPR, c0 = (lane % LPR) * VE;
@@ -369,21 +398,26 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 // (tcgen05 products have at least 64 rows, of which 8 would be used, and read their operands from
 // shared memory; the reading of K and V bounds this, not the products.)  A's rows 8 to 15 hold what
 // the rounding of P to bf16 drops, itself rounded to bf16: P has 16 bits, and both parts of Y are
-// summed in fp32.
-template <int D>
+// summed in fp32.  A tile comes by cp.async S tiles ahead into the warp's own part of shared memory.
+// There a row's 16-byte groups are permuted so that the eight lanes of an access meet no bank twice:
+// of keys by bit 2 with the row's parity, of values by bits 1 and 2 with the row's bits 1 and 2.
+template <int DK>  // 32-channel groups of a row
 struct Tensor {
   using T = __nv_bfloat16;
   static constexpr int GG = 8, R = 16;
-  static constexpr int S = 2, kSlots = D / 8;  // stages, a lane's 16-byte slots of one
-  static constexpr int kRing = kWarps * S * kSlots * 512;
-  static constexpr int kCtas = D == 64 ? 4 : 3;
-  uint32_t q[D / 32][4];  // the lane's groups of head r's query
-  float z[D / 64][8][4], m, l;
+  static constexpr int DV = (DK + 1) / 2;  // 64-channel groups of a row
+  static constexpr int kRow = 8 * DV;      // 16-byte groups of a row in shared memory
+  static constexpr int kStage = 2 * R * kRow;
+  static constexpr int S = DK <= 2 ? 3 : 2;  // stages
+  static constexpr int kRing = kWarps * S * kStage * 16;
+  static constexpr int kCtas = DK <= 2 ? 4 : 3;
+  uint32_t q[DK][4];  // the lane's groups of head r's query
+  float z[DV][8][4], m, l;
 
   __device__ __forceinline__ void start(const PagedProblem& p, const T* qb, int ng, int lane) {
     const int r = lane >> 2, t = lane & 3;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i)
+    for (int i = 0; i < DK; ++i)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int c = 8 * (t + 4 * i) + 2 * e;
@@ -393,7 +427,7 @@ struct Tensor {
         q[i][e] = lo | hi << 16;
       }
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i)
+    for (int i = 0; i < DV; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
@@ -401,70 +435,83 @@ struct Tensor {
     m = -INFINITY;
     l = 0.f;
   }
-  // Rows off of a tile (lane l: its row l % 16) into a stage of the lane's slots.
+  // A tile into a stage, kRow lanes to a row, so that an access meets as few lines as there are; lane
+  // l has looked up row l % 16 (element offset off).
   __device__ __forceinline__ void fetch(const PagedProblem& p, const T* kb, const T* vb, long long off,
-                                        uint4* stage, int lane) {
-    const int r = lane >> 2, t = lane & 3;
-    uint32_t dst = smem_u32(stage);
+                                        uint4* stage, int lane) const {
+    constexpr int PER = 32 / kRow;  // rows of an access
+    const int c = lane % kRow, r0 = lane / kRow;
+    const uint32_t base = smem_u32(stage);
+    const bool in = 8 * c < p.d;
 #pragma unroll
-    for (int n = 0; n < 2; ++n) {
-      const T* row = kb + __shfl_sync(0xffffffffu, off, 8 * n + r);
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i, dst += 512) {
-        const int c = 8 * (t + 4 * i);
-        cp16(dst, row + (c < p.d ? c : 0), c < p.d);
-      }
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const T* row = vb + __shfl_sync(0xffffffffu, off, 2 * t + (k & 1) + 8 * (k >> 1));
-#pragma unroll
-      for (int i = 0; i < D / 64; ++i, dst += 512) {
-        const int c = 8 * (r + 8 * i);
-        cp16(dst, row + (c < p.d ? c : 0), c < p.d);
+    for (int k = 0; k < R / PER; ++k) {
+      const int row = r0 + PER * k;
+      const long long at = __shfl_sync(0xffffffffu, off, row) + 8 * c;
+      if (in) {
+        cp16(base + 16 * (row * kRow + (c ^ (row & 1) << 2)), kb + at);
+        cp16(base + 16 * ((R + row) * kRow + (c ^ (row >> 1 & 3) << 1)), vb + at);
       }
     }
   }
   __device__ __forceinline__ void run(const PagedProblem& p, int b, const T* kb, const T* vb, int ra,
                                       int rb, uint4* ring, int warp, int lane) {
     constexpr int step = kWarps * R;
-    uint4* mine = ring + warp * S * kSlots * 32 + lane;
+    uint4* mine = ring + warp * S * kStage;
     int j = ra + warp * R;
+    if (p.d < 64 * DV) {  // channels past the row's end: zeros (the results were in their place)
+      for (int i = lane; i < S * kStage; i += 32) mine[i] = make_uint4(0, 0, 0, 0);
+      __syncwarp();
+    }
     // rows past the end read the last one, and are left out of the tile
-    auto row = [&](int at) { return at < rb ? row_at(p, b, min(at + (lane & 15), rb - 1)) : 0; };
+    const int own = lane & 15;
+    auto id = [&](int at) { return at < rb ? id_at(p, b, min(at + own, rb - 1)) : 0; };
+    int next[S + 1];
+#pragma unroll
+    for (int st = 0; st <= S; ++st) next[st] = id(j + st * step);
 #pragma unroll
     for (int st = 0; st < S; ++st) {
-      if (j + st * step < rb) fetch(p, kb, vb, row(j + st * step), mine + st * kSlots * 32, lane);
+      const int at = j + st * step;
+      if (at < rb) fetch(p, kb, vb, row_of(p, next[st], min(at + own, rb - 1)), mine + st * kStage, lane);
       cp_commit();
     }
-    long long next = row(j + S * step);
+    int ahead = next[S];
     for (int st = 0; j < rb; j += step, st = st + 1 == S ? 0 : st + 1) {
+      const int at = j + S * step;
+      const int later = id(at + step);
       cp_wait<S - 1>();
-      uint4* stage = mine + st * kSlots * 32;
-      tile(p, stage, j, rb, lane);
-      if (j + S * step < rb) fetch(p, kb, vb, next, stage, lane);
+      __syncwarp();
+      uint4* stage = mine + st * kStage;
+      if (j + R <= rb)
+        tile<true>(p, stage, j, rb, lane);
+      else
+        tile<false>(p, stage, j, rb, lane);
+      __syncwarp();
+      if (at < rb) fetch(p, kb, vb, row_of(p, ahead, min(at + own, rb - 1)), stage, lane);
       cp_commit();
-      next = row(j + (S + 1) * step);
+      ahead = later;
     }
     cp_wait<0>();
   }
+  template <bool FULL>
   __device__ __forceinline__ void tile(const PagedProblem& p, const uint4* stage, int j, int rb,
                                        int lane) {
-    const int t = lane & 3;
+    const int r = lane >> 2, t = lane & 3;
+    const uint4* ks = stage + r * kRow + t;
+    const uint4* vs = stage + (R + 2 * t) * kRow + (r ^ 2 * t);
     float E[4], mx = -INFINITY;
     bool in[4];
 #pragma unroll
     for (int n = 0; n < 2; ++n) {
       float s[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const uint4 k = stage[(n * (D / 32) + i) * 32];
+      for (int i = 0; i < DK; ++i) {
+        const uint4 k = ks[8 * n * kRow + 4 * (i ^ (r & 1))];
         mma(s, q[i][0], 0, q[i][1], 0, k.x, k.y);
         mma(s, q[i][2], 0, q[i][3], 0, k.z, k.w);
       }
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
-        in[2 * n + k] = j + 8 * n + 2 * t + k < rb;
+        in[2 * n + k] = FULL || j + 8 * n + 2 * t + k < rb;
         E[2 * n + k] = silu(s[k] * p.inv_sqrt_d);
         if (in[2 * n + k]) mx = fmaxf(mx, E[2 * n + k]);
       }
@@ -476,7 +523,7 @@ struct Tensor {
       m = mn;
       l *= sc;
 #pragma unroll
-      for (int i = 0; i < D / 64; ++i)
+      for (int i = 0; i < DV; ++i)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
 #pragma unroll
@@ -492,11 +539,11 @@ struct Tensor {
       lo[n] = pack_bf16x2(a - __uint_as_float(hi[n] << 16), c - __uint_as_float(hi[n] & 0xffff0000u));
     }
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
+    for (int i = 0; i < DV; ++i) {
       uint32_t v[4][4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint4 x = stage[(D / 16 + k * (D / 64) + i) * 32];
+        const uint4 x = vs[((k & 1) + 8 * (k >> 1)) * kRow + 8 * i];
         v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w;
       }
 #pragma unroll
@@ -516,7 +563,7 @@ struct Tensor {
       sm.l[warp][r] = l;
     }
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i)
+    for (int i = 0; i < DV; ++i)
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
@@ -529,29 +576,21 @@ template <typename Core>
 __global__ void __launch_bounds__(kThreads, Core::kCtas)
     run_kernel(PagedProblem p, float* part) {
   using TI = typename Core::T;
+  constexpr int GG = Core::GG;
   // the ring, and then in its place the results
   extern __shared__ uint4 ring[];
-  Smem<Core::GG>& sm = *reinterpret_cast<Smem<Core::GG>*>(ring);
+  Smem<GG>& sm = *reinterpret_cast<Smem<GG>*>(ring);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
-  const Sums at = scan_requests(p, blockIdx.x, -1, blockIdx.x == 0);
-  // as many runs as CTAs, or one for each unit where there are fewer of these
-  const long long U = at.all * p.HG, N = min((long long)gridDim.x, U);
-  if ((long long)blockIdx.x >= N) return;
-  const long long r0 = (long long)blockIdx.x * U / N, r1 = ((long long)blockIdx.x + 1) * U / N;
-  int b = at.b;
+  const Place at = find_place(p, blockIdx.x, gridDim.x, -1, blockIdx.x == 0);
+  if ((int)blockIdx.x >= at.cut.runs) return;
+  const long long r0 = at.cut.begin(blockIdx.x), r1 = at.cut.begin(blockIdx.x + 1);
+  int b = at.b, len = length_of(p, b, false), n_u = units_of(len);
   long long base = at.before * p.HG;  // the request's first unit
+  int hg = (int)quotient(r0 - base, n_u);
   const int heads = p.H / p.Hk, groups = p.HG / p.Hk;
   for (long long u = r0; u < r1;) {
-    int len = length_of(p, b, false), n_u = units_of(len);
-    while (u >= base + (long long)n_u * p.HG) {
-      base += (long long)n_u * p.HG;
-      ++b;
-      len = length_of(p, b, false);
-      n_u = units_of(len);
-    }
-    const int hg = (int)((u - base) / n_u), kh = hg / groups, g0 = hg % groups * p.GG;
-    const int ng = min(p.GG, heads - g0);
+    const int kh = hg / groups, g0 = hg % groups * p.GG, ng = min(p.GG, heads - g0);
     const long long s0 = base + (long long)hg * n_u, s1 = s0 + n_u;  // the head's units
     const long long e = min(r1, s1);
     const int ra = (int)(u - s0) * kUnit, rb = min((int)(e - s0) * kUnit, max(len - 1, 0));
@@ -565,49 +604,69 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
     core.run(p, b, kb, vb, ra, rb, ring, warp, lane);
     if (Core::kRing > 0) __syncthreads();
     core.finish(p, sm, warp, lane);
-    long long self = 0;
-    if (whole && len > 0) {
-      self = row_at(p, b, len - 1);
+    const bool own_row = whole && len > 0;
+    const long long self = own_row ? row_at(p, b, len - 1) : 0;
+    if (own_row) {
       for (int g = warp; g < ng; g += kWarps) {
         const float s = self_dot<TI>(p, qb + (long long)g * p.qsH, kb + self, lane);
         if (lane == 0) sm.self[g] = s;
       }
     }
     __syncthreads();
-    const int c = threadIdx.x;
-    if (c < p.d) {
-      const float vi = whole && len > 0 ? ldf(vb + self + c) : 0.f;
-      for (int g = 0; g < ng; ++g) {
-        float M = -INFINITY, L = 0.f, Z = 0.f;
+    // a head per thread: the warps' weights, the gate
+    if ((int)threadIdx.x < ng) {
+      const int g = threadIdx.x;
+      float M = -INFINITY, L = 0.f, a[kWarps];
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm.m[w][g]);
+      for (int w = 0; w < kWarps; ++w) M = fmaxf(M, sm.m[w][g]);
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
-          const float a = sm.l[w][g] == 0.f ? 0.f : expf(sm.m[w][g] - M);
-          L = fmaf(a, sm.l[w][g], L);
-          Z = fmaf(a, sm.z[w][g][c], Z);
-        }
-        if (whole) {
-          epilogue<TI>(p, b, h0 + g, len, len > 0 ? sm.self[g] : 0.f, M, L, Z, c, vi);
-        } else {  // slot 0: the run's first head (begun before it), 1: its last
-          float* o = part + (((long long)blockIdx.x * 2 + (u == s0)) * p.GG + g) * kPart;
-          if (c == 0) {
-            o[0] = M;
-            o[1] = L;
-          }
-          o[2 + c] = Z;
-        }
+      for (int w = 0; w < kWarps; ++w) {
+        const float l = sm.l[w][g];
+        a[w] = l == 0.f ? 0.f : expf(sm.m[w][g] - M);
+        L = fmaf(a[w], l, L);
+      }
+      const float scale = whole ? len > 1 ? 1.0f / L : 0.f : 1.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) sm.m[w][g] = a[w] * scale;
+      if (whole) {
+        const Gate gate = gate_of(p, len, len > 0 ? sm.self[g] : 0.f, M, L);
+        sm.self[g] = gate.g;
+        p.logz[(long long)b * p.H + h0 + g] = gate.lz;
+      } else {
+        float* o = part + (((long long)blockIdx.x * 2 + (u == s0)) * p.GG + g) * kPart;
+        o[0] = M;
+        o[1] = L;
+      }
+    }
+    __syncthreads();
+    TI* out = reinterpret_cast<TI*>(p.out) + (long long)b * p.qsB + (long long)h0 * p.qsH;
+    for (int i = threadIdx.x; i < ng * p.d; i += kThreads) {
+      const int g = GG == 1 ? 0 : i / p.d, c = i - g * p.d;
+      float Z = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) Z = fmaf(sm.m[w][g], sm.z[w][g][c], Z);
+      if (whole) {
+        const float vi = own_row ? ldf(vb + self + c) : 0.f;
+        out[(long long)g * p.qsH + c] = (TI)fmaf(sm.self[g], Z - vi, vi);
+      } else {  // slot 0: the run's first head (begun before it), 1: its last
+        part[(((long long)blockIdx.x * 2 + (u == s0)) * p.GG + g) * kPart + 2 + c] = Z;
       }
     }
     __syncthreads();  // sm is written again
     u = e;
+    if (++hg == p.HG && u < r1) {
+      base += (long long)n_u * p.HG;
+      hg = 0;
+      len = length_of(p, ++b, false);
+      n_u = units_of(len);
+    }
   }
 }
 
 // Heads that several runs share: a CTA per (request, query head).  The runs' weights a thread each,
 // then their z with kAhead loads in flight.
 template <typename TI>
-__global__ void __launch_bounds__(kThreads) join_kernel(PagedProblem p, const float* part, int most) {
+__global__ void __launch_bounds__(kThreads, 8) join_kernel(PagedProblem p, const float* part, int most) {
   constexpr int kAhead = 16;
   __shared__ float self, red[kWarps], w[kThreads], lw[kThreads];
   const int b = blockIdx.x / p.H, h = blockIdx.x % p.H, c = threadIdx.x;
@@ -615,12 +674,11 @@ __global__ void __launch_bounds__(kThreads) join_kernel(PagedProblem p, const fl
   const int heads = p.H / p.Hk, groups = p.HG / p.Hk;
   const int kh = h / heads, hg = kh * groups + (h - kh * heads) / p.GG, g = (h - kh * heads) % p.GG;
   pdl_wait_and_launch();
-  const Sums at = scan_requests(p, 0, b, false);
+  const Place at = find_place(p, 0, most, b, false);
   const int len = length_of(p, b, false);
-  const long long U = at.all * p.HG, n_u = units_of(len), s0 = at.before * p.HG + hg * n_u;
-  const long long runs = min((long long)most, U);
+  const long long n_u = units_of(len), s0 = at.before * p.HG + hg * n_u;
   // the runs that hold the head's first and last unit
-  const int k0 = (int)(((s0 + 1) * runs - 1) / U), k1 = (int)(((s0 + n_u) * runs - 1) / U);
+  const int k0 = at.cut.owner(s0), k1 = at.cut.owner(s0 + n_u - 1);
   if (k0 == k1) return;  // (finished there)
   const long long row = row_at(p, b, len - 1) + (long long)kh * p.sC;
   const float vi = c < p.d ? ldf(reinterpret_cast<const TI*>(p.v) + row + c) : 0.f;
@@ -665,7 +723,11 @@ __global__ void __launch_bounds__(kThreads) join_kernel(PagedProblem p, const fl
       }
     }
   }
-  if (c < p.d) epilogue<TI>(p, b, h, len, self, M, L, Z, c, vi);
+  if (c >= p.d) return;
+  const Gate gate = gate_of(p, len, self, M, L);
+  reinterpret_cast<TI*>(p.out)[(long long)b * p.qsB + (long long)h * p.qsH + c] =
+      (TI)fmaf(gate.g, Z / L - vi, vi);
+  if (c == 0) p.logz[(long long)b * p.H + h] = gate.lz;
 }
 
 template <typename Core>
@@ -678,7 +740,7 @@ cudaError_t launch_core(const PagedProblem& p, float* part, cudaStream_t s) {
     return e;
   }
   constexpr int smem = Core::kRing > (int)sizeof(Smem<Core::GG>) ? Core::kRing : (int)sizeof(Smem<Core::GG>);
-  if (smem > 48 * 1024 &&
+  if (smem > 40 * 1024 &&  // (48 KB, less what the kernel declares)
       (e = cudaFuncSetAttribute(run_kernel<Core>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem)) !=
           cudaSuccess) {
     note_failure("paged decode: shared memory");
@@ -720,8 +782,10 @@ cudaError_t launch_t(PagedProblem p, float* part, cudaStream_t s) {
   for (long long x : {p.sP, p.sR, p.sC}) low |= (uintptr_t)(x * (long long)sizeof(TI));
   if (low % 16 == 0 && p.d % VE == 0) {
     if constexpr (sizeof(TI) == 2) {
-      if (G > 1 && p.d <= 64) return launch_core<Tensor<64>>(p, part, s);
-      if (G > 1) return launch_core<Tensor<128>>(p, part, s);
+      if (G > 1 && p.d <= 32) return launch_core<Tensor<1>>(p, part, s);
+      if (G > 1 && p.d <= 64) return launch_core<Tensor<2>>(p, part, s);
+      if (G > 1 && p.d <= 96) return launch_core<Tensor<3>>(p, part, s);
+      if (G > 1) return launch_core<Tensor<4>>(p, part, s);
     }
     if (n <= most / 4) return launch_lanes<TI, most / 4, true>(p, part, s);
     if (n <= most / 2) return launch_lanes<TI, most / 2, true>(p, part, s);
