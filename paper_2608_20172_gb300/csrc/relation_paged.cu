@@ -344,8 +344,9 @@ struct Lanes {
     }
   }
   // this warp's tiles of rows ra .. rb - 1
-  __device__ __forceinline__ void run(const PagedProblem& p, int b, const TI* kb, const TI* vb, int ra,
-                                      int rb, uint4*, int warp, int lane) {
+  __device__ __forceinline__ void run(const PagedProblem& p, int b, const TI* qb, int ng, const TI* kb,
+                                      const TI* vb, int ra, int rb, uint4*, int warp, int lane) {
+    start(p, qb, ng, lane);
     // rows past the end read the last one, and are left out of the tile
     auto row = [&](int j) { return min(j + lane % R, rb - 1); };
     int j = ra + warp * R;
@@ -416,16 +417,18 @@ struct Tensor {
 
   __device__ __forceinline__ void start(const PagedProblem& p, const T* qb, int ng, int lane) {
     const int r = lane >> 2, t = lane & 3;
+    const T* x = qb + (long long)min(r, ng - 1) * p.qsH + 8 * t;  // (d is a multiple of 8)
+    const bool whole = (reinterpret_cast<uintptr_t>(x) & 15u) == 0;
 #pragma unroll
-    for (int i = 0; i < DK; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = 8 * (t + 4 * i) + 2 * e;
-        const T* x = qb + (long long)r * p.qsH + c;  // (d is a multiple of 8)
-        const bool in = r < ng && c < p.d;
-        const unsigned lo = in ? __bfloat16_as_ushort(x[0]) : 0, hi = in ? __bfloat16_as_ushort(x[1]) : 0;
-        q[i][e] = lo | hi << 16;
-      }
+    for (int i = 0; i < DK; ++i) {
+      uint4 w = make_uint4(0, 0, 0, 0);
+      if (r < ng && 32 * i + 8 * t < p.d)
+        w = whole ? load_group<T, true>(x, 32 * i, 32 * i + 8) : load_group<T, false>(x, 32 * i, 32 * i + 8);
+      q[i][0] = w.x;
+      q[i][1] = w.y;
+      q[i][2] = w.z;
+      q[i][3] = w.w;
+    }
 #pragma unroll
     for (int i = 0; i < DV; ++i)
 #pragma unroll
@@ -453,8 +456,8 @@ struct Tensor {
       }
     }
   }
-  __device__ __forceinline__ void run(const PagedProblem& p, int b, const T* kb, const T* vb, int ra,
-                                      int rb, uint4* ring, int warp, int lane) {
+  __device__ __forceinline__ void run(const PagedProblem& p, int b, const T* qb, int ng, const T* kb,
+                                      const T* vb, int ra, int rb, uint4* ring, int warp, int lane) {
     constexpr int step = kWarps * R;
     uint4* mine = ring + warp * S * kStage;
     int j = ra + warp * R;
@@ -475,6 +478,7 @@ struct Tensor {
       cp_commit();
     }
     int ahead = next[S];
+    start(p, qb, ng, lane);
     for (int st = 0; j < rb; j += step, st = st + 1 == S ? 0 : st + 1) {
       const int at = j + S * step;
       const int later = id(at + step);
@@ -600,8 +604,7 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
     const int h0 = kh * heads + g0;
     const TI* qb = reinterpret_cast<const TI*>(p.q) + (long long)b * p.qsB + (long long)h0 * p.qsH;
     Core core;
-    core.start(p, qb, ng, lane);
-    core.run(p, b, kb, vb, ra, rb, ring, warp, lane);
+    core.run(p, b, qb, ng, kb, vb, ra, rb, ring, warp, lane);
     if (Core::kRing > 0) __syncthreads();
     core.finish(p, sm, warp, lane);
     const bool own_row = whole && len > 0;
