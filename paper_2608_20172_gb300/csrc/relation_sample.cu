@@ -37,8 +37,8 @@ constexpr int kMaxSlice = 32 * 1024;  // tokens of a CTA
 constexpr int kIndexBits = 22;        // of the key: 30 bits of w, then the index from the top down
 constexpr int kFirst = 87;            // the exponent of 2^-40, below which a weight is 0
 constexpr int kDigit = 8;             // further digits
-constexpr int kList = 768;            // tokens that are ranked against each other
-constexpr int kAlone = 128;           // so few that every CTA ranks them all
+constexpr int kList = 1024;           // tokens of a bin that every CTA goes through by itself,
+constexpr int kRanked = 32;           // and that are ranked against each other
 
 // A slice of at most 2^(32 - LOW) tokens: its bins' sums of LOW-bit numbers stay below 2^32.
 constexpr int low_bits(bool wide) { return wide ? 17 : 18; }
@@ -48,28 +48,32 @@ template <int LOW>
 struct Smem {
   static constexpr int kBins = bins_of(LOW);
   union {
-    unsigned hist[2][kBins];          // this CTA's bins: tokens, sums of the low bits
-    struct {                          // later:
-      unsigned part[4][1 << kDigit];  // a digit's histogram: tokens, the masses in 14-bit parts,
-      unsigned d_count[1 << kDigit];  // the cluster's
-      u64 d_mass[1 << kDigit];
-    };
-    struct {                          // and in turn:
-      u64 all[kList];                 // keys of the cluster's tokens in the cut's bin
-      u64 extra[kThreads];            // kept mass of every run that lies in that bin
+    unsigned hist[2][kBins];            // this CTA's bins: tokens, sums of the low bits
+    struct {                            // later:
+      u64 all[kList];                   // keys of the cluster's tokens in the cut's bin
+      union {
+        struct {
+          unsigned part[4][1 << kDigit];  // a digit's histogram: tokens, the masses in 14-bit parts,
+          unsigned d_count[1 << kDigit];  // its sums
+          u64 d_mass[1 << kDigit];
+        };
+        u64 extra[kThreads];            // kept mass of every run that lies in that bin
+      };
     };
   };
   unsigned count[kBins];              // the cluster's bins: tokens and masses
   u64 mass[kBins];
   u64 list[2][kList];                 // this CTA's tokens in the cut's bin, of the first and second cut
   int sizes[2][kMaxCluster], n_list;  // every CTA's number of them
-  u64 scan[2][kWarps], total;
+  u64 few[kRanked];                   // the last of them
+  u64 scan_mass[kWarps], total;
+  unsigned scan_count[kWarps];
   u64 kept[kMaxCluster];              // of every CTA: its kept mass,
   float max[kMaxCluster];             // its largest logit (NaN: it has one)
   float red[kWarps];
   // what the threads tell each other
-  unsigned bin, inside;
-  u64 above_count, above_mass, key, key_mass;
+  unsigned bin, inside, above_count;
+  u64 above_mass, key, key_mass;
 };
 
 // floor(2^40 w) for 0 <= w <= 1 from the bits of w.  (The conversion instruction to 64 bits bounds a
@@ -106,30 +110,34 @@ __device__ __forceinline__ u64 mass_of(int bin, unsigned count, u64 low) {
 }
 
 // This thread's exclusive sums over the block.
-__device__ __forceinline__ void block_scan(u64 (*part)[kWarps], u64& a, u64& b) {
+template <typename S>
+__device__ __forceinline__ void block_scan(S& sm, unsigned& c, u64& m) {
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  u64 as = a, bs = b;
+  unsigned cs = c;
+  u64 ms = m;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const u64 x = __shfl_up_sync(0xffffffffu, as, o), y = __shfl_up_sync(0xffffffffu, bs, o);
+    const unsigned x = __shfl_up_sync(0xffffffffu, cs, o);
+    const u64 y = __shfl_up_sync(0xffffffffu, ms, o);
     if (lane >= o) {
-      as += x;
-      bs += y;
+      cs += x;
+      ms += y;
     }
   }
-  __syncthreads();  // part is free
+  __syncthreads();  // the sums of the last scan have been read
   if (lane == 31) {
-    part[0][warp] = as;
-    part[1][warp] = bs;
+    sm.scan_count[warp] = cs;
+    sm.scan_mass[warp] = ms;
   }
   __syncthreads();
-  a = as - a;
-  b = bs - b;
+  c = cs - c;
+  m = ms - m;
 #pragma unroll
   for (int i = 0; i < kWarps; ++i) {
-    const u64 x = part[0][i], y = part[1][i];
-    a += i < warp ? x : 0;
-    b += i < warp ? y : 0;
+    const unsigned x = sm.scan_count[i];
+    const u64 y = sm.scan_mass[i];
+    c += i < warp ? x : 0;
+    m += i < warp ? y : 0;
   }
 }
 
@@ -139,9 +147,11 @@ struct Bins {
   const unsigned* count;
   const u64* mass;
   int first, last;  // from, and down to but without
-  u64 c, m;
-  __device__ __forceinline__ Bins(const unsigned* count, const u64* mass, int bins, u64 above_count,
-                                  u64 above_mass, u64 (*part)[kWarps], u64* total)
+  unsigned c;
+  u64 m;
+  template <typename S>
+  __device__ __forceinline__ Bins(S& sm, const unsigned* count, const u64* mass, int bins,
+                                  unsigned above_count, u64 above_mass, u64* total)
       : count(count), mass(mass), c(0), m(0) {
     const int per = (bins + kThreads - 1) / kThreads;
     first = bins - 1 - (int)threadIdx.x * per;
@@ -151,7 +161,7 @@ struct Bins {
       m += mass[d];
     }
     const u64 own = m;
-    block_scan(part, c, m);
+    block_scan(sm, c, m);
     if (total && threadIdx.x == kThreads - 1) *total = m + own;
     c += above_count;
     m += above_mass;
@@ -162,17 +172,19 @@ struct Bins {
   __device__ __forceinline__ void find(S& sm, bool by_mass, u64 want) const {
     if (threadIdx.x == 0) sm.inside = 0;
     __syncthreads();
-    u64 ca = c, ma = m;
+    unsigned ca = c;
+    u64 ma = m;
     for (int d = first; d > last; --d) {
-      const u64 before = by_mass ? ma : ca, own = by_mass ? mass[d] : count[d];
-      if (before < want && want <= before + own) {
+      const unsigned n = count[d];
+      const u64 q = mass[d];
+      if (by_mass ? ma < want && want <= ma + q : ca < want && want <= (u64)ca + n) {
         sm.bin = d;
-        sm.inside = count[d];
+        sm.inside = n;
         sm.above_count = ca;
         sm.above_mass = ma;
       }
-      ca += count[d];
-      ma += mass[d];
+      ca += n;
+      ma += q;
     }
     __syncthreads();
   }
@@ -196,10 +208,47 @@ __device__ __forceinline__ void add_bins(cg::cluster_group& cl, S& sm, unsigned*
   cl.sync();
 }
 
+// Sums of fixed_of in 32-bit operations: floor(2^20 w) is what remains of w 2^20 + 2^23 when the sum
+// is cut to its 24 bits, and the rest of w 2^20 gives the next 20 bits in the same way; both numbers
+// are added up with the bits of 2^23, which `value` takes off again.  At most 2^11 weights.
+struct Mass {
+  unsigned hi = 0, lo = 0, n = 0;
+  __device__ __forceinline__ void add(float w) {
+    const float t = __fmaf_rz(w, 1048576.f, 8388608.f);
+    const float f = __fmaf_rn(t, 1048576.f, -8796093022208.f);  // 2^20 floor(2^20 w)
+    const float r = __fadd_rz(__fmaf_rn(w, 1099511627776.f, -f), 8388608.f);
+    hi += __float_as_uint(t);
+    lo += __float_as_uint(r);
+    ++n;
+  }
+  __device__ __forceinline__ u64 value() const {
+    const unsigned bias = n * 0x4b000000u;
+    return ((u64)(hi - bias) << 20) + (lo - bias);
+  }
+};
+
 // A thread's run of the slice, w[i0 .. i1).
 struct Run {
   int i0, i1, len;
 };
+
+__device__ __forceinline__ void clear(unsigned* x, int n) {
+  for (int i = threadIdx.x; i < n; i += kThreads) x[i] = 0;
+}
+// A key's digit at `shift` into the digit's histogram.
+template <typename S>
+__device__ __forceinline__ void count_digit(S& sm, u64 key, int shift, int bits) {
+  const unsigned d = (unsigned)(key >> shift) & ((1u << bits) - 1);
+  const u64 q = weight_of_key(key);
+  atomicAdd(&sm.part[0][d], 1u);
+  atomicAdd(&sm.part[1][d], (unsigned)q & 0x3fff);
+  atomicAdd(&sm.part[2][d], (unsigned)(q >> 14) & 0x3fff);
+  atomicAdd(&sm.part[3][d], (unsigned)(q >> 28));
+}
+template <typename S>
+__device__ __forceinline__ u64 part_mass(const S& sm, int i) {
+  return (u64)sm.part[1][i] + ((u64)sm.part[2][i] << 14) + ((u64)sm.part[3][i] << 28);
+}
 
 // The key of the cut that lies in sm.bin, among sm.inside tokens, and the mass down to and with it.
 // *above (if set) gets the mass of this thread's run down to the cut, without weights below min_p.
@@ -210,22 +259,24 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
   const int tid = threadIdx.x, C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   u64 prefix = sm.bin + ((u64)kFirst << (23 - LOW));  // the key's bits from `shift` up
   int shift = kIndexBits + LOW;
-  u64 above_count = sm.above_count, above_mass = sm.above_mass;
+  unsigned above_count = sm.above_count;
+  u64 above_mass = sm.above_mass;
+  auto narrow = [&](int bits) {  // to the digit's bin
+    Bins(sm, sm.d_count, sm.d_mass, 1 << kDigit, above_count, above_mass, nullptr)
+        .find(sm, by_mass, want);
+    prefix = prefix << bits | sm.bin;
+    above_count = sm.above_count;
+    above_mass = sm.above_mass;
+  };
   while (sm.inside > kList) {
     const int bits = min(kDigit, shift);
     shift -= bits;
     __syncthreads();
-    for (int i = tid; i < 4 << kDigit; i += kThreads) (&sm.part[0][0])[i] = 0;
+    clear(&sm.part[0][0], 4 << kDigit);
     __syncthreads();
     for (int i = run.i0; i < run.i1; ++i) {
       const u64 key = key_of(w[i], j0 + i);
-      if (key >> (shift + bits) != prefix) continue;
-      const unsigned d = (unsigned)(key >> shift) & ((1u << bits) - 1);
-      const u64 q = fixed_of(w[i]);
-      atomicAdd(&sm.part[0][d], 1u);
-      atomicAdd(&sm.part[1][d], (unsigned)q & 0x3fff);
-      atomicAdd(&sm.part[2][d], (unsigned)(q >> 14) & 0x3fff);
-      atomicAdd(&sm.part[3][d], (unsigned)(q >> 28));
+      if (key >> (shift + bits) == prefix) count_digit(sm, key, shift, bits);
     }
     add_bins(cl, sm, sm.d_count, sm.d_mass, 1 << kDigit, [&](int i, unsigned& c, u64& m) {
 #pragma unroll
@@ -233,37 +284,34 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
         if (r >= C) break;
         const Smem<LOW>* o = cl.map_shared_rank(&sm, r);
         c += o->part[0][i];
-        m += (u64)o->part[1][i] + ((u64)o->part[2][i] << 14) + ((u64)o->part[3][i] << 28);
+        m += part_mass(*o, i);
       }
     });
-    Bins(sm.d_count, sm.d_mass, 1 << kDigit, above_count, above_mass, sm.scan, nullptr)
-        .find(sm, by_mass, want);
-    prefix = prefix << bits | sm.bin;
-    above_count = sm.above_count;
-    above_mass = sm.above_mass;
+    narrow(bits);
   }
   // The bin's tokens, of all CTAs, and the run's mass above it.  (Mostly the weight's bits alone
   // tell where a token lies.)
   if (tid == 0) sm.n_list = 0;
   __syncthreads();
   u64* list = sm.list[which];
-  u64 sum = 0;
-  const unsigned high = shift >= kIndexBits ? (unsigned)prefix : 0;
+  Mass sum;
+  if (shift >= kIndexBits) {
+    const int right = shift - kIndexBits;
+    const unsigned high = (unsigned)prefix;
 #pragma unroll 4
-  for (int i = run.i0; i < run.i1; ++i) {
-    const float x = w[i];
-    bool in, over;
-    if (shift >= kIndexBits) {
-      const unsigned bits = __float_as_uint(x) >> (shift - kIndexBits);
-      in = bits == high;
-      over = bits > high;
-    } else {
-      const u64 key = key_of(x, j0 + i) >> shift;
-      in = key == prefix;
-      over = key > prefix;
+    for (int i = run.i0; i < run.i1; ++i) {
+      const float x = w[i];
+      const unsigned bits = __float_as_uint(x) >> right;
+      if (bits == high) list[atomicAdd(&sm.n_list, 1)] = key_of(x, j0 + i);
+      if (above) sum.add(bits > high && !(x < min_p) ? x : 0.f);
     }
-    if (in) list[atomicAdd(&sm.n_list, 1)] = key_of(x, j0 + i);
-    if (over && !(x < min_p)) sum += fixed_of(x);
+  } else {
+    for (int i = run.i0; i < run.i1; ++i) {
+      const float x = w[i];
+      const u64 key = key_of(x, j0 + i), high = key >> shift;
+      if (high == prefix) list[atomicAdd(&sm.n_list, 1)] = key;
+      if (above) sum.add(high > prefix && !(x < min_p) ? x : 0.f);
+    }
   }
   __syncthreads();
   const int mine = sm.n_list;
@@ -278,49 +326,52 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
     for (int i = tid; i < m; i += kThreads) sm.all[total + i] = from[i];
     total += m;
   }
-  sm.extra[tid] = 0;
+  // from here on every CTA by itself: further digits of these tokens,
+  unsigned left = total;
+  while (left > kRanked) {
+    const int bits = min(kDigit, shift);
+    shift -= bits;
+    clear(&sm.part[0][0], 4 << kDigit);
+    __syncthreads();
+    for (int i = tid; i < total; i += kThreads) {
+      const u64 key = sm.all[i];
+      if (key >> (shift + bits) == prefix) count_digit(sm, key, shift, bits);
+    }
+    __syncthreads();
+    for (int i = tid; i < 1 << kDigit; i += kThreads) {
+      sm.d_count[i] = sm.part[0][i];
+      sm.d_mass[i] = part_mass(sm, i);
+    }
+    __syncthreads();
+    narrow(bits);
+    left = sm.inside;
+  }
+  // and the last ones' ranks
+  if (tid == 0) sm.n_list = 0;
   __syncthreads();
-  // Few tokens: every CTA ranks them all.  More: its own, and tells the others of the cut.
-  const bool alone = total <= kAlone;
-  const u64* ranked = alone ? sm.all : list;
-  const int n_ranked = alone ? total : mine;
-  int group = 32;  // threads of a token
-  while (group > 1 && n_ranked * group > kThreads) group >>= 1;
-  const int sub = tid % group;
-  for (int g0 = 0; g0 < n_ranked; g0 += kThreads / group) {
-    const int g = g0 + tid / group;
-    const u64 key = g < n_ranked ? ranked[g] : ~0ull;
-    u64 c = 0, m = 0;
-#pragma unroll 4
-    for (int i = sub; i < total; i += group) {
-      const u64 other = sm.all[i];
+  for (int i = tid; i < total; i += kThreads) {
+    const u64 key = sm.all[i];
+    if (key >> shift == prefix) sm.few[atomicAdd(&sm.n_list, 1)] = key;
+  }
+  __syncthreads();
+  if (tid < (int)left) {
+    const u64 key = sm.few[tid], q = weight_of_key(key);
+    unsigned c = above_count;
+    u64 m = above_mass;
+    for (int i = 0; i < (int)left; ++i) {
+      const u64 other = sm.few[i];
       if (other > key) {
         ++c;
         m += weight_of_key(other);
       }
     }
-    for (int o = group >> 1; o > 0; o >>= 1) {
-      c += __shfl_xor_sync(0xffffffffu, c, o);
-      m += __shfl_xor_sync(0xffffffffu, m, o);
-    }
-    if (g < n_ranked && sub == 0) {
-      c += above_count;
-      m += above_mass;
-      const u64 q = weight_of_key(key);
-      if (by_mass ? m < want && want <= m + q : c + 1 == want) {
-        for (int r = 0; r < C; ++r) {
-          Smem<LOW>* o = alone ? &sm : cl.map_shared_rank(&sm, r);
-          o->key = key;
-          o->key_mass = m + q;
-          if (alone) break;
-        }
-      }
+    if (by_mass ? m < want && want <= m + q : c + 1 == want) {
+      sm.key = key;
+      sm.key_mass = m + q;
     }
   }
-  if (alone)
-    __syncthreads();
-  else
-    cl.sync();
+  if (above) sm.extra[tid] = 0;
+  __syncthreads();
   const u64 found = sm.key;
   *mass = sm.key_mass;
   if (above) {
@@ -331,9 +382,9 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
         atomicAdd(&sm.extra[at / run.len], weight_of_key(key));
     }
     __syncthreads();
-    *above = sum + sm.extra[tid];
+    *above = sum.value() + sm.extra[tid];
   }
-  __syncthreads();  // (sm.key and the lists' neighbours are written again)
+  __syncthreads();  // (sm.key and the digit's histogram are written again)
   return found;
 }
 
@@ -446,21 +497,28 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
   // (greedy: a difference times infinity)
   const float slope = greedy ? INFINITY : scale;
   u64 sum = 0;
-#pragma unroll 4
-  for (int i = i0; i < i1; ++i) {
+  auto weight_of = [&](int i) {
     const float v = w[i];
-    const float e = v == M ? 1.f : expf(__fmul_rn(__fsub_rn(v, M), slope));
-    w[i] = e;
-    if (by_k || by_p) {
-      const unsigned bits = __float_as_uint(e);
+    return w[i] = v == M ? 1.f : expf(__fmul_rn(__fsub_rn(v, M), slope));
+  };
+  if (by_k || by_p) {
+#pragma unroll 4
+    for (int i = i0; i < i1; ++i) {
+      const unsigned bits = __float_as_uint(weight_of(i));
       const int bin = (int)(bits >> LOW) - (kFirst << (23 - LOW));
       if (bin >= 0) {
         atomicAdd(&sm.hist[0][bin], 1u);
-        atomicAdd(&sm.hist[1][bin], low_part<LOW>(bits));
+        if (by_p) atomicAdd(&sm.hist[1][bin], low_part<LOW>(bits));  // (counts alone find the k-th)
       }
-    } else if (!(e < min_p)) {
-      sum += fixed_of(e);
     }
+  } else {
+    Mass kept;
+#pragma unroll 4
+    for (int i = i0; i < i1; ++i) {
+      const float e = weight_of(i);
+      kept.add(e < min_p ? 0.f : e);
+    }
+    sum = kept.value();
   }
   u64 least = 0;
   if (by_k || by_p) {
@@ -480,7 +538,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
       }
       m = mass_of<LOW>(i, c, low);
     });
-    const Bins bins(sm.count, sm.mass, S::kBins, 0, 0, sm.scan, &sm.total);
+    const Bins bins(sm, sm.count, sm.mass, S::kBins, 0, 0, &sm.total);
     __syncthreads();
     u64 mass = sm.total;
     bool summed = false;
@@ -497,8 +555,11 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
       least = find_key<LOW>(cl, sm, w, run, j0, 1, true, (u64)max(want, 1LL), min_p, &mass, &sum);
       summed = true;
     }
-    if (!summed)  // fewer than k tokens with a weight
-      for (int i = i0; i < i1; ++i) sum += w[i] < min_p ? 0 : fixed_of(w[i]);
+    if (!summed) {  // fewer than k tokens with a weight
+      Mass kept;
+      for (int i = i0; i < i1; ++i) kept.add(w[i] < min_p ? 0.f : w[i]);
+      sum = kept.value();
+    }
   }
   // the kept weights in the order of the indices
   const unsigned least_w = (unsigned)(least >> kIndexBits);
@@ -508,8 +569,9 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
     const bool in = bits > least_w || (bits == least_w && j0 + i <= last_j);
     return in && !(w[i] < min_p) ? fixed_of(w[i]) : 0;
   };
-  u64 before = sum, none = 0;
-  block_scan(sm.scan, before, none);
+  u64 before = sum;
+  unsigned none = 0;
+  block_scan(sm, none, before);
   if (tid == kThreads - 1) sm.total = before + sum;
   __syncthreads();
   if (tid < C) cl.map_shared_rank(&sm, tid)->kept[rank] = sm.total;
