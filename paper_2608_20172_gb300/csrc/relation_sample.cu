@@ -33,7 +33,8 @@ using u64 = unsigned long long;
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kMaxSlice = 32 * 1024;  // tokens of a CTA
+constexpr int kMaxSlice = 32 * 1024;  // tokens of a CTA,
+constexpr int kShort = 16 * 1024;     // and of one that shares an SM with another
 constexpr int kIndexBits = 22;        // of the key: 30 bits of w, then the index from the top down
 constexpr int kFirst = 87;            // the exponent of 2^-40, below which a weight is 0
 constexpr int kDigit = 8;             // further digits
@@ -130,15 +131,26 @@ __device__ __forceinline__ void block_scan(S& sm, unsigned& c, u64& m) {
     sm.scan_mass[warp] = ms;
   }
   __syncthreads();
-  c = cs - c;
-  m = ms - m;
+  if (warp == 0 && lane < kWarps) {
+    const unsigned c0 = sm.scan_count[lane];
+    const u64 m0 = sm.scan_mass[lane];
+    unsigned x = c0;
+    u64 y = m0;
 #pragma unroll
-  for (int i = 0; i < kWarps; ++i) {
-    const unsigned x = sm.scan_count[i];
-    const u64 y = sm.scan_mass[i];
-    c += i < warp ? x : 0;
-    m += i < warp ? y : 0;
+    for (int o = 1; o < kWarps; o <<= 1) {
+      const unsigned xo = __shfl_up_sync(0xffffu, x, o);
+      const u64 yo = __shfl_up_sync(0xffffu, y, o);
+      if (lane >= o) {
+        x += xo;
+        y += yo;
+      }
+    }
+    sm.scan_count[lane] = x - c0;
+    sm.scan_mass[lane] = y - m0;
   }
+  __syncthreads();
+  c = cs - c + sm.scan_count[warp];
+  m = ms - m + sm.scan_mass[warp];
 }
 
 // A histogram's bins from the highest down, a run of them per thread, and the sums above this
@@ -261,13 +273,6 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
   int shift = kIndexBits + LOW;
   unsigned above_count = sm.above_count;
   u64 above_mass = sm.above_mass;
-  auto narrow = [&](int bits) {  // to the digit's bin
-    Bins(sm, sm.d_count, sm.d_mass, 1 << kDigit, above_count, above_mass, nullptr)
-        .find(sm, by_mass, want);
-    prefix = prefix << bits | sm.bin;
-    above_count = sm.above_count;
-    above_mass = sm.above_mass;
-  };
   while (sm.inside > kList) {
     const int bits = min(kDigit, shift);
     shift -= bits;
@@ -287,7 +292,11 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
         m += part_mass(*o, i);
       }
     });
-    narrow(bits);
+    Bins(sm, sm.d_count, sm.d_mass, 1 << kDigit, above_count, above_mass, nullptr)
+        .find(sm, by_mass, want);
+    prefix = prefix << bits | sm.bin;
+    above_count = sm.above_count;
+    above_mass = sm.above_mass;
   }
   // The bin's tokens, of all CTAs, and the run's mass above it.  (Mostly the weight's bits alone
   // tell where a token lies.)
@@ -338,12 +347,46 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
       if (key >> (shift + bits) == prefix) count_digit(sm, key, shift, bits);
     }
     __syncthreads();
-    for (int i = tid; i < 1 << kDigit; i += kThreads) {
-      sm.d_count[i] = sm.part[0][i];
-      sm.d_mass[i] = part_mass(sm, i);
+    if (tid < 32) {  // one warp, 8 bins a lane, from the highest down
+      constexpr int kPer = (1 << kDigit) / 32;
+      const int first = (1 << kDigit) - 1 - tid * kPer;
+      unsigned c = 0;
+      u64 m = 0;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) {
+        c += sm.part[0][first - i];
+        m += part_mass(sm, first - i);
+      }
+      unsigned ca = c;
+      u64 ma = m;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const unsigned x = __shfl_up_sync(0xffffffffu, ca, o);
+        const u64 y = __shfl_up_sync(0xffffffffu, ma, o);
+        if (tid >= o) {
+          ca += x;
+          ma += y;
+        }
+      }
+      ca += above_count - c;
+      ma += above_mass - m;
+      for (int i = 0; i < kPer; ++i) {
+        const unsigned n = sm.part[0][first - i];
+        const u64 q = part_mass(sm, first - i);
+        if (by_mass ? ma < want && want <= ma + q : ca < want && want <= (u64)ca + n) {
+          sm.bin = first - i;
+          sm.inside = n;
+          sm.above_count = ca;
+          sm.above_mass = ma;
+        }
+        ca += n;
+        ma += q;
+      }
     }
     __syncthreads();
-    narrow(bits);
+    prefix = prefix << bits | sm.bin;
+    above_count = sm.above_count;
+    above_mass = sm.above_mass;
     left = sm.inside;
   }
   // and the last ones' ranks
@@ -621,10 +664,17 @@ cudaError_t launch_low(const SampleProblem& p, int cluster, int slice, cudaStrea
 
 template <typename TI>
 cudaError_t launch_t(const SampleProblem& p, cudaStream_t s) {
-  int cluster = 1;  // at least 4096 tokens per CTA
-  while (cluster < kMaxCluster && p.V > 4096 * cluster) cluster *= 2;
+  // As many CTAs per row as the GPU holds at once over all rows (two per SM), but 4096 tokens each and
+  // no more than kShort, where there is a choice: what a CTA waits for its cluster costs the same
+  // whatever its slice, so that longer slices in one round beat shorter ones in two (64 rows of 50257:
+  // 35 us with 8 CTAs a row, 27 with 4).
+  auto up = [](int a, int b) { return (a + b - 1) / b; };
+  const int fit = 2 * 152 / p.R, need = up(p.V, kShort - 8), most = up(p.V, 4096);
+  int cluster = fit < need ? need : fit;
+  cluster = cluster < most ? cluster : most;
+  cluster = cluster < 1 ? 1 : cluster < kMaxCluster ? cluster : kMaxCluster;
   const int slice = ((p.V + cluster - 1) / cluster + 7) / 8 * 8;
-  if (slice <= 1 << (32 - low_bits(false))) return launch_low<TI, low_bits(false)>(p, cluster, slice, s);
+  if (slice <= kShort) return launch_low<TI, low_bits(false)>(p, cluster, slice, s);
   return launch_low<TI, low_bits(true)>(p, cluster, slice, s);
 }
 
