@@ -535,10 +535,14 @@ def page_plan(lengths, counts, block_table, free_pages, free_state, page_size: i
     if not _is_table(block_table, B, dev):
         raise ValueError("block_table must be an int32 [B, cols] tensor with contiguous rows on "
                          "the operands' device")
-    if out is None:  # one allocation, the slots first
-        slots, positions, starts, new, state = torch.empty(
-            3 * n + 2 * B + 3, dtype=_I32, device=lengths.device).split((2 * n, n, B + 1, B, 2))
-        out = PagePlan(slots.view(_I64), positions, starts, new, state)
+    if out is None:  # (five small allocations take less than one and its views)
+        on = lengths.device
+        slots = torch.empty(n, dtype=_I64, device=on)
+        positions = torch.empty(n, dtype=_I32, device=on)
+        starts = torch.empty(B + 1, dtype=_I32, device=on)
+        new = torch.empty(B, dtype=_I32, device=on)
+        state = torch.empty(2, dtype=_I32, device=on)
+        out = PagePlan(slots, positions, starts, new, state)
     else:
         slots, positions, starts, new, state = out
         _need("out.slots", slots, dev, _I64, n)
