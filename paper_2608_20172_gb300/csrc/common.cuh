@@ -65,6 +65,11 @@ struct Sum2 {
   }
 };
 
+// r / page for 0 <= r < 2^31 (page_division, kernels.h)
+__device__ __forceinline__ int page_of(int r, int page, unsigned mul, int shift) {
+  return page == 1 ? r : (int)(__umulhi((unsigned)r, mul) >> shift);
+}
+
 __device__ __forceinline__ unsigned long long globaltimer_ns() {
   unsigned long long t;
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));

@@ -239,8 +239,20 @@ struct PlanProblem {
   int* dev_status;      // nullable
   long long t_stride;
   int B, page, cols, n_pages, n_tokens;
+  unsigned page_mul;    // (set by the launcher: page_division)
+  int page_shift;
 };
-cudaError_t launch_plan(const PlanProblem& p, cudaStream_t s);
+cudaError_t launch_plan(PlanProblem p, cudaStream_t s);
+
+// Division of 0 <= r < 2^31 by a page size by multiplication (page_of, common.cuh): with
+// l = ceil(log2 page) >= 1 and M = floor(2^(31 + l) / page) + 1, r M is off by less than 2^(31 + l)
+// from r 2^(31 + l) / page.
+inline void page_division(int page, unsigned* mul, int* shift) {
+  int l = 1;
+  while (l < 31 && (1 << l) < page) ++l;
+  *mul = page > 1 ? (unsigned)((1ull << (31 + l)) / page + 1) : 0;
+  *shift = l - 1;
+}
 
 // New tokens into a paged cache (relation_append.cu): relation_cache_append's arguments.
 struct AppendProblem {

@@ -124,10 +124,8 @@ __device__ __forceinline__ int units_of(int len) {
   return len > 1 ? (len - 2) / kUnit + 1 : 1;
 }
 
-// r / page for 0 <= r < 2^31: with l = ceil(log2 page) >= 1 and M = floor(2^(31 + l) / page) + 1 the
-// product r M is off by less than 2^(31 + l) from r 2^(31 + l) / page (launch_t)
 __device__ __forceinline__ int page_of(const PagedProblem& p, int r) {
-  return p.page == 1 ? r : (int)(__umulhi((unsigned)r, p.page_mul) >> p.page_shift);
+  return rel::page_of(r, p.page, p.page_mul, p.page_shift);
 }
 // The page id of row r of request b, and with it the element offset of the row's head 0.  In two
 // steps, so that a loop can ask for an id a tile before it uses it.
@@ -777,10 +775,7 @@ cudaError_t launch_t(PagedProblem p, float* part, cudaStream_t s) {
   const int G = p.H / p.Hk, n = (p.d + VE - 1) / VE;
   p.GG = heads_at_once(G);
   p.HG = p.Hk * ((G + p.GG - 1) / p.GG);
-  int l = 1;
-  while (l < 31 && (1 << l) < p.page) ++l;
-  p.page_mul = p.page > 1 ? (unsigned)((1ull << (31 + l)) / p.page + 1) : 0;
-  p.page_shift = l - 1;
+  page_division(p.page, &p.page_mul, &p.page_shift);
   uintptr_t low = reinterpret_cast<uintptr_t>(p.k) | reinterpret_cast<uintptr_t>(p.v);
   for (long long x : {p.sP, p.sR, p.sC}) low |= (uintptr_t)(x * (long long)sizeof(TI));
   if (low % 16 == 0 && p.d % VE == 0) {
