@@ -217,9 +217,16 @@ cudaError_t launch_tok(const Args& ar, cudaStream_t s) {
 
 template <typename TI, int CH>
 cudaError_t launch_ch(const Args& ar, cudaStream_t s) {
-  // 8 tokens share the set-up of a CTA once there are CTAs for every SM
-  if (ar.p.N >= 8 * 152) return launch_tok<TI, CH, 8>(ar, s);
-  return launch_tok<TI, CH, 1>(ar, s);
+  // Tokens that share a CTA's set-up (row lookups, angles): few where the grid is short, whose time is
+  // one CTA's, more where the CTAs come in rounds.  us with 1, 2, 4, 8 tokens, one call after the other
+  // in a graph: 262 tokens of 8 x 96 bf16 3.0, 2.8, 3.6, 4.9; 1832 of 12 x 96 8.6, 7.4, 9.0, 10.5;
+  // 1821 of 2 x 32 6.5, 4.6, 2.9, 2.8; 11720 of 8 x 48 38, 23, 15, 14; 32768 of 16 x 128 152, 129,
+  // 125, 126 (6.4 TB/s).
+  const long long items = (long long)ar.p.H * (ar.p.d / CH), want = ar.p.N * items <= 400000 ? 160 : 1024;
+  if (items >= want) return launch_tok<TI, CH, 1>(ar, s);
+  if (2 * items >= want) return launch_tok<TI, CH, 2>(ar, s);
+  if (4 * items >= want) return launch_tok<TI, CH, 4>(ar, s);
+  return launch_tok<TI, CH, 8>(ar, s);
 }
 
 template <typename TI>
