@@ -359,7 +359,8 @@ relation_status relation_cache_append(const void* p1, const void* p2, const void
  *   workspace   device scratch of relation_paged_decode_workspace_size(H, cache, dt) bytes, 16-byte
  *               aligned; it does not grow with the batch or the cache.
  * fp32 or bf16 with any 1 <= d_h <= 128; pages whose pointers and strides are multiples of 16 bytes,
- * with d_h a multiple of 16 bytes, are read in 16-byte groups, any others element by element.  A
+ * with d_h a multiple of 16 bytes, are read in 16-byte groups, any others element by element.
+ * cols * page_size is at most 2^31 - 8192 (else RELATION_ERR_UNSUPPORTED).  A
  * length outside its range makes the request idle, a page id outside [0, n_pages) reads page 0 (the
  * request's result is then undefined); both are reported to dev_status (if given) as
  * RELATION_ERR_INVALID_ARG.  Asynchronous on `stream`; nothing is allocated.

@@ -550,7 +550,8 @@ relation_status relation_paged_decode(const void* q, const void* k_pages, const 
     return RELATION_ERR_INVALID_ARG;
   if ((st = check_scalars(lambda, tau_s)) != RELATION_OK) return st;
   if (cache.d_h > 128) return RELATION_ERR_UNSUPPORTED;
-  if ((long long)B * H > 0x7fffffffLL || (long long)cols * cache.page_size > 0x7fffffffLL)
+  // (row numbers a few tiles past the last one fit in 32 bits)
+  if ((long long)B * H > 0x7fffffffLL || (long long)cols * cache.page_size > 0x7fffe000LL)
     return RELATION_ERR_UNSUPPORTED;
   if ((st = check_elements({q, k_pages, v_pages, o}, elem_size(dt))) != RELATION_OK) return st;
   if ((st = check_elements({block_table, lengths, logz}, 4)) != RELATION_OK) return st;

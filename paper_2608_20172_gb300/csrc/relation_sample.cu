@@ -495,6 +495,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
   const int C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
   const int row = (int)blockIdx.x / C, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int j0 = min(p.V, rank * slice), n = min(slice, p.V - j0);
+  cl.barrier_arrive();  // (waited for before the first access to another CTA's shared memory)
   pdl_wait_and_launch();
   const float temperature = p.temperature ? p.temperature[row] : 1.f, u = p.u[row];
   const bool greedy = temperature == 0.f;
@@ -515,6 +516,7 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
   for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
   if (lane == 0) sm.red[warp] = mx;
   __syncthreads();
+  cl.barrier_wait();
   if (tid < C) {  // to every CTA
 #pragma unroll
     for (int i = 0; i < kWarps; ++i) mx = max_nan(mx, sm.red[i]);

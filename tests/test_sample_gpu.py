@@ -124,6 +124,30 @@ def test_plain_sampling(dtype, V):
     compare(logits(rng, 3, V, dtype), rng, temperature=[0.3, 1.0, 2.5])
 
 
+@pytest.mark.parametrize("V", [131071, 131073, 150001, 262144])
+def test_long_slices(V):
+    """Vocabularies on both sides of the longest slice that shares an SM, up to the longest served."""
+    rng = np.random.default_rng(V)
+    x = logits(rng, 3, V)
+    compare(x, rng, top_k=[0, 40, 3000], top_p=[0.9, 0.95, 1.0], share=0)
+    compare(logits(rng, 3, V, torch.bfloat16), rng, top_p=0.8, share=0)
+    compare(torch.zeros((2, V), device=DEV), rng, top_k=[V - 7, 5], share=0)
+
+
+@pytest.mark.parametrize("R", [38, 43, 50, 60, 76, 101, 152, 153, 320])
+def test_clusters_of_any_size(R):
+    """A row's CTAs by the number of rows: 8 down to 1."""
+    rng = np.random.default_rng(R)
+    x = logits(rng, R, 20011, torch.bfloat16)
+    u = rng.random(R).astype(np.float32)
+    kw = dict(temperature=rng.choice([0.0, 0.7, 1.0], R), top_k=rng.choice([0, 5, 300], R),
+              top_p=rng.choice([1.0, 0.9], R), min_p=rng.choice([0.0, 0.05], R))
+    whole, _ = call(x, u, **kw)
+    for r in range(R):
+        one = {n: (int if n == "top_k" else float)(v[r]) for n, v in kw.items()}
+        assert whole[0][r] == defined(x[r].float(), u[r], **one)[0]
+
+
 @pytest.mark.parametrize("ties", [False, True])
 @pytest.mark.parametrize("V", [2, 50, 4000, 32000, 100003])
 def test_top_k(V, ties):
