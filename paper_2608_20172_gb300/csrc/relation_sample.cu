@@ -74,7 +74,7 @@ struct Smem {
   float red[kWarps];
   // what the threads tell each other
   unsigned bin, inside, above_count;
-  u64 above_mass, key, key_mass;
+  u64 above_mass, key, key_mass, wanted;
 };
 
 // floor(2^40 w) for 0 <= w <= 1 from the bits of w.  (The conversion instruction to 64 bits bounds a
@@ -84,6 +84,10 @@ __device__ __forceinline__ u64 fixed_of(float w) {
   const int left = (int)(bits >> 23) - 110;
   const unsigned top = (bits & 0x7fffffu) | 0x800000u;
   return left >= 0 ? (u64)top << left : (u64)(top >> min(-left, 31));
+}
+// floor(p mass).  (By one thread: in all of them, the chip's few fp64 units take 2000 cycles.)
+__device__ __forceinline__ long long share_of(float p, u64 mass) {
+  return (long long)floor((double)p * (double)(long long)mass);
 }
 __device__ __forceinline__ u64 key_of(float w, int j) {
   return (u64)__float_as_uint(w) << kIndexBits | (u64)((1 << kIndexBits) - 1 - j);
@@ -595,9 +599,11 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
       }
     }
     if (by_p) {
-      const long long want = (long long)floor((double)top_p * (double)(long long)mass);
-      bins.find(sm, true, (u64)max(want, 1LL));
-      least = find_key<LOW>(cl, sm, w, run, j0, 1, true, (u64)max(want, 1LL), min_p, &mass, &sum);
+      if (tid == 0) sm.wanted = (u64)max(share_of(top_p, mass), 1LL);
+      __syncthreads();
+      const u64 want = sm.wanted;
+      bins.find(sm, true, want);
+      least = find_key<LOW>(cl, sm, w, run, j0, 1, true, want, min_p, &mass, &sum);
       summed = true;
     }
     if (!summed) {  // fewer than k tokens with a weight
@@ -626,8 +632,9 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
     if (r < rank) before += sm.kept[r];
     total += sm.kept[r];
   }
-  const u64 target =
-      (u64)min((long long)floor((double)u * (double)(long long)total), (long long)total - 1);
+  if (tid == 0) sm.wanted = (u64)min(share_of(u, total), (long long)total - 1);
+  __syncthreads();
+  const u64 target = sm.wanted;
   const unsigned hit = __ballot_sync(0xffffffffu, before <= target && target < before + sum);
   if (!hit) return;
   // the warp goes through the run that was hit
