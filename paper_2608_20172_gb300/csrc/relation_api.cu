@@ -551,7 +551,7 @@ relation_status relation_paged_decode(const void* q, const void* k_pages, const 
   if ((st = check_scalars(lambda, tau_s)) != RELATION_OK) return st;
   if (cache.d_h > 128) return RELATION_ERR_UNSUPPORTED;
   // (row numbers a few tiles past the last one fit in 32 bits)
-  if ((long long)B * H > 0x7fffffffLL || (long long)cols * cache.page_size > 0x7fffe000LL)
+  if ((long long)B * H > 0x7fff0000LL || (long long)cols * cache.page_size > 0x7fffe000LL)
     return RELATION_ERR_UNSUPPORTED;
   if ((st = check_elements({q, k_pages, v_pages, o}, elem_size(dt))) != RELATION_OK) return st;
   if ((st = check_elements({block_table, lengths, logz}, 4)) != RELATION_OK) return st;

@@ -119,10 +119,11 @@ __device__ __forceinline__ int length_of(const PagedProblem& p, int b, bool repo
   if (report && p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
   return 0;
 }
-// Units of a head: also one where there is no history
-__device__ __forceinline__ int units_of(int len) {
-  return len > 1 ? (len - 2) / kUnit + 1 : 1;
-}
+// Units of a head: its rows' and one for what every head costs (a head of few rows takes 4400 cycles, a
+// unit of 64 rows 2300 to 6500 by its width); none without history, where the join writes the row.
+// (With a unit for each such row, a batch of 32 with two of them waited 12 of 49 us for the CTA that
+// had them.)
+__device__ __forceinline__ int units_of(int len) { return len > 1 ? (len - 2) / kUnit + 2 : 0; }
 
 __device__ __forceinline__ int page_of(const PagedProblem& p, int r) {
   return rel::page_of(r, p.page, p.page_mul, p.page_shift);
@@ -156,7 +157,7 @@ struct Cut {
   int runs, more;
   __device__ __forceinline__ Cut(long long U, int ctas) : U(U) {
     runs = (int)min((long long)ctas, U);
-    each = quotient(U, runs);
+    each = quotient(U, max(runs, 1));
     more = (int)(U - each * runs);
   }
   __device__ __forceinline__ long long begin(int k) const { return k * each + min(k, more); }
@@ -166,22 +167,28 @@ struct Cut {
   }
 };
 
-// Where a CTA begins: a request and the units (per head) before it; and the cut.
+// A head that run k begins inside of, where it is the first to do so: run k - 1 holds the head's start,
+// run `last` its end (request -1: there is no such head).
+struct Split {
+  int b, hg, last, len;
+};
+
+// Where run `run` of at most `ctas` begins: the request, its length and the units (per head) before it;
+// and the cut.
 struct Place {
-  int b;
+  int b, len;
   long long before;
   Cut cut;
 };
-// b_stop >= 0: that request; else the one that holds the first unit of run `run` of `ctas`.
-__device__ __forceinline__ Place find_place(const PagedProblem& p, int run, int ctas, int b_stop,
-                                            bool report) {
+__device__ __forceinline__ Place find_place(const PagedProblem& p, int run, int ctas) {
   __shared__ long long part[kWarps], found;
-  __shared__ int found_b;
+  __shared__ int found_b, found_len;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int per = (p.B + kThreads - 1) / kThreads;
   const int lo = min(p.B, (int)threadIdx.x * per), hi = min(p.B, lo + per);
   long long x = 0;
-  for (int b = lo; b < hi; ++b) x += units_of(length_of(p, b, report));
+  int len = 0;  // the thread's last request's
+  for (int b = lo; b < hi; ++b) x += units_of(len = length_of(p, b, false));
   long long s = x;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
@@ -197,27 +204,25 @@ __device__ __forceinline__ Place find_place(const PagedProblem& p, int run, int 
     all += part[w];
   }
   const Cut cut(all * p.HG, ctas);
-  if (b_stop >= 0) {
-    if (lo <= b_stop && b_stop < hi) {
-      for (int b = lo; b < b_stop; ++b) before += units_of(length_of(p, b, false));
-      found = before;
-      found_b = b_stop;
-    }
-  } else if (run < cut.runs) {
+  if (run < cut.runs) {
     const long long u = cut.begin(run);
     if (before * p.HG <= u && u < (before + x) * p.HG) {  // (one thread's requests hold it)
       int b = lo;
       for (; b < hi - 1; ++b) {
-        const int n = units_of(length_of(p, b, false));
-        if (u < (before + n) * p.HG) break;
+        const int own = length_of(p, b, false), n = units_of(own);
+        if (u < (before + n) * p.HG) {
+          len = own;
+          break;
+        }
         before += n;
       }
       found = before;
       found_b = b;
+      found_len = len;
     }
   }
   __syncthreads();
-  return {found_b, found, cut};
+  return {found_b, found_len, found, cut};
 }
 
 // A row's gate g and logZ from q . k_self and the history's M and L
@@ -226,7 +231,7 @@ struct Gate {
 };
 __device__ __forceinline__ Gate gate_of(const PagedProblem& p, int len, float qk, float M, float L) {
   const float S = 1.0f / (1.0f + expf(-(qk * p.inv_sqrt_d) / p.tau_s));
-  if (len < 2) return {0.f, len < 1 ? -INFINITY : S};
+  if (len < 2) return {0.f, S};
   const float A = M + logf(L) - p.lambda * logf((float)len);
   // (logaddexp written so that NaN stays NaN)
   return {1.0f / (1.0f + expf(S - A)),
@@ -576,7 +581,7 @@ struct Tensor {
 
 template <typename Core>
 __global__ void __launch_bounds__(kThreads, Core::kCtas)
-    run_kernel(PagedProblem p, float* part) {
+    run_kernel(PagedProblem p, Split* splits, float* part) {
   using TI = typename Core::T;
   constexpr int GG = Core::GG;
   // the ring, and then in its place the results
@@ -584,18 +589,27 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
   Smem<GG>& sm = *reinterpret_cast<Smem<GG>*>(ring);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
-  const Place at = find_place(p, blockIdx.x, gridDim.x, -1, blockIdx.x == 0);
-  if ((int)blockIdx.x >= at.cut.runs) return;
-  const long long r0 = at.cut.begin(blockIdx.x), r1 = at.cut.begin(blockIdx.x + 1);
-  int b = at.b, len = length_of(p, b, false), n_u = units_of(len);
+  const int k = (int)blockIdx.x;
+  const Place at = find_place(p, k, gridDim.x);
+  if (k >= at.cut.runs) {
+    if (threadIdx.x == 0) splits[k].b = -1;
+    return;
+  }
+  const long long r0 = at.cut.begin(k), r1 = at.cut.begin(k + 1);
+  int b = at.b, len = at.len, n_u = units_of(len);
   long long base = at.before * p.HG;  // the request's first unit
   int hg = (int)quotient(r0 - base, n_u);
+  if (threadIdx.x == 0) {
+    const long long s0 = base + (long long)hg * n_u;
+    const bool first = k > 0 && s0 < r0 && at.cut.begin(k - 1) <= s0;
+    splits[k] = {first ? b : -1, hg, first ? at.cut.owner(s0 + n_u - 1) : 0, len};
+  }
   const int heads = p.H / p.Hk, groups = p.HG / p.Hk;
   for (long long u = r0; u < r1;) {
     const int kh = hg / groups, g0 = hg % groups * p.GG, ng = min(p.GG, heads - g0);
     const long long s0 = base + (long long)hg * n_u, s1 = s0 + n_u;  // the head's units
     const long long e = min(r1, s1);
-    const int ra = (int)(u - s0) * kUnit, rb = min((int)(e - s0) * kUnit, max(len - 1, 0));
+    const int ra = (int)(u - s0) * kUnit, rb = min((int)(e - s0) * kUnit, len - 1);
     const bool whole = u == s0 && e == s1;
     const TI* kb = reinterpret_cast<const TI*>(p.k) + (long long)kh * p.sC;
     const TI* vb = reinterpret_cast<const TI*>(p.v) + (long long)kh * p.sC;
@@ -605,9 +619,8 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
     core.run(p, b, qb, ng, kb, vb, ra, rb, ring, warp, lane);
     if (Core::kRing > 0) __syncthreads();
     core.finish(p, sm, warp, lane);
-    const bool own_row = whole && len > 0;
-    const long long self = own_row ? row_at(p, b, len - 1) : 0;
-    if (own_row) {
+    const long long self = whole ? row_at(p, b, len - 1) : 0;
+    if (whole) {
       for (int g = warp; g < ng; g += kWarps) {
         const float s = self_dot<TI>(p, qb + (long long)g * p.qsH, kb + self, lane);
         if (lane == 0) sm.self[g] = s;
@@ -626,31 +639,33 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
         a[w] = l == 0.f ? 0.f : expf(sm.m[w][g] - M);
         L = fmaf(a[w], l, L);
       }
-      const float scale = whole ? len > 1 ? 1.0f / L : 0.f : 1.f;
+      const float scale = whole ? 1.0f / L : 1.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) sm.m[w][g] = a[w] * scale;
       if (whole) {
-        const Gate gate = gate_of(p, len, len > 0 ? sm.self[g] : 0.f, M, L);
+        const Gate gate = gate_of(p, len, sm.self[g], M, L);
         sm.self[g] = gate.g;
         p.logz[(long long)b * p.H + h0 + g] = gate.lz;
       } else {
-        float* o = part + (((long long)blockIdx.x * 2 + (u == s0)) * p.GG + g) * kPart;
+        float* o = part + (((long long)k * 2 + (u == s0)) * p.GG + g) * kPart;
         o[0] = M;
         o[1] = L;
       }
     }
     __syncthreads();
     TI* out = reinterpret_cast<TI*>(p.out) + (long long)b * p.qsB + (long long)h0 * p.qsH;
-    for (int i = threadIdx.x; i < ng * p.d; i += kThreads) {
-      const int g = GG == 1 ? 0 : i / p.d, c = i - g * p.d;
-      float Z = 0.f;
+    // a column per thread, two heads at a time where a row takes half of them
+    const int half = p.d <= kThreads / 2, c = threadIdx.x & (kThreads >> half) - 1;
+    if (c < p.d) {
+      const float vi = whole ? ldf(vb + self + c) : 0.f;
+      for (int g = threadIdx.x != c; g < ng; g += 1 + half) {
+        float Z = 0.f;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) Z = fmaf(sm.m[w][g], sm.z[w][g][c], Z);
-      if (whole) {
-        const float vi = own_row ? ldf(vb + self + c) : 0.f;
-        out[(long long)g * p.qsH + c] = (TI)fmaf(sm.self[g], Z - vi, vi);
-      } else {  // slot 0: the run's first head (begun before it), 1: its last
-        part[(((long long)blockIdx.x * 2 + (u == s0)) * p.GG + g) * kPart + 2 + c] = Z;
+        for (int w = 0; w < kWarps; ++w) Z = fmaf(sm.m[w][g], sm.z[w][g][c], Z);
+        if (whole)
+          out[(long long)g * p.qsH + c] = (TI)fmaf(sm.self[g], Z - vi, vi);
+        else  // slot 0: the run's first head (begun before it), 1: its last
+          part[(((long long)k * 2 + (u == s0)) * p.GG + g) * kPart + 2 + c] = Z;
       }
     }
     __syncthreads();  // sm is written again
@@ -658,29 +673,50 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
     if (++hg == p.HG && u < r1) {
       base += (long long)n_u * p.HG;
       hg = 0;
-      len = length_of(p, ++b, false);
-      n_u = units_of(len);
+      do n_u = units_of(len = length_of(p, ++b, false));
+      while (n_u == 0);
     }
   }
 }
 
-// Heads that several runs share: a CTA per (request, query head).  The runs' weights a thread each,
-// then their z with kAhead loads in flight.
+// Request b without history: y = v_self and logZ = S, or zero and -inf (idle); a head per warp.
 template <typename TI>
-__global__ void __launch_bounds__(kThreads, 8) join_kernel(PagedProblem p, const float* part, int most) {
+__device__ __forceinline__ void first_row(const PagedProblem& p, int b, int h) {
+  const int len = length_of(p, b, h == 0), lane = threadIdx.x & 31;
+  if (len > 1 || h >= p.H) return;
+  const TI* q = reinterpret_cast<const TI*>(p.q) + (long long)b * p.qsB + (long long)h * p.qsH;
+  TI* out = reinterpret_cast<TI*>(p.out) + (long long)b * p.qsB + (long long)h * p.qsH;
+  const long long at = (len > 0 ? row_at(p, b, 0) : 0) + (long long)(h / (p.H / p.Hk)) * p.sC;
+  const TI* v = reinterpret_cast<const TI*>(p.v) + at;
+  float lz = -INFINITY;
+  for (int c = lane; c < p.d; c += 32) out[c] = len > 0 ? v[c] : (TI)0.f;
+  if (len > 0)
+    lz = gate_of(p, len, self_dot<TI>(p, q, reinterpret_cast<const TI*>(p.k) + at, lane), 0.f, 1.f).lz;
+  if (lane == 0) p.logz[(long long)b * p.H + h] = lz;
+}
+
+// The heads that several runs share: a CTA per run (of `most`) that might be the second of one, and
+// query head, the runs' weights a thread each, then their z with kAhead loads in flight.  Behind them
+// a warp per request and head, for the requests without history.
+template <typename TI>
+__global__ void __launch_bounds__(kThreads, 8)
+    join_kernel(PagedProblem p, const Split* splits, const float* part, int most) {
   constexpr int kAhead = 16;
   __shared__ float self, red[kWarps], w[kThreads], lw[kThreads];
-  const int b = blockIdx.x / p.H, h = blockIdx.x % p.H, c = threadIdx.x;
-  const int warp = c >> 5, lane = c & 31;
+  const int c = threadIdx.x, warp = c >> 5, lane = c & 31;
+  const int k0 = (int)blockIdx.x / p.GG, g = (int)blockIdx.x % p.GG;  // run, head
   const int heads = p.H / p.Hk, groups = p.HG / p.Hk;
-  const int kh = h / heads, hg = kh * groups + (h - kh * heads) / p.GG, g = (h - kh * heads) % p.GG;
   pdl_wait_and_launch();
-  const Place at = find_place(p, 0, most, b, false);
-  const int len = length_of(p, b, false);
-  const long long n_u = units_of(len), s0 = at.before * p.HG + hg * n_u;
-  // the runs that hold the head's first and last unit
-  const int k0 = at.cut.owner(s0), k1 = at.cut.owner(s0 + n_u - 1);
-  if (k0 == k1) return;  // (finished there)
+  if (k0 >= most - 1) {
+    const int i = (int)blockIdx.x - (most - 1) * p.GG, per = (p.H + kWarps - 1) / kWarps;
+    first_row<TI>(p, i / per, i % per * kWarps + warp);
+    return;
+  }
+  const Split at = splits[k0 + 1];
+  if (at.b < 0) return;
+  const int kh = at.hg / groups, in_group = at.hg % groups * p.GG + g;
+  if (in_group >= heads) return;
+  const int b = at.b, h = kh * heads + in_group, len = at.len, k1 = at.last;
   const long long row = row_at(p, b, len - 1) + (long long)kh * p.sC;
   const float vi = c < p.d ? ldf(reinterpret_cast<const TI*>(p.v) + row + c) : 0.f;
   if (warp == kWarps - 1) {
@@ -748,10 +784,13 @@ cudaError_t launch_core(const PagedProblem& p, float* part, cudaStream_t s) {
     return e;
   }
   const int runs = nsm * Core::kCtas < kMaxCtas ? nsm * Core::kCtas : kMaxCtas;
-  e = launch_pdl(run_kernel<Core>, dim3(runs), kThreads, smem, s, 1, p, part);
+  Split* splits = reinterpret_cast<Split*>(part);
+  part += kMaxCtas * sizeof(Split) / sizeof(float);
+  e = launch_pdl(run_kernel<Core>, dim3(runs), kThreads, smem, s, 1, p, splits, part);
   if (e != cudaSuccess) { note_failure("paged decode: launch"); return e; }
-  e = launch_pdl(join_kernel<typename Core::T>, dim3((unsigned)p.B * p.H), kThreads, 0, s, 1, p,
-                 (const float*)part, runs);
+  e = launch_pdl(join_kernel<typename Core::T>, 
+                 dim3((unsigned)((runs - 1) * p.GG + p.B * ((p.H + kWarps - 1) / kWarps))), kThreads, 0, s,
+                 1, p, (const Split*)splits, (const float*)part, runs);
   if (e != cudaSuccess) note_failure("paged decode: join launch");
   return e;
 }
@@ -797,7 +836,8 @@ cudaError_t launch_t(PagedProblem p, float* part, cudaStream_t s) {
 }  // namespace paged
 
 size_t paged_workspace_bytes(int H, int Hk) {
-  return (size_t)paged::kMaxCtas * 2 * paged::heads_at_once(H / Hk) * paged::kPart * sizeof(float);
+  return (size_t)paged::kMaxCtas * (sizeof(paged::Split) + 2 * paged::heads_at_once(H / Hk) *
+                                                              paged::kPart * sizeof(float));
 }
 
 cudaError_t launch_paged(const PagedProblem& p, void* workspace, cudaStream_t s) {
