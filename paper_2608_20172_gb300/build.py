@@ -3,7 +3,9 @@
 Each ``csrc/*.cu`` file is compiled to an object in parallel with
 ``nvcc -gencode arch=compute_103a,code=sm_103a -O3 -lineinfo``, then the objects are
 linked into ``paper_2608_20172_gb300/_build/librelation.so`` with the static CUDA
-runtime.  The driver API entry point used for TMA descriptors is resolved at run
+runtime.  Beside it ``csrc/torch_calls.cpp``, the serving calls of the Python binding in native
+code, becomes ``_build/relation_calls.so`` (host code against torch's headers; where these are
+not installed the binding does the same in Python).  The driver API entry point used for TMA descriptors is resolved at run
 time through the runtime, so the library loads on machines without a GPU driver.
 """
 from __future__ import annotations
@@ -13,6 +15,8 @@ import glob
 import hashlib
 import os
 import subprocess
+import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -20,6 +24,7 @@ CSRC = os.path.join(HERE, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(BUILD, "librelation.so")
+CALLS = os.path.join(BUILD, "relation_calls.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
@@ -48,10 +53,54 @@ def _deps_digest() -> str:
     return h.hexdigest()
 
 
+def build_calls(force: bool = False) -> str | None:
+    """Compile relation_calls.so; returns its path, None where it cannot be built."""
+    import torch
+
+    src = os.path.join(CSRC, "torch_calls.cpp")
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(_nvcc())) or "/usr/local/cuda"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include",
+           f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}/include", f"-I{INCLUDE}", src,
+           f"-L{root}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+    h = hashlib.sha256()
+    for f in (src, os.path.join(INCLUDE, "relation.h")):
+        with open(f, "rb") as fh:
+            h.update(fh.read())
+    h.update((" ".join(cmd) + torch.__version__ + sys.version).encode())
+    stamp = CALLS + ".stamp"
+    if not force and os.path.exists(CALLS) and os.path.exists(stamp) and \
+            open(stamp).read().strip() == h.hexdigest():
+        return CALLS
+    tmp = CALLS + f".tmp{os.getpid()}"
+    try:
+        r = subprocess.run(cmd + ["-o", tmp], capture_output=True, text=True)
+    except OSError as e:
+        print(f"relation_calls.so not built: {e}", file=sys.stderr)
+        return None
+    if r.returncode != 0:
+        print(f"relation_calls.so not built:\n{r.stderr}", file=sys.stderr)
+        return None
+    os.replace(tmp, CALLS)
+    with open(stamp, "w") as f:
+        f.write(h.hexdigest())
+    return CALLS
+
+
 def build(force: bool = False, verbose: bool = False, extra_flags=None) -> str:
     """Compile and link librelation.so; returns its path.  Skips work when the
     sources are unchanged since the last build."""
     os.makedirs(BUILD, exist_ok=True)
+    with cf.ThreadPoolExecutor(max_workers=1) as beside:
+        calls = beside.submit(build_calls, force)
+        lib = _build_lib(force, verbose, extra_flags)
+        calls.result()
+    return lib
+
+
+def _build_lib(force, verbose, extra_flags) -> str:
     stamp = os.path.join(BUILD, "librelation.stamp")
     digest = _deps_digest() + (" ".join(extra_flags) if extra_flags else "")
     if not force and os.path.exists(LIB) and os.path.exists(stamp):
