@@ -40,6 +40,7 @@ constexpr int kFirst = 87;            // the exponent of 2^-40, below which a we
 constexpr int kDigit = 8;             // further digits
 constexpr int kList = 1024;           // tokens of a bin that every CTA goes through by itself,
 constexpr int kRanked = 32;           // and that are ranked against each other
+constexpr int kFew = kThreads / 4;    // tokens from the top on that settle top-k and top-p together
 
 // A slice of at most 2^(32 - LOW) tokens: its bins' sums of LOW-bit numbers stay below 2^32.
 constexpr int low_bits(bool wide) { return wide ? 17 : 18; }
@@ -435,6 +436,70 @@ __device__ __forceinline__ u64 find_key(cg::cluster_group& cl, Smem<LOW>& sm, co
   return found;
 }
 
+// Both cuts where the bins down to the one with the k-th token, sm.bin, hold at most kFew tokens: these
+// are ranked against each other, four threads to a token.  The last kept token's key; *above gets the
+// kept mass of this thread's run, without weights below min_p.
+template <int LOW>
+__device__ __forceinline__ u64 find_few(cg::cluster_group& cl, Smem<LOW>& sm, const float* w,
+                                        const Run& run, int j0, unsigned k, float top_p, float min_p,
+                                        u64* above) {
+  const int tid = threadIdx.x, C = (int)cl.num_blocks(), rank = (int)cl.block_rank();
+  const unsigned low = ((unsigned)sm.bin << LOW) + ((unsigned)kFirst << 23);
+  if (tid == 0) sm.n_list = 0;
+  __syncthreads();
+  u64* list = sm.list[0];
+#pragma unroll 4
+  for (int i = run.i0; i < run.i1; ++i)
+    if (__float_as_uint(w[i]) >= low) list[atomicAdd(&sm.n_list, 1)] = key_of(w[i], j0 + i);
+  __syncthreads();
+  const int mine = sm.n_list;
+  if (tid < C) cl.map_shared_rank(&sm, tid)->sizes[0][rank] = mine;
+  cl.sync();
+  int total = 0;
+#pragma unroll
+  for (int r = 0; r < kMaxCluster; ++r) {
+    if (r >= C) break;
+    const int m = sm.sizes[0][r];
+    if (tid >= total && tid < total + m) sm.all[tid] = cl.map_shared_rank(list, r)[tid - total];
+    total += m;
+  }
+  sm.extra[tid] = 0;
+  __syncthreads();
+  const int g = tid >> 2;
+  const u64 key = g < total ? sm.all[g] : ~0ull, q = g < total ? weight_of_key(key) : 0;
+  unsigned c = 0;
+  u64 m = 0;
+#pragma unroll 4
+  for (int i = tid & 3; i < total; i += 4) {
+    const u64 other = sm.all[i];
+    if (other > key) {
+      ++c;
+      m += weight_of_key(other);
+    }
+  }
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    c += __shfl_xor_sync(0xffffffffu, c, o);
+    m += __shfl_xor_sync(0xffffffffu, m, o);
+  }
+  const bool one = (tid & 3) == 0 && g < total && c < k;
+  if (one && c + 1 == k) sm.wanted = (u64)max(share_of(top_p, m + q), 1LL);
+  __syncthreads();
+  const u64 want = sm.wanted;
+  if (one && m < want && (c + 1 == k || want <= m + q)) sm.key = key;
+  __syncthreads();
+  const u64 found = sm.key;
+  for (int i = tid; i < mine; i += kThreads) {
+    const u64 own = list[i];
+    const int at = (1 << kIndexBits) - 1 - (int)(own & ((1 << kIndexBits) - 1)) - j0;
+    if (own >= found && !(__uint_as_float((unsigned)(own >> kIndexBits)) < min_p))
+      atomicAdd(&sm.extra[at / run.len], weight_of_key(own));
+  }
+  __syncthreads();
+  *above = sm.extra[tid];
+  return found;
+}
+
 // The larger of two, NaN if one is
 __device__ __forceinline__ float max_nan(float a, float b) {
   float r;
@@ -591,20 +656,25 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
     __syncthreads();
     u64 mass = sm.total;
     bool summed = false;
-    if (by_k) {
-      bins.find(sm, false, (u64)k);
-      if (sm.inside) {
+    if (by_k) bins.find(sm, false, (u64)k);
+    const unsigned inside = by_k ? sm.inside : 0;
+    if (by_p && inside && sm.above_count + inside <= kFew) {
+      // (one row of 32000, k 50, p 0.9: 11.6 us, 13.0 with two cuts one after the other)
+      least = find_few<LOW>(cl, sm, w, run, j0, (unsigned)k, top_p, min_p, &sum);
+      summed = true;
+    } else {
+      if (inside) {
         least = find_key<LOW>(cl, sm, w, run, j0, 0, false, (u64)k, min_p, &mass, by_p ? nullptr : &sum);
         summed = !by_p;
       }
-    }
-    if (by_p) {
-      if (tid == 0) sm.wanted = (u64)max(share_of(top_p, mass), 1LL);
-      __syncthreads();
-      const u64 want = sm.wanted;
-      bins.find(sm, true, want);
-      least = find_key<LOW>(cl, sm, w, run, j0, 1, true, want, min_p, &mass, &sum);
-      summed = true;
+      if (by_p) {
+        if (tid == 0) sm.wanted = (u64)max(share_of(top_p, mass), 1LL);
+        __syncthreads();
+        const u64 want = sm.wanted;
+        bins.find(sm, true, want);
+        least = find_key<LOW>(cl, sm, w, run, j0, 1, true, want, min_p, &mass, &sum);
+        summed = true;
+      }
     }
     if (!summed) {  // fewer than k tokens with a weight
       Mass kept;
