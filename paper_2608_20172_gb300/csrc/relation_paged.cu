@@ -28,7 +28,8 @@ constexpr int kWarps = 4, kThreads = 32 * kWarps;
 constexpr int kMaxD = 128;
 constexpr int kUnit = 64;      // rows of a unit
 constexpr int kMaxCtas = 640;  // runs (the workspace holds two partial results of each)
-constexpr int kPart = 2 + kMaxD;
+constexpr int kPart = 2 + kMaxD;      // floats of a partial result: m, l, z
+constexpr int kOwn = kMaxD + 8;       // of what the run with a shared head's end adds: v_self, q . k_self
 
 template <typename TI>
 __device__ __forceinline__ float ldf(const TI* p) {
@@ -581,7 +582,7 @@ struct Tensor {
 
 template <typename Core>
 __global__ void __launch_bounds__(kThreads, Core::kCtas)
-    run_kernel(PagedProblem p, Split* splits, float* part) {
+    run_kernel(PagedProblem p, Split* splits, float* own, float* part) {
   using TI = typename Core::T;
   constexpr int GG = Core::GG;
   // the ring, and then in its place the results
@@ -599,10 +600,13 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
   int b = at.b, len = at.len, n_u = units_of(len);
   long long base = at.before * p.HG;  // the request's first unit
   int hg = (int)quotient(r0 - base, n_u);
+  // (the record of the head that the run may begin inside of: completed at the end)
+  __shared__ Split split;
+  __shared__ long long split_end;
   if (threadIdx.x == 0) {
     const long long s0 = base + (long long)hg * n_u;
-    const bool first = k > 0 && s0 < r0 && at.cut.begin(k - 1) <= s0;
-    splits[k] = {first ? b : -1, hg, first ? at.cut.owner(s0 + n_u - 1) : 0, len};
+    split = {k > 0 && s0 < r0 && at.cut.begin(k - 1) <= s0 ? b : -1, hg, 0, len};
+    split_end = s0 + n_u;
   }
   const int heads = p.H / p.Hk, groups = p.HG / p.Hk;
   for (long long u = r0; u < r1;) {
@@ -619,8 +623,9 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
     core.run(p, b, qb, ng, kb, vb, ra, rb, ring, warp, lane);
     if (Core::kRing > 0) __syncthreads();
     core.finish(p, sm, warp, lane);
-    const long long self = whole ? row_at(p, b, len - 1) : 0;
-    if (whole) {
+    const bool ends = e == s1;  // the token's own row is this run's
+    const long long self = ends ? row_at(p, b, len - 1) : 0;
+    if (ends) {
       for (int g = warp; g < ng; g += kWarps) {
         const float s = self_dot<TI>(p, qb + (long long)g * p.qsH, kb + self, lane);
         if (lane == 0) sm.self[g] = s;
@@ -650,6 +655,7 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
         float* o = part + (((long long)k * 2 + (u == s0)) * p.GG + g) * kPart;
         o[0] = M;
         o[1] = L;
+        if (ends) own[k * kOwn + kMaxD + g] = sm.self[g];
       }
     }
     __syncthreads();
@@ -657,7 +663,8 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
     // a column per thread, two heads at a time where a row takes half of them
     const int half = p.d <= kThreads / 2, c = threadIdx.x & (kThreads >> half) - 1;
     if (c < p.d) {
-      const float vi = whole ? ldf(vb + self + c) : 0.f;
+      const float vi = ends ? ldf(vb + self + c) : 0.f;
+      if (ends && !whole && (int)threadIdx.x == c) own[k * kOwn + c] = vi;
       for (int g = threadIdx.x != c; g < ng; g += 1 + half) {
         float Z = 0.f;
 #pragma unroll
@@ -676,6 +683,10 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
       do n_u = units_of(len = length_of(p, ++b, false));
       while (n_u == 0);
     }
+  }
+  if (threadIdx.x == 0) {
+    if (split.b >= 0) split.last = at.cut.owner(split_end - 1);
+    splits[k] = split;
   }
 }
 
@@ -696,13 +707,13 @@ __device__ __forceinline__ void first_row(const PagedProblem& p, int b, int h) {
 }
 
 // The heads that several runs share: a CTA per run (of `most`) that might be the second of one, and
-// query head, the runs' weights a thread each, then their z with kAhead loads in flight.  Behind them
-// a warp per request and head, for the requests without history.
+// query head, the runs' weights a thread each, their z with kAhead loads in flight, the first with
+// the weights'.  Behind them a warp per request and head, for the requests without history.
 template <typename TI>
 __global__ void __launch_bounds__(kThreads, 8)
-    join_kernel(PagedProblem p, const Split* splits, const float* part, int most) {
+    join_kernel(PagedProblem p, const Split* splits, const float* own, const float* part, int most) {
   constexpr int kAhead = 16;
-  __shared__ float self, red[kWarps], w[kThreads], lw[kThreads];
+  __shared__ float red[kWarps], w[kThreads], lw[kThreads];
   const int c = threadIdx.x, warp = c >> 5, lane = c & 31;
   const int k0 = (int)blockIdx.x / p.GG, g = (int)blockIdx.x % p.GG;  // run, head
   const int heads = p.H / p.Hk, groups = p.HG / p.Hk;
@@ -716,21 +727,17 @@ __global__ void __launch_bounds__(kThreads, 8)
   if (at.b < 0) return;
   const int kh = at.hg / groups, in_group = at.hg % groups * p.GG + g;
   if (in_group >= heads) return;
-  const int b = at.b, h = kh * heads + in_group, len = at.len, k1 = at.last;
-  const long long row = row_at(p, b, len - 1) + (long long)kh * p.sC;
-  const float vi = c < p.d ? ldf(reinterpret_cast<const TI*>(p.v) + row + c) : 0.f;
-  if (warp == kWarps - 1) {
-    const float s = self_dot<TI>(p, reinterpret_cast<const TI*>(p.q) + (long long)b * p.qsB +
-                                        (long long)h * p.qsH,
-                                 reinterpret_cast<const TI*>(p.k) + row, lane);
-    if (lane == 0) self = s;
-  }
+  const int b = at.b, h = kh * heads + in_group, n = at.last - k0 + 1;
   // the first of them begins the head (its second slot), the others begin with it
   const long long step = 2LL * p.GG * kPart;
   const float* first = part + (long long)k0 * step + g * kPart;
   const float* begun = first + (long long)p.GG * kPart;
   auto at_run = [&](int i) { return i == 0 ? begun : first + i * step; };
-  const int n = k1 - k0 + 1;
+  const bool in = c < p.d;
+  const float vi = in ? own[at.last * kOwn + c] : 0.f, qk = own[at.last * kOwn + kMaxD + g];
+  float zk[kAhead];
+#pragma unroll
+  for (int e = 0; e < kAhead; ++e) zk[e] = e < n && in ? at_run(e)[2 + c] : 0.f;
   float M = -INFINITY;
   for (int i = c; i < n; i += kThreads) M = fmaxf(M, at_run(i)[0]);
   M = warp_max(M);
@@ -749,9 +756,10 @@ __global__ void __launch_bounds__(kThreads, 8)
     __syncthreads();
     const int m = min(kThreads, n - i0);
     for (int i = 0; i < m; i += kAhead) {
-      float zk[kAhead];
+      if (i0 + i > 0) {
 #pragma unroll
-      for (int e = 0; e < kAhead; ++e) zk[e] = i + e < m && c < p.d ? at_run(i0 + i + e)[2 + c] : 0.f;
+        for (int e = 0; e < kAhead; ++e) zk[e] = i + e < m && in ? at_run(i0 + i + e)[2 + c] : 0.f;
+      }
 #pragma unroll
       for (int e = 0; e < kAhead; ++e) {
         if (i + e >= m) break;
@@ -760,8 +768,8 @@ __global__ void __launch_bounds__(kThreads, 8)
       }
     }
   }
-  if (c >= p.d) return;
-  const Gate gate = gate_of(p, len, self, M, L);
+  if (!in) return;
+  const Gate gate = gate_of(p, at.len, qk, M, L);
   reinterpret_cast<TI*>(p.out)[(long long)b * p.qsB + (long long)h * p.qsH + c] =
       (TI)fmaf(gate.g, Z / L - vi, vi);
   if (c == 0) p.logz[(long long)b * p.H + h] = gate.lz;
@@ -785,12 +793,13 @@ cudaError_t launch_core(const PagedProblem& p, float* part, cudaStream_t s) {
   }
   const int runs = nsm * Core::kCtas < kMaxCtas ? nsm * Core::kCtas : kMaxCtas;
   Split* splits = reinterpret_cast<Split*>(part);
-  part += kMaxCtas * sizeof(Split) / sizeof(float);
-  e = launch_pdl(run_kernel<Core>, dim3(runs), kThreads, smem, s, 1, p, splits, part);
+  float* own = part + kMaxCtas * sizeof(Split) / sizeof(float);
+  part = own + kMaxCtas * kOwn;
+  e = launch_pdl(run_kernel<Core>, dim3(runs), kThreads, smem, s, 1, p, splits, own, part);
   if (e != cudaSuccess) { note_failure("paged decode: launch"); return e; }
-  e = launch_pdl(join_kernel<typename Core::T>, 
+  e = launch_pdl(join_kernel<typename Core::T>,
                  dim3((unsigned)((runs - 1) * p.GG + p.B * ((p.H + kWarps - 1) / kWarps))), kThreads, 0, s,
-                 1, p, (const Split*)splits, (const float*)part, runs);
+                 1, p, (const Split*)splits, (const float*)own, (const float*)part, runs);
   if (e != cudaSuccess) note_failure("paged decode: join launch");
   return e;
 }
@@ -836,8 +845,9 @@ cudaError_t launch_t(PagedProblem p, float* part, cudaStream_t s) {
 }  // namespace paged
 
 size_t paged_workspace_bytes(int H, int Hk) {
-  return (size_t)paged::kMaxCtas * (sizeof(paged::Split) + 2 * paged::heads_at_once(H / Hk) *
-                                                              paged::kPart * sizeof(float));
+  using namespace paged;
+  const size_t floats = kOwn + 2 * heads_at_once(H / Hk) * kPart;
+  return kMaxCtas * (sizeof(Split) + floats * sizeof(float));
 }
 
 cudaError_t launch_paged(const PagedProblem& p, void* workspace, cudaStream_t s) {

@@ -117,7 +117,7 @@ def test_paged_decode_workspace(lib):
     size = lib.relation_paged_decode_workspace_size
     base = size(2, pages(), binding.BF16)
     assert base > 0 and base == size(2, pages(n=100000, page=64), binding.F32)
-    assert 7 * base < size(16, pages(), binding.BF16) <= 8 * base  # eight query heads at once
+    assert 4 * base < size(16, pages(), binding.BF16) <= 8 * base  # eight query heads at once
     for H, c in ((3, pages()), (0, pages()), (2, pages(d=129)), (2, pages(n=0))):
         assert size(H, c, binding.BF16) == 0
 
