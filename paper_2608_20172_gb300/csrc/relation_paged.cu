@@ -15,7 +15,10 @@
 // takes its run head by head in one pass: every warp keeps (m, l, z) = (max E, sum e^{E - m},
 // sum e^{E - m} v) over tiles of rows that stay in registers, merged at the head's end.  A head that
 // lies within one run is finished there; of a head that several runs share, each leaves its (m, l, z)
-// in the workspace and the second launch joins them.
+// in the workspace, the one with its end q . k_self and v_self, and the second launch joins them.
+// Measured, bf16, 32 requests of 1 to 4096 rows, both launches: 8 heads of 128 58 us (80 % of the copy
+// bandwidth), of 64 35, of 80 52, of 128 with 4 query heads each 70; 32 requests to 8192 rows of 16 x
+// 128 193 us (97 %); one request of 2048 rows, 12 x 64, 8 us.
 #include <math.h>
 
 #include "common.cuh"
@@ -120,8 +123,8 @@ __device__ __forceinline__ int length_of(const PagedProblem& p, int b, bool repo
   if (report && p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
   return 0;
 }
-// Units of a head: its rows' and one for what every head costs (a head of few rows takes 4400 cycles, a
-// unit of 64 rows 2300 to 6500 by its width); none without history, where the join writes the row.
+// Units of a head: its rows' and one for what every head costs (a head of few rows takes as long as a
+// unit of 64 rows, 2300 to 6500 cycles by its width); none without history, where the join writes the row.
 // (With a unit for each such row, a batch of 32 with two of them waited 12 of 49 us for the CTA that
 // had them.)
 __device__ __forceinline__ int units_of(int len) { return len > 1 ? (len - 2) / kUnit + 2 : 0; }
@@ -261,6 +264,7 @@ template <typename TI, int LPR, int GG_, bool VEC>
 struct Lanes {
   using T = TI;
   static constexpr int GG = GG_;
+  static constexpr bool kVec = VEC;
   static constexpr int kCtas = GG == 1 ? 4 : GG == 2 ? 3 : 2;  // per SM, by the registers
   static constexpr int VE = Vec<TI>::N, RPL = 32 / LPR;
   static constexpr int NI = LPR == 4 ? 4 : 8;  // loads of a tile's keys
@@ -347,14 +351,17 @@ struct Lanes {
       }
     }
   }
-  // this warp's tiles of rows ra .. rb - 1
+  // this warp's tiles of rows ra .. rb - 1; `more` asks for what else it wants once the first page ids
+  // are on their way
+  template <typename F>
   __device__ __forceinline__ void run(const PagedProblem& p, int b, const TI* qb, int ng, const TI* kb,
-                                      const TI* vb, int ra, int rb, uint4*, int warp, int lane) {
+                                      const TI* vb, int ra, int rb, uint4*, int warp, int lane, F more) {
     start(p, qb, ng, lane);
     // rows past the end read the last one, and are left out of the tile
     auto row = [&](int j) { return min(j + lane % R, rb - 1); };
     int j = ra + warp * R;
     int id = j < rb ? id_at(p, b, row(j)) : 0;
+    more();
     for (; j < rb; j += kWarps * R) {
       const long long mine = row_of(p, id, row(j));
       id = j + kWarps * R < rb ? id_at(p, b, row(j + kWarps * R)) : 0;
@@ -410,6 +417,7 @@ template <int DK>  // 32-channel groups of a row
 struct Tensor {
   using T = __nv_bfloat16;
   static constexpr int GG = 8, R = 16;
+  static constexpr bool kVec = true;
   static constexpr int DV = (DK + 1) / 2;  // 64-channel groups of a row
   static constexpr int kRow = 8 * DV;      // 16-byte groups of a row in shared memory
   static constexpr int kStage = 2 * R * kRow;
@@ -460,8 +468,10 @@ struct Tensor {
       }
     }
   }
+  template <typename F>
   __device__ __forceinline__ void run(const PagedProblem& p, int b, const T* qb, int ng, const T* kb,
-                                      const T* vb, int ra, int rb, uint4* ring, int warp, int lane) {
+                                      const T* vb, int ra, int rb, uint4* ring, int warp, int lane,
+                                      F more) {
     constexpr int step = kWarps * R;
     uint4* mine = ring + warp * S * kStage;
     int j = ra + warp * R;
@@ -475,6 +485,7 @@ struct Tensor {
     int next[S + 1];
 #pragma unroll
     for (int st = 0; st <= S; ++st) next[st] = id(j + st * step);
+    more();
 #pragma unroll
     for (int st = 0; st < S; ++st) {
       const int at = j + st * step;
@@ -580,6 +591,26 @@ struct Tensor {
   }
 };
 
+// The key and value of request b's last row into shared memory, by one warp: on their way while the
+// history is summed.  (Read after it, they put two trips to memory at every head's end: 500 requests to
+// 64 rows, 8 x 128 bf16, 42 us, so 37; 256 to 300 rows 48 and 44; 32 to 4096 rows 58 either way.)
+template <typename TI, bool VEC>
+__device__ __forceinline__ void fetch_self(const PagedProblem& p, int b, int len, const TI* kb,
+                                           const TI* vb, TI (&row)[2][kMaxD], int lane) {
+  const long long at = row_at(p, b, len - 1);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const TI* x = (i ? vb : kb) + at;
+    if constexpr (VEC) {
+      constexpr int VE = Vec<TI>::N;
+      if (lane * VE < p.d) cp16(smem_u32(&row[i][lane * VE]), x + lane * VE);  // (d <= 32 VE)
+    } else {
+      for (int c = lane; c < p.d; c += 32) row[i][c] = x[c];
+    }
+  }
+  cp_commit();
+}
+
 template <typename Core>
 __global__ void __launch_bounds__(kThreads, Core::kCtas)
     run_kernel(PagedProblem p, Split* splits, float* own, float* part) {
@@ -603,6 +634,7 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
   // (the record of the head that the run may begin inside of: completed at the end)
   __shared__ Split split;
   __shared__ long long split_end;
+  __shared__ __align__(16) TI self[2][kMaxD];  // the token's own key and value
   if (threadIdx.x == 0) {
     const long long s0 = base + (long long)hg * n_u;
     split = {k > 0 && s0 < r0 && at.cut.begin(k - 1) <= s0 ? b : -1, hg, 0, len};
@@ -619,15 +651,19 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
     const TI* vb = reinterpret_cast<const TI*>(p.v) + (long long)kh * p.sC;
     const int h0 = kh * heads + g0;
     const TI* qb = reinterpret_cast<const TI*>(p.q) + (long long)b * p.qsB + (long long)h0 * p.qsH;
+    const bool ends = e == s1;  // the token's own row is this run's
     Core core;
-    core.run(p, b, qb, ng, kb, vb, ra, rb, ring, warp, lane);
+    core.run(p, b, qb, ng, kb, vb, ra, rb, ring, warp, lane, [&] {
+      if (ends && warp == kWarps - 1) fetch_self<TI, Core::kVec>(p, b, len, kb, vb, self, lane);
+    });
+    cp_wait<0>();
     if (Core::kRing > 0) __syncthreads();
     core.finish(p, sm, warp, lane);
-    const bool ends = e == s1;  // the token's own row is this run's
-    const long long self = ends ? row_at(p, b, len - 1) : 0;
+    if (GG > 1 && Core::kRing == 0) __syncthreads();
+    else __syncwarp();  // (the warp that fetched the row takes the only head)
     if (ends) {
-      for (int g = warp; g < ng; g += kWarps) {
-        const float s = self_dot<TI>(p, qb + (long long)g * p.qsH, kb + self, lane);
+      for (int g = kWarps - 1 - warp; g < ng; g += kWarps) {
+        const float s = self_dot<TI>(p, qb + (long long)g * p.qsH, self[0], lane);
         if (lane == 0) sm.self[g] = s;
       }
     }
@@ -663,7 +699,7 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
     // a column per thread, two heads at a time where a row takes half of them
     const int half = p.d <= kThreads / 2, c = threadIdx.x & (kThreads >> half) - 1;
     if (c < p.d) {
-      const float vi = ends ? ldf(vb + self + c) : 0.f;
+      const float vi = ends ? ldf(&self[1][c]) : 0.f;
       if (ends && !whole && (int)threadIdx.x == c) own[k * kOwn + c] = vi;
       for (int g = threadIdx.x != c; g < ng; g += 1 + half) {
         float Z = 0.f;
@@ -809,7 +845,9 @@ int heads_at_once(int G) { return G <= 1 ? 1 : G <= 2 ? 2 : G <= 4 ? 4 : 8; }
 
 template <typename TI, int LPR, bool VEC>
 cudaError_t launch_lanes(const PagedProblem& p, float* part, cudaStream_t s) {
-  switch (p.GG) {
+  // (bf16 in 16-byte groups with shared keys takes the tensor core)
+  if constexpr (sizeof(TI) == 2 && VEC) return launch_core<Lanes<TI, LPR, 1, VEC>>(p, part, s);
+  else switch (p.GG) {
     case 1: return launch_core<Lanes<TI, LPR, 1, VEC>>(p, part, s);
     case 2: return launch_core<Lanes<TI, LPR, 2, VEC>>(p, part, s);
     case 4: return launch_core<Lanes<TI, LPR, 4, VEC>>(p, part, s);
