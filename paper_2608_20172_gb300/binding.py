@@ -187,15 +187,6 @@ def _same_layout(ref: torch.Tensor, *others: torch.Tensor):
             raise ValueError("all tensors must live on the same CUDA device")
 
 
-def _like(t: torch.Tensor) -> torch.Tensor:
-    """An output with t's shape, dtype, device and strides.  The C ABI writes an output
-    with its input's element strides, which torch.empty_like does not keep for a view that
-    is not dense (e.g. a slice of a padded tensor); for a contiguous one it does."""
-    if type(t) is torch.Tensor and t.is_contiguous():
-        return torch.empty_like(t)
-    return torch.empty_strided(t.size(), t.stride(), dtype=t.dtype, device=t.device)
-
-
 # torch.cuda.current_stream().cuda_stream without the Stream object, where torch has it
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -206,6 +197,52 @@ def _stream(stream) -> int:
             return torch.cuda.current_stream().cuda_stream
         return _raw_stream(torch.cuda.current_device())
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _owned(stream, device, make, result=True):
+    """make()'s tensor in the memory of the stream that the call runs on.  Memory of the caller's
+    stream would go back to the allocator while the call's kernels are still queued on `stream`
+    (scratch does when the call returns), and its last use on the caller's stream need not be over
+    when they begin.  A result is used on the caller's stream too, and waits for it when it is freed."""
+    given = None if stream is None else _stream(stream)
+    if given is None or given == _stream(None):
+        return make()
+    if not isinstance(stream, torch.cuda.Stream):
+        # (the default stream: 0, or cudaStreamLegacy, 1; ExternalStream takes 0 for none given)
+        stream = torch.cuda.ExternalStream(given, device=device) if given > 1 else \
+            torch.cuda.default_stream(device)
+    here = torch.cuda.current_stream(device)
+    with torch.cuda.stream(stream):
+        t = make()
+    if result:
+        t.record_stream(here)
+    return t
+
+
+def _like(t: torch.Tensor, stream=None) -> torch.Tensor:
+    """An output with t's shape, dtype, device and strides, of the call's stream.  The C ABI writes
+    an output with its input's element strides, which torch.empty_like does not keep for a view
+    that is not dense (e.g. a slice of a padded tensor); for a contiguous one it does."""
+    if stream is not None:
+        return _owned(stream, t.device, lambda: _like(t))
+    if type(t) is torch.Tensor and t.is_contiguous():
+        return torch.empty_like(t)
+    return torch.empty_strided(t.size(), t.stride(), dtype=t.dtype, device=t.device)
+
+
+def _new(size, dtype, device, stream=None) -> torch.Tensor:
+    """A dense output of the call's stream."""
+    if stream is None:
+        return torch.empty(size, dtype=dtype, device=device)
+    return _owned(stream, device, lambda: torch.empty(size, dtype=dtype, device=device))
+
+
+def _scratch(nbytes: int, device, stream=None) -> torch.Tensor:
+    """Device bytes that only the call's kernels use."""
+    if stream is None:
+        return torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return _owned(stream, device, lambda: torch.empty(nbytes, dtype=torch.uint8, device=device),
+                  result=False)
 
 
 def _ptr(t):
@@ -222,11 +259,11 @@ def fwd(q, k, v, lam: float, tau_s: float = 2.0, *, kernel: str = "auto", out=No
     _same_layout(q, k, v)
     B, T, H, _ = q.shape
     if out is None:
-        out = _like(q)
+        out = _like(q, stream)
     else:
         _same_layout(q, out)
     if logz is None:
-        logz = torch.empty((B, H, T), device=q.device, dtype=torch.float32)
+        logz = _new((B, H, T), torch.float32, q.device, stream)
     rc = load().relation_fwd_ex(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(logz), float(lam),
                                 float(tau_s), shape_of(q), _dtype_code(q), KERNELS[kernel],
                                 _ptr(dev_status), _stream(stream))
@@ -242,13 +279,13 @@ def fwd_flow(q, k, v, lam: float, tau_s: float = 2.0, *, kernel: str = "auto", o
     _same_layout(q, k, v)
     B, T, H, _ = q.shape
     if out is None:
-        out = _like(q)
+        out = _like(q, stream)
     else:
         _same_layout(q, out)
     if logz is None:
-        logz = torch.empty((B, H, T), device=q.device, dtype=torch.float32)
+        logz = _new((B, H, T), torch.float32, q.device, stream)
     if self_flow is None:
-        self_flow = torch.empty((B, H, T), device=q.device, dtype=torch.float32)
+        self_flow = _new((B, H, T), torch.float32, q.device, stream)
     rc = load().relation_fwd_flow(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(logz),
                                   _ptr(self_flow), float(lam), float(tau_s), shape_of(q),
                                   _dtype_code(q), KERNELS[kernel], _ptr(dev_status),
@@ -268,7 +305,7 @@ def linear_fwd(p1, p2, v, alpha, tau_s: float = 2.0, *, kernel: str = "auto", ou
             tuple(alpha.stride()) != tuple(p1.stride()):
         raise ValueError("alpha must be fp32 with p1's shape and strides")
     if out is None:
-        out = _like(p1)
+        out = _like(p1, stream)
     else:
         _same_layout(p1, out)
     rc = load().relation_linear_fwd_ex(_ptr(p1), _ptr(p2), _ptr(v), _ptr(alpha), _ptr(out),
@@ -299,9 +336,9 @@ def fwd_state(q, k, v, causal: bool, *, out=None, dev_status=None, stream=None):
         _same_layout(q, k, v)
     B, Tq, H, d = q.shape
     if out is None:
-        out = (torch.empty((B, H, Tq), dtype=torch.float32, device=q.device),
-               torch.empty((B, H, Tq), dtype=torch.float32, device=q.device),
-               torch.empty((B, H, Tq, d), dtype=torch.float32, device=q.device))
+        out = (_new((B, H, Tq), torch.float32, q.device, stream),
+               _new((B, H, Tq), torch.float32, q.device, stream),
+               _new((B, H, Tq, d), torch.float32, q.device, stream))
     m, l, z = out
     _check_summary(out, B, H, Tq, d, q.device)
     rc = load().relation_fwd_state(_ptr(q), _ptr(k), _ptr(v), _ptr(m), _ptr(l), _ptr(z),
@@ -336,10 +373,10 @@ def state_finish(q, k, v, state, lam: float, tau_s: float = 2.0, pos0: int = 0, 
     m, l, z = state
     B, T, H, d = q.shape
     if out is None:
-        out = _like(q)
+        out = _like(q, stream)
     else:
         _same_layout(q, out)
-    logz = torch.empty((B, H, T), dtype=torch.float32, device=q.device) if logz is None else logz
+    logz = _new((B, H, T), torch.float32, q.device, stream) if logz is None else logz
     _check_summary(state, B, H, T, d, q.device)
     if tuple(logz.shape) != (B, H, T) or logz.dtype != torch.float32 or not logz.is_contiguous():
         raise ValueError("logz must be a dense fp32 [B, H, T] tensor")
@@ -366,11 +403,11 @@ def linear_fwd_ws(p1, p2, v, alpha, tau_s: float = 2.0, *, workspace=None, out=N
             tuple(alpha.stride()) != tuple(p1.stride()):
         raise ValueError("alpha must be fp32 with p1's shape and strides")
     if out is None:
-        out = _like(p1)
+        out = _like(p1, stream)
     else:
         _same_layout(p1, out)
     if workspace is None:
-        workspace = torch.empty(max(linear_fwd_workspace_size(p1), 16), dtype=torch.uint8, device=p1.device)
+        workspace = _scratch(max(linear_fwd_workspace_size(p1), 16), p1.device, stream)
     rc = load().relation_linear_fwd_ws(_ptr(p1), _ptr(p2), _ptr(v), _ptr(alpha), _ptr(out),
                                        float(tau_s), shape_of(p1), _dtype_code(p1),
                                        _ptr(workspace), workspace.numel(), _ptr(dev_status),
@@ -396,11 +433,10 @@ def linear_bwd(p1, p2, v, alpha, dy, tau_s: float = 2.0, *, kernel: str = "auto"
     if alpha.dtype != torch.float32 or tuple(alpha.shape) != tuple(p1.shape) or \
             tuple(alpha.stride()) != tuple(p1.stride()):
         raise ValueError("alpha must be fp32 with p1's shape and strides")
-    dp1, dp2, dv = _like(p1), _like(p1), _like(p1)
-    dalpha = _like(alpha)
+    dp1, dp2, dv = _like(p1, stream), _like(p1, stream), _like(p1, stream)
+    dalpha = _like(alpha, stream)
     if workspace is None:
-        workspace = torch.empty(max(linear_bwd_workspace_size(p1, kernel), 16), device=p1.device,
-                                dtype=torch.uint8)
+        workspace = _scratch(max(linear_bwd_workspace_size(p1, kernel), 16), p1.device, stream)
     rc = load().relation_linear_bwd_ex(_ptr(p1), _ptr(p2), _ptr(v), _ptr(alpha), _ptr(dy),
                                        _ptr(dp1), _ptr(dp2), _ptr(dv), _ptr(dalpha),
                                        float(tau_s), shape_of(p1), _dtype_code(p1),
@@ -412,12 +448,14 @@ def linear_bwd(p1, p2, v, alpha, dy, tau_s: float = 2.0, *, kernel: str = "auto"
     return dp1, dp2, dv, dalpha
 
 
-def _layer_args(theta, pairing, rope_base, x):
+def _layer_args(theta, pairing, rope_base, x, stream):
     if theta.dtype != torch.float32 or theta.device != x.device or theta.numel() != x.shape[2] // 2:
         raise ValueError("theta must be fp32 [H/2] on the inputs' device")
     if pairing not in (0, 1):
         raise ValueError("pairing must be 0 (pairs (0,1), (2,3), ...) or 1 ((1,2), ..., (H-1,0))")
-    return theta.contiguous(), int(pairing), float(rope_base)
+    if not theta.is_contiguous():
+        theta = _owned(stream, x.device, theta.contiguous, result=False)
+    return theta, int(pairing), float(rope_base)
 
 
 def layer_prep(p1, p2, info, theta, pairing: int = 0, rope_base: float = 1.0e4, *, out=None,
@@ -425,9 +463,9 @@ def layer_prep(p1, p2, info, theta, pairing: int = 0, rope_base: float = 1.0e4, 
     """The layer's transforms before the operator: returns (q, k, v) = (RoPE(p1),
     RoPE(p2), Givens(info)) for [B, T, H, d] inputs of one layout, theta fp32 [H/2]."""
     _same_layout(p1, p2, info)
-    theta, pairing, rope_base = _layer_args(theta, pairing, rope_base, p1)
+    theta, pairing, rope_base = _layer_args(theta, pairing, rope_base, p1, stream)
     if out is None:
-        q, k, v = _like(p1), _like(p1), _like(p1)
+        q, k, v = _like(p1, stream), _like(p1, stream), _like(p1, stream)
     else:
         q, k, v = out
         _same_layout(p1, q, k, v)
@@ -448,12 +486,11 @@ def layer_grad(dq, dk, dv, info, theta, pairing: int = 0, rope_base: float = 1.0
                workspace=None, stream=None):
     """Gradient of layer_prep: returns (dp1, dp2, dinfo, dtheta)."""
     _same_layout(dq, dk, dv, info)
-    theta, pairing, rope_base = _layer_args(theta, pairing, rope_base, dq)
-    dp1, dp2, dinfo = _like(dq), _like(dq), _like(dq)
-    dtheta = _like(theta)
+    theta, pairing, rope_base = _layer_args(theta, pairing, rope_base, dq, stream)
+    dp1, dp2, dinfo = _like(dq, stream), _like(dq, stream), _like(dq, stream)
+    dtheta = _like(theta, stream)
     if workspace is None:
-        workspace = torch.empty(max(layer_grad_workspace_size(dq), 16), device=dq.device,
-                                dtype=torch.uint8)
+        workspace = _scratch(max(layer_grad_workspace_size(dq), 16), dq.device, stream)
     rc = load().relation_layer_grad(_ptr(dq), _ptr(dk), _ptr(dv), _ptr(info), _ptr(theta),
                                     pairing, rope_base, _ptr(dp1), _ptr(dp2), _ptr(dinfo),
                                     _ptr(dtheta), shape_of(dq), _dtype_code(dq), _ptr(workspace),
@@ -480,13 +517,13 @@ def decode(q, k_cache, v_cache, lengths, lam: float, tau_s: float = 2.0, *, out=
         raise ValueError("q must be [B, H, d] with d contiguous, of the cache's dtype")
     if lengths.dtype != torch.int32 or lengths.numel() != B or not lengths.is_contiguous():
         raise ValueError("lengths must be a contiguous int32 tensor of B entries")
-    out = _like(q) if out is None else out
+    out = _like(q, stream) if out is None else out
     if out.stride() != q.stride():
         raise ValueError("out must have q's layout")
     if logz is None:
-        logz = torch.empty((B, H), device=q.device, dtype=torch.float32)
+        logz = _new((B, H), torch.float32, q.device, stream)
     if workspace is None:
-        workspace = torch.empty(decode_workspace_size(k_cache), device=q.device, dtype=torch.uint8)
+        workspace = _scratch(decode_workspace_size(k_cache), q.device, stream)
     rc = load().relation_decode(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(lengths), _ptr(out),
                                 _ptr(logz), float(lam), float(tau_s), shape_of(k_cache),
                                 q.stride(0), q.stride(1), _dtype_code(q), _ptr(workspace),
@@ -578,11 +615,11 @@ def page_plan(lengths, counts, block_table, free_pages, free_state, page_size: i
                          "the operands' device")
     if out is None:  # (five small allocations take less than one and its views)
         on = lengths.device
-        slots = torch.empty(n, dtype=_I64, device=on)
-        positions = torch.empty(n, dtype=_I32, device=on)
-        starts = torch.empty(B + 1, dtype=_I32, device=on)
-        new = torch.empty(B, dtype=_I32, device=on)
-        state = torch.empty(2, dtype=_I32, device=on)
+        slots = _new(n, _I64, on, stream)
+        positions = _new(n, _I32, on, stream)
+        starts = _new(B + 1, _I32, on, stream)
+        new = _new(B, _I32, on, stream)
+        state = _new(2, _I32, on, stream)
         out = PagePlan(slots, positions, starts, new, state)
     else:
         slots, positions, starts, new, state = out
@@ -631,7 +668,7 @@ def cache_append(p1, p2, info, theta, positions, slots, k_pages, v_pages, pairin
     if p1 is None:
         out = None
     elif out is None:
-        out = _like(p1)
+        out = _like(p1, stream)
     for t in (p2, info) if p1 is None else (p2, info, p1, out):
         if t.dtype is not dtype or t.get_device() != dev or t.shape != shape or t.stride() != st:
             raise ValueError("p1, p2, info and out need the same shape and strides and the pages' "
@@ -681,18 +718,17 @@ def paged_decode(q, k_pages, v_pages, block_table, lengths, lam: float, tau_s: f
         raise ValueError("block_table must be an int32 [B, cols] tensor with contiguous rows on "
                          "the pages' device")
     if out is None:
-        out = _like(q)
+        out = _like(q, stream)
     elif out.shape != shape or out.stride() != st or out.dtype is not q.dtype or \
             out.get_device() != dev:
         raise ValueError("out must have q's layout")
     if logz is None:
-        logz = torch.empty((B, H), device=q.device, dtype=_F32)
+        logz = _new((B, H), _F32, q.device, stream)
     else:
         _need("logz", logz, dev, _F32, B * H)
     lib, dt = load(), _dtype_code(q)
     if workspace is None:
-        workspace = torch.empty(lib.relation_paged_decode_workspace_size(H, pages, dt),
-                                device=q.device, dtype=torch.uint8)
+        workspace = _scratch(lib.relation_paged_decode_workspace_size(H, pages, dt), q.device, stream)
     rc = lib.relation_paged_decode(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
                                    block_table.data_ptr(), block_table.shape[1],
                                    block_table.stride(0), lengths.data_ptr(), out.data_ptr(),
@@ -728,7 +764,7 @@ def sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, o
     if min_p is not None:
         _need("min_p", min_p, dev, _F32, R)
     if out is None:
-        out = (torch.empty(R, dtype=_I32, device=u.device), torch.empty_like(u), torch.empty_like(u))
+        out = (_new(R, _I32, u.device, stream), _like(u, stream), _like(u, stream))
         token, logprob, logz = out
     else:
         token, logprob, logz = out
@@ -756,13 +792,13 @@ def bwd(q, k, v, o, dout, logz, lam: float, tau_s: float = 2.0, *, kernel: str =
     given = [t for t in (dq, dk, dv) if t is not None]
     if given:
         _same_layout(q, *given)
-    dq = _like(q) if dq is None else dq
-    dk = _like(q) if dk is None else dk
-    dv = _like(q) if dv is None else dv
+    dq = _like(q, stream) if dq is None else dq
+    dk = _like(q, stream) if dk is None else dk
+    dv = _like(q, stream) if dv is None else dv
     if dlambda is None:
-        dlambda = torch.empty(1, device=q.device, dtype=torch.float32)
+        dlambda = _new(1, torch.float32, q.device, stream)
     if workspace is None:
-        workspace = torch.empty(workspace_size(q), device=q.device, dtype=torch.uint8)
+        workspace = _scratch(workspace_size(q), q.device, stream)
     rc = load().relation_bwd_stages(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(logz),
                                     _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dlambda), float(lam),
                                     float(tau_s), shape_of(q), _dtype_code(q),
