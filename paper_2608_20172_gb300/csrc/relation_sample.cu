@@ -734,9 +734,14 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
 
 template <typename TI, int LOW>
 cudaError_t launch_low(const SampleProblem& p, int cluster, int slice, cudaStream_t s) {
-  const int smem = ((int)sizeof(Smem<LOW>) + 15) / 16 * 16 + (slice + 4) * (int)sizeof(float);
+  // The limit is the kernel's, for every host thread: set to the longest slice's need, whatever this call
+  // launches with (a limit by the call could be lowered by another thread before the launch).
+  constexpr int fixed = ((int)sizeof(Smem<LOW>) + 15) / 16 * 16;
+  constexpr int longest = fixed + ((LOW == low_bits(true) ? kMaxSlice : kShort) + 4) * (int)sizeof(float);
+  static_assert(longest <= 227 * 1024, "shared memory of a CTA");
+  const int smem = fixed + (slice + 4) * (int)sizeof(float);
   cudaError_t e = cudaFuncSetAttribute(sample_kernel<TI, LOW>,
-                                       cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+                                       cudaFuncAttributeMaxDynamicSharedMemorySize, longest);
   if (e != cudaSuccess) { note_failure("sample: shared memory"); return e; }
   e = launch_pdl(sample_kernel<TI, LOW>, dim3((unsigned)p.R * cluster), kThreads, smem, s, cluster, p,
                  slice);
