@@ -299,6 +299,18 @@ struct Lanes {
       kr[i] = load_group<TI, VEC>(kb + off, c0, p.d);
       vr[i] = load_group<TI, VEC>(vb + off, c0, p.d);
     }
+    // No value of a row past the end: its weight is 0, and 0 times an infinity would be NaN.  Before the
+    // scores or after them, by the registers (us before and after them, 32 requests to 4096 rows, 8 key
+    // heads of 128: unaligned bf16 with 1, 2, 8 query heads each 99 and 109, 107 and 142, 237 and 224; fp32
+    // in 16-byte groups with 4 170 and 146).
+    auto cut = [&] {
+      if (j + R <= rb) return;
+#pragma unroll
+      for (int i = 0; i < NI; ++i)
+        if (j + i * RPL + group >= rb) vr[i] = make_uint4(0, 0, 0, 0);
+    };
+    constexpr bool kEarly = sizeof(TI) == 2 && !VEC && GG <= 2;
+    if constexpr (kEarly) cut();
     float P[GG];
 #pragma unroll
     for (int g = 0; g < GG; ++g) {
@@ -339,6 +351,7 @@ struct Lanes {
       P[g] = in ? fast_exp(E - m[g]) : 0.f;
       if (lane % DUP == 0) l[g] += P[g];
     }
+    if constexpr (!kEarly) cut();
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       float x[VE];
@@ -397,6 +410,12 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
       "{%0,%1,%2,%3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// A sum's parts by the weights' leading bits and by what these leave.  The leading weights are positive,
+// so that an infinite value makes their part what the whole is; the others are of either sign, or 0.
+__device__ __forceinline__ float whole_of(float hi, float lo) {
+  return fabsf(hi) < INFINITY ? hi + lo : hi;
 }
 
 // The same for 2 to 8 query heads that share bf16 keys (16-byte groups), on the tensor core, 16 rows
@@ -562,7 +581,8 @@ struct Tensor {
       uint32_t v[4][4];
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
-        const uint4 x = vs[((k & 1) + 8 * (k >> 1)) * kRow + 8 * i];
+        uint4 x = vs[((k & 1) + 8 * (k >> 1)) * kRow + 8 * i];
+        if (!FULL && !in[k]) x = make_uint4(0, 0, 0, 0);  // (0 times an infinity would be NaN)
         v[k][0] = x.x; v[k][1] = x.y; v[k][2] = x.z; v[k][3] = x.w;
       }
 #pragma unroll
@@ -587,7 +607,7 @@ struct Tensor {
       for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int k = 0; k < 2; ++k)
-          sm.z[warp][r][8 * (2 * t + k + 8 * i) + e] = z[i][e][k] + z[i][e][k + 2];
+          sm.z[warp][r][8 * (2 * t + k + 8 * i) + e] = whole_of(z[i][e][k], z[i][e][k + 2]);
   }
 };
 
