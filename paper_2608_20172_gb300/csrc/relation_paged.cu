@@ -242,6 +242,12 @@ __device__ __forceinline__ Gate gate_of(const PagedProblem& p, int len, float qk
           A > S ? A + log1pf(expf(S - A)) : S + log1pf(expf(A - S))};
 }
 
+// (1 - g) v + g z for 0 < g < 1.  With an infinite v the one product would be one of a difference of
+// infinities; the sum has the infinity's value (and NaN where z or g has it).
+__device__ __forceinline__ float mix(float g, float z, float v) {
+  return fabsf(v) < INFINITY ? fmaf(g, z - v, v) : fmaf(0.f, g, z + v);
+}
+
 // q . k_self by one warp
 template <typename TI>
 __device__ __forceinline__ float self_dot(const PagedProblem& p, const TI* q, const TI* k, int lane) {
@@ -726,7 +732,7 @@ __global__ void __launch_bounds__(kThreads, Core::kCtas)
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) Z = fmaf(sm.m[w][g], sm.z[w][g][c], Z);
         if (whole)
-          out[(long long)g * p.qsH + c] = (TI)fmaf(sm.self[g], Z - vi, vi);
+          out[(long long)g * p.qsH + c] = (TI)mix(sm.self[g], Z, vi);
         else  // slot 0: the run's first head (begun before it), 1: its last
           part[(((long long)k * 2 + (u == s0)) * p.GG + g) * kPart + 2 + c] = Z;
       }
@@ -827,7 +833,7 @@ __global__ void __launch_bounds__(kThreads, 8)
   if (!in) return;
   const Gate gate = gate_of(p, at.len, qk, M, L);
   reinterpret_cast<TI*>(p.out)[(long long)b * p.qsB + (long long)h * p.qsH + c] =
-      (TI)fmaf(gate.g, Z / L - vi, vi);
+      (TI)mix(gate.g, Z / L, vi);
   if (c == 0) p.logz[(long long)b * p.H + h] = gate.lz;
 }
 
