@@ -381,7 +381,8 @@ relation_status relation_paged_decode(const void* q, const void* k_pages, const 
  *   u           device float[R] in [0, 1].
  *   temperature, top_k, top_p, min_p : device float / int / float / float [R], each may be null
  *               (1, none, none, none).  temperature 0 takes the largest logit, the lowest index
- *               of equal ones.  top_k <= 0 or >= V, top_p >= 1 and min_p <= 0 keep every token.
+ *               of equal ones.  top_k <= 0 or >= V, top_p >= 1 or NaN and min_p <= 0 or NaN keep
+ *               every token.
  * Token j weighs w_j = exp((x_j - max x) / temperature) in fp32, summed as the whole number
  * floor(2^40 w_j), so that the result is the same for any batch.  Tokens are ordered by descending
  * w_j, equal ones by index; the first top_k are kept, of these the shortest beginning that holds

@@ -574,7 +574,8 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(SampleProblem p, int s
   const float scale = greedy ? 1.f : __fdiv_rn(1.f, temperature);
   const int k = greedy ? 1 : p.top_k ? p.top_k[row] : 0;
   const float top_p = p.top_p ? p.top_p[row] : 1.f;
-  const float min_p = p.min_p ? fminf(p.min_p[row], 1.f) : 0.f;
+  float min_p = p.min_p ? p.min_p[row] : 0.f;
+  min_p = min_p > 0.f ? fminf(min_p, 1.f) : 0.f;  // (NaN: no cut, as a NaN top_p)
   const bool valid = temperature >= 0.f && temperature < INFINITY && u >= 0.f && u <= 1.f;
   const bool by_k = k > 0 && k < p.V, by_p = top_p < 1.f;
   // the slice, and the row's largest logit
