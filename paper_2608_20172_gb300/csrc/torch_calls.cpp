@@ -53,11 +53,8 @@ T* optional(PyObject* x, at::ScalarType type, int64_t n, c10::DeviceIndex device
 int* status_of(PyObject* x) { return x == Py_None ? nullptr : data<int>(tensor(x)); }
 int integer(PyObject* x) {
   if (!PyLong_CheckExact(x)) throw Decline();
-  const long v = PyLong_AsLong(x);
-  if (v < -0x7fffffffL || v > 0x7fffffffL) {
-    PyErr_Clear();
-    throw Decline();
-  }
+  const long v = PyLong_AsLong(x);  // (-1 and an error past 64 bits)
+  if (v < -0x7fffffffL || v > 0x7fffffffL || (v == -1 && PyErr_Occurred())) throw Decline();
   return (int)v;
 }
 float real(PyObject* x) {
