@@ -249,6 +249,17 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _status(t, device: int):
+    """dev_status's pointer: an int32 that the kernels of a call on cuda:`device` may write (on that
+    device, or in pinned host memory)."""
+    if t is None:
+        return None
+    if t.dtype is not torch.int32 or t.numel() < 1 or not (t.get_device() == device or
+                                                           (t.device.type == "cpu" and t.is_pinned())):
+        raise ValueError("dev_status must be an int32 tensor on the operands' CUDA device")
+    return t.data_ptr()
+
+
 def workspace_size(q: torch.Tensor) -> int:
     return int(load().relation_bwd_workspace_size(shape_of(q), _dtype_code(q)))
 
@@ -266,7 +277,7 @@ def fwd(q, k, v, lam: float, tau_s: float = 2.0, *, kernel: str = "auto", out=No
         logz = _new((B, H, T), torch.float32, q.device, stream)
     rc = load().relation_fwd_ex(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(logz), float(lam),
                                 float(tau_s), shape_of(q), _dtype_code(q), KERNELS[kernel],
-                                _ptr(dev_status), _stream(stream))
+                                _status(dev_status, q.get_device()), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_fwd")
     return out, logz
@@ -288,7 +299,7 @@ def fwd_flow(q, k, v, lam: float, tau_s: float = 2.0, *, kernel: str = "auto", o
         self_flow = _new((B, H, T), torch.float32, q.device, stream)
     rc = load().relation_fwd_flow(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(logz),
                                   _ptr(self_flow), float(lam), float(tau_s), shape_of(q),
-                                  _dtype_code(q), KERNELS[kernel], _ptr(dev_status),
+                                  _dtype_code(q), KERNELS[kernel], _status(dev_status, q.get_device()),
                                   _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_fwd_flow")
@@ -310,7 +321,7 @@ def linear_fwd(p1, p2, v, alpha, tau_s: float = 2.0, *, kernel: str = "auto", ou
         _same_layout(p1, out)
     rc = load().relation_linear_fwd_ex(_ptr(p1), _ptr(p2), _ptr(v), _ptr(alpha), _ptr(out),
                                        float(tau_s), shape_of(p1), _dtype_code(p1),
-                                       KERNELS[kernel], _ptr(dev_status),
+                                       KERNELS[kernel], _status(dev_status, p1.get_device()),
                                        _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_linear_fwd_ex")
@@ -343,7 +354,7 @@ def fwd_state(q, k, v, causal: bool, *, out=None, dev_status=None, stream=None):
     _check_summary(out, B, H, Tq, d, q.device)
     rc = load().relation_fwd_state(_ptr(q), _ptr(k), _ptr(v), _ptr(m), _ptr(l), _ptr(z),
                                    shape_of(q), shape_of(k), int(bool(causal)), _dtype_code(q),
-                                   _ptr(dev_status), _stream(stream))
+                                   _status(dev_status, k.get_device()), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_fwd_state")
     return m, l, z
@@ -410,8 +421,8 @@ def linear_fwd_ws(p1, p2, v, alpha, tau_s: float = 2.0, *, workspace=None, out=N
         workspace = _scratch(max(linear_fwd_workspace_size(p1), 16), p1.device, stream)
     rc = load().relation_linear_fwd_ws(_ptr(p1), _ptr(p2), _ptr(v), _ptr(alpha), _ptr(out),
                                        float(tau_s), shape_of(p1), _dtype_code(p1),
-                                       _ptr(workspace), workspace.numel(), _ptr(dev_status),
-                                       _stream(stream))
+                                       _ptr(workspace), workspace.numel(),
+                                       _status(dev_status, p1.get_device()), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_linear_fwd_ws")
     return out
@@ -442,7 +453,7 @@ def linear_bwd(p1, p2, v, alpha, dy, tau_s: float = 2.0, *, kernel: str = "auto"
                                        float(tau_s), shape_of(p1), _dtype_code(p1),
                                        KERNELS[kernel], _ptr(workspace),
                                        workspace.numel() * workspace.element_size(),
-                                       _ptr(dev_status), _stream(stream))
+                                       _status(dev_status, p1.get_device()), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_linear_bwd_ex")
     return dp1, dp2, dv, dalpha
@@ -527,8 +538,8 @@ def decode(q, k_cache, v_cache, lengths, lam: float, tau_s: float = 2.0, *, out=
     rc = load().relation_decode(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(lengths), _ptr(out),
                                 _ptr(logz), float(lam), float(tau_s), shape_of(k_cache),
                                 q.stride(0), q.stride(1), _dtype_code(q), _ptr(workspace),
-                                workspace.numel() * workspace.element_size(), _ptr(dev_status),
-                                _stream(stream))
+                                workspace.numel() * workspace.element_size(),
+                                _status(dev_status, k_cache.get_device()), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_decode")
     return out, logz
@@ -633,7 +644,7 @@ def page_plan(lengths, counts, block_table, free_pages, free_state, page_size: i
                                    block_table.stride(0), free_pages.data_ptr(), n_pages,
                                    free_state.data_ptr(), state.data_ptr(), new.data_ptr(),
                                    starts.data_ptr(), slots.data_ptr(), positions.data_ptr(), n,
-                                   _ptr(dev_status), _stream(stream))
+                                   _status(dev_status, dev), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_page_plan")
     return out
@@ -685,7 +696,7 @@ def cache_append(p1, p2, info, theta, positions, slots, k_pages, v_pages, pairin
                                       int(pairing), float(rope_base), _ptr(positions),
                                       slots.data_ptr(), _ptr(out), N, st[0], st[1],
                                       k_pages.data_ptr(), v_pages.data_ptr(), pages,
-                                      _dtype_code(p2), _ptr(dev_status), _stream(stream))
+                                      _dtype_code(p2), _status(dev_status, dev), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_cache_append")
     return out
@@ -734,8 +745,8 @@ def paged_decode(q, k_pages, v_pages, block_table, lengths, lam: float, tau_s: f
                                    block_table.stride(0), lengths.data_ptr(), out.data_ptr(),
                                    logz.data_ptr(), float(lam), float(tau_s), B, H, pages, st[0],
                                    st[1], dt, workspace.data_ptr(),
-                                   workspace.numel() * workspace.element_size(), _ptr(dev_status),
-                                   _stream(stream))
+                                   workspace.numel() * workspace.element_size(),
+                                   _status(dev_status, dev), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_paged_decode")
     return out, logz
@@ -774,7 +785,7 @@ def sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, o
     rc = load().relation_sample(logits.data_ptr(), R, V, st[0], dt, u.data_ptr(),
                                 _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                                 token.data_ptr(), logprob.data_ptr(), logz.data_ptr(),
-                                _ptr(dev_status), _stream(stream))
+                                _status(dev_status, dev), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_sample")
     return out
@@ -803,7 +814,7 @@ def bwd(q, k, v, o, dout, logz, lam: float, tau_s: float = 2.0, *, kernel: str =
                                     _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dlambda), float(lam),
                                     float(tau_s), shape_of(q), _dtype_code(q),
                                     _ptr(workspace), workspace.numel() * workspace.element_size(),
-                                    KERNELS[kernel], int(stages), _ptr(dev_status),
+                                    KERNELS[kernel], int(stages), _status(dev_status, q.get_device()),
                                     _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_bwd")
@@ -828,7 +839,7 @@ def bwd_no_alloc(q, k, v, o, dout, logz, lam: float, tau_s: float = 2.0, *,
     rc = load().relation_bwd_static(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(logz),
                                     _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dlambda), float(lam),
                                     float(tau_s), shape_of(q), _dtype_code(q), KERNELS[kernel],
-                                    _ptr(dev_status), _stream(stream))
+                                    _status(dev_status, q.get_device()), _stream(stream))
     if rc != OK:
         raise RelationError(rc, "relation_bwd_static")
     return dq, dk, dv, dlambda
@@ -836,8 +847,8 @@ def bwd_no_alloc(q, k, v, o, dout, logz, lam: float, tau_s: float = 2.0, *,
 
 def selftest_wait_timeout(dev_status: torch.Tensor, timeout_us: int = 1000, stream=None) -> int:
     """Launch the bounded-wait self-test; returns the launch status."""
-    return int(load().relation_selftest_wait_timeout(_ptr(dev_status), int(timeout_us),
-                                                     _stream(stream)))
+    return int(load().relation_selftest_wait_timeout(
+        _status(dev_status, torch.cuda.current_device()), int(timeout_us), _stream(stream)))
 
 
 class RelationFunction(torch.autograd.Function):

@@ -49,8 +49,13 @@ template <typename T>
 T* optional(PyObject* x, at::ScalarType type, int64_t n, c10::DeviceIndex device) {
   return x == Py_None ? nullptr : data<T>(dense(x, type, n, device));
 }
-// None or the tensor's pointer, as the binding takes it
-int* status_of(PyObject* x) { return x == Py_None ? nullptr : data<int>(tensor(x)); }
+// None or what the kernels may write: an int of the device
+int* status_of(PyObject* x, c10::DeviceIndex device) {
+  if (x == Py_None) return nullptr;
+  const at::Tensor& t = tensor(x);
+  if (t.scalar_type() != at::kInt || t.numel() < 1 || !t.is_cuda() || t.get_device() != device) throw Decline();
+  return data<int>(t);
+}
 int integer(PyObject* x) {
   if (!PyLong_CheckExact(x)) throw Decline();
   const long v = PyLong_AsLong(x);  // (-1 and an error past 64 bits)
@@ -121,7 +126,7 @@ PyObject* page_plan(PyObject* const* a) {
   if (g_page_plan(data<int>(lengths), data<int>(counts), (int)B, page, data<int>(tab), (int)tab.size(1),
                   tab.stride(0), data<int>(ring), (int)ring.numel(), data<int>(state), data<int>(after),
                   data<int>(next), data<int>(starts), reinterpret_cast<long long*>(data<int64_t>(slots)),
-                  data<int>(positions), n, status_of(a[7]), current_stream()) != RELATION_OK)
+                  data<int>(positions), n, status_of(a[7], dev), current_stream()) != RELATION_OK)
     throw Decline();
   return tuple(slots, positions, starts, next, after);
 }
@@ -146,7 +151,7 @@ PyObject* cache_append(PyObject* const* a) {
   if (g_cache_append(p1.data_ptr(), p2.data_ptr(), info.data_ptr(), theta, pairing, real(a[9]), positions,
                      reinterpret_cast<const long long*>(data<int64_t>(slots)), q.data_ptr(), (int)N,
                      p1.stride(0), p1.stride(1), k.data_ptr(), v.data_ptr(), c, type_of(p1),
-                     status_of(a[10]), current_stream()) != RELATION_OK)
+                     status_of(a[10], dev), current_stream()) != RELATION_OK)
     throw Decline();
   return wrap(std::move(q));
 }
@@ -170,7 +175,7 @@ PyObject* paged_decode(PyObject* const* a) {
   if (g_paged_decode(q.data_ptr(), k.data_ptr(), v.data_ptr(), data<int>(tab), (int)tab.size(1),
                      tab.stride(0), data<int>(lengths), y.data_ptr(), data<float>(logz), real(a[5]),
                      real(a[6]), (int)B, (int)H, c, q.stride(0), q.stride(1), dt, ws.data_ptr(), bytes,
-                     status_of(a[7]), current_stream()) != RELATION_OK)
+                     status_of(a[7], dev), current_stream()) != RELATION_OK)
     throw Decline();
   return tuple(y, logz);
 }
@@ -191,7 +196,7 @@ PyObject* sample(PyObject* const* a) {
   at::Tensor token = at::empty({R}, u.options().dtype(at::kInt)), logprob = at::empty({R}, u.options()),
              logz = at::empty({R}, u.options());
   if (g_sample(x.data_ptr(), (int)R, (int)x.size(1), x.stride(0), dt, data<float>(u), temperature, top_k,
-               top_p, min_p, data<int>(token), data<float>(logprob), data<float>(logz), status_of(a[6]),
+               top_p, min_p, data<int>(token), data<float>(logprob), data<float>(logz), status_of(a[6], dev),
                current_stream()) != RELATION_OK)
     throw Decline();
   return tuple(token, logprob, logz);
