@@ -245,6 +245,14 @@ def _scratch(nbytes: int, device, stream=None) -> torch.Tensor:
                   result=False)
 
 
+def _queue(stream, device: int) -> int:
+    """The stream of a call whose operands are on cuda:`device`: given, or the current one.  The
+    library launches on the current device."""
+    if device != torch.cuda.current_device():
+        raise ValueError(f"the operands are on cuda:{device}, which is not the current device")
+    return _stream(stream)
+
+
 def _ptr(t):
     return None if t is None else t.data_ptr()
 
@@ -277,7 +285,7 @@ def fwd(q, k, v, lam: float, tau_s: float = 2.0, *, kernel: str = "auto", out=No
         logz = _new((B, H, T), torch.float32, q.device, stream)
     rc = load().relation_fwd_ex(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(logz), float(lam),
                                 float(tau_s), shape_of(q), _dtype_code(q), KERNELS[kernel],
-                                _status(dev_status, q.get_device()), _stream(stream))
+                                _status(dev_status, q.get_device()), _queue(stream, q.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_fwd")
     return out, logz
@@ -300,7 +308,7 @@ def fwd_flow(q, k, v, lam: float, tau_s: float = 2.0, *, kernel: str = "auto", o
     rc = load().relation_fwd_flow(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(logz),
                                   _ptr(self_flow), float(lam), float(tau_s), shape_of(q),
                                   _dtype_code(q), KERNELS[kernel], _status(dev_status, q.get_device()),
-                                  _stream(stream))
+                                  _queue(stream, q.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_fwd_flow")
     return out, logz, self_flow
@@ -322,7 +330,7 @@ def linear_fwd(p1, p2, v, alpha, tau_s: float = 2.0, *, kernel: str = "auto", ou
     rc = load().relation_linear_fwd_ex(_ptr(p1), _ptr(p2), _ptr(v), _ptr(alpha), _ptr(out),
                                        float(tau_s), shape_of(p1), _dtype_code(p1),
                                        KERNELS[kernel], _status(dev_status, p1.get_device()),
-                                       _stream(stream))
+                                       _queue(stream, p1.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_linear_fwd_ex")
     return out
@@ -354,7 +362,7 @@ def fwd_state(q, k, v, causal: bool, *, out=None, dev_status=None, stream=None):
     _check_summary(out, B, H, Tq, d, q.device)
     rc = load().relation_fwd_state(_ptr(q), _ptr(k), _ptr(v), _ptr(m), _ptr(l), _ptr(z),
                                    shape_of(q), shape_of(k), int(bool(causal)), _dtype_code(q),
-                                   _status(dev_status, k.get_device()), _stream(stream))
+                                   _status(dev_status, k.get_device()), _queue(stream, k.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_fwd_state")
     return m, l, z
@@ -370,7 +378,7 @@ def state_merge(state, other, *, stream=None):
     _check_summary(other, B, H, T, d, z.device)
     rc = load().relation_state_merge(_ptr(m), _ptr(l), _ptr(z), _ptr(m2), _ptr(l2), _ptr(z2),
                                      Shape(B, T, H, d, T * H * d, H * d, d),
-                                     _stream(stream))
+                                     _queue(stream, z.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_state_merge")
     return state
@@ -394,7 +402,7 @@ def state_finish(q, k, v, state, lam: float, tau_s: float = 2.0, pos0: int = 0, 
     rc = load().relation_state_finish(_ptr(q), _ptr(k), _ptr(v), _ptr(m), _ptr(l), _ptr(z),
                                       _ptr(out), _ptr(logz), _ptr(self_flow), float(lam),
                                       float(tau_s), int(pos0), shape_of(q), _dtype_code(q),
-                                      _stream(stream))
+                                      _queue(stream, q.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_state_finish")
     return out, logz
@@ -422,7 +430,8 @@ def linear_fwd_ws(p1, p2, v, alpha, tau_s: float = 2.0, *, workspace=None, out=N
     rc = load().relation_linear_fwd_ws(_ptr(p1), _ptr(p2), _ptr(v), _ptr(alpha), _ptr(out),
                                        float(tau_s), shape_of(p1), _dtype_code(p1),
                                        _ptr(workspace), workspace.numel(),
-                                       _status(dev_status, p1.get_device()), _stream(stream))
+                                       _status(dev_status, p1.get_device()),
+                                       _queue(stream, p1.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_linear_fwd_ws")
     return out
@@ -453,7 +462,8 @@ def linear_bwd(p1, p2, v, alpha, dy, tau_s: float = 2.0, *, kernel: str = "auto"
                                        float(tau_s), shape_of(p1), _dtype_code(p1),
                                        KERNELS[kernel], _ptr(workspace),
                                        workspace.numel() * workspace.element_size(),
-                                       _status(dev_status, p1.get_device()), _stream(stream))
+                                       _status(dev_status, p1.get_device()),
+                                       _queue(stream, p1.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_linear_bwd_ex")
     return dp1, dp2, dv, dalpha
@@ -482,7 +492,7 @@ def layer_prep(p1, p2, info, theta, pairing: int = 0, rope_base: float = 1.0e4, 
         _same_layout(p1, q, k, v)
     rc = load().relation_layer_prep(_ptr(p1), _ptr(p2), _ptr(info), _ptr(theta), pairing,
                                     rope_base, _ptr(q), _ptr(k), _ptr(v), shape_of(p1),
-                                    _dtype_code(p1), _stream(stream))
+                                    _dtype_code(p1), _queue(stream, p1.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_layer_prep")
     return q, k, v
@@ -506,7 +516,7 @@ def layer_grad(dq, dk, dv, info, theta, pairing: int = 0, rope_base: float = 1.0
                                     pairing, rope_base, _ptr(dp1), _ptr(dp2), _ptr(dinfo),
                                     _ptr(dtheta), shape_of(dq), _dtype_code(dq), _ptr(workspace),
                                     workspace.numel() * workspace.element_size(),
-                                    _stream(stream))
+                                    _queue(stream, dq.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_layer_grad")
     return dp1, dp2, dinfo, dtheta
@@ -539,7 +549,8 @@ def decode(q, k_cache, v_cache, lengths, lam: float, tau_s: float = 2.0, *, out=
                                 _ptr(logz), float(lam), float(tau_s), shape_of(k_cache),
                                 q.stride(0), q.stride(1), _dtype_code(q), _ptr(workspace),
                                 workspace.numel() * workspace.element_size(),
-                                _status(dev_status, k_cache.get_device()), _stream(stream))
+                                _status(dev_status, k_cache.get_device()),
+                                _queue(stream, k_cache.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_decode")
     return out, logz
@@ -644,7 +655,7 @@ def page_plan(lengths, counts, block_table, free_pages, free_state, page_size: i
                                    block_table.stride(0), free_pages.data_ptr(), n_pages,
                                    free_state.data_ptr(), state.data_ptr(), new.data_ptr(),
                                    starts.data_ptr(), slots.data_ptr(), positions.data_ptr(), n,
-                                   _status(dev_status, dev), _stream(stream))
+                                   _status(dev_status, dev), _queue(stream, dev))
     if rc != OK:
         raise RelationError(rc, "relation_page_plan")
     return out
@@ -696,7 +707,7 @@ def cache_append(p1, p2, info, theta, positions, slots, k_pages, v_pages, pairin
                                       int(pairing), float(rope_base), _ptr(positions),
                                       slots.data_ptr(), _ptr(out), N, st[0], st[1],
                                       k_pages.data_ptr(), v_pages.data_ptr(), pages,
-                                      _dtype_code(p2), _status(dev_status, dev), _stream(stream))
+                                      _dtype_code(p2), _status(dev_status, dev), _queue(stream, dev))
     if rc != OK:
         raise RelationError(rc, "relation_cache_append")
     return out
@@ -746,7 +757,7 @@ def paged_decode(q, k_pages, v_pages, block_table, lengths, lam: float, tau_s: f
                                    logz.data_ptr(), float(lam), float(tau_s), B, H, pages, st[0],
                                    st[1], dt, workspace.data_ptr(),
                                    workspace.numel() * workspace.element_size(),
-                                   _status(dev_status, dev), _stream(stream))
+                                   _status(dev_status, dev), _queue(stream, dev))
     if rc != OK:
         raise RelationError(rc, "relation_paged_decode")
     return out, logz
@@ -785,7 +796,7 @@ def sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, o
     rc = load().relation_sample(logits.data_ptr(), R, V, st[0], dt, u.data_ptr(),
                                 _ptr(temperature), _ptr(top_k), _ptr(top_p), _ptr(min_p),
                                 token.data_ptr(), logprob.data_ptr(), logz.data_ptr(),
-                                _status(dev_status, dev), _stream(stream))
+                                _status(dev_status, dev), _queue(stream, dev))
     if rc != OK:
         raise RelationError(rc, "relation_sample")
     return out
@@ -815,7 +826,7 @@ def bwd(q, k, v, o, dout, logz, lam: float, tau_s: float = 2.0, *, kernel: str =
                                     float(tau_s), shape_of(q), _dtype_code(q),
                                     _ptr(workspace), workspace.numel() * workspace.element_size(),
                                     KERNELS[kernel], int(stages), _status(dev_status, q.get_device()),
-                                    _stream(stream))
+                                    _queue(stream, q.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_bwd")
     return dq, dk, dv, dlambda
@@ -839,7 +850,7 @@ def bwd_no_alloc(q, k, v, o, dout, logz, lam: float, tau_s: float = 2.0, *,
     rc = load().relation_bwd_static(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(dout), _ptr(logz),
                                     _ptr(dq), _ptr(dk), _ptr(dv), _ptr(dlambda), float(lam),
                                     float(tau_s), shape_of(q), _dtype_code(q), KERNELS[kernel],
-                                    _status(dev_status, q.get_device()), _stream(stream))
+                                    _status(dev_status, q.get_device()), _queue(stream, q.get_device()))
     if rc != OK:
         raise RelationError(rc, "relation_bwd_static")
     return dq, dk, dv, dlambda

@@ -24,8 +24,11 @@ decltype(&relation_sample) g_sample;
 
 struct Decline {};  // the binding's own way
 
-relation_stream_t current_stream() {
-  return reinterpret_cast<relation_stream_t>(c10::cuda::getCurrentCUDAStream().stream());
+// The current stream; the library launches on the current device, which has to be the operands'
+relation_stream_t current_stream(c10::DeviceIndex device) {
+  const c10::cuda::CUDAStream s = c10::cuda::getCurrentCUDAStream();
+  if (s.device_index() != device) throw Decline();
+  return reinterpret_cast<relation_stream_t>(s.stream());
 }
 
 const at::Tensor& tensor(PyObject* x) {
@@ -126,7 +129,7 @@ PyObject* page_plan(PyObject* const* a) {
   if (g_page_plan(data<int>(lengths), data<int>(counts), (int)B, page, data<int>(tab), (int)tab.size(1),
                   tab.stride(0), data<int>(ring), (int)ring.numel(), data<int>(state), data<int>(after),
                   data<int>(next), data<int>(starts), reinterpret_cast<long long*>(data<int64_t>(slots)),
-                  data<int>(positions), n, status_of(a[7], dev), current_stream()) != RELATION_OK)
+                  data<int>(positions), n, status_of(a[7], dev), current_stream(dev)) != RELATION_OK)
     throw Decline();
   return tuple(slots, positions, starts, next, after);
 }
@@ -151,7 +154,7 @@ PyObject* cache_append(PyObject* const* a) {
   if (g_cache_append(p1.data_ptr(), p2.data_ptr(), info.data_ptr(), theta, pairing, real(a[9]), positions,
                      reinterpret_cast<const long long*>(data<int64_t>(slots)), q.data_ptr(), (int)N,
                      p1.stride(0), p1.stride(1), k.data_ptr(), v.data_ptr(), c, type_of(p1),
-                     status_of(a[10], dev), current_stream()) != RELATION_OK)
+                     status_of(a[10], dev), current_stream(dev)) != RELATION_OK)
     throw Decline();
   return wrap(std::move(q));
 }
@@ -175,7 +178,7 @@ PyObject* paged_decode(PyObject* const* a) {
   if (g_paged_decode(q.data_ptr(), k.data_ptr(), v.data_ptr(), data<int>(tab), (int)tab.size(1),
                      tab.stride(0), data<int>(lengths), y.data_ptr(), data<float>(logz), real(a[5]),
                      real(a[6]), (int)B, (int)H, c, q.stride(0), q.stride(1), dt, ws.data_ptr(), bytes,
-                     status_of(a[7], dev), current_stream()) != RELATION_OK)
+                     status_of(a[7], dev), current_stream(dev)) != RELATION_OK)
     throw Decline();
   return tuple(y, logz);
 }
@@ -197,7 +200,7 @@ PyObject* sample(PyObject* const* a) {
              logz = at::empty({R}, u.options());
   if (g_sample(x.data_ptr(), (int)R, (int)x.size(1), x.stride(0), dt, data<float>(u), temperature, top_k,
                top_p, min_p, data<int>(token), data<float>(logprob), data<float>(logz), status_of(a[6], dev),
-               current_stream()) != RELATION_OK)
+               current_stream(dev)) != RELATION_OK)
     throw Decline();
   return tuple(token, logprob, logz);
 }
