@@ -55,7 +55,11 @@ def _deps_digest() -> str:
 
 def build_calls(force: bool = False) -> str | None:
     """Compile relation_calls.so; returns its path, None where it cannot be built."""
-    import torch
+    try:
+        import torch
+    except ImportError as e:
+        print(f"relation_calls.so not built: {e}", file=sys.stderr)
+        return None
 
     src = os.path.join(CSRC, "torch_calls.cpp")
     root = os.path.dirname(torch.__file__)
