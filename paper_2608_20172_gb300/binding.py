@@ -15,6 +15,7 @@ import importlib.machinery
 import importlib.util
 import os
 import threading
+import warnings
 from typing import NamedTuple
 
 import torch
@@ -560,13 +561,13 @@ def decode(q, k_cache, v_cache, lengths, lam: float, tau_s: float = 2.0, *, out=
 # allocated, the current stream) goes through csrc/torch_calls.cpp, which checks, allocates and calls
 # the library in native code (host time of page_plan, cache_append, paged_decode and sample: 8, 8, 9 and
 # 6 us a call, 19, 16, 21 and 14 in Python) and answers None to whatever it does not take; then, and
-# where it is not built, the code here does the same and says what is wrong.
+# where there is none to use, the code here does the same and says what is wrong.
 _I32, _I64, _F32 = torch.int32, torch.int64, torch.float32
 _calls = None
 
 
 class _NoCalls:
-    """Stands for relation_calls.so where it is not built: takes nothing."""
+    """Stands for relation_calls.so where there is none to use: takes nothing."""
 
     @staticmethod
     def page_plan(*_):
@@ -575,22 +576,35 @@ class _NoCalls:
     cache_append = paged_decode = sample = page_plan
 
 
+def _load_calls(lib):
+    """relation_calls.so, bound to the library's functions; _NoCalls where it is not built, and with
+    a warning where it does not load or is not that of these sources and this torch."""
+    from . import build
+
+    if not os.path.exists(CALLS_PATH):
+        return _NoCalls
+    try:
+        if not build.calls_current(CALLS_PATH):
+            raise ImportError("built from other sources or for another torch")
+        loader = importlib.machinery.ExtensionFileLoader("relation_calls", CALLS_PATH)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_loader("relation_calls", loader))
+    except ImportError as e:
+        warnings.warn(f"relation_calls.so is not used ({e}): the serving calls run through Python; "
+                      "paper_2608_20172_gb300.build.build() builds it", RuntimeWarning, stacklevel=4)
+        return _NoCalls
+    m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.relation_page_plan, lib.relation_cache_append, lib.relation_paged_decode,
+        lib.relation_paged_decode_workspace_size, lib.relation_sample)))
+    return m
+
+
 def _native():
-    """relation_calls.so, bound to the library's functions."""
+    """The serving calls in native code."""
     global _calls
     lib = load()
     with _lock:
         if _calls is None:
-            if os.path.exists(CALLS_PATH):
-                loader = importlib.machinery.ExtensionFileLoader("relation_calls", CALLS_PATH)
-                m = importlib.util.module_from_spec(
-                    importlib.util.spec_from_loader("relation_calls", loader))
-                m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-                    lib.relation_page_plan, lib.relation_cache_append, lib.relation_paged_decode,
-                    lib.relation_paged_decode_workspace_size, lib.relation_sample)))
-                _calls = m
-            else:
-                _calls = _NoCalls
+            _calls = _load_calls(lib)
     return _calls
 
 

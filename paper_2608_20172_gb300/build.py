@@ -29,6 +29,7 @@ CALLS = os.path.join(BUILD, "relation_calls.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
               "--expt-relaxed-constexpr", f"-I{INCLUDE}", f"-I{CSRC}"]
+CALLS_FLAGS = ["-O2", "-std=c++17", "-fPIC", "-shared"]
 
 
 def _nvcc() -> str:
@@ -53,43 +54,64 @@ def _deps_digest() -> str:
     return h.hexdigest()
 
 
+def _calls_digest(torch) -> str:
+    """Of what relation_calls.so is made from and for: its sources, this torch and this Python."""
+    h = hashlib.sha256()
+    for f in (os.path.join(CSRC, "torch_calls.cpp"), os.path.join(INCLUDE, "relation.h")):
+        with open(f, "rb") as fh:
+            h.update(fh.read())
+    h.update(f"{torch.__version__} {torch._C._GLIBCXX_USE_CXX11_ABI} {sys.version} "
+             f"{CALLS_FLAGS}".encode())
+    return h.hexdigest()
+
+
+def calls_current(path: str) -> bool:
+    """Whether the relation_calls.so at path was built from these sources for this torch."""
+    import torch
+
+    try:
+        with open(path + ".stamp") as f:
+            return os.path.exists(path) and f.read().strip() == _calls_digest(torch)
+    except OSError:
+        return False
+
+
+def _calls_not_built(why) -> None:
+    """Say so, and leave no file of an earlier build: it is not that of these sources."""
+    print(f"relation_calls.so not built: {why}", file=sys.stderr)
+    for f in (CALLS + ".stamp", CALLS):
+        if os.path.exists(f):
+            os.remove(f)
+
+
 def build_calls(force: bool = False) -> str | None:
     """Compile relation_calls.so; returns its path, None where it cannot be built."""
     try:
         import torch
     except ImportError as e:
-        print(f"relation_calls.so not built: {e}", file=sys.stderr)
-        return None
+        return _calls_not_built(e)
 
-    src = os.path.join(CSRC, "torch_calls.cpp")
+    if not force and calls_current(CALLS):
+        return CALLS
     root = os.path.dirname(torch.__file__)
     cuda = os.path.dirname(os.path.dirname(_nvcc())) or "/usr/local/cuda"
-    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared",
+    tmp = CALLS + f".tmp{os.getpid()}"
+    cmd = ["g++", *CALLS_FLAGS,
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
            f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include",
-           f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}/include", f"-I{INCLUDE}", src,
-           f"-L{root}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
-    h = hashlib.sha256()
-    for f in (src, os.path.join(INCLUDE, "relation.h")):
-        with open(f, "rb") as fh:
-            h.update(fh.read())
-    h.update((" ".join(cmd) + torch.__version__ + sys.version).encode())
-    stamp = CALLS + ".stamp"
-    if not force and os.path.exists(CALLS) and os.path.exists(stamp) and \
-            open(stamp).read().strip() == h.hexdigest():
-        return CALLS
-    tmp = CALLS + f".tmp{os.getpid()}"
+           f"-I{sysconfig.get_paths()['include']}", f"-I{cuda}/include", f"-I{INCLUDE}",
+           os.path.join(CSRC, "torch_calls.cpp"),
+           f"-L{root}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda", "-o", tmp]
+    digest = _calls_digest(torch)
     try:
-        r = subprocess.run(cmd + ["-o", tmp], capture_output=True, text=True)
+        r = subprocess.run(cmd, capture_output=True, text=True)
     except OSError as e:
-        print(f"relation_calls.so not built: {e}", file=sys.stderr)
-        return None
+        return _calls_not_built(e)
     if r.returncode != 0:
-        print(f"relation_calls.so not built:\n{r.stderr}", file=sys.stderr)
-        return None
+        return _calls_not_built(f"\n{r.stderr}")
     os.replace(tmp, CALLS)
-    with open(stamp, "w") as f:
-        f.write(h.hexdigest())
+    with open(CALLS + ".stamp", "w") as f:
+        f.write(digest)
     return CALLS
 
 
