@@ -755,9 +755,17 @@ cudaError_t launch_t(const SampleProblem& p, cudaStream_t s) {
   // As many CTAs per row as the GPU holds at once over all rows (two per SM), but 4096 tokens each and
   // no more than kShort, where there is a choice: what a CTA waits for its cluster costs the same
   // whatever its slice, so that longer slices in one round beat shorter ones in two (64 rows of 50257:
-  // 35 us with 8 CTAs a row, 27 with 4).
+  // 35 us with 8 CTAs a row, 27 with 4).  (Of slices past kShort one CTA fits an SM; they come with
+  // the largest cluster whatever fits.)
+  int dev = 0, nsm = 0;
+  cudaError_t e;
+  if ((e = cudaGetDevice(&dev)) != cudaSuccess ||
+      (e = cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev)) != cudaSuccess) {
+    note_failure("sample: device attributes");
+    return e;
+  }
   auto up = [](int a, int b) { return (a + b - 1) / b; };
-  const int fit = 2 * 152 / p.R, need = up(p.V, kShort - 8), most = up(p.V, 4096);
+  const int fit = 2 * nsm / p.R, need = up(p.V, kShort - 8), most = up(p.V, 4096);
   int cluster = fit < need ? need : fit;
   cluster = cluster < most ? cluster : most;
   cluster = cluster < 1 ? 1 : cluster < kMaxCluster ? cluster : kMaxCluster;
