@@ -559,7 +559,7 @@ def decode(q, k_cache, v_cache, lengths, lam: float, tau_s: float = 2.0, *, out=
 
 # The calls of a serving step are short, so that the host's time counts.  The common call (outputs to be
 # allocated, the current stream) goes through csrc/torch_calls.cpp, which checks, allocates and calls
-# the library in native code (host time of page_plan, cache_append, paged_decode and sample: 8, 8, 9 and
+# the library in native code (host time of page_plan, cache_append, paged_decode and sample: 8, 5, 9 and
 # 6 us a call, 19, 16, 21 and 14 in Python) and answers None to whatever it does not take; then, and
 # where there is none to use, the code here does the same and says what is wrong.
 _I32, _I64, _F32 = torch.int32, torch.int64, torch.float32

@@ -8,17 +8,21 @@
 // where row r of request b lies in row r % page of page table[b][r / page].  G = H / H_kv query heads
 // share a key/value head.
 //
-// Bound by memory: every cached key and value is read once, for all query heads that share it.  The
-// history of all requests and key/value heads is cut into units of kUnit rows, and the units, in the
-// order of requests, heads and rows, into as many equal runs as there are CTAs resident: ragged
-// lengths leave no CTA idle, and nothing is launched for the rows that a table could hold.  A CTA
-// takes its run head by head in one pass: every warp keeps (m, l, z) = (max E, sum e^{E - m},
-// sum e^{E - m} v) over tiles of rows that stay in registers, merged at the head's end.  A head that
-// lies within one run is finished there; of a head that several runs share, each leaves its (m, l, z)
-// in the workspace, the one with its end q . k_self and v_self, and the second launch joins them.
-// Measured, bf16, 32 requests of 1 to 4096 rows, both launches: 8 heads of 128 58 us (80 % of the copy
-// bandwidth), of 64 35, of 80 52, of 128 with 4 query heads each 70; 32 requests to 8192 rows of 16 x
-// 128 193 us (97 %); one request of 2048 rows, 12 x 64, 8 us.
+// Bound by memory: every cached key and value is gone through once for up to eight query heads that
+// share it, and once more for each further eight (32 requests to 4096 rows, 8 key heads of 128 bf16: 8
+// query heads each 68 us, 9 108, 16 114).  The history of all requests and key/value heads is cut into
+// units of kUnit rows, and the units, in the order of requests, heads and rows, into as many equal runs
+// as there are CTAs resident: ragged lengths leave no CTA idle, and nothing is launched for the rows
+// that a table could hold.  A CTA takes its run head by head in one pass: every warp keeps
+// (m, l, z) = (max E, sum e^{E - m}, sum e^{E - m} v) over tiles of rows that stay in registers, merged
+// at the head's end.  A head that lies within one run is finished there; of a head that several runs
+// share, each leaves its (m, l, z) in the workspace, the one with its end q . k_self and v_self, and the
+// second launch joins them.
+// Measured, 32 requests of 1 to 4096 rows, 8 key heads, both launches: bf16 of 128 51 us (81 % of the
+// copy bandwidth), of 64 38, of 80 43, of 128 with 2, 4, 8 query heads each 62, 63, 69; fp32 of 128 with
+// 1, 2, 4, 8 query heads each 93, 99, 146, 205 (90, 84, 57, 41 %: with 8 the products take 20 % of the
+// FMA pipe, and 8 warps an SM, by 246 registers, wait for their loads).  32 requests to 8192 rows of
+// 16 x 128 bf16 188 us (97 %); one request of 2048 rows, 12 x 64, 8 us.
 #include <math.h>
 
 #include "common.cuh"
@@ -90,7 +94,6 @@ __device__ __forceinline__ uint4 load_group(const TI* row, int c, int d) {
 // 2^x by the special function unit (2 ulp), and through it e^x, whose argument's rounding adds
 // |x| 2^-24: the weights e^{E - m} are at most 1 and lose what is far below the largest.
 __device__ __forceinline__ float fast_exp(float x) { return ex2_approx(x * 1.4426950408889634f); }
-// (a denominator past 2^126 gives 0 in place of at most 1e-36)
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -100,6 +103,7 @@ __device__ __forceinline__ void cp_wait() {
   asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
+// (a denominator past 2^126 gives 0 in place of at most 1e-36)
 __device__ __forceinline__ float silu(float u) { return __fdividef(u, 1.0f + fast_exp(-u)); }
 // The running maximum is raised only where a score exceeds it by more than this: weights up to
 // e^kSlack are as exact as those below 1, and a raise touches every accumulator.
@@ -271,7 +275,8 @@ struct Lanes {
   using T = TI;
   static constexpr int GG = GG_;
   static constexpr bool kVec = VEC;
-  static constexpr int kCtas = GG == 1 ? 4 : GG == 2 ? 3 : 2;  // per SM, by the registers
+  // per SM, by the registers (unaligned bf16 with 8 query heads spills 276 to 316 bytes even so)
+  static constexpr int kCtas = GG == 1 ? 4 : GG == 2 ? 3 : 2;
   static constexpr int VE = Vec<TI>::N, RPL = 32 / LPR;
   static constexpr int NI = LPR == 4 ? 4 : 8;  // loads of a tile's keys
   static constexpr int R = RPL * NI;           // rows of a tile
@@ -619,7 +624,8 @@ struct Tensor {
 
 // The key and value of request b's last row into shared memory, by one warp: on their way while the
 // history is summed.  (Read after it, they put two trips to memory at every head's end: 500 requests to
-// 64 rows, 8 x 128 bf16, 42 us, so 37; 256 to 300 rows 48 and 44; 32 to 4096 rows 58 either way.)
+// 64 rows, 8 x 128 bf16, 42 us, so 37; 256 to 300 rows 48 and 44; 32 to 4096 rows 58 either way, in fp32
+// 103 and 105, 8 x 80 80 and 84.)
 template <typename TI, bool VEC>
 __device__ __forceinline__ void fetch_self(const PagedProblem& p, int b, int len, const TI* kb,
                                            const TI* vb, TI (&row)[2][kMaxD], int lane) {
