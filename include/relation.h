@@ -403,6 +403,48 @@ relation_status relation_sample(const void* logits, int R, int V, long long s_ro
                                 relation_stream_t stream);
 
 /*
+ * relation_logprobs: the log probabilities of given tokens, with every row's entropy and its most
+ * likely tokens.  For a row x of logits at temperature T, p_j = exp(x_j / T) / sum_i exp(x_i / T).
+ *   logits      [R][V] in dt, row stride s_row (element alignment), V <= 2^30.  -inf masks a token.
+ *   targets     device int[R]: the given token of every row; negative: none.
+ *   temperature device float[R], > 0, or null (1).
+ *   logprob     device float[R]: log p of the given token (0 where there is none).
+ *   entropy     device float[R]: -sum_j p_j log p_j.
+ *   logz        device float[R]: log sum_j exp(x_j / T).
+ *   top_tokens, top_logprobs : device int / float [R][top], 0 <= top <= 32 (else
+ *               RELATION_ERR_UNSUPPORTED; null where top is 0): the tokens with the largest logits in
+ *               descending order, equal ones by index, and their log p; -1 and -inf where fewer
+ *               tokens are unmasked.
+ * A row without an unmasked token has logz = -inf, entropy 0 and logprob -inf (0 without a given
+ * token); one with a NaN, or with a temperature that is not positive and finite (reported to
+ * dev_status, if given, as RELATION_ERR_INVALID_ARG), NaN in all of them and tokens -1.  A given
+ * token >= V has logprob NaN and is reported likewise.  Logits of +inf share the probability among
+ * them.  Sums in fp32.  Asynchronous on `stream`; one launch; nothing is allocated.
+ */
+relation_status relation_logprobs(const void* logits, int R, int V, long long s_row,
+                                  relation_dtype dt, const int* targets, const float* temperature,
+                                  float* logprob, float* entropy, float* logz, int top,
+                                  int* top_tokens, float* top_logprobs, int* dev_status,
+                                  relation_stream_t stream);
+
+/*
+ * relation_logprobs_grad: the gradient of relation_logprobs's logprob, entropy and logz,
+ *   dlogits_j = (1 / T) (g (delta_jy - p_j) - h p_j (log p_j + entropy) + k p_j)
+ * with y the given token and g, h, k = dlogprob, dentropy, dlogz (device float[R], each may be null:
+ * 0; g counts as 0 in a row without a given token).
+ *   logz, entropy : the forward's for the same logits, targets and temperature.
+ *   dlogits     [R][V] in dt, row stride s_out; it may be the logits (s_out = s_row).
+ * A row whose logz is -inf gets zeros, one whose logz is NaN or whose given token is >= V NaN.
+ * Asynchronous on `stream`; one launch; nothing is allocated.
+ */
+relation_status relation_logprobs_grad(const void* logits, int R, int V, long long s_row,
+                                       relation_dtype dt, const int* targets,
+                                       const float* temperature, const float* logz,
+                                       const float* entropy, const float* dlogprob,
+                                       const float* dentropy, const float* dlogz, void* dlogits,
+                                       long long s_out, relation_stream_t stream);
+
+/*
  * Context parallelism (sequence sharding) of the forward.  The Exchange summary of a query
  * row over a set of history keys is (m, l, z): l = sum_j exp(E_ij - m) and
  * z = sum_j exp(E_ij - m) I~_j over those keys, for any log-scale m (here an upper bound of
@@ -483,6 +525,56 @@ relation_status relation_layer_grad(const void* dq, const void* dk, const void* 
                                     float rope_base, void* dp1, void* dp2, void* dinfo,
                                     float* dtheta, relation_shape shp, relation_dtype dt,
                                     void* workspace, size_t ws_bytes, relation_stream_t stream);
+
+/* A rotation by positions: channel pairs, their frequencies and a factor. */
+typedef struct relation_rotary {
+  const double* freqs; /* device double[d_rot / 2]: radians a position of every pair, finite    */
+  int d_rot;           /* the first d_rot channels are turned (even; 0: none, freqs may be null) */
+  int layout;          /* 0: pairs (2p, 2p + 1); 1: pairs (p, p + d_rot / 2)                     */
+  float scale;         /* the turned channels are multiplied by it (1 for a plain rotation)      */
+} relation_rotary;
+
+/*
+ * relation_norm_rope: queries and keys normed head by head and rotated by their positions in one
+ * pass, for layers that relation_layer_prep's full rotation of RoFormer's pairs does not serve.  A
+ * row x of d_h channels at position m becomes
+ *   n_c = w_c x_c / sqrt(mean x^2 + eps)         (norm = 1; norm = 0: n_c = w_c x_c)
+ *   (n_a, n_b) -> scale (n_a cos - n_b sin, n_a sin + n_b cos)   by the angle m freqs[p], every pair p,
+ * and the channels from d_rot on stay n_c.
+ *   p1, p2 : [B][T][H][d_h] in dt with the strides of shp_q and shp_k, which agree in B, T and d_h and
+ *            may differ in H; q and k have their layouts and may alias them.  p2 and k may both be
+ *            null (shp_k is then not read).
+ *   w1, w2 : device float[d_h], the norms' weights of the queries and the keys; null: 1.
+ *   positions : device int[B T]; null: t in every sequence.  A negative one is padding: zeros.
+ * fp32 or bf16 (arithmetic in fp32, angles as 64-bit parts of a turn at every position), any d_h up to
+ * 256, B T up to 2^30 (else RELATION_ERR_UNSUPPORTED).  Rows whose pointers and strides are multiples
+ * of 16 bytes, with d_h (and, for layout 1, d_rot / 2) made of 16-byte groups, move in such groups,
+ * any others element by element.  With rope_base 0, relation_cache_append takes the result.
+ * Asynchronous on `stream`; one launch; nothing is allocated.
+ */
+relation_status relation_norm_rope(const void* p1, const void* p2, const float* w1, const float* w2,
+                                   int norm, float eps, relation_rotary rotary,
+                                   const int* positions, void* q, void* k, relation_shape shp_q,
+                                   relation_shape shp_k, relation_dtype dt,
+                                   relation_stream_t stream);
+
+/*
+ * Gradient of relation_norm_rope: from dq, dk and the forward's p1, p2 (layouts as there),
+ *   dp1, dp2 : in their layouts; each may alias its dq or p1 (dk or p2).  Zeros for padding.
+ *   dw1, dw2 : device float[d_h], the weights' gradients summed over all rows that are not padding
+ *              (overwritten; in a fixed order, deterministic); each may be null.
+ *   workspace : device scratch of relation_norm_rope_grad_workspace_size(shp_q, dt) bytes, 16-byte
+ *              aligned; may be null where dw1 and dw2 are.
+ * Asynchronous on `stream`; two launches (one without dw1 and dw2).
+ */
+size_t relation_norm_rope_grad_workspace_size(relation_shape shp_q, relation_dtype dt);
+relation_status relation_norm_rope_grad(const void* dq, const void* dk, const void* p1,
+                                        const void* p2, const float* w1, const float* w2, int norm,
+                                        float eps, relation_rotary rotary, const int* positions,
+                                        void* dp1, void* dp2, float* dw1, float* dw2,
+                                        relation_shape shp_q, relation_shape shp_k,
+                                        relation_dtype dt, void* workspace, size_t ws_bytes,
+                                        relation_stream_t stream);
 
 /* Bytes of device workspace relation_bwd needs for this shape and dtype (0 on a bad
  * shape).  The content of the workspace need not be initialised. */

@@ -13,6 +13,7 @@ from __future__ import annotations
 import ctypes
 import importlib.machinery
 import importlib.util
+import math
 import os
 import threading
 import warnings
@@ -44,7 +45,9 @@ EXPORTED = ("relation_fwd", "relation_fwd_ex", "relation_bwd", "relation_bwd_ex"
             "relation_linear_bwd_ex", "relation_linear_bwd_ex_workspace_size", "relation_layer_prep",
             "relation_layer_grad", "relation_layer_grad_workspace_size", "relation_page_plan",
             "relation_cache_append", "relation_paged_decode",
-            "relation_paged_decode_workspace_size", "relation_sample")
+            "relation_paged_decode_workspace_size", "relation_sample", "relation_logprobs",
+            "relation_logprobs_grad", "relation_norm_rope", "relation_norm_rope_grad",
+            "relation_norm_rope_grad_workspace_size")
 
 
 class RelationLibraryMissing(RuntimeError):
@@ -70,6 +73,11 @@ class Pages(ctypes.Structure):
     _fields_ = [("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("H", ctypes.c_int),
                 ("d_h", ctypes.c_int), ("sP", ctypes.c_longlong), ("sR", ctypes.c_longlong),
                 ("sH", ctypes.c_longlong)]
+
+
+class RotaryArgs(ctypes.Structure):
+    _fields_ = [("freqs", ctypes.c_void_p), ("d_rot", ctypes.c_int), ("layout", ctypes.c_int),
+                ("scale", ctypes.c_float)]
 
 
 _lock = threading.Lock()
@@ -128,6 +136,14 @@ def load(path: str | None = None):
         lib.relation_paged_decode_workspace_size.argtypes = [i, Pages, i]
         lib.relation_paged_decode_workspace_size.restype = sz
         lib.relation_sample.argtypes = [vp, i, i, ll, i, vp, vp, vp, vp, vp, vp, vp, vp, ip, vp]
+        lib.relation_logprobs.argtypes = [vp, i, i, ll, i, vp, vp, vp, vp, vp, i, vp, vp, ip, vp]
+        lib.relation_logprobs_grad.argtypes = [vp, i, i, ll, i, vp, vp, vp, vp, vp, vp, vp, vp, ll, vp]
+        lib.relation_norm_rope.argtypes = [vp, vp, vp, vp, i, f, RotaryArgs, vp, vp, vp, Shape, Shape, i,
+                                           vp]
+        lib.relation_norm_rope_grad.argtypes = [vp, vp, vp, vp, vp, vp, i, f, RotaryArgs, vp, vp, vp, vp,
+                                                vp, Shape, Shape, i, vp, sz, vp]
+        lib.relation_norm_rope_grad_workspace_size.argtypes = [Shape, i]
+        lib.relation_norm_rope_grad_workspace_size.restype = sz
         lib.relation_linear_bwd_workspace_size.restype = ctypes.c_size_t
         lib.relation_decode_workspace_size.restype = ctypes.c_size_t
         lib.relation_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, f, f, Shape, i, vp,
@@ -523,6 +539,137 @@ def layer_grad(dq, dk, dv, info, theta, pairing: int = 0, rope_base: float = 1.0
     return dp1, dp2, dinfo, dtheta
 
 
+class Rotary(NamedTuple):
+    """A rotation by positions (relation_rotary); ``rotary`` makes the usual ones."""
+    freqs: torch.Tensor | None   # float64 [d_rot / 2]: radians a position of every pair; None: no rotation
+    layout: str = "interleaved"  # pairs (2p, 2p + 1), or "half": (p, p + d_rot / 2)
+    scale: float = 1.0           # the turned channels are multiplied by it
+
+
+LAYOUTS = {"interleaved": 0, "half": 1}
+
+
+def rotary(d_rot: int, base: float = 1.0e4, *, layout: str = "interleaved", scaling: str = "none",
+           factor: float = 1.0, context: int = 0, device="cuda") -> Rotary:
+    """The rotation of the first d_rot channels with frequencies base^(-2p/d_rot), scaled from a
+    ``context`` that a model has seen to one ``factor`` times as long:
+      "linear"  every frequency divided by the factor,
+      "ntk"     the base raised so that the slowest pair is, and the fastest stays,
+      "yarn"    pairs that turn less than once in the context divided, those that turn more than 32
+                times as they are, between them in proportion (Peng et al., arXiv 2309.00071), and
+                scale 1 + 0.1 ln(factor)."""
+    if d_rot < 2 or d_rot % 2 or not base > 0 or not factor >= 1 or layout not in LAYOUTS:
+        raise ValueError("d_rot must be even and positive, base positive, factor at least 1 and layout "
+                         "'interleaved' or 'half'")
+    p = torch.arange(0, d_rot, 2, dtype=torch.float64) / d_rot
+    scale = 1.0
+    if scaling == "ntk":
+        if d_rot == 2:
+            raise ValueError("ntk needs two pairs at least")
+        base = base * factor ** (d_rot / (d_rot - 2))
+    f = torch.exp(p * -math.log(base))
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "yarn":
+        if context < 1:
+            raise ValueError("yarn needs the context that the model has seen")
+        keep = ((context * f / (2 * math.pi) - 1) / 31).clamp(0, 1)
+        f = f * keep + f / factor * (1 - keep)
+        scale = 1.0 + 0.1 * math.log(factor)
+    elif scaling not in ("none", "ntk"):
+        raise ValueError("scaling must be 'none', 'linear', 'ntk' or 'yarn'")
+    return Rotary(f.to(device), layout, scale)
+
+
+def _head_rows(t) -> Shape:
+    """relation_shape of [B, T, H, d] or of tokens [N, H, d], d contiguous."""
+    shape, st = t.shape, t.stride()
+    if len(shape) not in (3, 4) or st[-1] != 1 or t.get_device() < 0:
+        raise ValueError("expected a CUDA [B, T, H, d] or [N, H, d] tensor with d contiguous")
+    return Shape(1, *shape, 1, *st[:2]) if len(shape) == 3 else Shape(*shape, *st[:3])
+
+
+def _norm_rope_args(p1, p2, rot, positions, w1, w2, others):
+    """The device, the shapes and the rotation of a norm_rope call; others: (tensor, the input that it
+    has to be like)."""
+    dev, shp = p1.get_device(), _head_rows(p1)
+    shk = Shape(0, 0, 0, 0, 0, 0, 0) if p2 is None else _head_rows(p2)
+    if p2 is not None and (p2.dtype is not p1.dtype or p2.get_device() != dev or
+                           p2.dim() != p1.dim() or p2.shape[:-2] != p1.shape[:-2] or
+                           p2.shape[-1] != p1.shape[-1]):
+        raise ValueError("p1 and p2 may differ in the number of heads alone, not in dtype or device")
+    for t, like in others:
+        if t.shape != like.shape or t.stride() != like.stride() or t.dtype is not like.dtype or \
+                t.get_device() != dev:
+            raise ValueError("outputs and gradients need their input's shape, strides, dtype and device")
+    for w in (w1, w2):
+        if w is not None:
+            _need("w1 and w2", w, dev, _F32, p1.shape[-1])
+    if positions is not None:
+        _need("positions", positions, dev, _I32, shp.B * shp.T)
+    if rot is None or rot.freqs is None:
+        return dev, shp, shk, RotaryArgs(None, 0, 0, 1.0)
+    _need("rotary.freqs", rot.freqs, dev, torch.float64, rot.freqs.numel())
+    if rot.layout not in LAYOUTS:
+        raise ValueError("rotary.layout must be 'interleaved' or 'half'")
+    return dev, shp, shk, RotaryArgs(rot.freqs.data_ptr(), 2 * rot.freqs.numel(), LAYOUTS[rot.layout],
+                                     float(rot.scale))
+
+
+def norm_rope(p1, p2, rotary: Rotary | None, positions=None, w1=None, w2=None, *, norm: bool = True,
+              eps: float = 1.0e-6, out=None, stream=None):
+    """Queries and keys normed per head (RMS, weights w1 and w2 fp32 [d] or None) and rotated by their
+    positions: returns (q, k) for p1 [B, T, H, d] or [N, H, d] and p2 likewise with heads of its own
+    (None: k is None).  positions int32, one a token (None: 0 .. T - 1 in every sequence); negative:
+    padding, zeros.  ``norm=False``: the rotation (and the weights) alone.  See relation_norm_rope."""
+    if out is None:
+        q, k = _like(p1, stream), None if p2 is None else _like(p2, stream)
+    else:
+        q, k = out
+        if (k is None) != (p2 is None):
+            raise ValueError("out must be (q, k) with k None where p2 is")
+    dev, shp, shk, rot = _norm_rope_args(p1, p2, rotary, positions, w1, w2,
+                                         [(q, p1)] + ([] if p2 is None else [(k, p2)]))
+    rc = load().relation_norm_rope(p1.data_ptr(), _ptr(p2), _ptr(w1), _ptr(w2), int(norm), float(eps), rot,
+                                   _ptr(positions), q.data_ptr(), _ptr(k), shp, shk, _dtype_code(p1),
+                                   _queue(stream, dev))
+    if rc != OK:
+        raise RelationError(rc, "relation_norm_rope")
+    return q, k
+
+
+def norm_rope_grad_workspace_size(p1) -> int:
+    """Device bytes norm_rope_grad needs for queries p1 [B, T, H, d] or [N, H, d]."""
+    return int(load().relation_norm_rope_grad_workspace_size(_head_rows(p1), _dtype_code(p1)))
+
+
+def norm_rope_grad(dq, dk, p1, p2, rotary: Rotary | None, positions=None, w1=None, w2=None, *,
+                   norm: bool = True, eps: float = 1.0e-6, weights: bool = True, workspace=None,
+                   stream=None):
+    """Gradient of norm_rope: returns (dp1, dp2, dw1, dw2) from dq and dk (laid out like p1 and p2);
+    dp2 and dw2 are None where p2 is, dw1 and dw2 with ``weights=False``."""
+    if (dk is None) != (p2 is None):
+        raise ValueError("dk and p2 belong together")
+    dp1, dp2 = _like(p1, stream), None if p2 is None else _like(p2, stream)
+    dev, shp, shk, rot = _norm_rope_args(p1, p2, rotary, positions, w1, w2,
+                                         [(dq, p1)] + ([] if p2 is None else [(dk, p2)]))
+    d, lib = p1.shape[-1], load()
+    dw1 = _new(d, _F32, p1.device, stream) if weights else None
+    dw2 = _new(d, _F32, p1.device, stream) if weights and p2 is not None else None
+    if weights and workspace is None:
+        workspace = _scratch(lib.relation_norm_rope_grad_workspace_size(shp, _dtype_code(p1)), p1.device,
+                             stream)
+    rc = lib.relation_norm_rope_grad(dq.data_ptr(), _ptr(dk), p1.data_ptr(), _ptr(p2), _ptr(w1), _ptr(w2),
+                                     int(norm), float(eps), rot, _ptr(positions), dp1.data_ptr(),
+                                     _ptr(dp2), _ptr(dw1), _ptr(dw2), shp, shk, _dtype_code(p1),
+                                     _ptr(workspace),
+                                     0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                     _queue(stream, dev))
+    if rc != OK:
+        raise RelationError(rc, "relation_norm_rope_grad")
+    return dp1, dp2, dw1, dw2
+
+
 def decode_workspace_size(k_cache) -> int:
     """Device bytes relation_decode needs for a [B, T, H, d] cache of this dtype."""
     return int(load().relation_decode_workspace_size(shape_of(k_cache), _dtype_code(k_cache)))
@@ -816,6 +963,79 @@ def sample(logits, u, *, temperature=None, top_k=None, top_p=None, min_p=None, o
     return out
 
 
+class Logprobs(NamedTuple):
+    """What logprobs returns; the last two are None where no alternatives were asked for."""
+    logprob: torch.Tensor               # fp32 [R]: of the given token, 0 where there is none
+    entropy: torch.Tensor               # fp32 [R]
+    logz: torch.Tensor                  # fp32 [R]: log of the sum of exp(logits / temperature)
+    top_tokens: torch.Tensor | None     # int32 [R, top]: the most likely tokens, -1 past the unmasked
+    top_logprobs: torch.Tensor | None   # fp32 [R, top]
+
+
+def _logit_rows(logits):
+    """(R, V, row stride) of logits [R, V]."""
+    if logits.dim() != 2 or logits.stride(1) != 1 or logits.get_device() < 0:
+        raise ValueError("logits must be a CUDA [R, V] tensor with contiguous rows")
+    return (*logits.shape, logits.stride(0))
+
+
+def logprobs(logits, targets, *, temperature=None, top: int = 0, out: Logprobs | None = None,
+             dev_status=None, stream=None) -> Logprobs:
+    """Log probabilities of given tokens, the rows' entropies and their ``top`` most likely tokens:
+    logits [R, V] (fp32 or bf16, rows may be strided), targets int32 [R] (negative: none), temperature
+    fp32 [R] or None.  See relation_logprobs."""
+    dev, dt, (R, V, st), top = logits.get_device(), _dtype_code(logits), _logit_rows(logits), int(top)
+    _need("targets", targets, dev, _I32, R)
+    if temperature is not None:
+        _need("temperature", temperature, dev, _F32, R)
+    if out is None:
+        on = logits.device
+        logprob, entropy, logz = (_new(R, _F32, on, stream) for _ in range(3))
+        tokens = _new((R, top), _I32, on, stream) if top > 0 else None
+        out = Logprobs(logprob, entropy, logz, tokens,
+                       _new((R, top), _F32, on, stream) if top > 0 else None)
+    else:
+        for name, t in zip(out._fields[:3], out):
+            _need(f"out.{name}", t, dev, _F32, R)
+        if top > 0:
+            _need("out.top_tokens", out.top_tokens, dev, _I32, R * top)
+            _need("out.top_logprobs", out.top_logprobs, dev, _F32, R * top)
+    rc = load().relation_logprobs(logits.data_ptr(), R, V, st, dt, targets.data_ptr(), _ptr(temperature),
+                                  out.logprob.data_ptr(), out.entropy.data_ptr(), out.logz.data_ptr(),
+                                  top, _ptr(out.top_tokens), _ptr(out.top_logprobs),
+                                  _status(dev_status, dev), _queue(stream, dev))
+    if rc != OK:
+        raise RelationError(rc, "relation_logprobs")
+    return out
+
+
+def logprobs_grad(logits, targets, logz, entropy, dlogprob=None, dentropy=None, dlogz=None, *,
+                  temperature=None, out=None, stream=None):
+    """Gradient of logprobs's logprob, entropy and logz with respect to the logits: dlogits [R, V] in
+    their dtype, from the forward's logz and entropy and the gradients fp32 [R] (None: 0).  ``out`` may be
+    the logits."""
+    dev, dt, (R, V, st) = logits.get_device(), _dtype_code(logits), _logit_rows(logits)
+    _need("targets", targets, dev, _I32, R)
+    for name, t in (("logz", logz), ("entropy", entropy)):
+        _need(name, t, dev, _F32, R)
+    for name, t in (("dlogprob", dlogprob), ("dentropy", dentropy), ("dlogz", dlogz),
+                    ("temperature", temperature)):
+        if t is not None:
+            _need(name, t, dev, _F32, R)
+    if out is None:
+        out = _like(logits, stream)
+    elif out.shape != logits.shape or out.stride(1) != 1 or out.dtype is not logits.dtype or \
+            out.get_device() != dev:
+        raise ValueError("out must be [R, V] with contiguous rows, of the logits' dtype and device")
+    rc = load().relation_logprobs_grad(logits.data_ptr(), R, V, st, dt, targets.data_ptr(),
+                                       _ptr(temperature), logz.data_ptr(), entropy.data_ptr(),
+                                       _ptr(dlogprob), _ptr(dentropy), _ptr(dlogz), out.data_ptr(),
+                                       out.stride(0), _queue(stream, dev))
+    if rc != OK:
+        raise RelationError(rc, "relation_logprobs_grad")
+    return out
+
+
 BWD_PREPARE, BWD_TILES, BWD_FINALIZE, BWD_ALL = 1, 2, 4, 7
 
 
@@ -894,3 +1114,41 @@ class RelationFunction(torch.autograd.Function):
             dy = _like(q).copy_(dy)
         dq, dk, dv, dl = bwd(q, k, v, y, dy, logz, ctx.lam, ctx.tau_s, kernel=ctx.kernel)
         return dq, dk, dv, dl.reshape(()).to(torch.float32), None, None
+
+
+class NormRopeFunction(torch.autograd.Function):
+    """Autograd wrapper of norm_rope: (q, k) = f(p1, p2, w1, w2); w1 and w2 may be None."""
+
+    @staticmethod
+    def forward(ctx, p1, p2, w1, w2, rotary, positions=None, norm=True, eps=1.0e-6):
+        q, k = norm_rope(p1, p2, rotary, positions, w1, w2, norm=norm, eps=eps)
+        freqs = None if rotary is None else rotary.freqs
+        ctx.save_for_backward(p1, p2, w1, w2, freqs, positions)
+        ctx.rotary, ctx.norm, ctx.eps = None if rotary is None else rotary[1:], norm, eps
+        return q, k
+
+    @staticmethod
+    def backward(ctx, dq, dk):
+        p1, p2, w1, w2, freqs, positions = ctx.saved_tensors
+        rot = None if ctx.rotary is None else Rotary(freqs, *ctx.rotary)
+        dq, dk = (None if g is None else g if g.stride() == x.stride() and g.dtype == x.dtype
+                  else _like(x).copy_(g) for g, x in ((dq, p1), (dk if p2 is not None else None, p2)))
+        dp1, dp2, dw1, dw2 = norm_rope_grad(dq, dk, p1, p2, rot, positions, w1, w2, norm=ctx.norm,
+                                            eps=ctx.eps, weights=w1 is not None or w2 is not None)
+        return dp1, dp2, None if w1 is None else dw1, None if w2 is None else dw2, None, None, None, None
+
+
+class LogprobsFunction(torch.autograd.Function):
+    """Autograd wrapper of logprobs: (logprob, entropy, logz) = f(logits) for given targets."""
+
+    @staticmethod
+    def forward(ctx, logits, targets, temperature=None):
+        r = logprobs(logits, targets, temperature=temperature)
+        ctx.save_for_backward(logits, targets, temperature, r.logz, r.entropy)
+        return r.logprob, r.entropy, r.logz
+
+    @staticmethod
+    def backward(ctx, dlogprob, dentropy, dlogz):
+        logits, targets, temperature, logz, entropy = ctx.saved_tensors
+        g = (x.contiguous() for x in (dlogprob, dentropy, dlogz))
+        return logprobs_grad(logits, targets, logz, entropy, *g, temperature=temperature), None, None

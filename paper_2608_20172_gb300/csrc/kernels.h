@@ -315,6 +315,60 @@ struct SampleProblem {
 int sample_max_vocabulary();
 cudaError_t launch_sample(const SampleProblem& p, cudaStream_t s);
 
+// Queries and keys normed per head and rotated, and the gradient (relation_norm_rope.cu):
+// relation_norm_rope's and relation_norm_rope_grad's arguments; [0] the queries, [1] the keys.
+struct NormRopeProblem {
+  const void* in[2];    // P1, P2: [B][T][H][d]; [1] may be null (H[1] = 0)
+  const void* dout[2];  // grad: dQ, dK (null forward)
+  void* out[2];         // Q, K, or dP1, dP2
+  const float* w[2];    // [d], nullable
+  float* dw[2];         // grad: [d], nullable
+  float* part;          // grad: partial sums (null: no dw)
+  const double* freqs;  // [d_rot / 2] radians a position
+  const int* positions; // [B T], nullable
+  float scale, eps;
+  int norm, half, d_rot;
+  int B, T, d, H[2];
+  long long sB[2], sT[2], sH[2];
+  relation_dtype dtype;
+};
+size_t norm_rope_grad_workspace_bytes(int tokens, int d);
+cudaError_t launch_norm_rope(const NormRopeProblem& p, bool grad, cudaStream_t s);
+
+// Log probabilities of given tokens, and the logits' gradient (relation_logprobs.cu):
+// relation_logprobs's and relation_logprobs_grad's arguments.
+struct LogprobsProblem {
+  const void* logits;        // [R][V], row stride s_row
+  const int* targets;        // [R]
+  const float* temperature;  // [R], nullable
+  float* logprob;            // [R]
+  float* entropy;
+  float* logz;
+  int* top_tokens;           // [R][top]
+  float* top_logprobs;
+  int* dev_status;
+  int R, V, top;
+  long long s_row;
+  relation_dtype dtype;
+};
+struct LogprobsGradProblem {
+  const void* logits;        // [R][V], row stride s_row
+  const int* targets;        // [R]
+  const float* temperature;  // [R], nullable
+  const float* logz;         // [R] each: the forward's,
+  const float* entropy;
+  const float* dlogprob;     // and their gradients, nullable
+  const float* dentropy;
+  const float* dlogz;
+  void* dlogits;             // [R][V], row stride s_out
+  int R, V;
+  long long s_row, s_out;
+  relation_dtype dtype;
+};
+int logprobs_max_top();
+cudaError_t launch_logprobs(const LogprobsProblem& p, cudaStream_t s);
+cudaError_t launch_logprobs_grad(const LogprobsGradProblem& p, cudaStream_t s);
+
 cudaError_t launch_selftest_wait(int* dev_status, int timeout_us, cudaStream_t s);
 
 // Where the last failing CUDA step of this thread happened (reported by

@@ -589,6 +589,137 @@ relation_status relation_sample(const void* logits, int R, int V, long long s_ro
   return from_cuda(rel::launch_sample(p, reinterpret_cast<cudaStream_t>(stream)));
 }
 
+relation_status relation_logprobs(const void* logits, int R, int V, long long s_row,
+                                  relation_dtype dt, const int* targets, const float* temperature,
+                                  float* logprob, float* entropy, float* logz, int top,
+                                  int* top_tokens, float* top_logprobs, int* dev_status,
+                                  relation_stream_t stream) {
+  relation_status st;
+  if (dt != RELATION_F32 && dt != RELATION_BF16) return RELATION_ERR_INVALID_ARG;
+  if (R < 1 || V < 1 || (R > 1 && s_row < V) || top < 0) return RELATION_ERR_INVALID_ARG;
+  if ((st = check_elements({logits}, elem_size(dt))) != RELATION_OK) return st;
+  if ((st = check_elements({targets, logprob, entropy, logz}, 4)) != RELATION_OK) return st;
+  if (top > 0 && (st = check_elements({top_tokens, top_logprobs}, 4)) != RELATION_OK) return st;
+  for (const void* x : {(const void*)temperature, (const void*)dev_status})
+    if (reinterpret_cast<uintptr_t>(x) & 3u) return RELATION_ERR_ALIGNMENT;
+  if (top > rel::logprobs_max_top() || V > (1 << 30) || R > (1 << 27)) return RELATION_ERR_UNSUPPORTED;
+  rel::LogprobsProblem p{};
+  p.logits = logits; p.targets = targets; p.temperature = temperature; p.logprob = logprob;
+  p.entropy = entropy; p.logz = logz; p.top_tokens = top_tokens; p.top_logprobs = top_logprobs;
+  p.dev_status = dev_status; p.R = R; p.V = V; p.top = top; p.s_row = s_row; p.dtype = dt;
+  return from_cuda(rel::launch_logprobs(p, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+relation_status relation_logprobs_grad(const void* logits, int R, int V, long long s_row,
+                                       relation_dtype dt, const int* targets,
+                                       const float* temperature, const float* logz,
+                                       const float* entropy, const float* dlogprob,
+                                       const float* dentropy, const float* dlogz, void* dlogits,
+                                       long long s_out, relation_stream_t stream) {
+  relation_status st;
+  if (dt != RELATION_F32 && dt != RELATION_BF16) return RELATION_ERR_INVALID_ARG;
+  if (R < 1 || V < 1 || (R > 1 && (s_row < V || s_out < V))) return RELATION_ERR_INVALID_ARG;
+  if ((st = check_elements({logits, dlogits}, elem_size(dt))) != RELATION_OK) return st;
+  if (dlogits == logits && R > 1 && s_out != s_row) return RELATION_ERR_INVALID_ARG;
+  if ((st = check_elements({targets, logz, entropy}, 4)) != RELATION_OK) return st;
+  for (const void* x : {(const void*)temperature, (const void*)dlogprob, (const void*)dentropy,
+                        (const void*)dlogz})
+    if (reinterpret_cast<uintptr_t>(x) & 3u) return RELATION_ERR_ALIGNMENT;
+  // (a CTA takes at least 4096 elements of a row)
+  if (V > (1 << 30) || (long long)R * (V / 4096 + 2) > 0x7fffffffLL) return RELATION_ERR_UNSUPPORTED;
+  rel::LogprobsGradProblem p{};
+  p.logits = logits; p.targets = targets; p.temperature = temperature; p.logz = logz;
+  p.entropy = entropy; p.dlogprob = dlogprob; p.dentropy = dentropy; p.dlogz = dlogz;
+  p.dlogits = dlogits; p.R = R; p.V = V; p.s_row = s_row; p.s_out = s_out; p.dtype = dt;
+  return from_cuda(rel::launch_logprobs_grad(p, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+namespace {
+
+// The arguments that relation_norm_rope and its gradient share; p is filled from them
+relation_status norm_rope_problem(const void* p1, const void* p2, const float* w1, const float* w2, int norm,
+                                  float eps, const relation_rotary& rot, const int* positions,
+                                  const relation_shape& sq, const relation_shape& sk, relation_dtype dt,
+                                  rel::NormRopeProblem* p) {
+  relation_status st;
+  if (dt != RELATION_F32 && dt != RELATION_BF16) return RELATION_ERR_INVALID_ARG;
+  if ((norm != 0 && norm != 1) || (rot.layout != 0 && rot.layout != 1)) return RELATION_ERR_INVALID_ARG;
+  if (!isfinite(eps) || eps < 0.0f || !isfinite(rot.scale)) return RELATION_ERR_INVALID_ARG;
+  if (sq.B < 1 || sq.T < 1 || sq.H < 1 || sq.d_h < 1 || sq.sB < 1 || sq.sT < 1 || sq.sH < 1)
+    return RELATION_ERR_INVALID_ARG;
+  if (p2 && (sk.B != sq.B || sk.T != sq.T || sk.d_h != sq.d_h || sk.H < 1 || sk.sB < 1 || sk.sT < 1 ||
+             sk.sH < 1))
+    return RELATION_ERR_INVALID_ARG;
+  if (rot.d_rot < 0 || rot.d_rot > sq.d_h || rot.d_rot % 2) return RELATION_ERR_INVALID_ARG;
+  if (rot.d_rot > 0 && (st = check_elements({rot.freqs}, 8)) != RELATION_OK) return st;
+  if ((st = check_elements({p1}, elem_size(dt))) != RELATION_OK) return st;
+  for (const void* x : {(const void*)w1, (const void*)w2, (const void*)positions})
+    if (reinterpret_cast<uintptr_t>(x) & 3u) return RELATION_ERR_ALIGNMENT;
+  if (sq.d_h > 256 || (long long)sq.B * sq.T > (1 << 30)) return RELATION_ERR_UNSUPPORTED;
+  // (a CTA's rows are counted in 32 bits)
+  if ((long long)sq.H + (p2 ? sk.H : 0) > (1 << 24)) return RELATION_ERR_UNSUPPORTED;
+  p->in[0] = p1; p->in[1] = p2; p->w[0] = w1; p->w[1] = w2;
+  p->freqs = rot.freqs; p->d_rot = rot.d_rot; p->half = rot.layout; p->scale = rot.scale;
+  p->positions = positions; p->eps = eps; p->norm = norm;
+  p->B = sq.B; p->T = sq.T; p->d = sq.d_h; p->dtype = dt;
+  p->H[0] = sq.H; p->sB[0] = sq.sB; p->sT[0] = sq.sT; p->sH[0] = sq.sH;
+  if (p2) {
+    p->H[1] = sk.H; p->sB[1] = sk.sB; p->sT[1] = sk.sT; p->sH[1] = sk.sH;
+  }
+  return RELATION_OK;
+}
+
+}  // namespace
+
+relation_status relation_norm_rope(const void* p1, const void* p2, const float* w1, const float* w2,
+                                   int norm, float eps, relation_rotary rotary,
+                                   const int* positions, void* q, void* k, relation_shape shp_q,
+                                   relation_shape shp_k, relation_dtype dt,
+                                   relation_stream_t stream) {
+  relation_status st;
+  rel::NormRopeProblem p{};
+  if ((p2 == nullptr) != (k == nullptr)) return RELATION_ERR_INVALID_ARG;
+  if ((st = norm_rope_problem(p1, p2, w1, w2, norm, eps, rotary, positions, shp_q, shp_k, dt, &p)) != RELATION_OK)
+    return st;
+  if ((st = check_elements({q}, elem_size(dt))) != RELATION_OK) return st;
+  if (p2 && (st = check_elements({p2, k}, elem_size(dt))) != RELATION_OK) return st;
+  p.out[0] = q; p.out[1] = k;
+  return from_cuda(rel::launch_norm_rope(p, false, reinterpret_cast<cudaStream_t>(stream)));
+}
+
+size_t relation_norm_rope_grad_workspace_size(relation_shape shp, relation_dtype dt) {
+  if (dt != RELATION_F32 && dt != RELATION_BF16) return 0;
+  if (shp.B < 1 || shp.T < 1 || shp.d_h < 1 || shp.d_h > 256 || (long long)shp.B * shp.T > (1 << 30)) return 0;
+  return rel::norm_rope_grad_workspace_bytes(shp.B * shp.T, shp.d_h);
+}
+
+relation_status relation_norm_rope_grad(const void* dq, const void* dk, const void* p1,
+                                        const void* p2, const float* w1, const float* w2, int norm,
+                                        float eps, relation_rotary rotary, const int* positions,
+                                        void* dp1, void* dp2, float* dw1, float* dw2,
+                                        relation_shape shp_q, relation_shape shp_k,
+                                        relation_dtype dt, void* workspace, size_t ws_bytes,
+                                        relation_stream_t stream) {
+  relation_status st;
+  rel::NormRopeProblem p{};
+  if ((p2 == nullptr) != (dk == nullptr) || (p2 == nullptr) != (dp2 == nullptr) || (!p2 && dw2))
+    return RELATION_ERR_INVALID_ARG;
+  if ((st = norm_rope_problem(p1, p2, w1, w2, norm, eps, rotary, positions, shp_q, shp_k, dt, &p)) != RELATION_OK)
+    return st;
+  if ((st = check_elements({dq, dp1}, elem_size(dt))) != RELATION_OK) return st;
+  if (p2 && (st = check_elements({dk, p2, dp2}, elem_size(dt))) != RELATION_OK) return st;
+  for (const void* x : {(const void*)dw1, (const void*)dw2})
+    if (reinterpret_cast<uintptr_t>(x) & 3u) return RELATION_ERR_ALIGNMENT;
+  if (dw1 || dw2) {
+    if (!workspace || ws_bytes < rel::norm_rope_grad_workspace_bytes(p.B * p.T, p.d))
+      return RELATION_ERR_WORKSPACE;
+    if (!aligned16(workspace)) return RELATION_ERR_ALIGNMENT;
+    p.part = static_cast<float*>(workspace);
+  }
+  p.dout[0] = dq; p.dout[1] = dk; p.out[0] = dp1; p.out[1] = dp2; p.dw[0] = dw1; p.dw[1] = dw2;
+  return from_cuda(rel::launch_norm_rope(p, true, reinterpret_cast<cudaStream_t>(stream)));
+}
+
 size_t relation_bwd_workspace_size(relation_shape shp, relation_dtype dt) {
   if (check_shape(shp, dt) != RELATION_OK) return 0;
   return rel::bwd_workspace_bytes(shp.B, shp.H, shp.T, shp.d_h);

@@ -1,0 +1,496 @@
+// relation_logprobs.cu -- log probabilities of given tokens, the rows' entropies and top alternatives,
+// and the logits' gradient.
+//
+// A row x_0 .. x_{V-1} at temperature T, M = max x, t_j = (x_j - M) / T:
+//   l = sum e^{t_j},  logZ = M / T + log l,  log p_j = t_j - log l,
+//   H = -sum p_j log p_j = log l - sum t_j e^{t_j} / l.
+// M, l and sum t e^t are taken in one pass: every thread keeps the three of its own elements, and two
+// such triples join by t' = t - (M' - M) / T:  l' = l f,  (sum)' = f (sum - l (M' - M) / T),
+// f = e^{-(M' - M) / T}.
+// The K largest: every thread's maximum is known after the pass.  With W whole warps at work, the least
+// over them of a warp's ceil(K / W)-th largest maximum of a lane is reached by at least K elements, so only
+// lanes whose maximum is not below it can hold one of the K; their warp goes through these lanes' elements
+// again (from L2: a few hundred elements of a row in place of all) and keeps its K largest in a sorted
+// list, one per lane.  The lists' elements are ranked against each other.
+// Gradient, of g log p_y + h H + k logZ:
+//   dx_j = (1 / T) (g (delta_jy - p_j) - h p_j (log p_j + H) + k p_j).
+//
+// Bound by memory: the logits are read once (gradient: and written).  Few rows are shared by clusters
+// of CTAs that join through distributed shared memory.
+#include <math.h>
+
+#include "common.cuh"
+#include "kernels.h"
+
+namespace rel {
+namespace logprobs {
+
+using u64 = unsigned long long;
+
+constexpr int kThreads = 512, kWarps = kThreads / 32;
+constexpr int kMaxTop = 32;
+constexpr int kMaxCluster = 8;
+
+template <typename TI>
+struct Vec;
+template <>
+struct Vec<float> {
+  static constexpr int N = 4;
+  static __device__ __forceinline__ void unpack(const uint4& w, float (&x)[4]) {
+    x[0] = __uint_as_float(w.x); x[1] = __uint_as_float(w.y);
+    x[2] = __uint_as_float(w.z); x[3] = __uint_as_float(w.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]),
+                      __float_as_uint(x[3]));
+  }
+};
+template <>
+struct Vec<__nv_bfloat16> {
+  static constexpr int N = 8;
+  static __device__ __forceinline__ void unpack(const uint4& w, float (&x)[8]) {
+    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(u[i] << 16);
+      x[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    return make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]),
+                      pack_bf16x2(x[6], x[7]));
+  }
+};
+
+// A row in groups of 16 aligned bytes: group g holds elements g N - off .. + N - 1, the first and the
+// last group in part.
+template <typename TI>
+struct Row {
+  static constexpr int N = Vec<TI>::N;
+  const TI* x;
+  int V, off, groups;
+  __device__ __forceinline__ Row(const TI* row, int V_) : x(row), V(V_) {
+    off = (int)(reinterpret_cast<uintptr_t>(row) % 16 / sizeof(TI));
+    groups = (V + off + N - 1) / N;
+  }
+  __device__ __forceinline__ bool whole(int g) const { return g * N >= off && g * N - off + N <= V; }
+  __device__ __forceinline__ uint4 raw(int g) const {
+    return *reinterpret_cast<const uint4*>(x + (g * N - off));
+  }
+  // the group's elements, -inf outside the row
+  __device__ __forceinline__ void load(int g, float (&v)[N]) const {
+    if (whole(g)) {
+      Vec<TI>::unpack(raw(g), v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const int c = g * N - off + j;
+        v[j] = c >= 0 && c < V ? (float)x[c] : -INFINITY;
+      }
+    }
+  }
+};
+
+// max, sum of e^t, sum of t e^t in units of log 2 (t log2 e)
+struct Sums {
+  float m = -INFINITY, l = 0.f, s = 0.f;
+  // to the scale of a maximum that is not below this one's
+  __device__ __forceinline__ void raise(float to, float k2) {
+    const float d = (m - to) * k2, f = ex2_approx(d);
+    if (m == -INFINITY) {  // (nothing yet, or a NaN)
+      m = to;
+      return;
+    }
+    s = f > 0.f ? f * fmaf(l, d, s) : 0.f;
+    l *= f;
+    m = to;
+  }
+  __device__ __forceinline__ void join(float m2, float l2, float s2, float k2) {
+    Sums o;
+    o.m = m2; o.l = l2; o.s = s2;
+    const float to = fmaxf(m, m2);
+    if (to == -INFINITY) {
+      l += l2;
+      return;
+    }
+    raise(to, k2);
+    o.raise(to, k2);
+    l += o.l;
+    s += o.s;
+  }
+};
+
+// Keys that order elements by value, the largest first, equal ones by index (0: none).  -0 is 0.
+__device__ __forceinline__ unsigned ordered(float x) {
+  const unsigned u = __float_as_uint(x + 0.f);
+  return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ __forceinline__ float value_of(unsigned o) {
+  return __uint_as_float(o & 0x80000000u ? o & 0x7fffffffu : ~o);
+}
+__device__ __forceinline__ u64 key_of(float x, int i) { return (u64)ordered(x) << 32 | (unsigned)~i; }
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::
+                   : "memory");
+}
+__device__ __forceinline__ uint32_t peer(const void* p, uint32_t rank) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_u32(p)), "r"(rank));
+  return r;
+}
+__device__ __forceinline__ float peer_f(uint32_t a) {
+  float v;
+  asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+  return v;
+}
+__device__ __forceinline__ u64 peer_u64(uint32_t a) {
+  u64 v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(a) : "memory");
+  return v;
+}
+
+struct Smem {
+  float m[kWarps], l[kWarps], s[kWarps];
+  float cm, cl, cs;          // this CTA's
+  unsigned low[kWarps];      // a warp's bound for the K largest
+  int n;                     // keys in `list`
+  u64 list[kMaxCluster * kMaxTop > kWarps * kMaxTop ? kMaxCluster * kMaxTop : kWarps * kMaxTop];
+  u64 best[kMaxTop];         // this CTA's K largest
+};
+
+// The rank of `key` among the n of list (no two are the same)
+__device__ __forceinline__ int rank_of(u64 key, const u64* list, int n) {
+  int r = 0;
+  for (int i = 0; i < n; ++i) r += list[i] > key;
+  return r;
+}
+
+template <typename TI>
+__global__ void __launch_bounds__(kThreads) logprobs_kernel(const __grid_constant__ LogprobsProblem p, int n_cl) {
+  constexpr int N = Vec<TI>::N;
+  __shared__ Smem sm;
+  pdl_wait_and_launch();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int row = (int)blockIdx.x / n_cl, rank = n_cl > 1 ? (int)cluster_rank() : 0;
+  const Row<TI> x(static_cast<const TI*>(p.logits) + (long long)row * p.s_row, p.V);
+  const float T = p.temperature ? p.temperature[row] : 1.f, scale = 1.f / T, k2 = scale * kLog2e;
+  const int target = p.targets[row];
+  const bool bad_t = !(T > 0.f) || !isfinite(T) || !isfinite(k2), bad_y = target >= p.V;
+  // this CTA's groups, and a thread's: first + thread, + kThreads, ...
+  const int g0 = (int)((long long)x.groups * rank / n_cl), g1 = (int)((long long)x.groups * (rank + 1) / n_cl);
+  Sums a;
+  auto take = [&](const float (&v)[N]) {
+    float mx = v[0];
+#pragma unroll
+    for (int j = 1; j < N; ++j) mx = fmaxf(mx, v[j]);
+    if (mx > a.m) a.raise(mx, k2);
+    const float m = a.m == -INFINITY ? 0.f : a.m;  // (masked so far: every weight is 0)
+    float l = 0.f, s = 0.f;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float t = (v[j] - m) * k2, w = ex2_approx(t);
+      l += w;
+      s = w > 0.f ? fmaf(w, t, s) : s;
+    }
+    a.l += l;
+    a.s += s;
+  };
+  {
+    constexpr int U = 4;  // loads in flight
+    int g = g0 + (int)threadIdx.x;
+    for (; g + (U - 1) * kThreads < g1; g += U * kThreads) {
+      float v[U][N];
+      uint4 w[U];
+      bool all = true;
+#pragma unroll
+      for (int i = 0; i < U; ++i) all &= x.whole(g + i * kThreads);
+      if (all) {
+#pragma unroll
+        for (int i = 0; i < U; ++i) w[i] = x.raw(g + i * kThreads);
+#pragma unroll
+        for (int i = 0; i < U; ++i) Vec<TI>::unpack(w[i], v[i]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < U; ++i) x.load(g + i * kThreads, v[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < U; ++i) take(v[i]);
+    }
+    for (; g < g1; g += kThreads) {
+      float v[N];
+      x.load(g, v);
+      take(v);
+    }
+  }
+  const float mine = a.m;
+  // the CTA's sums
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float m2 = __shfl_xor_sync(0xffffffffu, a.m, o), l2 = __shfl_xor_sync(0xffffffffu, a.l, o),
+                s2 = __shfl_xor_sync(0xffffffffu, a.s, o);
+    // (the lower lane's first, so that both lanes have the same bits)
+    if (lane & o) {
+      Sums b;
+      b.m = m2; b.l = l2; b.s = s2;
+      b.join(a.m, a.l, a.s, k2);
+      a = b;
+    } else {
+      a.join(m2, l2, s2, k2);
+    }
+  }
+  if (lane == 0) {
+    sm.m[warp] = a.m; sm.l[warp] = a.l; sm.s[warp] = a.s;
+  }
+  // a bound that at least K elements of the CTA reach
+  const int K = p.top, full = min(kWarps, (g1 - g0) / 32), take_n = full ? (K + full - 1) / full : 0;
+  const unsigned key = mine == -INFINITY ? 0u : ordered(mine);
+  if (K > 0) {
+    unsigned rest = key, low = 0;
+    for (int i = 0; i < take_n; ++i) {
+      low = __reduce_max_sync(0xffffffffu, rest);
+      const unsigned who = __ballot_sync(0xffffffffu, rest == low);
+      if (lane == __ffs(who) - 1) rest = 0;
+    }
+    if (lane == 0) sm.low[warp] = low;
+    if (threadIdx.x == 0) sm.n = 0;
+  }
+  __syncthreads();
+  {
+    Sums c;
+    c.m = sm.m[0]; c.l = sm.l[0]; c.s = sm.s[0];
+    for (int i = 1; i < kWarps; ++i) c.join(sm.m[i], sm.l[i], sm.s[i], k2);
+    a = c;
+  }
+  if (K > 0) {
+    unsigned low = full && take_n <= 32 ? sm.low[0] : 0u;
+    for (int i = 1; i < full; ++i) low = min(low, sm.low[i]);
+    low = max(low, 1u);
+    // the warp's K largest among the elements of its lanes that reach the bound, one a lane
+    u64 best = 0;
+    unsigned who = __ballot_sync(0xffffffffu, key >= low);
+    const int slices = (g1 - g0 + kThreads - 1) / kThreads;  // a lane's groups, one to a lane each
+    while (who) {
+      const int of = __ffs(who) - 1;
+      who &= who - 1;
+      for (int i0 = 0; i0 < slices; i0 += 32) {
+        const int g = g0 + (warp * 32 + of) + (i0 + lane) * kThreads;
+        float v[N];
+        if (i0 + lane < slices && g < g1) {
+          x.load(g, v);
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j) v[j] = -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          // (-inf and NaN are never kept)
+          const u64 k = v[j] > -INFINITY && ordered(v[j]) >= low ? key_of(v[j], g * N - x.off + j) : 0;
+          const u64 least = __shfl_sync(0xffffffffu, best, K - 1);
+          unsigned in = __ballot_sync(0xffffffffu, k > least);
+          while (in) {
+            const u64 next = __shfl_sync(0xffffffffu, k, __ffs(in) - 1);
+            in &= in - 1;
+            const int at = __popc(__ballot_sync(0xffffffffu, best > next));
+            const u64 up = __shfl_up_sync(0xffffffffu, best, 1);
+            best = lane == at ? next : lane > at ? up : best;
+          }
+        }
+      }
+    }
+    const unsigned have = __ballot_sync(0xffffffffu, lane < K && best != 0);
+    int at = 0;
+    if (lane == 0 && have) at = atomicAdd(&sm.n, __popc(have));
+    at = __shfl_sync(0xffffffffu, at, 0) + lane;
+    if (have >> lane & 1) sm.list[at] = best;
+    if (threadIdx.x < kMaxTop) sm.best[threadIdx.x] = 0;
+    __syncthreads();
+    const int n = sm.n;
+    if ((int)threadIdx.x < n) {
+      const u64 mykey = sm.list[threadIdx.x];
+      const int r = rank_of(mykey, sm.list, n);
+      if (r < K) sm.best[r] = mykey;
+    }
+  }
+  if (n_cl > 1) {
+    if (threadIdx.x == 0) {
+      sm.cm = a.m; sm.cl = a.l; sm.cs = a.s;
+    }
+    __syncthreads();
+    cluster_sync();
+    if (rank == 0) {
+      Sums c;
+      for (int i = 0; i < n_cl; ++i) {
+        const float m2 = peer_f(peer(&sm.cm, i)), l2 = peer_f(peer(&sm.cl, i)), s2 = peer_f(peer(&sm.cs, i));
+        c.join(m2, l2, s2, k2);
+      }
+      a = c;
+      if (K > 0) {
+        const int n = n_cl * K;
+        for (int e = threadIdx.x; e < n; e += kThreads) sm.list[e] = peer_u64(peer(&sm.best[e % K], e / K));
+        __syncthreads();
+        u64 mykey = 0;
+        int r = 0;
+        if ((int)threadIdx.x < n) {
+          mykey = sm.list[threadIdx.x];
+          r = rank_of(mykey, sm.list, n);
+        }
+        // (this CTA's own list has been read: sm.best can take the row's)
+        __syncthreads();
+        if (threadIdx.x < kMaxTop) sm.best[threadIdx.x] = 0;
+        __syncthreads();
+        if (mykey && r < K) sm.best[r] = mykey;
+      }
+    }
+    cluster_sync();  // this CTA's shared memory has been read
+    if (rank != 0) return;
+  }
+  __syncthreads();
+  // rows without a finite maximum: +inf shares the probability, -inf has none, NaN is NaN
+  if (!isfinite(a.m)) {
+    int inf = 0, nan = 0;
+    for (int c = threadIdx.x; c < p.V; c += kThreads) {
+      const float v = (float)x.x[c];
+      inf += v == INFINITY;
+      nan |= v != v;
+    }
+    nan = __syncthreads_or(nan);
+    if (threadIdx.x == 0) sm.n = 0;
+    __syncthreads();
+    if (inf) atomicAdd(&sm.n, inf);
+    __syncthreads();
+    a.l = nan ? NAN : a.m == INFINITY ? (float)sm.n : 0.f;
+    a.s = 0.f;
+  }
+  const bool none = a.m == -INFINITY && a.l == 0.f;
+  const float logl = bad_t ? NAN : logf(a.l);
+  auto logp = [&](float v) {  // of a value of the row
+    if (none && !bad_t) return -INFINITY;
+    const float t = v == a.m ? 0.f : (v - a.m) * scale;
+    return t - logl;
+  };
+  if (threadIdx.x == 0) {
+    p.logz[row] = none ? (bad_t ? NAN : -INFINITY) : fmaf(a.m, scale, logl);
+    p.entropy[row] = none ? (bad_t ? NAN : 0.f) : logl - kLn2 * (a.s / a.l);
+    const bool nan = logl != logl;
+    p.logprob[row] = bad_y || nan ? NAN : target < 0 ? 0.f : logp((float)x.x[target]);
+    if ((bad_t || bad_y) && p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
+  }
+  if ((int)threadIdx.x < K) {
+    const u64 k = sm.best[threadIdx.x];
+    const bool nan = logl != logl;
+    p.top_tokens[(long long)row * K + threadIdx.x] = nan || !k ? -1 : (int)~(unsigned)k;
+    p.top_logprobs[(long long)row * K + threadIdx.x] =
+        nan ? NAN : !k ? -INFINITY : logp(value_of((unsigned)(k >> 32)));
+  }
+}
+
+// Gradient: a CTA takes kChunk groups of a row.
+constexpr int kGradThreads = 256, kGradU = 4, kChunk = kGradThreads * kGradU;
+
+template <typename TI, bool VEC>
+__global__ void __launch_bounds__(kGradThreads)
+    logprobs_grad_kernel(const __grid_constant__ LogprobsGradProblem p, int chunks) {
+  constexpr int N = Vec<TI>::N;
+  pdl_wait_and_launch();
+  const int row = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)(blockIdx.x - (unsigned)row * chunks);
+  const Row<TI> x(static_cast<const TI*>(p.logits) + (long long)row * p.s_row, p.V);
+  TI* out = static_cast<TI*>(p.dlogits) + (long long)row * p.s_out;
+  uint4 w[kGradU];
+  const int first = chunk * kChunk + (int)threadIdx.x;
+#pragma unroll
+  for (int i = 0; i < kGradU; ++i)
+    if (x.whole(first + i * kGradThreads)) w[i] = x.raw(first + i * kGradThreads);
+  const float T = p.temperature ? p.temperature[row] : 1.f, scale = 1.f / T;
+  const float logz = p.logz[row], H = p.entropy[row];
+  const int target = p.targets[row];
+  const float g = p.dlogprob && target >= 0 ? p.dlogprob[row] : 0.f;
+  const float h = p.dentropy ? p.dentropy[row] : 0.f, k = p.dlogz ? p.dlogz[row] : 0.f;
+  const float kg = target >= p.V ? NAN : k - g;  // (a token outside the row has no log probability)
+  const bool none = logz == -INFINITY;
+  auto grad = [&](float v, int c) {
+    float lp = fmaf(v, scale, -logz);
+    // the equal largest ones share the probability where logz does not hold their logarithm: +inf, or
+    // nothing but the type's lowest value
+    if (fabsf(logz) > 1e30f)
+      lp = (logz == INFINITY ? v == INFINITY : lp >= -1e-6f * fabsf(logz)) ? -H : -INFINITY;
+    const float q = ex2_approx(lp * kLog2e);
+    float d = q == 0.f ? 0.f : q * (kg - h * (lp + H));
+    if (kg != kg) d = kg;
+    if (c == target) d += g;
+    return none ? 0.f : d * scale;
+  };
+#pragma unroll
+  for (int i = 0; i < kGradU; ++i) {
+    const int gr = first + i * kGradThreads;
+    if (gr >= x.groups) break;
+    const int c0 = gr * N - x.off;
+    if (x.whole(gr)) {
+      float v[N];
+      Vec<TI>::unpack(w[i], v);
+#pragma unroll
+      for (int j = 0; j < N; ++j) v[j] = grad(v[j], c0 + j);
+      if (VEC) {
+        *reinterpret_cast<uint4*>(out + c0) = Vec<TI>::pack(v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) out[c0 + j] = (TI)v[j];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (c0 + j >= 0 && c0 + j < p.V) out[c0 + j] = (TI)grad((float)x.x[c0 + j], c0 + j);
+    }
+  }
+}
+
+template <typename TI>
+cudaError_t launch_t(const LogprobsProblem& p, cudaStream_t s) {
+  int dev = 0, nsm = 148;
+  if (cudaGetDevice(&dev) != cudaSuccess ||
+      cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
+    nsm = 148;
+  // clusters while all rows' CTAs are resident at once and each keeps 4096 elements
+  int cl = 1;
+  while (cl < kMaxCluster && 2LL * cl * p.R <= nsm && p.V / (2 * cl) >= 4096) cl *= 2;
+  const cudaError_t e = launch_pdl(logprobs_kernel<TI>, dim3((unsigned)p.R * cl), kThreads, 0, s, cl, p, cl);
+  if (e != cudaSuccess) note_failure("log probabilities: launch");
+  return e;
+}
+
+template <typename TI>
+cudaError_t launch_grad_t(const LogprobsGradProblem& p, cudaStream_t s) {
+  // a row's groups at any alignment
+  const int groups = (p.V + 2 * Vec<TI>::N - 2) / Vec<TI>::N, chunks = (groups + kChunk - 1) / kChunk;
+  const long long grid = (long long)p.R * chunks;
+  if (grid > 0x7fffffffLL) return cudaErrorInvalidConfiguration;
+  // 16-byte stores where every row of the output lies like its row of logits
+  const long long es = sizeof(TI);
+  const bool vec = (reinterpret_cast<uintptr_t>(p.logits) - reinterpret_cast<uintptr_t>(p.dlogits)) % 16 == 0 &&
+                   (p.R == 1 || (p.s_row - p.s_out) * es % 16 == 0);
+  const cudaError_t e =
+      vec ? launch_pdl(logprobs_grad_kernel<TI, true>, dim3((unsigned)grid), kGradThreads, 0, s, 1, p, chunks)
+          : launch_pdl(logprobs_grad_kernel<TI, false>, dim3((unsigned)grid), kGradThreads, 0, s, 1, p, chunks);
+  if (e != cudaSuccess) note_failure("log probabilities, gradient: launch");
+  return e;
+}
+
+}  // namespace logprobs
+
+int logprobs_max_top() { return logprobs::kMaxTop; }
+
+cudaError_t launch_logprobs(const LogprobsProblem& p, cudaStream_t s) {
+  return p.dtype == RELATION_F32 ? logprobs::launch_t<float>(p, s) : logprobs::launch_t<__nv_bfloat16>(p, s);
+}
+
+cudaError_t launch_logprobs_grad(const LogprobsGradProblem& p, cudaStream_t s) {
+  return p.dtype == RELATION_F32 ? logprobs::launch_grad_t<float>(p, s)
+                                 : logprobs::launch_grad_t<__nv_bfloat16>(p, s);
+}
+
+}  // namespace rel
