@@ -25,7 +25,7 @@ namespace normrope {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kMaxD = 256;
-constexpr int kMaxParts = 1216;  // CTAs that leave a partial sum of dw
+constexpr int kMaxParts = 1216;  // CTAs at most, each of which leaves a partial sum of dw backward
 
 // GE consecutive elements: 16 bytes of an aligned row, or one element
 template <typename TI, int GE>
@@ -97,275 +97,224 @@ struct Place {
   }
 };
 
-// The turns (cos, sin) s of a CTA's tokens; pairs past the last one of a group that the turned part
-// ends in stay as they are.
-template <int TOK>
-__device__ __forceinline__ void fill_turns(float2 (&turn)[TOK][kMaxD / 2], const int (&pos)[TOK],
-                                           const NormRopeProblem& p, int nt) {
-  const int half = p.d_rot / 2, n = min(p.d / 2, (half + 3) & ~3);
-  for (int c = threadIdx.x; c < n; c += kThreads) {
-    if (c >= half) {
-      for (int tt = 0; tt < nt; ++tt) turn[tt][c] = make_float2(1.f, 0.f);
-      continue;
-    }
-    const double t = p.freqs[c] * 0.15915494309189533576888376337251;  // turns a position
-    const unsigned long long step =
-        (unsigned long long)__double2ll_rn((t - rint(t)) * 9223372036854775808.0) << 1;
-    for (int tt = 0; tt < nt; ++tt) {
-      const unsigned long long at = (unsigned long long)max(pos[tt], 0) * step;
-      float s, co;
-      sincospif((float)(int)(at >> 32) * 0x1p-31f, &s, &co);
-      turn[tt][c] = make_float2(co * p.scale, s * p.scale);
-    }
-  }
-}
-
 __device__ __forceinline__ float lanes_sum(float x, int lanes) {
   for (int o = lanes >> 1; o > 0; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
   return x;
 }
 
-// A lane's two groups turned (SIGN 1) or turned back (-1)
+// A lane's two groups turned (sign 1) or turned back (-1) by their pairs' (cos, sin)
 template <int GE, bool ACROSS>
-__device__ __forceinline__ void turned(float (&x)[GE], float (&y)[GE], const float2* t, int pa, int pb,
-                                       float sign) {
+__device__ __forceinline__ void turned(float (&x)[GE], float (&y)[GE], const float2 (&cs)[GE], float sign) {
   if constexpr (ACROSS) {
-    if (pa < 0) return;
 #pragma unroll
     for (int j = 0; j < GE; ++j) {
-      const float2 cs = t[pa + j];
-      const float s = cs.y * sign, a = x[j], b = y[j];
-      x[j] = a * cs.x - b * s;
-      y[j] = a * s + b * cs.x;
+      const float s = cs[j].y * sign, a = x[j], b = y[j];
+      x[j] = a * cs[j].x - b * s;
+      y[j] = a * s + b * cs[j].x;
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < GE / 2; ++j) {
-      if (pa >= 0) {
-        const float2 cs = t[pa + j];
-        const float s = cs.y * sign, a = x[2 * j], b = x[2 * j + 1];
-        x[2 * j] = a * cs.x - b * s;
-        x[2 * j + 1] = a * s + b * cs.x;
-      }
-      if (pb >= 0) {
-        const float2 cs = t[pb + j];
-        const float s = cs.y * sign, a = y[2 * j], b = y[2 * j + 1];
-        y[2 * j] = a * cs.x - b * s;
-        y[2 * j + 1] = a * s + b * cs.x;
-      }
+    for (int j = 0; j < GE; ++j) {
+      float(&v)[GE] = j < GE / 2 ? x : y;
+      const int e = 2 * (j < GE / 2 ? j : j - GE / 2);
+      const float s = cs[j].y * sign, a = v[e], b = v[e + 1];
+      v[e] = a * cs[j].x - b * s;
+      v[e + 1] = a * s + b * cs[j].x;
     }
   }
 }
 
-// Element offset of token n, in the tensors of the queries (which 0) or keys (1)
-__device__ __forceinline__ long long token_at(const NormRopeProblem& p, int which, int n) {
-  const int b = n / p.T, t = n - b * p.T;
-  return (long long)b * p.sB[which] + (long long)t * p.sT[which];
+// The parts of a turn that a position adds to the angles of a lane's pairs of a table, 2^-64 each: pairs
+// lane, lane + 32, ...
+struct Steps {
+  unsigned long long s[kMaxD / 64];
+  __device__ __forceinline__ Steps(const NormRopeProblem& p, int lane) {
+#pragma unroll
+    for (int i = 0; i < kMaxD / 64; ++i) {
+      s[i] = 0;
+      if (lane + 32 * i < p.d_rot / 2) {
+        const double t = p.freqs[lane + 32 * i] * 0.15915494309189533576888376337251;
+        s[i] = (unsigned long long)__double2ll_rn((t - rint(t)) * 9223372036854775808.0) << 1;
+      }
+    }
+  }
+};
+
+// The turns (cos, sin) s of one token, by its warp; pairs past the last one of a group that the turned
+// part ends in stay as they are.
+__device__ __forceinline__ void fill_turns(float2* turn, int pos, const Steps& st, const NormRopeProblem& p,
+                                           int lane) {
+  const int half = p.d_rot / 2, n = min(p.d / 2, (half + 3) & ~3);
+  __syncwarp();
+#pragma unroll
+  for (int i = 0; i < kMaxD / 64; ++i) {
+    const int c = lane + 32 * i;
+    if (c < n) {
+      const unsigned long long at = (unsigned long long)max(pos, 0) * st.s[i];
+      float s, co;
+      sincospif((float)(int)(at >> 32) * 0x1p-31f, &s, &co);
+      turn[c] = c < half ? make_float2(co * p.scale, s * p.scale) : make_float2(1.f, 0.f);
+    }
+  }
+  __syncwarp();
 }
 
-template <int TOK>
-__device__ __forceinline__ void fill_positions(int (&pos)[TOK], const NormRopeProblem& p, int t0) {
-  if (threadIdx.x < TOK) {
-    const int n = min(t0 + (int)threadIdx.x, p.B * p.T - 1);
-    pos[threadIdx.x] = p.positions ? p.positions[n] : n % p.T;
-  }
-}
-__device__ __forceinline__ void fill_weights(float (&w)[2][kMaxD], const NormRopeProblem& p) {
-  for (int e = threadIdx.x; e < 2 * p.d; e += kThreads) {
-    const int which = e >= p.d, c = e - which * p.d;
-    w[which][c] = p.w[which] ? p.w[which][c] : 1.f;
-  }
-}
-
-template <typename TI, int GE, bool ACROSS, int IT, int TOK>
+// Forward, and with GRAD backward.  A warp takes whole tokens, 32 / lanes of a token's heads at a time, first
+// all its tokens' queries, then the keys: a lane's weights stay in registers, its turns for a token's heads,
+// and backward its columns' dw.
+template <typename TI, int GE, bool ACROSS, int IT, bool GRAD>
 __global__ void __launch_bounds__(kThreads)
     norm_rope_kernel(const __grid_constant__ NormRopeProblem p, int lanes) {
   using G = Group<TI, GE>;
-  __shared__ __align__(16) float2 turn[TOK][kMaxD / 2];
-  __shared__ __align__(16) float w[2][kMaxD];
-  __shared__ int pos[TOK];
+  constexpr int U = GRAD ? 1 : 2;  // rows of a lane at a time; the next ones are on their way
+  __shared__ __align__(16) float2 turns[kWarps][kMaxD / 2];
+  __shared__ float sums[kWarps][GRAD ? kMaxD : 1];
   pdl_wait_and_launch();
-  const int N = p.B * p.T, t0 = (int)blockIdx.x * TOK, nt = min(TOK, N - t0);
-  const int per = p.H[0] + p.H[1], rows = nt * per, step = kThreads / lanes;
-  const Place<GE, ACROSS, IT> at(threadIdx.x % lanes, lanes, p.d, p.d_rot, p.half);
-  struct Row {
-    int which, tt;
-    long long off;
-    typename G::Raw a[IT], b[IT];
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int N = p.B * p.T, slots = 32 / lanes, slot = lane / lanes;
+  const Place<GE, ACROSS, IT> at(lane % lanes, lanes, p.d, p.d_rot, p.half);
+  const Steps steps(p, lane);
+  float2* turn = turns[warp];
+  struct Rows {
+    typename G::Raw x[U][2][IT], y[GRAD ? U : 1][2][IT];
   };
-  auto fetch = [&](int r, Row& row) {  // (clamped: a group of lanes past the end takes the last row)
-    r = min(r, rows - 1);
-    row.tt = r / per;
-    const int h = r - row.tt * per;
-    row.which = h >= p.H[0];
-    row.off = token_at(p, row.which, t0 + row.tt) + (long long)(h - row.which * p.H[0]) * p.sH[row.which];
-    const TI* src = static_cast<const TI*>(p.in[row.which]) + row.off;
-#pragma unroll
-    for (int it = 0; it < IT; ++it) {
-      if (at.a[it] >= 0) row.a[it] = G::load(src + at.a[it]);
-      if (at.b[it] >= 0) row.b[it] = G::load(src + at.b[it]);
-    }
-  };
-  auto finish = [&](const Row& row, bool live) {
-    float x[IT][GE], y[IT][GE], ss = 0.f;
-#pragma unroll
-    for (int it = 0; it < IT; ++it) {
-#pragma unroll
-      for (int j = 0; j < GE; ++j) x[it][j] = y[it][j] = 0.f;
-      if (at.a[it] >= 0) G::unpack(row.a[it], x[it]);
-      if (at.b[it] >= 0) G::unpack(row.b[it], y[it]);
-#pragma unroll
-      for (int j = 0; j < GE; ++j) ss = fmaf(x[it][j], x[it][j], fmaf(y[it][j], y[it][j], ss));
-    }
-    ss = lanes_sum(ss, lanes);
-    const float r = p.norm ? rsqrtf(ss / (float)p.d + p.eps) : 1.f;
-    const bool none = pos[row.tt] < 0;
-    TI* dst = static_cast<TI*>(p.out[row.which]) + row.off;
-#pragma unroll
-    for (int it = 0; it < IT; ++it) {
-#pragma unroll
-      for (int j = 0; j < GE; ++j) {
-        x[it][j] *= r * w[row.which][max(at.a[it], 0) + j];
-        y[it][j] *= r * w[row.which][max(at.b[it], 0) + j];
-      }
-      turned<GE, ACROSS>(x[it], y[it], turn[row.tt], at.pa[it], at.pb[it], 1.f);
-#pragma unroll
-      for (int j = 0; j < GE; ++j) {
-        x[it][j] = none ? 0.f : x[it][j];
-        y[it][j] = none ? 0.f : y[it][j];
-      }
-      if (live && at.a[it] >= 0) G::store(dst + at.a[it], x[it]);
-      if (live && at.b[it] >= 0) G::store(dst + at.b[it], y[it]);
-    }
-  };
-  Row r0, r1;
-  const int first = threadIdx.x / lanes;
-  fetch(first, r0);
-  fetch(first + step, r1);
-  fill_positions<TOK>(pos, p, t0);
-  fill_weights(w, p);
-  __syncthreads();
-  fill_turns<TOK>(turn, pos, p, nt);
-  __syncthreads();
-  // (whole warps: the sums are shuffles)
-  for (int r = first; r - first < rows; r += 2 * step) {
-    if (r != first) {
-      fetch(r, r0);
-      fetch(r + step, r1);
-    }
-    finish(r0, r < rows);
-    finish(r1, r + step < rows);
-  }
-}
-
-// Backward.  CTAs walk the tokens in steps of the grid and keep their columns' dw; the sums over a
-// CTA's rows are in a fixed order, and dw_kernel adds the CTAs' up.
-template <typename TI, int GE, bool ACROSS, int IT, int TOK>
-__global__ void __launch_bounds__(kThreads)
-    norm_rope_grad_kernel(const __grid_constant__ NormRopeProblem p, int lanes) {
-  using G = Group<TI, GE>;
-  __shared__ __align__(16) float2 turn[TOK][kMaxD / 2];
-  __shared__ __align__(16) float w[2][kMaxD];
-  __shared__ float sums[kWarps][kMaxD];
-  __shared__ int pos[TOK];
-  pdl_wait_and_launch();
-  const int N = p.B * p.T, tiles = (N + TOK - 1) / TOK, step = kThreads / lanes;
-  const Place<GE, ACROSS, IT> at(threadIdx.x % lanes, lanes, p.d, p.d_rot, p.half);
-  float acc[2][2][IT][GE];
-#pragma unroll
-  for (int e = 0; e < 4 * IT * GE; ++e) (&acc[0][0][0][0])[e] = 0.f;
-  fill_weights(w, p);
-  for (int tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-    const int t0 = tile * TOK, nt = min(TOK, N - t0);
-    __syncthreads();
-    fill_positions<TOK>(pos, p, t0);
-    __syncthreads();
-    fill_turns<TOK>(turn, pos, p, nt);
-    __syncthreads();
-#pragma unroll
-    for (int which = 0; which < 2; ++which) {
-      const int H = p.H[which], rows = nt * H;
-      for (int r0 = 0; r0 < rows; r0 += step) {
-        const int r = r0 + (int)threadIdx.x / lanes;
-        const int tt = min(r, rows - 1) / H, h = min(r, rows - 1) - tt * H;
-        const bool live = r < rows;
-        const long long off = token_at(p, which, t0 + tt) + (long long)h * p.sH[which];
-        const TI* sx = static_cast<const TI*>(p.in[which]) + off;
-        const TI* sy = static_cast<const TI*>(p.dout[which]) + off;
-        float x[2][IT][GE], u[2][IT][GE], ss = 0.f, dot = 0.f;
-#pragma unroll
-        for (int it = 0; it < IT; ++it) {
-#pragma unroll
-          for (int j = 0; j < GE; ++j) x[0][it][j] = x[1][it][j] = u[0][it][j] = u[1][it][j] = 0.f;
-          if (at.a[it] >= 0) {
-            G::unpack(G::load(sx + at.a[it]), x[0][it]);
-            G::unpack(G::load(sy + at.a[it]), u[0][it]);
-          }
-          if (at.b[it] >= 0) {
-            G::unpack(G::load(sx + at.b[it]), x[1][it]);
-            G::unpack(G::load(sy + at.b[it]), u[1][it]);
-          }
-        }
-#pragma unroll
-        for (int it = 0; it < IT; ++it) {
-          turned<GE, ACROSS>(u[0][it], u[1][it], turn[tt], at.pa[it], at.pb[it], -1.f);
-#pragma unroll
-          for (int j = 0; j < GE; ++j) {
-            ss = fmaf(x[0][it][j], x[0][it][j], fmaf(x[1][it][j], x[1][it][j], ss));
-            const float wa = w[which][max(at.a[it], 0) + j], wb = w[which][max(at.b[it], 0) + j];
-            dot = fmaf(x[0][it][j] * wa, u[0][it][j], fmaf(x[1][it][j] * wb, u[1][it][j], dot));
-          }
-        }
-        const bool none = pos[tt] < 0;
-        float rn = 1.f, mean = 0.f;
-        if (p.norm) {
-          ss = lanes_sum(ss, lanes);
-          dot = lanes_sum(dot, lanes);
-          rn = rsqrtf(ss / (float)p.d + p.eps);
-          mean = dot * rn / (float)p.d;  // mean of x^ w u
-        }
-        TI* dst = static_cast<TI*>(p.out[which]) + off;
-#pragma unroll
-        for (int it = 0; it < IT; ++it) {
-#pragma unroll
-          for (int side = 0; side < 2; ++side) {
-            const int c = side ? at.b[it] : at.a[it];
-            float dx[GE];
-#pragma unroll
-            for (int j = 0; j < GE; ++j) {
-              const float xh = x[side][it][j] * rn;
-              dx[j] = none ? 0.f : rn * (w[which][max(c, 0) + j] * u[side][it][j] - xh * mean);
-              if (live && !none) acc[which][side][it][j] = fmaf(u[side][it][j], xh, acc[which][side][it][j]);
-            }
-            if (live && c >= 0) G::store(dst + c, dx);
-          }
-        }
-      }
-    }
-  }
-  if (!p.part) return;
-  // the CTA's sums: lanes of the same columns by shuffles, then the warps in order
-#pragma unroll
+#pragma unroll 1
   for (int which = 0; which < 2; ++which) {
-    __syncthreads();
+    const int H = p.H[which];
+    const TI* in = static_cast<const TI*>(which ? p.in[1] : p.in[0]);
+    const TI* din = static_cast<const TI*>(which ? p.dout[1] : p.dout[0]);
+    TI* out = static_cast<TI*>(which ? p.out[1] : p.out[0]);
+    const float* wp = which ? p.w[1] : p.w[0];
+    const long long sB = which ? p.sB[1] : p.sB[0], sT = which ? p.sT[1] : p.sT[0],
+                    sH = which ? p.sH[1] : p.sH[0];
+    float w[2][IT][GE], acc[2][IT][GE];
 #pragma unroll
     for (int it = 0; it < IT; ++it)
 #pragma unroll
-      for (int side = 0; side < 2; ++side) {
-        const int c = side ? at.b[it] : at.a[it];
+      for (int j = 0; j < GE; ++j) {
+        w[0][it][j] = wp && H && at.a[it] >= 0 ? wp[at.a[it] + j] : 1.f;
+        w[1][it][j] = wp && H && at.b[it] >= 0 ? wp[at.b[it] + j] : 1.f;
+        acc[0][it][j] = acc[1][it][j] = 0.f;
+      }
+    for (int n = (int)blockIdx.x * kWarps + warp; n < N && H > 0; n += (int)gridDim.x * kWarps) {
+      const int b = n / p.T, t = n - b * p.T, pos = p.positions ? p.positions[n] : t;
+      const long long base = (long long)b * sB + (long long)t * sT;
+      auto fetch = [&](int h, Rows& r) {  // (clamped: lanes past the end take the last head)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const long long off = base + (long long)min(h + u * slots, H - 1) * sH;
+#pragma unroll
+          for (int it = 0; it < IT; ++it)
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+              const int c = side ? at.b[it] : at.a[it];
+              if (c < 0) continue;
+              r.x[u][side][it] = G::load(in + off + c);
+              if (GRAD) r.y[u][side][it] = G::load(din + off + c);
+            }
+        }
+      };
+      Rows now, next;
+      fetch(slot, now);
+      fill_turns(turn, pos, steps, p, lane);
+      float2 cs[IT][GE];  // ACROSS: of the pairs (a + j, b + j); else a's pairs, then b's
+#pragma unroll
+      for (int it = 0; it < IT; ++it)
 #pragma unroll
         for (int j = 0; j < GE; ++j) {
-          float x = acc[which][side][it][j];
-          for (int o = 16; o >= lanes; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
-          if ((threadIdx.x & 31) < lanes && c >= 0) sums[threadIdx.x >> 5][c + j] = x;
+          const int first = ACROSS || j < GE / 2 ? at.pa[it] : at.pb[it] - GE / 2;
+          const bool is = ACROSS || j < GE / 2 ? at.pa[it] >= 0 : at.pb[it] >= 0;
+          cs[it][j] = is ? turn[first + j] : make_float2(1.f, 0.f);
         }
-      }
-    __syncthreads();
-    for (int c = threadIdx.x; c < p.d; c += kThreads) {
-      float x = sums[0][c];
+#pragma unroll 1
+      for (int h0 = 0; h0 < H; h0 += U * slots) {
+        if (h0 + U * slots < H) fetch(h0 + U * slots + slot, next);
 #pragma unroll
-      for (int i = 1; i < kWarps; ++i) x += sums[i][c];
-      p.part[((long long)blockIdx.x * 2 + which) * p.d + c] = x;
+        for (int u = 0; u < U; ++u) {
+          const int h = h0 + u * slots + slot;
+          float x[2][IT][GE], y[2][IT][GE], ss = 0.f, dot = 0.f;
+#pragma unroll
+          for (int it = 0; it < IT; ++it)
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+              const bool is = (side ? at.b[it] : at.a[it]) >= 0;
+#pragma unroll
+              for (int j = 0; j < GE; ++j) x[side][it][j] = y[side][it][j] = 0.f;
+              if (is) {
+                G::unpack(now.x[u][side][it], x[side][it]);
+                if (GRAD) G::unpack(now.y[GRAD ? u : 0][side][it], y[side][it]);
+              }
+            }
+#pragma unroll
+          for (int it = 0; it < IT; ++it) {
+            if (GRAD) turned<GE, ACROSS>(y[0][it], y[1][it], cs[it], -1.f);
+#pragma unroll
+            for (int j = 0; j < GE; ++j)
+#pragma unroll
+              for (int side = 0; side < 2; ++side) {
+                ss = fmaf(x[side][it][j], x[side][it][j], ss);
+                if (GRAD) dot = fmaf(x[side][it][j] * w[side][it][j], y[side][it][j], dot);
+              }
+          }
+          const bool none = pos < 0, live = h < H;
+          float r = 1.f, mean = 0.f;
+          if (p.norm) {
+            ss = lanes_sum(ss, lanes);
+            r = rsqrtf(ss / (float)p.d + p.eps);
+            if (GRAD) mean = lanes_sum(dot, lanes) * r / (float)p.d;  // mean of x^ w u
+          }
+          TI* dst = out + base + (long long)min(h, H - 1) * sH;
+#pragma unroll
+          for (int it = 0; it < IT; ++it) {
+#pragma unroll
+            for (int side = 0; side < 2; ++side)
+#pragma unroll
+              for (int j = 0; j < GE; ++j) {
+                float& v = x[side][it][j];
+                if (GRAD) {
+                  const float xh = v * r, u_ = y[side][it][j];
+                  if (live && !none) acc[side][it][j] = fmaf(u_, xh, acc[side][it][j]);
+                  v = r * (w[side][it][j] * u_ - xh * mean);
+                } else {
+                  v *= r * w[side][it][j];
+                }
+              }
+            if (!GRAD) turned<GE, ACROSS>(x[0][it], x[1][it], cs[it], 1.f);
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+              const int c = side ? at.b[it] : at.a[it];
+#pragma unroll
+              for (int j = 0; j < GE; ++j) x[side][it][j] = none ? 0.f : x[side][it][j];
+              if (live && c >= 0) G::store(dst + c, x[side][it]);
+            }
+          }
+        }
+        now = next;
+      }
+    }
+    if constexpr (GRAD) {
+      if (!p.part) continue;
+      // the CTA's sums: lanes of the same columns by shuffles, then the warps in order
+      __syncthreads();
+#pragma unroll
+      for (int it = 0; it < IT; ++it)
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+          const int c = side ? at.b[it] : at.a[it];
+#pragma unroll
+          for (int j = 0; j < GE; ++j) {
+            float x = acc[side][it][j];
+            for (int o = 16; o >= lanes; o >>= 1) x += __shfl_xor_sync(0xffffffffu, x, o);
+            if (lane < lanes && c >= 0) sums[warp][c + j] = x;
+          }
+        }
+      __syncthreads();
+      for (int c = threadIdx.x; c < p.d; c += kThreads) {
+        float x = sums[0][c];
+#pragma unroll
+        for (int i = 1; i < kWarps; ++i) x += sums[i][c];
+        p.part[((long long)blockIdx.x * 2 + which) * p.d + c] = x;
+      }
     }
   }
 }
@@ -387,24 +336,22 @@ __global__ void __launch_bounds__(256) dw_kernel(const float* part, int n, int d
   }
 }
 
-constexpr int kGradTok = 4;
-
 template <typename TI, int GE, bool ACROSS, int IT>
 cudaError_t launch_t(const NormRopeProblem& p, bool grad, cudaStream_t s) {
   // lanes of a row: its groups in twos (ACROSS: the turned ones and the others apart)
   const int half = p.d_rot / 2 / GE, rest = (p.d - (ACROSS ? p.d_rot : 0) + GE - 1) / GE;
-  int need = ACROSS ? half + (rest + 1) / 2 : (rest + 1) / 2, lanes = 1;
+  const int need = ACROSS ? half + (rest + 1) / 2 : (rest + 1) / 2;
+  int lanes = 1;
   while (lanes < need && lanes < 32) lanes *= 2;
-  const int N = p.B * p.T;
+  const int tiles = (p.B * p.T + kWarps - 1) / kWarps, grid = tiles < kMaxParts ? tiles : kMaxParts;
   cudaError_t e;
   if (grad) {
-    const int tiles = (N + kGradTok - 1) / kGradTok, grid = tiles < kMaxParts ? tiles : kMaxParts;
-    e = launch_pdl(norm_rope_grad_kernel<TI, GE, ACROSS, IT, kGradTok>, dim3(grid), kThreads, 0, s, 1, p, lanes);
+    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, true>, dim3(grid), kThreads, 0, s, 1, p, lanes);
     if (e == cudaSuccess && p.part)
       e = launch_pdl(dw_kernel, dim3((2 * p.d + 7) / 8), 256, 0, s, 1, (const float*)p.part, grid, p.d,
                      p.dw[0], p.dw[1]);
   } else {
-    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, 2>, dim3((N + 1) / 2), kThreads, 0, s, 1, p, lanes);
+    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, false>, dim3(grid), kThreads, 0, s, 1, p, lanes);
   }
   if (e != cudaSuccess) note_failure("norm with rotation: launch");
   return e;
@@ -416,7 +363,9 @@ cudaError_t launch_g(const NormRopeProblem& p, bool grad, cudaStream_t s) {
   for (int i = 0; i < 2; ++i) {
     if (!p.in[i]) continue;
     for (const void* x : {p.in[i], p.dout[i], (const void*)p.out[i]}) low |= reinterpret_cast<uintptr_t>(x);
-    for (long long x : {p.sB[i], p.sT[i], p.sH[i]}) low |= (uintptr_t)(x * (long long)sizeof(TI));
+    // (the stride of a dimension of one entry is never used)
+    for (long long x : {p.B > 1 ? p.sB[i] : 0, p.T > 1 ? p.sT[i] : 0, p.H[i] > 1 ? p.sH[i] : 0})
+      low |= (uintptr_t)(x * (long long)sizeof(TI));
   }
   const bool whole = low % 16 == 0 && p.d % GE == 0;
   if (p.half && whole && p.d_rot % (2 * GE) == 0) return launch_t<TI, GE, true, 1>(p, grad, s);
@@ -427,7 +376,7 @@ cudaError_t launch_g(const NormRopeProblem& p, bool grad, cudaStream_t s) {
 }  // namespace normrope
 
 size_t norm_rope_grad_workspace_bytes(int tokens, int d) {
-  const int tiles = (tokens + normrope::kGradTok - 1) / normrope::kGradTok;
+  const int tiles = (tokens + normrope::kWarps - 1) / normrope::kWarps;
   return (size_t)(tiles < normrope::kMaxParts ? tiles : normrope::kMaxParts) * 2 * d * sizeof(float);
 }
 
