@@ -375,6 +375,44 @@ relation_status relation_paged_decode(const void* q, const void* k_pages, const 
                                       relation_stream_t stream);
 
 /*
+ * relation_paged_chunk: several new tokens of every request over the paged cache: a piece of a prompt,
+ * drafted tokens to be checked, or one token (relation_paged_decode's row).  The token at position p
+ * of request b takes rows 0 .. p - 1 of the request as its history and row p as its own, which
+ * relation_cache_append has written before: Y and logZ of row p as relation_fwd over the request's
+ * rows 0 .. p.
+ *   q           [N][H][d_h] queries of the step's tokens, element strides q_sT, q_sH (d_h contiguous);
+ *               o likewise.  H is a multiple of cache.H: query heads h G .. h G + G - 1 share key/value
+ *               head h, G = H / cache.H.
+ *   block_table device int[B][cols], row stride table_stride: entries up to the largest position's
+ *               page are read.
+ *   starts      device int[B + 1]: request b's tokens are starts[b] .. starts[b + 1] - 1 (as far as
+ *               there are N), starts ascending;
+ *   positions   device int[N]: every token's position, both as relation_page_plan writes them.  Tokens
+ *               of no request and those with a negative position (padding, requests that were not
+ *               served) get Y = 0 and logZ = -inf.
+ *   logz        [N][H] fp32 output.
+ *   workspace   device scratch of relation_paged_chunk_workspace_size(N, B, H, cols, cache, dt) bytes,
+ *               16-byte aligned.
+ * fp32 or bf16 with any 1 <= d_h <= 128; rows as in relation_paged_decode.  bf16 runs on the tensor
+ * cores (P rounded to bf16 for the product with the values, sums and states in fp32).  Keys and values
+ * behind a token's own row are not its business, whatever they hold: an infinite or NaN value among
+ * them leaves the row as it is.  cols * page_size is at most 2^31 - 8192, N H at most 2^31 - 65536
+ * (else RELATION_ERR_UNSUPPORTED).  A position of cols * page_size or more makes a token padding, a
+ * page id outside [0, n_pages) reads page 0 (the row is then undefined); both are reported to
+ * dev_status (if given) as RELATION_ERR_INVALID_ARG.  Asynchronous on `stream`; three launches; nothing
+ * is allocated.
+ */
+size_t relation_paged_chunk_workspace_size(int N, int B, int H, int cols, relation_pages cache,
+                                           relation_dtype dt);
+relation_status relation_paged_chunk(const void* q, const void* k_pages, const void* v_pages,
+                                     const int* block_table, int cols, long long table_stride,
+                                     const int* starts, const int* positions, void* o, float* logz,
+                                     float lambda, float tau_s, int N, int B, int H,
+                                     relation_pages cache, long long q_sT, long long q_sH,
+                                     relation_dtype dt, void* workspace, size_t ws_bytes,
+                                     int* dev_status, relation_stream_t stream);
+
+/*
  * relation_sample: the next token of every row of logits from a given uniform number.
  *   logits      [R][V] in dt, row stride s_row (element alignment), V <= 262144 (else
  *               RELATION_ERR_UNSUPPORTED).  -inf masks a token.

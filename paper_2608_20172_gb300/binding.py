@@ -47,7 +47,8 @@ EXPORTED = ("relation_fwd", "relation_fwd_ex", "relation_bwd", "relation_bwd_ex"
             "relation_cache_append", "relation_paged_decode",
             "relation_paged_decode_workspace_size", "relation_sample", "relation_logprobs",
             "relation_logprobs_grad", "relation_norm_rope", "relation_norm_rope_grad",
-            "relation_norm_rope_grad_workspace_size")
+            "relation_norm_rope_grad_workspace_size", "relation_paged_chunk",
+            "relation_paged_chunk_workspace_size")
 
 
 class RelationLibraryMissing(RuntimeError):
@@ -136,6 +137,10 @@ def load(path: str | None = None):
         lib.relation_paged_decode_workspace_size.argtypes = [i, Pages, i]
         lib.relation_paged_decode_workspace_size.restype = sz
         lib.relation_sample.argtypes = [vp, i, i, ll, i, vp, vp, vp, vp, vp, vp, vp, vp, ip, vp]
+        lib.relation_paged_chunk.argtypes = [vp, vp, vp, vp, i, ll, vp, vp, vp, vp, f, f, i, i, i, Pages, ll,
+                                             ll, i, vp, sz, ip, vp]
+        lib.relation_paged_chunk_workspace_size.argtypes = [i, i, i, i, Pages, i]
+        lib.relation_paged_chunk_workspace_size.restype = sz
         lib.relation_logprobs.argtypes = [vp, i, i, ll, i, vp, vp, vp, vp, vp, i, vp, vp, ip, vp]
         lib.relation_logprobs_grad.argtypes = [vp, i, i, ll, i, vp, vp, vp, vp, vp, vp, vp, vp, ll, vp]
         lib.relation_norm_rope.argtypes = [vp, vp, vp, vp, i, f, RotaryArgs, vp, vp, vp, Shape, Shape, i,
@@ -921,6 +926,56 @@ def paged_decode(q, k_pages, v_pages, block_table, lengths, lam: float, tau_s: f
                                    _status(dev_status, dev), _queue(stream, dev))
     if rc != OK:
         raise RelationError(rc, "relation_paged_decode")
+    return out, logz
+
+
+def paged_chunk_workspace_size(q, k_pages, block_table) -> int:
+    """Device bytes paged_chunk needs for queries [N, H, d] of requests with this table over these
+    pages."""
+    return int(load().relation_paged_chunk_workspace_size(
+        q.shape[0], block_table.shape[0], q.shape[1], block_table.shape[1], pages_of(k_pages, k_pages),
+        _dtype_code(k_pages)))
+
+
+def paged_chunk(q, k_pages, v_pages, block_table, starts, positions, lam: float, tau_s: float = 2.0, *,
+                out=None, logz=None, workspace=None, dev_status=None, stream=None):
+    """Several new tokens per request over [n_pages, page_size, Hk, d] pages that hold their rows already:
+    q [N, H, d] with H a multiple of Hk, block_table int32 [B, cols] (rows may be strided), starts int32
+    [B + 1] and positions int32 [N] as in a PagePlan (negative: padding).  Returns (Y [N, H, d], logZ
+    [N, H]); see relation_paged_chunk."""
+    pages = pages_of(k_pages, v_pages)
+    dev, shape, st = k_pages.get_device(), q.shape, q.stride()
+    if len(shape) != 3 or shape[2] != pages.d_h or st[2] != 1 or \
+            q.dtype is not k_pages.dtype or q.get_device() != dev:
+        raise ValueError("q must be [N, H, d] with d contiguous, of the pages' d, dtype and device")
+    N, H, _ = shape
+    B = starts.numel() - 1
+    _need("starts", starts, dev, _I32, B + 1)
+    _need("positions", positions, dev, _I32, N)
+    if not _is_table(block_table, B, dev):
+        raise ValueError("block_table must be an int32 [B, cols] tensor with contiguous rows on "
+                         "the pages' device, starts one of B + 1 entries")
+    if out is None:
+        out = _like(q, stream)
+    elif out.shape != shape or out.stride() != st or out.dtype is not q.dtype or \
+            out.get_device() != dev:
+        raise ValueError("out must have q's layout")
+    if logz is None:
+        logz = _new((N, H), _F32, q.device, stream)
+    else:
+        _need("logz", logz, dev, _F32, N * H)
+    lib, dt, cols = load(), _dtype_code(q), block_table.shape[1]
+    if workspace is None:
+        workspace = _scratch(lib.relation_paged_chunk_workspace_size(N, B, H, cols, pages, dt), q.device,
+                             stream)
+    rc = lib.relation_paged_chunk(q.data_ptr(), k_pages.data_ptr(), v_pages.data_ptr(),
+                                  block_table.data_ptr(), cols, block_table.stride(0), starts.data_ptr(),
+                                  positions.data_ptr(), out.data_ptr(), logz.data_ptr(), float(lam),
+                                  float(tau_s), N, B, H, pages, st[0], st[1], dt, workspace.data_ptr(),
+                                  workspace.numel() * workspace.element_size(),
+                                  _status(dev_status, dev), _queue(stream, dev))
+    if rc != OK:
+        raise RelationError(rc, "relation_paged_chunk")
     return out, logz
 
 

@@ -296,6 +296,28 @@ struct PagedProblem {
 size_t paged_workspace_bytes(int H, int Hk);
 cudaError_t launch_paged(const PagedProblem& p, void* workspace, cudaStream_t s);
 
+// Several new tokens per request over a paged cache (relation_chunk.cu): relation_paged_chunk's
+// arguments.
+struct ChunkProblem {
+  const void* q;        // [N][H][d] (element strides qsT, qsH)
+  const void* k;        // pages [n_pages][page][Hk][d] (element strides sP, sR, sC)
+  const void* v;
+  const int* table;     // [B][cols] page ids, row stride t_stride
+  const int* starts;    // [B + 1] request b's tokens
+  const int* positions; // [N]
+  void* out;            // like q
+  float* logz;          // [N][H]
+  int* dev_status;
+  float lambda, tau_s, inv_sqrt_d;
+  int N, B, H, Hk, d, limit, n_pages, page;  // limit: rows that a table holds
+  unsigned page_mul;    // (set by the launcher: page_division)
+  int page_shift;
+  long long t_stride, sP, sR, sC, qsT, qsH;
+  relation_dtype dtype;
+};
+size_t chunk_workspace_bytes(int N, int B, int H, int Hk, int d, int limit, relation_dtype dt);
+cudaError_t launch_chunk(ChunkProblem p, void* workspace, cudaStream_t s);
+
 // The next token of every row (relation_sample.cu): relation_sample's arguments.
 struct SampleProblem {
   const void* logits;        // [R][V], row stride s_row

@@ -568,6 +568,57 @@ relation_status relation_paged_decode(const void* q, const void* k_pages, const 
   return from_cuda(rel::launch_paged(p, workspace, reinterpret_cast<cudaStream_t>(stream)));
 }
 
+namespace {
+
+// The sizes of a relation_paged_chunk call
+relation_status check_chunk(int N, int B, int H, int cols, const relation_pages& cache, relation_dtype dt) {
+  relation_status st;
+  if ((st = check_pages(cache, dt)) != RELATION_OK) return st;
+  if (N < 1 || B < 1 || H < 1 || H % cache.H || cols < 1) return RELATION_ERR_INVALID_ARG;
+  if (cache.d_h > 128) return RELATION_ERR_UNSUPPORTED;
+  // (row numbers a few units past the last one, and tiles and their heads, fit in 32 bits)
+  if ((long long)cols * cache.page_size > 0x7fffe000LL || (long long)N * H > 0x7fff0000LL ||
+      ((long long)N + B) * H > 0x7fff0000LL)
+    return RELATION_ERR_UNSUPPORTED;
+  return RELATION_OK;
+}
+
+}  // namespace
+
+size_t relation_paged_chunk_workspace_size(int N, int B, int H, int cols, relation_pages cache,
+                                           relation_dtype dt) {
+  if (check_chunk(N, B, H, cols, cache, dt) != RELATION_OK) return 0;
+  return rel::chunk_workspace_bytes(N, B, H, cache.H, cache.d_h, cols * cache.page_size, dt);
+}
+
+relation_status relation_paged_chunk(const void* q, const void* k_pages, const void* v_pages,
+                                     const int* block_table, int cols, long long table_stride,
+                                     const int* starts, const int* positions, void* o, float* logz,
+                                     float lambda, float tau_s, int N, int B, int H,
+                                     relation_pages cache, long long q_sT, long long q_sH,
+                                     relation_dtype dt, void* workspace, size_t ws_bytes,
+                                     int* dev_status, relation_stream_t stream) {
+  relation_status st;
+  if ((st = check_chunk(N, B, H, cols, cache, dt)) != RELATION_OK) return st;
+  if (table_stride < cols || q_sT < 1 || q_sH < 1) return RELATION_ERR_INVALID_ARG;
+  if ((st = check_scalars(lambda, tau_s)) != RELATION_OK) return st;
+  if ((st = check_elements({q, k_pages, v_pages, o}, elem_size(dt))) != RELATION_OK) return st;
+  if ((st = check_elements({block_table, starts, positions, logz}, 4)) != RELATION_OK) return st;
+  if (reinterpret_cast<uintptr_t>(dev_status) & 3u) return RELATION_ERR_ALIGNMENT;
+  const int limit = cols * cache.page_size;
+  if (!workspace || ws_bytes < rel::chunk_workspace_bytes(N, B, H, cache.H, cache.d_h, limit, dt))
+    return RELATION_ERR_WORKSPACE;
+  if (!aligned16(workspace)) return RELATION_ERR_ALIGNMENT;
+  rel::ChunkProblem p{};
+  p.q = q; p.k = k_pages; p.v = v_pages; p.table = block_table; p.starts = starts;
+  p.positions = positions; p.out = o; p.logz = logz; p.dev_status = dev_status;
+  p.lambda = lambda; p.tau_s = tau_s; p.inv_sqrt_d = 1.0f / sqrtf((float)cache.d_h);
+  p.N = N; p.B = B; p.H = H; p.Hk = cache.H; p.d = cache.d_h; p.limit = limit;
+  p.n_pages = cache.n_pages; p.page = cache.page_size; p.t_stride = table_stride; p.sP = cache.sP;
+  p.sR = cache.sR; p.sC = cache.sH; p.qsT = q_sT; p.qsH = q_sH; p.dtype = dt;
+  return from_cuda(rel::launch_chunk(p, workspace, reinterpret_cast<cudaStream_t>(stream)));
+}
+
 relation_status relation_sample(const void* logits, int R, int V, long long s_row,
                                 relation_dtype dt, const float* u, const float* temperature,
                                 const int* top_k, const float* top_p, const float* min_p,

@@ -1,0 +1,1023 @@
+// relation_chunk.cu -- the Relation rows of several new tokens per request over a paged key/value cache.
+//
+// A token at zero-based position p of request b, against rows 0 .. p of the request (row r in page
+// table[b][r / page_size]), as in relation_paged.cu:
+//   E_j = SiLU(q . k_j / sqrt(d)) for j < p,  L^E = log sum_j e^{E_j},  S = sigmoid(q . k_p / (sqrt(d) tau_S)),
+//   A = L^E - lambda log(p + 1),  g = sigmoid(A - S),
+//   Y = (1 - g) v_p + g sum_j e^{E_j} v_j / sum_j e^{E_j},  logZ = logaddexp(S, A).
+// G = H / H_kv query heads share a key/value head.
+//
+// A tile is kRows (token, query head of one key head) pairs of a request, token-major: shared heads and
+// short chunks fill it together.  The host knows neither counts nor positions, so a first small kernel lays
+// out the work: the tiles of all requests, each cut along its keys into so many pieces that about as many
+// pieces as CTAs fit the GPU have equal length, in an order that keeps the tiles of a request's head side by
+// side (they read the same keys) with the longest first.  A tile of one piece is finished by its CTA; of
+// others every piece leaves its rows' (m, l, z), which a last kernel joins.
+//
+// bf16: the tensor-core forward's scan (relation_tc_fwd.cu, scan.cuh) with keys and values gathered from
+// their pages by cp.async.  fp32: register tiles on the CUDA cores.
+#include <math.h>
+
+#include <type_traits>
+
+#include "common.cuh"
+#include "kernels.h"
+#include "scan.cuh"
+
+namespace rel {
+namespace chunk {
+
+constexpr int kUnit = 64;  // keys that are loaded together; pieces are made of them
+constexpr int kPlanThreads = 1024;
+
+// The workspace: what the plan says, and the pieces' partial results.
+struct Item {
+  int tile, head, piece, slot;  // slot: of the partial result, -1: the tile's only piece
+};
+struct Tile {
+  int b, row0, pieces, n;  // request, first row within it, pieces, units of keys (as far as the plan knows)
+};
+struct Plan {
+  int* head;     // {items, tiles of several pieces}
+  int* first;    // [B + 1] first tile of a request
+  Tile* tiles;   // [max_tiles]
+  int* upto;     // [max_tiles + 1] pieces before a tile
+  int2* split;   // [max_split] tiles of several pieces: {tile, first slot}
+  Item* items;   // [max_items]
+  float4* stats; // [slots][rows] m, l, self evidence, whether the piece has it
+  float* z;      // [slots][rows][width]
+  int max_tiles, max_items, max_split, slots, rows, width;
+};
+
+// What a block sums exclusively over its threads; `total` for all of them
+__device__ __forceinline__ int block_scan(int x, int* part, int* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  int s = x;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int y = __shfl_up_sync(0xffffffffu, s, o);
+    if (lane >= o) s += y;
+  }
+  if (lane == 31) part[warp] = s;
+  __syncthreads();
+  if (warp == 0) {
+    int t = lane < warps ? part[lane] : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(0xffffffffu, t, o);
+      if (lane >= o) t += y;
+    }
+    part[lane] = t;
+  }
+  __syncthreads();
+  const int before = warp > 0 ? part[warp - 1] : 0;
+  *total = part[warps - 1];
+  __syncthreads();
+  return before + s - x;
+}
+
+// Request b's tokens, as far as the buffer holds them
+__device__ __forceinline__ int2 tokens_of(const ChunkProblem& p, int b) {
+  const int s0 = min(max(p.starts[b], 0), p.N), s1 = min(max(p.starts[b + 1], s0), p.N);
+  return make_int2(s0, s1);
+}
+
+__global__ void __launch_bounds__(kPlanThreads)
+    plan_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w, int rows, int target,
+                int least) {
+  __shared__ int part[32];
+  __shared__ unsigned long long work;
+  pdl_wait_and_launch();
+  const int G = p.H / p.Hk;
+  int tiles = 0, total;
+  for (int b0 = 0; b0 < p.B; b0 += kPlanThreads) {
+    const int b = b0 + (int)threadIdx.x;
+    int n = 0;
+    if (b < p.B) {
+      const int2 t = tokens_of(p, b);
+      n = (int)(((long long)(t.y - t.x) * G + rows - 1) / rows);
+    }
+    const int at = tiles + block_scan(n, part, &total);
+    if (b < p.B) w.first[b] = at;
+    tiles += total;
+  }
+  if (threadIdx.x == 0) {
+    w.first[p.B] = tiles;
+    work = 0;
+  }
+  __syncthreads();
+  tiles = min(tiles, w.max_tiles);  // (requests whose tokens overlap: not laid out past the workspace)
+  unsigned long long mine = 0;
+  for (int i = threadIdx.x; i < tiles; i += kPlanThreads) {
+    int lo = 0, hi = p.B;  // the last request whose first tile is not after this one
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (w.first[mid] <= i) lo = mid; else hi = mid;
+    }
+    const int2 t = tokens_of(p, lo);
+    const int row0 = (i - w.first[lo]) * rows;
+    const int last = t.x + min((row0 + rows - 1) / G, t.y - t.x - 1);
+    const int pos = p.positions[last], n = pos < 0 || pos >= p.limit ? 1 : pos / kUnit + 1;
+    w.tiles[i] = {lo, row0, 1, n};
+    mine += n;
+  }
+  for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
+  if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&work, mine);
+  __syncthreads();
+  const unsigned long long all = work * p.Hk;
+  const int cap = (int)min(max((unsigned long long)least, (all + target - 1) / target), 1ull << 30);
+  int pieces = 0, splits = 0, slots = 0;
+  for (int i0 = 0; i0 < tiles; i0 += kPlanThreads) {
+    const int i = i0 + (int)threadIdx.x;
+    int n = 0;
+    if (i < tiles) {
+      n = (w.tiles[i].n + cap - 1) / cap;
+      w.tiles[i].pieces = n;
+    }
+    const bool is = n > 1;
+    const int at = pieces + block_scan(n, part, &total);
+    if (i < tiles) w.upto[i] = at;
+    pieces += total;
+    const int slot = slots + block_scan(is ? n * p.Hk : 0, part, &total);
+    slots += total;
+    const int s = splits + block_scan(is, part, &total);
+    splits += total;
+    if (is) w.split[s] = make_int2(i, slot);
+    if (i < tiles) w.tiles[i].n = is ? slot : -1;
+  }
+  if (threadIdx.x == 0) {
+    w.upto[tiles] = pieces;
+    w.head[0] = pieces * p.Hk;
+    w.head[1] = splits;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < tiles; i += kPlanThreads) {
+    const Tile t = w.tiles[i];
+    const int end = min(w.first[t.b + 1], tiles), from = w.upto[w.first[t.b]], per = w.upto[end] - from;
+    for (int h = 0; h < p.Hk; ++h)
+      for (int k = 0; k < t.pieces; ++k)
+        w.items[from * p.Hk + h * per + w.upto[end] - w.upto[i + 1] + k] = {
+            i, h, k, t.n < 0 ? -1 : t.n + h * t.pieces + k};
+  }
+}
+
+// One item's rows and keys
+struct Work {
+  int tile, head, slot, b, s0, rows, row0, u0, u1, kmin, kmax;
+};
+
+// Row `key` of a request: element offset in the pages
+__device__ __forceinline__ long long page_row(const ChunkProblem& p, const int* table, int key, int head) {
+  const int col = page_of(key, p.page, p.page_mul, p.page_shift);
+  int id = table[col];
+  if ((unsigned)id >= (unsigned)p.n_pages) {
+    if (p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
+    id = 0;
+  }
+  return (long long)id * p.sP + (long long)(key - col * p.page) * p.sR + (long long)head * p.sC;
+}
+
+// This CTA's item: ROWS threads each take a row's position (-1: none) and its element offset in q.  False: no
+// item.
+template <int ROWS>
+__device__ __forceinline__ bool take_item(const ChunkProblem& p, const Plan& w, Work& k, int* pos,
+                                          long long* off, int* lowest, int* highest) {
+  if ((int)blockIdx.x >= w.head[0]) return false;
+  const Item it = w.items[blockIdx.x];
+  const Tile t = w.tiles[it.tile];
+  const int2 tok = tokens_of(p, t.b);
+  const int G = p.H / p.Hk;
+  if (threadIdx.x == 0) {
+    *lowest = 0x7fffffff;
+    *highest = -1;
+  }
+  __syncthreads();
+  k.tile = it.tile; k.head = it.head; k.slot = it.slot; k.b = t.b; k.s0 = tok.x; k.row0 = t.row0;
+  k.rows = min(ROWS, (tok.y - tok.x) * G - t.row0);
+  if (threadIdx.x < ROWS) {
+    const int r = threadIdx.x;
+    int at = -1;
+    off[r] = -1;
+    if (r < k.rows) {
+      const int f = t.row0 + r, token = tok.x + f / G;
+      at = p.positions[token];
+      if (at >= p.limit) {
+        if (p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
+        at = -1;
+      }
+      at = max(at, -1);
+      off[r] = (long long)token * p.qsT + (long long)(it.head * G + f % G) * p.qsH;
+    }
+    pos[r] = at;
+    const int lo = __reduce_min_sync(0xffffffffu, at < 0 ? 0x7fffffff : at),
+              hi = __reduce_max_sync(0xffffffffu, at);
+    if ((r & 31) == 0) {
+      atomicMin(lowest, lo);
+      atomicMax(highest, hi);
+    }
+  }
+  __syncthreads();
+  k.kmin = *lowest; k.kmax = *highest;
+  const int n = k.kmax < 0 ? 0 : k.kmax / kUnit + 1;
+  k.u0 = (int)((long long)n * it.piece / t.pieces);
+  k.u1 = (int)((long long)n * (it.piece + 1) / t.pieces);
+  return true;
+}
+
+// The epilogue's scalars of a row from m (log2), l and its self evidence
+struct Mix {
+  float g, self, inv_l, logz;
+  __device__ __forceinline__ Mix(const ChunkProblem& p, float m, float l, float u_self, int pos) {
+    const float S = 1.0f / (1.0f + __expf(-(u_self * p.inv_sqrt_d) / p.tau_s));
+    g = 0.f; self = 1.f; inv_l = 0.f; logz = S;  // empty history
+    if (!(l == 0.f)) {                           // (a NaN goes on)
+      const float A = m * kLn2 + logf(l) - p.lambda * logf((float)(pos + 1));
+      g = 1.0f / (1.0f + __expf(S - A));
+      self = 1.0f / (1.0f + __expf(A - S));
+      const float hi = fmaxf(S, A), lo = fminf(S, A);
+      logz = hi + log1pf(__expf(lo - hi)) + 0.f * (A + S);  // (NaN in either)
+      inv_l = 1.0f / l;
+    }
+  }
+  __device__ __forceinline__ float y(float z, float v) const { return fmaf(g, z * inv_l, self * v); }
+};
+
+// ---------------------------------------------------------------------------------------------------
+// bf16
+// ---------------------------------------------------------------------------------------------------
+constexpr int BM = 128;
+
+// Warps 0-3 scan (thread = row = TMEM lane), warp 4 loads, warp 5 issues the products; as the forward:
+// d <= 64 four CTAs per SM and steps of 32 keys, else two and steps of 64.
+template <int D>
+struct Cfg {
+  static constexpr int SK = D == 64 ? 32 : 64;
+  static constexpr int CTAS = D == 64 ? 4 : 2;
+  static constexpr int TMEM_COLS = D == 64 ? 128 : 256;
+  static constexpr int OCOL = 2 * SK;
+  static constexpr int STAGES = 2;
+  static constexpr int SPL = kUnit / SK;       // steps of a unit
+  static constexpr int THREADS = 192;
+  static constexpr int KB = D / 64;            // 128-byte blocks of a row
+  static constexpr int UT = kUnit * D * 2;     // bytes of a unit's keys or values
+  static constexpr int OFF_Q = 0;
+  static constexpr int OFF_K = BM * D * 2;
+  static constexpr int OFF_V = OFF_K + STAGES * UT;
+  static constexpr int OFF_BAR = OFF_V + STAGES * UT;
+  static constexpr int OFF_POS = OFF_BAR + 256;
+  static constexpr int OFF_ROW = OFF_POS + BM * 4;
+  static constexpr int SMEM = OFF_ROW + BM * 8 + 1024;  // + alignment
+  static_assert(CTAS * (SMEM + 1024) <= 233472, "CTAs per SM");
+  static_assert(OCOL + D <= TMEM_COLS, "TMEM");
+};
+enum : int { B_KF = 0, B_KE = 2, B_VF = 4, B_VE = 6, B_S = 8, B_P = 10, B_OD = 12, B_O = 14, N_BAR = 15 };
+
+// 16 bytes, or zeros where !real
+__device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool real) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(real ? 16 : 0)
+               : "memory");
+}
+__device__ __forceinline__ void cp_wait_all() { asm volatile("cp.async.wait_all;" ::: "memory"); }
+// One arrival of this thread on `bar` when its copies so far have landed
+__device__ __forceinline__ void cp_arrive(uint32_t bar) {
+  asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Elements c .. c + 7 of a row of d, zeros past its end
+__device__ __forceinline__ uint4 load8(const __nv_bfloat16* row, int c, int d) {
+  union {
+    uint4 w;
+    unsigned short h[8];
+  } u;
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    u.h[e] = c + e < d ? reinterpret_cast<const unsigned short*>(row)[c + e] : (unsigned short)0;
+  return u.w;
+}
+__device__ __forceinline__ uint32_t unfinite_halves(uint32_t w) {  // 0xffff for each that is
+  return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
+}
+
+template <int D, bool VEC>
+__global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
+    chunk_tc_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w) {
+  using C = Cfg<D>;
+  using BF = __nv_bfloat16;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>(
+      (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
+  const uint32_t sb = smem_u32(smem);
+  auto bar = [&](int i) -> uint32_t { return sb + C::OFF_BAR + 8u * (uint32_t)i; };
+  static_assert(N_BAR * 8 <= 192, "barrier slots");
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_BAR + 192);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 200);
+  volatile int* special = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 204);
+  int* bounds = reinterpret_cast<int*>(smem + C::OFF_BAR + 208);
+  int* pos = reinterpret_cast<int*>(smem + C::OFF_POS);
+  long long* row_off = reinterpret_cast<long long*>(smem + C::OFF_ROW);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+  pdl_wait();
+  Work k;
+  if (!take_item<BM>(p, w, k, pos, row_off, bounds, bounds + 1)) return;
+  const BF* Q = static_cast<const BF*>(p.q);
+  const BF* K = static_cast<const BF*>(p.k);
+  const BF* V = static_cast<const BF*>(p.v);
+  const int* table = p.table + (long long)k.b * p.t_stride;
+  const int units = k.u1 - k.u0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::STAGES; ++s) {
+      mbar_init(bar(B_KF + s), 32);
+      mbar_init(bar(B_KE + s), 1);
+      mbar_init(bar(B_VF + s), 32);
+      mbar_init(bar(B_VE + s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(bar(B_S + b), 1);
+      mbar_init(bar(B_P + b), 128);
+      mbar_init(bar(B_OD + b), 1);
+    }
+    mbar_init(bar(B_O), 1);
+    *abort_flag = 0;
+    *special = 0;
+    fence_mbar_init();
+  }
+  if (warp == 5) tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
+  // the queries, 16-byte groups swizzled within 128 bytes; zeros for rows and columns that there are not
+  for (int e = threadIdx.x; e < BM * (D / 8); e += C::THREADS) {
+    const int r = e / (D / 8), c = e % (D / 8);
+    const long long off = row_off[r];
+    const bool real = off >= 0 && 8 * c < p.d;
+    const uint32_t dst = C::OFF_Q + (c >> 3) * (BM * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+    if (VEC) {
+      cp16(sb + dst, real ? Q + off + 8 * c : Q, real);
+    } else {
+      *reinterpret_cast<uint4*>(smem + dst) = real ? load8(Q + off, 8 * c, p.d) : make_uint4(0, 0, 0, 0);
+    }
+  }
+  cp_wait_all();
+  fence_async_smem();
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = *tmem_slot;
+  const Abort ab{abort_flag, p.dev_status};
+
+  if (warp == 4) {
+    // ---------------------------------------------------------------- keys and values, unit by unit
+    auto rows_of = [&](int j, long long& o0, long long& o1) {  // a lane's two rows of unit j, -1: none
+      const int key = (k.u0 + j) * kUnit + lane;
+      o0 = j < units && key <= k.kmax ? page_row(p, table, key, k.head) : -1;
+      o1 = j < units && key + 32 <= k.kmax ? page_row(p, table, key + 32, k.head) : -1;
+    };
+    auto fetch = [&](const BF* base, uint32_t stage, long long o0, long long o1) {
+      constexpr int CH = D / 8, PER = 32 / CH;  // groups of a row, rows at a time
+      const int c = lane % CH;
+#pragma unroll 8
+      for (int i = 0; i < kUnit / PER; ++i) {
+        const int r = i * PER + lane / CH;
+        const long long off = __shfl_sync(0xffffffffu, i * PER < 32 ? o0 : o1, r & 31);
+        const bool real = off >= 0 && 8 * c < p.d;
+        const uint32_t dst = stage + (c >> 3) * (kUnit * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+        if (VEC) {
+          cp16(sb + dst, real ? base + off + 8 * c : base, real);
+        } else {
+          *reinterpret_cast<uint4*>(smem + dst) =
+              real ? load8(base + off, 8 * c, p.d) : make_uint4(0, 0, 0, 0);
+        }
+      }
+    };
+    long long o0, o1, n0, n1;
+    rows_of(0, o0, o1);
+    for (int j = 0; j < units; ++j) {
+      const int s = j % C::STAGES, u = j / C::STAGES;
+      rows_of(j + 1, n0, n1);  // (the next unit's pages are looked up meanwhile)
+      if (u > 0 && !mbar_wait_warp(bar(B_KE + s), (u - 1) & 1, ab)) break;
+      fetch(K, C::OFF_K + s * C::UT, o0, o1);
+      if (VEC) {
+        cp_arrive(bar(B_KF + s));
+      } else {
+        fence_async_smem();
+        mbar_arrive(bar(B_KF + s));
+      }
+      if (u > 0 && !mbar_wait_warp(bar(B_VE + s), (u - 1) & 1, ab)) break;
+      const uint32_t at = C::OFF_V + s * C::UT;
+      fetch(V, at, o0, o1);
+      if (VEC && (k.u0 + j) * kUnit + kUnit - 1 < k.kmin) {
+        cp_arrive(bar(B_VF + s));
+      } else {
+        // Keys that some row does not see have weight 0 there, which an infinite or NaN value would turn
+        // into NaN: such values are taken out here, and the rows that see them get them at the end.
+        cp_wait_all();
+        __syncwarp();
+        if ((k.u0 + j) * kUnit + kUnit - 1 >= k.kmin) {
+          uint32_t bad = 0;
+#pragma unroll
+          for (int half = 0; half < 2; ++half) {
+            const int r = lane + 32 * half;
+#pragma unroll 4
+            for (int c = 0; c < D / 8; ++c) {
+              uint4* x = reinterpret_cast<uint4*>(smem + at + (c >> 3) * (kUnit * 128) + r * 128 +
+                                                  (((c & 7) ^ (r & 7)) << 4));
+              uint4 v = *x;
+              const uint4 f = make_uint4(unfinite_halves(v.x), unfinite_halves(v.y), unfinite_halves(v.z),
+                                         unfinite_halves(v.w));
+              if (f.x | f.y | f.z | f.w) {
+                *x = make_uint4(v.x & ~f.x, v.y & ~f.y, v.z & ~f.z, v.w & ~f.w);
+                bad = 1;
+              }
+            }
+          }
+          if (bad) *special = 1;
+        }
+        fence_async_smem();
+        mbar_arrive(bar(B_VF + s));
+      }
+      o0 = n0;
+      o1 = n1;
+    }
+    cp_wait_all();
+  } else if (warp == 5) {
+    // ---------------------------------------------------------------- products (as the forward's)
+    constexpr uint32_t idesc_qk = idesc_bf16_f32(BM, C::SK, false, false);
+    constexpr uint32_t idesc_pv = idesc_bf16_f32(BM, D, false, true);
+    const int total = units * C::SPL;
+    auto issue_u = [&](int s) -> bool {
+      const int j = s / C::SPL, hh = s % C::SPL, st = j % C::STAGES, bf = s & 1;
+      if (hh == 0) {
+        if (!mbar_wait_warp(bar(B_KF + st), (j / C::STAGES) & 1, ab)) return false;
+        fence_async_smem();  // (cp.async wrote the unit through the generic proxy)
+        tc_fence_after();
+      }
+#pragma unroll
+      for (int kk = 0; kk < D / 16; ++kk) {
+        const uint32_t koff = (kk >> 2) * (BM * 128) + (kk & 3) * 32;
+        const uint32_t kkoff = (kk >> 2) * (kUnit * 128) + (kk & 3) * 32;
+        const uint64_t a = smem_desc_sw128(sb + C::OFF_Q + koff, 16, 1024);
+        const uint64_t bd = smem_desc_sw128(sb + C::OFF_K + st * C::UT + hh * C::SK * 128 + kkoff, 16, 1024);
+        mma_ss_w(tmem + bf * C::SK, a, bd, idesc_qk, kk > 0 ? 1u : 0u);
+      }
+      mma_commit_w(bar(B_S + bf));
+      if (hh == C::SPL - 1) mma_commit_w(bar(B_KE + st));
+      return true;
+    };
+    bool ok = true;
+    for (int s = 0; ok && s < 2 && s < total; ++s) ok = issue_u(s);
+    for (int s = 0; ok && s < total; ++s) {
+      const int j = s / C::SPL, hh = s % C::SPL, st = j % C::STAGES, bf = s & 1;
+      if (hh == 0) {
+        if (!(ok = mbar_wait_warp(bar(B_VF + st), (j / C::STAGES) & 1, ab))) break;
+        fence_async_smem();
+      }
+      if (!(ok = mbar_wait_warp(bar(B_P + bf), (s / 2) & 1, ab))) break;
+      tc_fence_after();
+#pragma unroll
+      for (int kk = 0; kk < C::SK / 16; ++kk) {
+        const uint64_t bd = smem_desc_sw128(sb + C::OFF_V + st * C::UT + (hh * C::SK + kk * 16) * 128,
+                                            kUnit * 128, 1024);
+        mma_ts_w(tmem + C::OCOL, tmem + bf * C::SK + kk * 8, bd, idesc_pv, (s > 0 || kk > 0) ? 1u : 0u);
+      }
+      mma_commit_w(bar(B_OD + bf));
+      if (hh == C::SPL - 1) mma_commit_w(bar(B_VE + st));
+      if (s + 2 < total && !(ok = issue_u(s + 2))) break;
+    }
+    mma_commit_w(bar(B_O));
+    __syncwarp();
+  } else {
+    // ---------------------------------------------------------------- scan and epilogue
+    const int t = threadIdx.x, at = pos[t];
+    const bool any = __any_sync(0xffffffffu, at >= 0);
+    // the first key that some row of the warp does not take as history
+    const int first = __reduce_min_sync(0xffffffffu, at < 0 ? 0x7fffffff : at);
+    const uint32_t trow = tmem + ((uint32_t)(warp * 32) << 16);
+    const float isd = p.inv_sqrt_d, ch = 0.5f * isd, c2k = ch * kLog2e, bk = isd * kLog2e;
+    // (the scale's rules are those of the forward)
+    float m = -INFINITY, m_next = -INFINITY, l = 0.f, u_self = 0.f;
+    bool ok = true;
+    auto rescale = [&](bool go, float mn, int s_done, float* scp) -> bool {
+      const float sc = go ? ex2_approx(m - mn) : 1.0f;
+      if (scp) *scp = sc;
+      if (!__any_sync(0xffffffffu, go)) return true;
+      if (s_done >= 0) {
+        if (!mbar_wait_warp(bar(B_OD + (s_done & 1)), (s_done / 2) & 1, ab)) return false;
+        tc_fence_after();
+#pragma unroll
+        for (int c0 = 0; c0 < D; c0 += 32) {
+          uint32_t z[32];
+          tmem_ld32(trow + C::OCOL + c0, z);
+          tmem_ld_wait();
+#pragma unroll
+          for (int c = 0; c < 32; ++c) z[c] = __float_as_uint(__uint_as_float(z[c]) * sc);
+          tmem_st16(trow + C::OCOL + c0, z);
+          tmem_st16(trow + C::OCOL + c0 + 16, z + 16);
+        }
+      }
+      l *= sc;
+      if (go) m = mn;
+      return true;
+    };
+    const int total = units * C::SPL;
+    for (int s = 0; s < total; ++s) {
+      const int bf = s & 1, key0 = k.u0 * kUnit + s * C::SK;
+      if (!(ok = mbar_wait_warp(bar(B_S + bf), (s / 2) & 1, ab))) break;
+      if (any) {
+        tc_fence_after();
+        if (!(ok = rescale(m_next > m, m_next, s - 1, nullptr))) break;
+        const uint32_t ucol = trow + bf * C::SK;
+        const int tl = at - key0;  // keys before tl are the row's history, tl its own
+        const bool diag = key0 + C::SK > first;
+        float umax;
+        float2 rs;
+        if constexpr (C::SK == 32) {
+          uint32_t U[32], pk[16];
+          tmem_ld32(ucol, U);
+          tmem_ld_wait();
+          if (__any_sync(0xffffffffu, m == -INFINITY)) {
+            const float um = diag ? tc::row_max32<true>(U, tl, u_self) : tc::row_max32<false>(U, tl, u_self);
+            if (m == -INFINITY && um != -INFINITY) m = fmaxf(um, 0.f) * bk;
+          }
+          rs = diag ? tc::scan_p32<true>(U, tl, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self, pk)
+                    : tc::scan_p32<false>(U, tl, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self, pk);
+          const float mt = umax == -INFINITY ? -INFINITY : fmaxf(umax, 0.f) * bk;
+          const bool jump = mt > m + tc::kStaleLog2;
+          if (__any_sync(0xffffffffu, jump)) {
+            if (!(ok = rescale(jump, fmaxf(mt, m_next), s - 1, nullptr))) break;
+            rs = diag ? tc::scan_p32<true>(U, tl, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self, pk)
+                      : tc::scan_p32<false>(U, tl, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self, pk);
+          }
+          tmem_st16(ucol, pk);
+        } else {
+          uint32_t U[tc::HN];
+          tmem_ld32(ucol, U);
+          tmem_ld32(ucol + 32, U + 32);
+          tmem_ld_wait();
+          if (__any_sync(0xffffffffu, m == -INFINITY)) {
+            const float um = diag ? tc::row_max<true>(U, tl, u_self) : tc::row_max<false>(U, tl, u_self);
+            if (m == -INFINITY && um != -INFINITY) m = fmaxf(um, 0.f) * bk;
+          }
+          rs = diag ? tc::scan_p<true>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self)
+                    : tc::scan_p<false>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self);
+          const float mt = umax == -INFINITY ? -INFINITY : fmaxf(umax, 0.f) * bk;
+          const bool jump = mt > m + tc::kStaleLog2;
+          if (__any_sync(0xffffffffu, jump)) {
+            if (!(ok = rescale(jump, fmaxf(mt, m_next), s - 1, nullptr))) break;
+            rs = diag ? tc::scan_p<true>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self)
+                      : tc::scan_p<false>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self);
+          }
+        }
+        const float mt = umax == -INFINITY ? -INFINITY : fmaxf(umax, 0.f) * bk;
+        if (mt > m + tc::kRescaleLog2) m_next = fmaxf(m_next, mt);
+        l += rs.x + rs.y;
+        tmem_st_wait();
+        tc_fence_before();
+      }
+      mbar_arrive(bar(B_P + bf));
+    }
+    if (ok) ok = mbar_wait_warp(bar(B_O), 0, ab);
+    tc_fence_after();
+    if (ok && __any_sync(0xffffffffu, row_off[t] >= 0)) {
+      const bool part = k.slot >= 0, live = at >= 0;
+      const long long own = live && !part ? page_row(p, table, at, k.head) : 0;
+      const bool fix = *special != 0;
+      // the first unit in which some row does not see every key, in this piece
+      const int j0 = max(k.kmin / kUnit, k.u0) * kUnit, j1 = min(at, k.u1 * kUnit);
+      const Mix mix(p, m, l, u_self, max(at, 0));
+      uint8_t* stage = smem + C::OFF_Q + warp * (32 * D * 2) + lane * 128;
+#pragma unroll
+      for (int c0 = 0; c0 < D; c0 += 32) {
+        uint32_t zr[32];
+        if (units > 0) {
+          tmem_ld32(trow + C::OCOL + c0, zr);
+          tmem_ld_wait();
+        }
+        float z[32];
+#pragma unroll
+        for (int c = 0; c < 32; ++c) z[c] = units > 0 ? __uint_as_float(zr[c]) : 0.f;
+        if (fix && live) {  // rare: the values that were taken out
+          for (int j = j0; j < j1; ++j) {
+            const BF* v = V + page_row(p, table, j, k.head);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+              const float x = c0 + c < p.d ? (float)v[c0 + c] : 0.f;
+              if (!isfinite(x)) z[c] += x;
+            }
+          }
+        }
+        if (part) {
+          float* dst = w.z + ((long long)k.slot * w.rows + t) * w.width + c0;
+          if (live)
+#pragma unroll
+            for (int c = 0; c < 32; c += 4)
+              if (c0 + c < w.width)
+                *reinterpret_cast<float4*>(dst + c) = make_float4(z[c], z[c + 1], z[c + 2], z[c + 3]);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 32; c += 8) {
+            uint4 vv = make_uint4(0, 0, 0, 0);
+            if (live && c0 + c < p.d)
+              vv = VEC ? *reinterpret_cast<const uint4*>(V + own + c0 + c) : load8(V + own, c0 + c, p.d);
+            const uint32_t vw[4] = {vv.x, vv.y, vv.z, vv.w};
+            uint32_t yw[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float2 vf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&vw[e]));
+              yw[e] = live ? pack_bf16x2(mix.y(z[c + 2 * e], vf.x), mix.y(z[c + 2 * e + 1], vf.y)) : 0u;
+            }
+            const int g = ((c0 & 63) + c) >> 3;
+            *reinterpret_cast<uint4*>(stage + (c0 >> 6) * (32 * 128) + ((g ^ (lane & 7)) << 4)) =
+                make_uint4(yw[0], yw[1], yw[2], yw[3]);
+          }
+        }
+      }
+      if (part) {
+        if (live)
+          w.stats[(long long)k.slot * w.rows + t] =
+              make_float4(m, l, u_self, at >= k.u0 * kUnit && at < k.u1 * kUnit ? 1.f : 0.f);
+      } else {
+        __syncwarp();
+        constexpr int CH = D / 8, PER = 32 / CH;
+        const int c = lane % CH;
+        for (int i = 0; i < 32; i += PER) {
+          const int r = i + lane / CH;
+          const long long off = row_off[warp * 32 + r];
+          if (off < 0 || 8 * c >= p.d) continue;
+          const uint4 y = *reinterpret_cast<const uint4*>(smem + C::OFF_Q + warp * (32 * D * 2) + r * 128 +
+                                                          (c >> 3) * (32 * 128) + (((c & 7) ^ (r & 7)) << 4));
+          BF* dst = static_cast<BF*>(p.out) + off + 8 * c;
+          if (VEC) {
+            *reinterpret_cast<uint4*>(dst) = y;
+          } else {
+            const uint32_t yw[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (8 * c + e < p.d)
+                reinterpret_cast<unsigned short*>(dst)[e] = (unsigned short)(yw[e >> 1] >> (16 * (e & 1)));
+          }
+        }
+      }
+      // a row without a position is padding: zero, logz -inf (by its tile's first piece)
+      if (row_off[t] >= 0 && (!part || !live)) {
+        const int f = k.row0 + t, G = p.H / p.Hk;
+        const int token = k.s0 + f / G, head = k.head * G + f % G;
+        if (!part || k.u0 == 0) {
+          p.logz[(long long)token * p.H + head] = live ? mix.logz : -INFINITY;
+          if (part)
+            for (int c = 0; c < p.d; ++c) static_cast<BF*>(p.out)[row_off[t] + c] = (BF)0.f;
+        }
+      }
+    }
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 5) {
+    tc_fence_after();
+    tmem_dealloc(tmem, C::TMEM_COLS);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// fp32: 64 rows by 64 keys on 256 threads.  A thread has 4 rows by 4 keys of the scores, then 4 rows by
+// D / 16 columns of the products with the values; the weights pass through the keys' shared memory.
+// ---------------------------------------------------------------------------------------------------
+constexpr int SM_ROWS = 64, kSimtThreads = 256;
+
+template <int D>
+struct SimtSmem {
+  float q[SM_ROWS][D + 4];
+  union {
+    float k[kUnit][D + 4];
+    float pr[SM_ROWS][kUnit + 4];
+  };
+  float v[kUnit][D];
+  long long off[SM_ROWS], row[kUnit];
+  int pos[SM_ROWS], bounds[2];
+  float self[SM_ROWS];
+};
+
+template <int D, bool VEC>
+__global__ void __launch_bounds__(kSimtThreads, 2)
+    chunk_simt_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w) {
+  extern __shared__ __align__(16) uint8_t raw[];
+  SimtSmem<D>& sm = *reinterpret_cast<SimtSmem<D>*>(raw);
+  pdl_wait();
+  Work k;
+  if (!take_item<SM_ROWS>(p, w, k, sm.pos, sm.off, sm.bounds, sm.bounds + 1)) return;
+  const float* Q = static_cast<const float*>(p.q);
+  const int* table = p.table + (long long)k.b * p.t_stride;
+  const int ty = threadIdx.x / 16, tx = threadIdx.x % 16;
+  // rows of D columns at the offsets `at` (-1: zeros) into shared memory
+  auto fetch = [&](const float* base, const long long* at, float* dst, int stride, int rows) {
+    for (int e = threadIdx.x; e < rows * (D / 4); e += kSimtThreads) {
+      const int r = e / (D / 4), c = 4 * (e % (D / 4));
+      const long long off = at[r];
+      if (VEC) {
+        const bool real = off >= 0 && c < p.d;
+        cp16(smem_u32(dst + r * stride + c), real ? base + off + c : base, real);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dst[r * stride + c + i] = off >= 0 && c + i < p.d ? base[off + c + i] : 0.f;
+      }
+    }
+  };
+  fetch(Q, sm.off, &sm.q[0][0], D + 4, SM_ROWS);
+  int at[4];
+  float m[4], l[4], o[4][D / 16];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    at[i] = sm.pos[4 * ty + i];
+    m[i] = -INFINITY;
+    l[i] = 0.f;
+#pragma unroll
+    for (int c = 0; c < D / 16; ++c) o[i][c] = 0.f;
+  }
+  for (int u = k.u0; u < k.u1; ++u) {
+    const int key0 = u * kUnit;
+    __syncthreads();  // the unit before has been used
+    if (threadIdx.x < kUnit)
+      sm.row[threadIdx.x] = key0 + (int)threadIdx.x <= k.kmax ? page_row(p, table, key0 + threadIdx.x, k.head) : -1;
+    __syncthreads();
+    fetch(static_cast<const float*>(p.k), sm.row, &sm.k[0][0], D + 4, kUnit);
+    fetch(static_cast<const float*>(p.v), sm.row, &sm.v[0][0], D, kUnit);
+    cp_wait_all();
+    __syncthreads();
+    float s[4][4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) s[i][j] = 0.f;
+#pragma unroll 4
+    for (int c = 0; c < D; c += 4) {
+      float4 a[4], b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(&sm.q[4 * ty + i][c]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[j] = *reinterpret_cast<const float4*>(&sm.k[tx + 16 * j][c]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[i][j] = fmaf(a[i].x, b[j].x, s[i][j]);
+          s[i][j] = fmaf(a[i].y, b[j].y, s[i][j]);
+          s[i][j] = fmaf(a[i].z, b[j].z, s[i][j]);
+          s[i][j] = fmaf(a[i].w, b[j].w, s[i][j]);
+        }
+    }
+    const bool masked = key0 + kUnit - 1 >= k.kmin;  // some row does not see every key
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float mx = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int key = key0 + tx + 16 * j;
+        const float x = s[i][j] * p.inv_sqrt_d;
+        if (key == at[i]) sm.self[4 * ty + i] = s[i][j];
+        // SiLU in units of log 2
+        s[i][j] = key < at[i] ? __fdividef(x, 1.0f + ex2_approx(-x * kLog2e)) * kLog2e : -INFINITY;
+        mx = fmaxf(mx, s[i][j]);
+      }
+#pragma unroll
+      for (int e = 1; e < 16; e <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, e));
+      const float to = fmaxf(m[i], mx), base = to == -INFINITY ? 0.f : to;
+      const float f = m[i] == -INFINITY ? 1.f : ex2_approx(m[i] - base);
+      m[i] = to;
+      l[i] *= f;
+#pragma unroll
+      for (int c = 0; c < D / 16; ++c) o[i][c] *= f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        s[i][j] = ex2_approx(s[i][j] - base);
+        l[i] += s[i][j];
+      }
+    }
+    __syncthreads();  // the keys have been read: the weights take their place
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sm.pr[4 * ty + i][tx + 16 * j] = s[i][j];
+    __syncthreads();
+    auto add = [&](auto mask) {
+#pragma unroll 2
+      for (int j = 0; j < kUnit; j += 4) {
+        float4 a[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) a[i] = *reinterpret_cast<const float4*>(&sm.pr[4 * ty + i][j]);
+#pragma unroll
+        for (int jj = 0; jj < 4; ++jj)
+#pragma unroll
+          for (int e = 0; e < D / 64; ++e) {
+            const float4 v = *reinterpret_cast<const float4*>(&sm.v[j + jj][64 * e + 4 * tx]);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float x = jj == 0 ? a[i].x : jj == 1 ? a[i].y : jj == 2 ? a[i].z : a[i].w;
+              // (a weight of 0 for a key that the row does not see would turn its infinity into NaN)
+              if (decltype(mask)::value && key0 + j + jj >= at[i]) continue;
+              o[i][4 * e] = fmaf(x, v.x, o[i][4 * e]);
+              o[i][4 * e + 1] = fmaf(x, v.y, o[i][4 * e + 1]);
+              o[i][4 * e + 2] = fmaf(x, v.z, o[i][4 * e + 2]);
+              o[i][4 * e + 3] = fmaf(x, v.w, o[i][4 * e + 3]);
+            }
+          }
+      }
+    };
+    if (masked) add(std::true_type()); else add(std::false_type());
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+#pragma unroll
+    for (int e = 1; e < 16; e <<= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], e);
+    const int r = 4 * ty + i;
+    if (sm.off[r] < 0) continue;
+    const bool live = at[i] >= 0, has = at[i] >= k.u0 * kUnit && at[i] < k.u1 * kUnit;
+    const float u_self = has ? sm.self[r] : 0.f;
+    if (k.slot >= 0 && live) {
+      float* dst = w.z + ((long long)k.slot * w.rows + r) * w.width;
+#pragma unroll
+      for (int e = 0; e < D / 64; ++e)
+        if (64 * e + 4 * tx < w.width)
+          *reinterpret_cast<float4*>(dst + 64 * e + 4 * tx) =
+              make_float4(o[i][4 * e], o[i][4 * e + 1], o[i][4 * e + 2], o[i][4 * e + 3]);
+      if (tx == 0)
+        w.stats[(long long)k.slot * w.rows + r] = make_float4(m[i], l[i], u_self, has ? 1.f : 0.f);
+      continue;
+    }
+    if (k.slot >= 0 && k.u0 > 0) continue;  // (padding: by its tile's first piece)
+    const Mix mix(p, m[i], l[i], u_self, max(at[i], 0));
+    const float* V = static_cast<const float*>(p.v) + (live ? page_row(p, table, at[i], k.head) : 0);
+    float* y = static_cast<float*>(p.out) + sm.off[r];
+#pragma unroll
+    for (int e = 0; e < D / 64; ++e)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const int col = 64 * e + 4 * tx + c;
+        if (col < p.d) y[col] = live ? mix.y(o[i][4 * e + c], V[col]) : 0.f;
+      }
+    if (tx == 0) {
+      const int f = k.row0 + r, G = p.H / p.Hk;
+      p.logz[(long long)(k.s0 + f / G) * p.H + k.head * G + f % G] = live ? mix.logz : -INFINITY;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// The rows of tiles of several pieces, a warp each; zeros for the tokens of no request.
+// ---------------------------------------------------------------------------------------------------
+constexpr int kJoinThreads = 256;
+
+template <typename TI>
+__global__ void __launch_bounds__(kJoinThreads)
+    join_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w) {
+  pdl_wait_and_launch();
+  const int lane = threadIdx.x & 31, G = p.H / p.Hk;
+  const long long first = ((long long)blockIdx.x * kJoinThreads + threadIdx.x) >> 5,
+                  step = (long long)gridDim.x * (kJoinThreads / 32);
+  const long long rows = (long long)w.head[1] * p.Hk * w.rows;
+  for (long long e = first; e < rows; e += step) {
+    const int r = (int)(e % w.rows), h = (int)(e / w.rows % p.Hk);
+    const int2 s = w.split[e / w.rows / p.Hk];
+    const Tile t = w.tiles[s.x];
+    const int2 tok = tokens_of(p, t.b);
+    const int f = t.row0 + r;
+    if (f >= (tok.y - tok.x) * G) continue;
+    const int token = tok.x + f / G, head = h * G + f % G, at = p.positions[token];
+    if (at < 0 || at >= p.limit) continue;  // (zeros have been written)
+    const long long slot = s.y + h * t.pieces;
+    float m = -INFINITY, l = 0.f, u_self = 0.f, z[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int k = lane; k < t.pieces; k += 32) m = fmaxf(m, w.stats[(slot + k) * w.rows + r].x);
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    for (int k0 = 0; k0 < t.pieces; k0 += 32) {
+      float4 st = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+      if (k0 + lane < t.pieces) st = w.stats[(slot + k0 + lane) * w.rows + r];
+      // no key seen: 0; m is -inf too where every score is NaN (l NaN): NaN
+      const float wt = st.x == -INFINITY ? 0.f * st.y : ex2_approx(st.x - m);
+      const unsigned who = __ballot_sync(0xffffffffu, st.w != 0.f);
+      if (who) u_self = __shfl_sync(0xffffffffu, st.z, __ffs(who) - 1);
+      const int n = min(32, t.pieces - k0);
+#pragma unroll 4
+      for (int k = 0; k < n; ++k) {
+        const float f = __shfl_sync(0xffffffffu, wt, k), lk = __shfl_sync(0xffffffffu, st.y, k);
+        if (lk == 0.f) continue;  // (and no z there)
+        l = fmaf(f, lk, l);
+        const float* src = w.z + ((slot + k0 + k) * w.rows + r) * w.width;
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+          if (lane + 32 * c < p.d) z[c] = fmaf(f, src[lane + 32 * c], z[c]);
+      }
+    }
+    const Mix mix(p, m, l, u_self, at);
+    const TI* V = static_cast<const TI*>(p.v) + page_row(p, p.table + (long long)t.b * p.t_stride, at, h);
+    TI* y = static_cast<TI*>(p.out) + (long long)token * p.qsT + (long long)head * p.qsH;
+#pragma unroll
+    for (int c = 0; c < 4; ++c)
+      if (lane + 32 * c < p.d) y[lane + 32 * c] = (TI)mix.y(z[c], (float)V[lane + 32 * c]);
+    if (lane == 0) p.logz[(long long)token * p.H + head] = mix.logz;
+  }
+  const int before = min(max(p.starts[0], 0), p.N), after = min(max(p.starts[p.B], before), p.N);
+  const long long none = (long long)(before + p.N - after) * p.H;
+  for (long long e = first; e < none; e += step) {
+    const int i = (int)(e / p.H), head = (int)(e % p.H), token = i < before ? i : after + i - before;
+    TI* y = static_cast<TI*>(p.out) + (long long)token * p.qsT + (long long)head * p.qsH;
+    for (int c = lane; c < p.d; c += 32) y[c] = (TI)0.f;
+    if (lane == 0) p.logz[(long long)token * p.H + head] = -INFINITY;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------------------------------
+struct Sizes {
+  int rows, target, least;  // rows of a tile, pieces aimed at, units that a piece has at least
+};
+Sizes sizes_of(int d, relation_dtype dt) {
+  if (dt == RELATION_F32) return {SM_ROWS, 304, 4};
+  return {BM, d <= 64 ? 608 : 304, 4};
+}
+
+// The plan's arrays in a workspace; the bytes of it
+size_t carve(Plan* w, uint8_t* base, int N, int B, int H, int Hk, int d, int limit, relation_dtype dt) {
+  const Sizes z = sizes_of(d, dt);
+  const long long G = H / Hk, rows = N * G;
+  // a request of n rows has ceil(n / tile) tiles, and no more requests than tokens have any
+  const long long tiles = (rows + (long long)(B < N ? B : N) * (z.rows - 1)) / z.rows + 1;
+  const long long units = ((long long)limit + kUnit - 1) / kUnit;
+  const long long most = (units + z.least - 1) / z.least;  // pieces of a tile
+  // Pieces are as long as the mean of `target` pieces at least: all tiles have one and `target` more are
+  // enough for the rest; a tile of several has them longer than half of that mean.
+  const long long items = tiles * Hk + (tiles * Hk * (most - 1) < z.target ? tiles * Hk * (most - 1) : z.target);
+  long long slots = 2LL * z.target;
+  if (tiles * Hk * most < slots) slots = tiles * Hk * most;
+  const long long split = tiles < slots ? tiles : slots;
+  w->max_tiles = (int)tiles;
+  w->max_items = (int)items;
+  w->max_split = (int)split;
+  w->slots = most > 1 ? (int)slots : 0;
+  w->rows = rows < z.rows ? (int)rows : z.rows;
+  w->width = (d + 3) & ~3;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    uint8_t* x = base + at;
+    at += (bytes + 15) & ~(size_t)15;
+    return x;
+  };
+  w->head = reinterpret_cast<int*>(take(16));
+  w->first = reinterpret_cast<int*>(take((size_t)(B + 1) * 4));
+  w->tiles = reinterpret_cast<Tile*>(take((size_t)tiles * sizeof(Tile)));
+  w->upto = reinterpret_cast<int*>(take((size_t)(tiles + 1) * 4));
+  w->split = reinterpret_cast<int2*>(take((size_t)split * 8));
+  w->items = reinterpret_cast<Item*>(take((size_t)items * sizeof(Item)));
+  w->stats = reinterpret_cast<float4*>(take((size_t)w->slots * w->rows * 16));
+  w->z = reinterpret_cast<float*>(take((size_t)w->slots * w->rows * w->width * 4));
+  return at;
+}
+
+template <typename K>
+cudaError_t launch_main(K kernel, int threads, int smem, const ChunkProblem& p, const Plan& w, cudaStream_t s) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(w.max_items), threads, smem, s, 1, p, w);
+  if (e != cudaSuccess) note_failure("chunk: launch");
+  return e;
+}
+
+template <bool VEC>
+cudaError_t launch_v(const ChunkProblem& p, const Plan& w, cudaStream_t s) {
+  if (p.dtype == RELATION_BF16)
+    return p.d <= 64 ? launch_main(chunk_tc_kernel<64, VEC>, Cfg<64>::THREADS, Cfg<64>::SMEM, p, w, s)
+                     : launch_main(chunk_tc_kernel<128, VEC>, Cfg<128>::THREADS, Cfg<128>::SMEM, p, w, s);
+  return p.d <= 64
+             ? launch_main(chunk_simt_kernel<64, VEC>, kSimtThreads, (int)sizeof(SimtSmem<64>), p, w, s)
+             : launch_main(chunk_simt_kernel<128, VEC>, kSimtThreads, (int)sizeof(SimtSmem<128>), p, w, s);
+}
+
+}  // namespace chunk
+
+size_t chunk_workspace_bytes(int N, int B, int H, int Hk, int d, int limit, relation_dtype dt) {
+  chunk::Plan w;
+  return chunk::carve(&w, nullptr, N, B, H, Hk, d, limit, dt);
+}
+
+cudaError_t launch_chunk(ChunkProblem p, void* workspace, cudaStream_t s) {
+  using namespace chunk;
+  page_division(p.page, &p.page_mul, &p.page_shift);
+  Plan w;
+  carve(&w, static_cast<uint8_t*>(workspace), p.N, p.B, p.H, p.Hk, p.d, p.limit, p.dtype);
+  const Sizes z = sizes_of(p.d, p.dtype);
+  cudaError_t e = launch_pdl(plan_kernel, dim3(1), kPlanThreads, 0, s, 1, p, w, z.rows, z.target, z.least);
+  if (e != cudaSuccess) {
+    note_failure("chunk: plan launch");
+    return e;
+  }
+  const int es = p.dtype == RELATION_F32 ? 4 : 2;
+  uintptr_t low = 0;
+  for (const void* x : {p.q, p.k, p.v, (const void*)p.out}) low |= reinterpret_cast<uintptr_t>(x);
+  for (long long x : {p.N > 1 ? p.qsT : 0, p.H > 1 ? p.qsH : 0, p.n_pages > 1 ? p.sP : 0,
+                      p.page > 1 ? p.sR : 0, p.Hk > 1 ? p.sC : 0, (long long)p.d})
+    low |= (uintptr_t)(x * es);
+  e = low % 16 == 0 ? launch_v<true>(p, w, s) : launch_v<false>(p, w, s);
+  if (e != cudaSuccess) return e;
+  e = p.dtype == RELATION_F32 ? launch_pdl(join_kernel<float>, dim3(304), kJoinThreads, 0, s, 1, p, w)
+                              : launch_pdl(join_kernel<__nv_bfloat16>, dim3(304), kJoinThreads, 0, s, 1, p, w);
+  if (e != cudaSuccess) note_failure("chunk: join launch");
+  return e;
+}
+
+}  // namespace rel
