@@ -14,8 +14,10 @@
 // side (they read the same keys) with the longest first.  A tile of one piece is finished by its CTA; of
 // others every piece leaves its rows' (m, l, z), which a last kernel joins.
 //
-// bf16: the tensor-core forward's scan (relation_tc_fwd.cu, scan.cuh) with keys and values gathered from
-// their pages by cp.async.  fp32: register tiles on the CUDA cores.
+// bf16: the tensor-core forward's scan (relation_tc_fwd.cu, scan.cuh) with keys and values fetched from
+// their pages by TMA, a box of rows that lie in one page at a time (cp.async, row by row, for pages whose
+// size is no multiple of 8).  fp32: register tiles on the CUDA cores.
+#include <cudaTypedefs.h>
 #include <math.h>
 
 #include <type_traits>
@@ -270,7 +272,9 @@ struct Cfg {
   static_assert(CTAS * (SMEM + 1024) <= 233472, "CTAs per SM");
   static_assert(OCOL + D <= TMEM_COLS, "TMEM");
 };
-enum : int { B_KF = 0, B_KE = 2, B_VF = 4, B_VE = 6, B_S = 8, B_P = 10, B_OD = 12, B_O = 14, N_BAR = 15 };
+enum : int { B_KF = 0, B_KE = 2, B_VF = 4, B_VE = 6, B_S = 8, B_P = 10, B_OD = 12, B_O = 14, B_VR = 15, N_BAR = 16 };
+// How a unit's rows are fetched: element by element, in 16-byte groups, by TMA in boxes of rows of a page
+enum : int { kElements = 0, kGroups = 1, kBoxes = 2 };
 
 // 16 bytes, or zeros where !real
 __device__ __forceinline__ void cp16(uint32_t dst, const void* src, bool real) {
@@ -297,9 +301,12 @@ __device__ __forceinline__ uint32_t unfinite_halves(uint32_t w) {  // 0xffff for
   return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
 
-template <int D, bool VEC>
+// box: rows of a TMA box (a power of two, 8 to 64, that divides the page size)
+template <int D, int LOAD>
 __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
-    chunk_tc_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w) {
+    chunk_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                    const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w, int box) {
+  constexpr bool VEC = LOAD != kElements;
   using C = Cfg<D>;
   using BF = __nv_bfloat16;
   extern __shared__ uint8_t smem_raw[];
@@ -327,11 +334,12 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) {
-      mbar_init(bar(B_KF + s), 32);
+      mbar_init(bar(B_KF + s), LOAD == kBoxes ? 1 : 32);
       mbar_init(bar(B_KE + s), 1);
-      mbar_init(bar(B_VF + s), 32);
+      mbar_init(bar(B_VF + s), LOAD == kBoxes ? 1 : 32);
       mbar_init(bar(B_VE + s), 1);
     }
+    mbar_init(bar(B_VR), 1);
     for (int b = 0; b < 2; ++b) {
       mbar_init(bar(B_S + b), 1);
       mbar_init(bar(B_P + b), 128);
@@ -365,92 +373,149 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
 
   if (warp == 4) {
     // ---------------------------------------------------------------- keys and values, unit by unit
-    auto rows_of = [&](int j, long long& o0, long long& o1) {  // a lane's two rows of unit j, -1: none
-      const int key = (k.u0 + j) * kUnit + lane;
-      o0 = j < units && key <= k.kmax ? page_row(p, table, key, k.head) : -1;
-      o1 = j < units && key + 32 <= k.kmax ? page_row(p, table, key + 32, k.head) : -1;
-    };
-    auto fetch = [&](const BF* base, uint32_t stage, long long o0, long long o1) {
-      constexpr int CH = D / 8, PER = 32 / CH;  // groups of a row, rows at a time
-      const int c = lane % CH;
-#pragma unroll 8
-      for (int i = 0; i < kUnit / PER; ++i) {
-        const int r = i * PER + lane / CH;
-        const long long off = __shfl_sync(0xffffffffu, i * PER < 32 ? o0 : o1, r & 31);
-        const bool real = off >= 0 && 8 * c < p.d;
-        const uint32_t dst = stage + (c >> 3) * (kUnit * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-        if (VEC) {
-          cp16(sb + dst, real ? base + off + 8 * c : base, real);
-        } else {
-          *reinterpret_cast<uint4*>(smem + dst) =
-              real ? load8(base + off, 8 * c, p.d) : make_uint4(0, 0, 0, 0);
-        }
-      }
-    };
-    long long o0, o1, n0, n1;
-    rows_of(0, o0, o1);
-    for (int j = 0; j < units; ++j) {
-      const int s = j % C::STAGES, u = j / C::STAGES;
-      rows_of(j + 1, n0, n1);  // (the next unit's pages are looked up meanwhile)
-      if (u > 0 && !mbar_wait_warp(bar(B_KE + s), (u - 1) & 1, ab)) break;
-      fetch(K, C::OFF_K + s * C::UT, o0, o1);
-      if (VEC) {
-        cp_arrive(bar(B_KF + s));
-      } else {
-        fence_async_smem();
-        mbar_arrive(bar(B_KF + s));
-      }
-      if (u > 0 && !mbar_wait_warp(bar(B_VE + s), (u - 1) & 1, ab)) break;
-      const uint32_t at = C::OFF_V + s * C::UT;
-      fetch(V, at, o0, o1);
-      if (VEC && (k.u0 + j) * kUnit + kUnit - 1 < k.kmin) {
-        cp_arrive(bar(B_VF + s));
-      } else {
-        // Keys that some row does not see have weight 0 there, which an infinite or NaN value would turn
-        // into NaN: such values are taken out here, and the rows that see them get them at the end.
-        cp_wait_all();
-        __syncwarp();
-        if ((k.u0 + j) * kUnit + kUnit - 1 >= k.kmin) {
-          uint32_t bad = 0;
+    // Keys that some row does not see have weight 0 there, which an infinite or NaN value would turn into
+    // NaN: in the units of such keys (and of rows behind the last key, whatever they hold) these values are
+    // taken out of shared memory, and the rows that see them get them at the end.
+    auto masked = [&](int j) { return (k.u0 + j) * kUnit + kUnit - 1 >= k.kmin; };
+    auto clean = [&](uint32_t at, int j) {
+      bool bad = false;
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            const int r = lane + 32 * half;
+      for (int half = 0; half < 2; ++half) {
+        const int r = lane + 32 * half;
 #pragma unroll 4
-            for (int c = 0; c < D / 8; ++c) {
-              uint4* x = reinterpret_cast<uint4*>(smem + at + (c >> 3) * (kUnit * 128) + r * 128 +
-                                                  (((c & 7) ^ (r & 7)) << 4));
-              uint4 v = *x;
-              const uint4 f = make_uint4(unfinite_halves(v.x), unfinite_halves(v.y), unfinite_halves(v.z),
-                                         unfinite_halves(v.w));
-              if (f.x | f.y | f.z | f.w) {
-                *x = make_uint4(v.x & ~f.x, v.y & ~f.y, v.z & ~f.z, v.w & ~f.w);
-                bad = 1;
-              }
-            }
+        for (int c = 0; c < D / 8; ++c) {
+          uint4* x = reinterpret_cast<uint4*>(smem + at + (c >> 3) * (kUnit * 128) + r * 128 +
+                                              (((c & 7) ^ (r & 7)) << 4));
+          const uint4 v = *x;
+          const uint4 f = make_uint4(unfinite_halves(v.x), unfinite_halves(v.y), unfinite_halves(v.z),
+                                     unfinite_halves(v.w));
+          if (f.x | f.y | f.z | f.w) {
+            *x = make_uint4(v.x & ~f.x, v.y & ~f.y, v.z & ~f.z, v.w & ~f.w);
+            bad |= (k.u0 + j) * kUnit + r <= k.kmax;
           }
-          if (bad) *special = 1;
         }
-        fence_async_smem();
-        mbar_arrive(bar(B_VF + s));
       }
-      o0 = n0;
-      o1 = n1;
+      if (bad) *special = 1;
+      fence_async_smem();
+      __syncwarp();
+    };
+    if constexpr (LOAD == kBoxes) {
+      // A lane has one box of a unit, of one 64-column block of the keys or the values
+      const int boxes = kUnit / box, mine = lane % boxes, kb = lane / boxes;
+      auto page_at = [&](int j) {  // {page, row in it} of the lane's box of unit j; -1: none
+        const int key = (k.u0 + j) * kUnit + mine * box;
+        if (j >= units || key > k.kmax || kb >= C::KB) return make_int2(-1, 0);
+        const int col = page_of(key, p.page, p.page_mul, p.page_shift);
+        int id = table[col];
+        if ((unsigned)id >= (unsigned)p.n_pages) {
+          if (p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
+          id = 0;
+        }
+        return make_int2(id, key - col * p.page);
+      };
+      auto fetch = [&](const CUtensorMap* map, uint32_t stage, uint32_t full, int2 at) {
+        const unsigned who = __ballot_sync(0xffffffffu, at.x >= 0);
+        if (lane == 0) mbar_arrive_expect_tx(full, __popc(who) * box * 128);
+        __syncwarp();
+        if (at.x >= 0)
+          tma_load_4d(sb + stage + kb * (kUnit * 128) + mine * box * 128, map, full, kb * 64, at.y, k.head, at.x);
+      };
+      int2 at = page_at(0);
+      int issued = 0, raw = 0;
+      for (int j = 0; j < units; ++j) {
+        const int s = j % C::STAGES, u = j / C::STAGES;
+        const int2 next = page_at(j + 1);  // (the next unit's pages are looked up meanwhile)
+        if (u > 0 && !mbar_wait_warp(bar(B_KE + s), (u - 1) & 1, ab)) break;
+        fetch(&tmK, C::OFF_K + s * C::UT, bar(B_KF + s), at);
+        issued = j + 1;
+        if (u > 0 && !mbar_wait_warp(bar(B_VE + s), (u - 1) & 1, ab)) break;
+        const uint32_t vs = C::OFF_V + s * C::UT;
+        if (!masked(j)) {
+          fetch(&tmV, vs, bar(B_VF + s), at);
+        } else {
+          fetch(&tmV, vs, bar(B_VR), at);
+          if (!mbar_wait_warp(bar(B_VR), raw & 1, ab)) break;
+          ++raw;
+          clean(vs, j);
+          if (lane == 0) mbar_arrive(bar(B_VF + s));
+        }
+        at = next;
+      }
+      if (ab.raised()) {  // copies in flight land before the CTA gives up its shared memory
+        for (int j = max(issued - C::STAGES, 0); j < issued; ++j) {
+          tc::drain_wait(bar(B_KF + j % C::STAGES), (j / C::STAGES) & 1);
+          tc::drain_wait(bar(B_VF + j % C::STAGES), (j / C::STAGES) & 1);
+        }
+        tc::drain_wait(bar(B_VR), raw & 1);
+      }
+    } else {
+      auto rows_of = [&](int j, long long& o0, long long& o1) {  // a lane's two rows of unit j, -1: none
+        const int key = (k.u0 + j) * kUnit + lane;
+        o0 = j < units && key <= k.kmax ? page_row(p, table, key, k.head) : -1;
+        o1 = j < units && key + 32 <= k.kmax ? page_row(p, table, key + 32, k.head) : -1;
+      };
+      auto fetch = [&](const BF* base, uint32_t stage, long long o0, long long o1) {
+        constexpr int CH = D / 8, PER = 32 / CH;  // groups of a row, rows at a time
+        const int c = lane % CH;
+#pragma unroll 8
+        for (int i = 0; i < kUnit / PER; ++i) {
+          const int r = i * PER + lane / CH;
+          const long long off = __shfl_sync(0xffffffffu, i * PER < 32 ? o0 : o1, r & 31);
+          const bool real = off >= 0 && 8 * c < p.d;
+          const uint32_t dst = stage + (c >> 3) * (kUnit * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+          if (VEC) {
+            cp16(sb + dst, real ? base + off + 8 * c : base, real);
+          } else {
+            *reinterpret_cast<uint4*>(smem + dst) =
+                real ? load8(base + off, 8 * c, p.d) : make_uint4(0, 0, 0, 0);
+          }
+        }
+      };
+      long long o0, o1, n0, n1;
+      rows_of(0, o0, o1);
+      for (int j = 0; j < units; ++j) {
+        const int s = j % C::STAGES, u = j / C::STAGES;
+        rows_of(j + 1, n0, n1);  // (the next unit's pages are looked up meanwhile)
+        if (u > 0 && !mbar_wait_warp(bar(B_KE + s), (u - 1) & 1, ab)) break;
+        fetch(K, C::OFF_K + s * C::UT, o0, o1);
+        if (VEC) {
+          cp_arrive(bar(B_KF + s));
+        } else {
+          fence_async_smem();
+          mbar_arrive(bar(B_KF + s));
+        }
+        if (u > 0 && !mbar_wait_warp(bar(B_VE + s), (u - 1) & 1, ab)) break;
+        const uint32_t at = C::OFF_V + s * C::UT;
+        fetch(V, at, o0, o1);
+        if (VEC && !masked(j)) {
+          cp_arrive(bar(B_VF + s));
+        } else {
+          cp_wait_all();
+          __syncwarp();
+          if (masked(j)) clean(at, j); else fence_async_smem();
+          mbar_arrive(bar(B_VF + s));
+        }
+        o0 = n0;
+        o1 = n1;
+      }
+      cp_wait_all();
     }
-    cp_wait_all();
   } else if (warp == 5) {
     // ---------------------------------------------------------------- products (as the forward's)
     constexpr uint32_t idesc_qk = idesc_bf16_f32(BM, C::SK, false, false);
-    constexpr uint32_t idesc_pv = idesc_bf16_f32(BM, D, false, true);
+    const int dk = (p.d + 15) / 16;  // 16-column steps; z has as many columns
+    const uint32_t idesc_pv = idesc_bf16_f32(BM, 16 * dk, false, true);
     const int total = units * C::SPL;
     auto issue_u = [&](int s) -> bool {
       const int j = s / C::SPL, hh = s % C::SPL, st = j % C::STAGES, bf = s & 1;
       if (hh == 0) {
         if (!mbar_wait_warp(bar(B_KF + st), (j / C::STAGES) & 1, ab)) return false;
-        fence_async_smem();  // (cp.async wrote the unit through the generic proxy)
+        if (LOAD != kBoxes) fence_async_smem();  // (cp.async wrote the unit through the generic proxy)
         tc_fence_after();
       }
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
+        if (kk >= dk) break;
         const uint32_t koff = (kk >> 2) * (BM * 128) + (kk & 3) * 32;
         const uint32_t kkoff = (kk >> 2) * (kUnit * 128) + (kk & 3) * 32;
         const uint64_t a = smem_desc_sw128(sb + C::OFF_Q + koff, 16, 1024);
@@ -467,7 +532,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
       const int j = s / C::SPL, hh = s % C::SPL, st = j % C::STAGES, bf = s & 1;
       if (hh == 0) {
         if (!(ok = mbar_wait_warp(bar(B_VF + st), (j / C::STAGES) & 1, ab))) break;
-        fence_async_smem();
+        if (LOAD != kBoxes) fence_async_smem();
       }
       if (!(ok = mbar_wait_warp(bar(B_P + bf), (s / 2) & 1, ab))) break;
       tc_fence_after();
@@ -503,6 +568,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
         tc_fence_after();
 #pragma unroll
         for (int c0 = 0; c0 < D; c0 += 32) {
+          if (c0 >= p.d) break;
           uint32_t z[32];
           tmem_ld32(trow + C::OCOL + c0, z);
           tmem_ld_wait();
@@ -583,8 +649,8 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
       const int j0 = max(k.kmin / kUnit, k.u0) * kUnit, j1 = min(at, k.u1 * kUnit);
       const Mix mix(p, m, l, u_self, max(at, 0));
       uint8_t* stage = smem + C::OFF_Q + warp * (32 * D * 2) + lane * 128;
-#pragma unroll
-      for (int c0 = 0; c0 < D; c0 += 32) {
+#pragma unroll 1
+      for (int c0 = 0; c0 < p.d; c0 += 32) {
         uint32_t zr[32];
         if (units > 0) {
           tmem_ld32(trow + C::OCOL + c0, zr);
@@ -970,22 +1036,52 @@ size_t carve(Plan* w, uint8_t* base, int N, int B, int H, int Hk, int d, int lim
   return at;
 }
 
-template <typename K>
-cudaError_t launch_main(K kernel, int threads, int smem, const ChunkProblem& p, const Plan& w, cudaStream_t s) {
+template <typename K, typename... A>
+cudaError_t launch_main(K kernel, int threads, int smem, const Plan& w, cudaStream_t s, const A&... args) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(w.max_items), threads, smem, s, 1, p, w);
+  if (e == cudaSuccess) e = launch_pdl(kernel, dim3(w.max_items), threads, smem, s, 1, args...);
   if (e != cudaSuccess) note_failure("chunk: launch");
   return e;
 }
 
-template <bool VEC>
-cudaError_t launch_v(const ChunkProblem& p, const Plan& w, cudaStream_t s) {
-  if (p.dtype == RELATION_BF16)
-    return p.d <= 64 ? launch_main(chunk_tc_kernel<64, VEC>, Cfg<64>::THREADS, Cfg<64>::SMEM, p, w, s)
-                     : launch_main(chunk_tc_kernel<128, VEC>, Cfg<128>::THREADS, Cfg<128>::SMEM, p, w, s);
-  return p.d <= 64
-             ? launch_main(chunk_simt_kernel<64, VEC>, kSimtThreads, (int)sizeof(SimtSmem<64>), p, w, s)
-             : launch_main(chunk_simt_kernel<128, VEC>, kSimtThreads, (int)sizeof(SimtSmem<128>), p, w, s);
+// 4-D map over pages [n_pages][page][Hk][d] of bf16: boxes of 64 columns and `rows` rows of one head and
+// page, 128-byte swizzle, zeros past column d
+bool make_map(CUtensorMap* m, const void* base, const ChunkProblem& p, int rows) {
+  static const PFN_cuTensorMapEncodeTiled_v12000 encode = [] {
+    void* ptr = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    const bool ok = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &ptr, 12000, cudaEnableDefault,
+                                                     &q) == cudaSuccess &&
+                    q == cudaDriverEntryPointSuccess;
+    return reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(ok ? ptr : nullptr);
+  }();
+  if (!encode) return false;
+  // (the stride of a dimension of one entry is never used: any that the encoder takes)
+  auto bytes = [](long long stride, int n) { return (cuuint64_t)(n > 1 ? stride * 2 : 16); };
+  cuuint64_t dims[4] = {(cuuint64_t)p.d, (cuuint64_t)p.page, (cuuint64_t)p.Hk, (cuuint64_t)p.n_pages};
+  cuuint64_t strides[3] = {bytes(p.sR, p.page), bytes(p.sC, p.Hk), bytes(p.sP, p.n_pages)};
+  cuuint32_t sizes[4] = {64, (cuuint32_t)rows, 1, 1}, step[4] = {1, 1, 1, 1};
+  return encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, sizes, step,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D>
+cudaError_t launch_tc(const ChunkProblem& p, const Plan& w, bool groups, cudaStream_t s) {
+  int box = kUnit;
+  while (p.page % box) box /= 2;
+  CUtensorMap mk{}, mv{};
+  if (groups && box >= 8 && make_map(&mk, p.k, p, box) && make_map(&mv, p.v, p, box))
+    return launch_main(chunk_tc_kernel<D, kBoxes>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, mk, mv, p, w, box);
+  if (groups) return launch_main(chunk_tc_kernel<D, kGroups>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, mk, mv, p, w, 0);
+  return launch_main(chunk_tc_kernel<D, kElements>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, mk, mv, p, w, 0);
+}
+
+template <int D>
+cudaError_t launch_simt(const ChunkProblem& p, const Plan& w, bool groups, cudaStream_t s) {
+  constexpr int smem = (int)sizeof(SimtSmem<D>);
+  return groups ? launch_main(chunk_simt_kernel<D, true>, kSimtThreads, smem, w, s, p, w)
+                : launch_main(chunk_simt_kernel<D, false>, kSimtThreads, smem, w, s, p, w);
 }
 
 }  // namespace chunk
@@ -1012,7 +1108,9 @@ cudaError_t launch_chunk(ChunkProblem p, void* workspace, cudaStream_t s) {
   for (long long x : {p.N > 1 ? p.qsT : 0, p.H > 1 ? p.qsH : 0, p.n_pages > 1 ? p.sP : 0,
                       p.page > 1 ? p.sR : 0, p.Hk > 1 ? p.sC : 0, (long long)p.d})
     low |= (uintptr_t)(x * es);
-  e = low % 16 == 0 ? launch_v<true>(p, w, s) : launch_v<false>(p, w, s);
+  const bool groups = low % 16 == 0;
+  e = p.dtype == RELATION_BF16 ? (p.d <= 64 ? launch_tc<64>(p, w, groups, s) : launch_tc<128>(p, w, groups, s))
+                               : (p.d <= 64 ? launch_simt<64>(p, w, groups, s) : launch_simt<128>(p, w, groups, s));
   if (e != cudaSuccess) return e;
   e = p.dtype == RELATION_F32 ? launch_pdl(join_kernel<float>, dim3(304), kJoinThreads, 0, s, 1, p, w)
                               : launch_pdl(join_kernel<__nv_bfloat16>, dim3(304), kJoinThreads, 0, s, 1, p, w);
