@@ -7,16 +7,17 @@
 // M, l and sum t e^t are taken in one pass: every thread keeps the three of its own elements, and two
 // such triples join by t' = t - (M' - M) / T:  l' = l f,  (sum)' = f (sum - l (M' - M) / T),
 // f = e^{-(M' - M) / T}.
-// The K largest: every thread's maximum is known after the pass.  With W whole warps at work, the least
-// over them of a warp's ceil(K / W)-th largest maximum of a lane is reached by at least K elements, so only
-// lanes whose maximum is not below it can hold one of the K; their warp goes through these lanes' elements
-// again (from L2: a few hundred elements of a row in place of all) and keeps its K largest in a sorted
-// list, one per lane.  The lists' elements are ranked against each other.
+// The K largest (K <= 32): every thread's maximum is known after the pass.  The K-th largest of 32 of
+// these maxima, the largest of the first warps' lanes, is reached by at least K elements, so only lanes
+// whose maximum is not below it can hold one of the K; their warp goes through these lanes' elements again
+// (from L2: a few hundred elements of a row in place of all) and keeps its K largest in a sorted list, one
+// per lane.  The lists' elements are ranked against each other.
 // Gradient, of g log p_y + h H + k logZ:
 //   dx_j = (1 / T) (g (delta_jy - p_j) - h p_j (log p_j + H) + k p_j).
 //
 // Bound by memory: the logits are read once (gradient: and written).  Few rows are shared by clusters
 // of CTAs that join through distributed shared memory.
+#include <float.h>
 #include <math.h>
 
 #include "common.cuh"
@@ -27,7 +28,6 @@ namespace logprobs {
 
 using u64 = unsigned long long;
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxTop = 32;
 constexpr int kMaxCluster = 8;
 
@@ -91,6 +91,21 @@ struct Row {
   }
 };
 
+__device__ __forceinline__ float max_nan(float a, float b) {  // NaN if either is
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
+template <int N>
+__device__ __forceinline__ float max_of(const float (&v)[N]) {
+  float m = fmaxf(v[0], v[1]);
+#pragma unroll
+  for (int j = 2; j < N; j += 2) {
+    asm("max.f32 %0, %0, %1, %2;" : "+f"(m) : "f"(v[j]), "f"(v[j + 1]));
+  }
+  return m;
+}
+
 // max, sum of e^t, sum of t e^t in units of log 2 (t log2 e)
 struct Sums {
   float m = -INFINITY, l = 0.f, s = 0.f;
@@ -105,18 +120,17 @@ struct Sums {
     l *= f;
     m = to;
   }
-  __device__ __forceinline__ void join(float m2, float l2, float s2, float k2) {
-    Sums o;
-    o.m = m2; o.l = l2; o.s = s2;
-    const float to = fmaxf(m, m2);
-    if (to == -INFINITY) {
-      l += l2;
-      return;
+  // the sums of the warp's lanes, the same bits in each
+  __device__ __forceinline__ void join_warp(float k2) {
+    float to = m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) to = fmaxf(to, __shfl_xor_sync(0xffffffffu, to, o));
+    if (to != -INFINITY) raise(to, k2);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+      l += __shfl_xor_sync(0xffffffffu, l, o);
+      s += __shfl_xor_sync(0xffffffffu, s, o);
     }
-    raise(to, k2);
-    o.raise(to, k2);
-    l += o.l;
-    s += o.s;
   }
 };
 
@@ -155,10 +169,11 @@ __device__ __forceinline__ u64 peer_u64(uint32_t a) {
   return v;
 }
 
+template <int kWarps>
 struct Smem {
   float m[kWarps], l[kWarps], s[kWarps];
   float cm, cl, cs;          // this CTA's
-  unsigned low[kWarps];      // a warp's bound for the K largest
+  unsigned top[32];          // the largest of the first warps' maxima
   int n;                     // keys in `list`
   u64 list[kMaxCluster * kMaxTop > kWarps * kMaxTop ? kMaxCluster * kMaxTop : kWarps * kMaxTop];
   u64 best[kMaxTop];         // this CTA's K largest
@@ -171,10 +186,11 @@ __device__ __forceinline__ int rank_of(u64 key, const u64* list, int n) {
   return r;
 }
 
-template <typename TI>
-__global__ void __launch_bounds__(kThreads) logprobs_kernel(const __grid_constant__ LogprobsProblem p, int n_cl) {
+template <typename TI, int kThreads>
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 8 : 2) logprobs_kernel(const __grid_constant__ LogprobsProblem p, int n_cl) {
   constexpr int N = Vec<TI>::N;
-  __shared__ Smem sm;
+  constexpr int kWarps = kThreads / 32;
+  __shared__ Smem<kWarps> sm;
   pdl_wait_and_launch();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int row = (int)blockIdx.x / n_cl, rank = n_cl > 1 ? (int)cluster_rank() : 0;
@@ -186,23 +202,26 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const __grid_constan
   const int g0 = (int)((long long)x.groups * rank / n_cl), g1 = (int)((long long)x.groups * (rank + 1) / n_cl);
   Sums a;
   auto take = [&](const float (&v)[N]) {
-    float mx = v[0];
-#pragma unroll
-    for (int j = 1; j < N; ++j) mx = fmaxf(mx, v[j]);
+    const float mx = max_of(v);
     if (mx > a.m) a.raise(mx, k2);
     const float m = a.m == -INFINITY ? 0.f : a.m;  // (masked so far: every weight is 0)
-    float l = 0.f, s = 0.f;
+    const float2 m2 = make_float2(-m, -m), kk = make_float2(k2, k2);
+    float2 l = make_float2(0.f, 0.f), s = l;
 #pragma unroll
-    for (int j = 0; j < N; ++j) {
-      const float t = (v[j] - m) * k2, w = ex2_approx(t);
-      l += w;
-      s = w > 0.f ? fmaf(w, t, s) : s;
+    for (int j = 0; j < N; j += 2) {
+      // (-inf would make t e^t NaN: e^t is 0 long before; a NaN stays one)
+      float2 t = __fmul2_rn(__fadd2_rn(make_float2(v[j], v[j + 1]), m2), kk);
+      t.x = max_nan(t.x, -300.f);
+      t.y = max_nan(t.y, -300.f);
+      const float2 w = make_float2(ex2_approx(t.x), ex2_approx(t.y));
+      l = __fadd2_rn(l, w);
+      s = __ffma2_rn(w, t, s);
     }
-    a.l += l;
-    a.s += s;
+    a.l += l.x + l.y;
+    a.s += s.x + s.y;
   };
   {
-    constexpr int U = 4;  // loads in flight
+    constexpr int U = kThreads == 256 ? 2 : 4;  // loads in flight
     int g = g0 + (int)threadIdx.x;
     for (; g + (U - 1) * kThreads < g1; g += U * kThreads) {
       float v[U][N];
@@ -229,72 +248,76 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const __grid_constan
     }
   }
   const float mine = a.m;
-  // the CTA's sums
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor_sync(0xffffffffu, a.m, o), l2 = __shfl_xor_sync(0xffffffffu, a.l, o),
-                s2 = __shfl_xor_sync(0xffffffffu, a.s, o);
-    // (the lower lane's first, so that both lanes have the same bits)
-    if (lane & o) {
-      Sums b;
-      b.m = m2; b.l = l2; b.s = s2;
-      b.join(a.m, a.l, a.s, k2);
-      a = b;
-    } else {
-      a.join(m2, l2, s2, k2);
-    }
-  }
+  // the CTA's sums: a warp's at its maximum, then the warps' by every warp
+  a.join_warp(k2);
   if (lane == 0) {
     sm.m[warp] = a.m; sm.l[warp] = a.l; sm.s[warp] = a.s;
   }
-  // a bound that at least K elements of the CTA reach
-  const int K = p.top, full = min(kWarps, (g1 - g0) / 32), take_n = full ? (K + full - 1) / full : 0;
-  const unsigned key = mine == -INFINITY ? 0u : ordered(mine);
+  // the largest maxima of the first `from` warps' lanes, 32 in all (fewer whole warps than one: no bound)
+  const int K = p.top, full = (g1 - g0) / 32;
+  int from = kWarps;
+  while (from > full) from /= 2;
   if (K > 0) {
-    unsigned rest = key, low = 0;
-    for (int i = 0; i < take_n; ++i) {
-      low = __reduce_max_sync(0xffffffffu, rest);
-      const unsigned who = __ballot_sync(0xffffffffu, rest == low);
-      if (lane == __ffs(who) - 1) rest = 0;
+    unsigned rest = mine == -INFINITY ? 0u : ordered(mine);
+    if (warp < from) {
+      for (int i = 0; i < 32 / from; ++i) {
+        const unsigned best = __reduce_max_sync(0xffffffffu, rest);
+        if (lane == __ffs(__ballot_sync(0xffffffffu, rest == best)) - 1) rest = 0;
+        if (lane == 0) sm.top[warp * (32 / from) + i] = best;
+      }
     }
-    if (lane == 0) sm.low[warp] = low;
     if (threadIdx.x == 0) sm.n = 0;
   }
   __syncthreads();
-  {
-    Sums c;
-    c.m = sm.m[0]; c.l = sm.l[0]; c.s = sm.s[0];
-    for (int i = 1; i < kWarps; ++i) c.join(sm.m[i], sm.l[i], sm.s[i], k2);
-    a = c;
+  a = Sums();
+  if (lane < kWarps) {
+    a.m = sm.m[lane]; a.l = sm.l[lane]; a.s = sm.s[lane];
   }
+  a.join_warp(k2);
   if (K > 0) {
-    unsigned low = full && take_n <= 32 ? sm.low[0] : 0u;
-    for (int i = 1; i < full; ++i) low = min(low, sm.low[i]);
-    low = max(low, 1u);
+    unsigned low = 0;
+    if (from > 0) {  // the K-th of them
+      const unsigned one = sm.top[lane];
+      int above = 0;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        const unsigned other = __shfl_sync(0xffffffffu, one, i);
+        above += other > one || (other == one && i < lane);
+      }
+      low = __shfl_sync(0xffffffffu, one, __ffs(__ballot_sync(0xffffffffu, above == K - 1)) - 1);
+    }
+    // (-inf and NaN are never kept)
+    const float least = low > ordered(-FLT_MAX) ? value_of(low) : -FLT_MAX;
     // the warp's K largest among the elements of its lanes that reach the bound, one a lane
     u64 best = 0;
-    unsigned who = __ballot_sync(0xffffffffu, key >= low);
-    const int slices = (g1 - g0 + kThreads - 1) / kThreads;  // a lane's groups, one to a lane each
+    unsigned who = __ballot_sync(0xffffffffu, mine >= least);
+    // such lanes' groups, one to a lane each, of as many of them at a time as there are lanes for
+    const int slices = (g1 - g0 + kThreads - 1) / kThreads;
+    int width = 1;
+    while (width < slices && width < 32) width *= 2;
     while (who) {
-      const int of = __ffs(who) - 1;
-      who &= who - 1;
-      for (int i0 = 0; i0 < slices; i0 += 32) {
-        const int g = g0 + (warp * 32 + of) + (i0 + lane) * kThreads;
+      int of = -1;
+      for (int i = 0; i < 32 && who; i += width) {
+        if (lane / width == i / width) of = __ffs(who) - 1;
+        who &= who - 1;
+      }
+      for (int i0 = 0; i0 < slices; i0 += width) {
+        const int i = i0 + lane % width, g = g0 + warp * 32 + of + i * kThreads;
         float v[N];
-        if (i0 + lane < slices && g < g1) {
+        if (of >= 0 && i < slices && g < g1) {
           x.load(g, v);
         } else {
 #pragma unroll
           for (int j = 0; j < N; ++j) v[j] = -INFINITY;
         }
+        if (!__any_sync(0xffffffffu, max_of(v) >= least)) continue;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-          // (-inf and NaN are never kept)
-          const u64 k = v[j] > -INFINITY && ordered(v[j]) >= low ? key_of(v[j], g * N - x.off + j) : 0;
-          const u64 least = __shfl_sync(0xffffffffu, best, K - 1);
-          unsigned in = __ballot_sync(0xffffffffu, k > least);
+          if (!__any_sync(0xffffffffu, v[j] >= least)) continue;
+          const u64 key = v[j] >= least ? key_of(v[j], g * N - x.off + j) : 0;
+          unsigned in = __ballot_sync(0xffffffffu, key > __shfl_sync(0xffffffffu, best, K - 1));
           while (in) {
-            const u64 next = __shfl_sync(0xffffffffu, k, __ffs(in) - 1);
+            const u64 next = __shfl_sync(0xffffffffu, key, __ffs(in) - 1);
             in &= in - 1;
             const int at = __popc(__ballot_sync(0xffffffffu, best > next));
             const u64 up = __shfl_up_sync(0xffffffffu, best, 1);
@@ -324,12 +347,11 @@ __global__ void __launch_bounds__(kThreads) logprobs_kernel(const __grid_constan
     __syncthreads();
     cluster_sync();
     if (rank == 0) {
-      Sums c;
-      for (int i = 0; i < n_cl; ++i) {
-        const float m2 = peer_f(peer(&sm.cm, i)), l2 = peer_f(peer(&sm.cl, i)), s2 = peer_f(peer(&sm.cs, i));
-        c.join(m2, l2, s2, k2);
+      a = Sums();
+      if (lane < n_cl) {
+        a.m = peer_f(peer(&sm.cm, lane)); a.l = peer_f(peer(&sm.cl, lane)); a.s = peer_f(peer(&sm.cs, lane));
       }
-      a = c;
+      a.join_warp(k2);
       if (K > 0) {
         const int n = n_cl * K;
         for (int e = threadIdx.x; e < n; e += kThreads) sm.list[e] = peer_u64(peer(&sm.best[e % K], e / K));
@@ -455,10 +477,15 @@ cudaError_t launch_t(const LogprobsProblem& p, cudaStream_t s) {
   if (cudaGetDevice(&dev) != cudaSuccess ||
       cudaDeviceGetAttribute(&nsm, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess)
     nsm = 148;
-  // clusters while all rows' CTAs are resident at once and each keeps 4096 elements
+  // Clusters while all rows' CTAs are resident at once and each keeps 4096 elements.  Of many rows eight
+  // CTAs of 256 threads fit an SM, so that some read while others join their sums (2048 rows of 50257
+  // bf16 with 20 alternatives: 59 us, four of 256 67, two of 512 95); of few, which end in one round, two of
+  // 512 with twice the loads in flight a thread (256 rows of 131072 fp32: 25 us against 33).
   int cl = 1;
   while (cl < kMaxCluster && 2LL * cl * p.R <= nsm && p.V / (2 * cl) >= 4096) cl *= 2;
-  const cudaError_t e = launch_pdl(logprobs_kernel<TI>, dim3((unsigned)p.R * cl), kThreads, 0, s, cl, p, cl);
+  const cudaError_t e =
+      p.R > 2 * nsm ? launch_pdl(logprobs_kernel<TI, 256>, dim3((unsigned)p.R), 256, 0, s, 1, p, 1)
+                    : launch_pdl(logprobs_kernel<TI, 512>, dim3((unsigned)p.R * cl), 512, 0, s, cl, p, cl);
   if (e != cudaSuccess) note_failure("log probabilities: launch");
   return e;
 }
