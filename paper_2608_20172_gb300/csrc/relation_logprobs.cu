@@ -433,40 +433,61 @@ __global__ void __launch_bounds__(kGradThreads)
   const int target = p.targets[row];
   const float g = p.dlogprob && target >= 0 ? p.dlogprob[row] : 0.f;
   const float h = p.dentropy ? p.dentropy[row] : 0.f, k = p.dlogz ? p.dlogz[row] : 0.f;
-  const float kg = target >= p.V ? NAN : k - g;  // (a token outside the row has no log probability)
-  const bool none = logz == -INFINITY;
+  // a = log2 p_j:  dx_j = 2^a (c0 + c1 a), and g / T more for the given token
+  const float s2 = scale * kLog2e, z2 = -logz * kLog2e;
+  const float c0 = target >= p.V ? NAN : (k - g - h * H) * scale;  // (a token outside the row has no log p)
+  const float c1 = -h * kLn2 * scale;
+  // Rows that take care: without a token (-inf), with NaN, and those whose logz does not hold the logarithm
+  // of the equal largest ones' number, +inf or nothing but the type's lowest value
+  const bool odd = !(fabsf(logz) <= 1e30f) || !isfinite(c0) || !isfinite(c1) || !isfinite(s2);
   auto grad = [&](float v, int c) {
-    float lp = fmaf(v, scale, -logz);
-    // the equal largest ones share the probability where logz does not hold their logarithm: +inf, or
-    // nothing but the type's lowest value
+    if (logz == -INFINITY) return 0.f;
+    float a = fmaf(v, s2, z2);
     if (fabsf(logz) > 1e30f)
-      lp = (logz == INFINITY ? v == INFINITY : lp >= -1e-6f * fabsf(logz)) ? -H : -INFINITY;
-    const float q = ex2_approx(lp * kLog2e);
-    float d = q == 0.f ? 0.f : q * (kg - h * (lp + H));
-    if (kg != kg) d = kg;
-    if (c == target) d += g;
-    return none ? 0.f : d * scale;
+      a = (logz == INFINITY ? v == INFINITY : a >= -1e-6f * fabsf(z2)) ? -H * kLog2e : -INFINITY;
+    const float q = ex2_approx(a);
+    const float d = c0 != c0 ? c0 : q == 0.f ? 0.f : q * fmaf(a, c1, c0);
+    return c == target ? fmaf(g, scale, d) : d;
   };
 #pragma unroll
   for (int i = 0; i < kGradU; ++i) {
     const int gr = first + i * kGradThreads;
     if (gr >= x.groups) break;
-    const int c0 = gr * N - x.off;
+    const int at = gr * N - x.off;
     if (x.whole(gr)) {
       float v[N];
       Vec<TI>::unpack(w[i], v);
+      if (odd) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) v[j] = grad(v[j], c0 + j);
-      if (VEC) {
-        *reinterpret_cast<uint4*>(out + c0) = Vec<TI>::pack(v);
+        for (int j = 0; j < N; ++j) v[j] = grad(v[j], at + j);
       } else {
 #pragma unroll
-        for (int j = 0; j < N; ++j) out[c0 + j] = (TI)v[j];
+        for (int j = 0; j < N; j += 2) {
+          float2 a = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(s2, s2), make_float2(z2, z2));
+          // (2^a is 0 long before -inf would make 2^a a NaN)
+          a.x = max_nan(a.x, -300.f);
+          a.y = max_nan(a.y, -300.f);
+          const float2 d = __fmul2_rn(make_float2(ex2_approx(a.x), ex2_approx(a.y)),
+                                      __ffma2_rn(a, make_float2(c1, c1), make_float2(c0, c0)));
+          v[j] = d.x;
+          v[j + 1] = d.y;
+        }
+        if ((unsigned)(target - at) < (unsigned)N) {
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (at + j == target) v[j] = fmaf(g, scale, v[j]);
+        }
+      }
+      if (VEC) {
+        *reinterpret_cast<uint4*>(out + at) = Vec<TI>::pack(v);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) out[at + j] = (TI)v[j];
       }
     } else {
 #pragma unroll
       for (int j = 0; j < N; ++j)
-        if (c0 + j >= 0 && c0 + j < p.V) out[c0 + j] = (TI)grad((float)x.x[c0 + j], c0 + j);
+        if (at + j >= 0 && at + j < p.V) out[at + j] = (TI)grad((float)x.x[at + j], at + j);
     }
   }
 }

@@ -33,7 +33,7 @@ struct Group {
   struct Raw {
     TI x;
   };
-  static __device__ __forceinline__ Raw load(const TI* p) { return {*p}; }
+  static __device__ __forceinline__ Raw load(const TI* p) { return Raw{*p}; }
   static __device__ __forceinline__ void unpack(const Raw& r, float (&x)[1]) { x[0] = (float)r.x; }
   static __device__ __forceinline__ void store(TI* p, const float (&x)[1]) { *p = (TI)x[0]; }
 };
@@ -102,24 +102,39 @@ __device__ __forceinline__ float lanes_sum(float x, int lanes) {
   return x;
 }
 
+// Two channels at a time: the packed fp32 instructions take the place of two
+__device__ __forceinline__ float2 two(float a, float b) { return make_float2(a, b); }
+template <int GE, typename F>
+__device__ __forceinline__ void each2(F f) {  // f(j) for channels j, j + 1
+#pragma unroll
+  for (int j = 0; j < GE; j += 2) f(j);
+}
+
 // A lane's two groups turned (sign 1) or turned back (-1) by their pairs' (cos, sin)
 template <int GE, bool ACROSS>
 __device__ __forceinline__ void turned(float (&x)[GE], float (&y)[GE], const float2 (&cs)[GE], float sign) {
-  if constexpr (ACROSS) {
-#pragma unroll
-    for (int j = 0; j < GE; ++j) {
-      const float s = cs[j].y * sign, a = x[j], b = y[j];
-      x[j] = a * cs[j].x - b * s;
-      y[j] = a * s + b * cs[j].x;
-    }
+  if constexpr (GE == 1) {
+    const float s = cs[0].y * sign, a = x[0], b = y[0];
+    x[0] = a * cs[0].x - b * s;
+    y[0] = a * s + b * cs[0].x;
+  } else if constexpr (ACROSS) {
+    each2<GE>([&](int j) {
+      const float2 c = two(cs[j].x, cs[j + 1].x), s = two(cs[j].y * sign, cs[j + 1].y * sign);
+      const float2 a = two(x[j], x[j + 1]), b = two(y[j], y[j + 1]);
+      const float2 u = __ffma2_rn(two(-b.x, -b.y), s, __fmul2_rn(a, c));
+      const float2 v = __ffma2_rn(a, s, __fmul2_rn(b, c));
+      x[j] = u.x; x[j + 1] = u.y;
+      y[j] = v.x; y[j + 1] = v.y;
+    });
   } else {
 #pragma unroll
     for (int j = 0; j < GE; ++j) {
       float(&v)[GE] = j < GE / 2 ? x : y;
       const int e = 2 * (j < GE / 2 ? j : j - GE / 2);
-      const float s = cs[j].y * sign, a = v[e], b = v[e + 1];
-      v[e] = a * cs[j].x - b * s;
-      v[e + 1] = a * s + b * cs[j].x;
+      const float s = cs[j].y * sign;
+      const float2 u = __ffma2_rn(two(v[e + 1], v[e]), two(-s, s), __fmul2_rn(two(v[e], v[e + 1]), two(cs[j].x, cs[j].x)));
+      v[e] = u.x;
+      v[e + 1] = u.y;
     }
   }
 }
@@ -150,7 +165,7 @@ __device__ __forceinline__ void fill_turns(float2* turn, int pos, const Steps& s
   for (int i = 0; i < kMaxD / 64; ++i) {
     const int c = lane + 32 * i;
     if (c < n) {
-      const unsigned long long at = (unsigned long long)max(pos, 0) * st.s[i];
+      const unsigned long long at = (unsigned long long)pos * st.s[i];
       float s, co;
       sincospif((float)(int)(at >> 32) * 0x1p-31f, &s, &co);
       turn[c] = c < half ? make_float2(co * p.scale, s * p.scale) : make_float2(1.f, 0.f);
@@ -163,7 +178,7 @@ __device__ __forceinline__ void fill_turns(float2* turn, int pos, const Steps& s
 // all its tokens' queries, then the keys: a lane's weights stay in registers, its turns for a token's heads,
 // and backward its columns' dw.
 template <typename TI, int GE, bool ACROSS, int IT, bool GRAD>
-__global__ void __launch_bounds__(kThreads)
+__global__ void __launch_bounds__(kThreads, 4)
     norm_rope_kernel(const __grid_constant__ NormRopeProblem p, int lanes) {
   using G = Group<TI, GE>;
   constexpr int U = GRAD ? 1 : 2;  // rows of a lane at a time; the next ones are on their way
@@ -175,6 +190,7 @@ __global__ void __launch_bounds__(kThreads)
   const Place<GE, ACROSS, IT> at(lane % lanes, lanes, p.d, p.d_rot, p.half);
   const Steps steps(p, lane);
   float2* turn = turns[warp];
+  const float inv_d = 1.f / (float)p.d;
   struct Rows {
     typename G::Raw x[U][2][IT], y[GRAD ? U : 1][2][IT];
   };
@@ -199,6 +215,18 @@ __global__ void __launch_bounds__(kThreads)
     for (int n = (int)blockIdx.x * kWarps + warp; n < N && H > 0; n += (int)gridDim.x * kWarps) {
       const int b = n / p.T, t = n - b * p.T, pos = p.positions ? p.positions[n] : t;
       const long long base = (long long)b * sB + (long long)t * sT;
+      if (pos < 0) {  // padding
+        for (int h = slot; h < H; h += slots)
+#pragma unroll
+          for (int it = 0; it < IT; ++it)
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+              const int c = side ? at.b[it] : at.a[it];
+              const float zero[GE] = {};
+              if (c >= 0) G::store(out + base + (long long)h * sH + c, zero);
+            }
+        continue;
+      }
       auto fetch = [&](int h, Rows& r) {  // (clamped: lanes past the end take the last head)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -208,6 +236,8 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
             for (int side = 0; side < 2; ++side) {
               const int c = side ? at.b[it] : at.a[it];
+              r.x[u][side][it] = typename G::Raw{};
+              if (GRAD) r.y[u][side][it] = typename G::Raw{};
               if (c < 0) continue;
               r.x[u][side][it] = G::load(in + off + c);
               if (GRAD) r.y[u][side][it] = G::load(din + off + c);
@@ -232,59 +262,71 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int h = h0 + u * slots + slot;
-          float x[2][IT][GE], y[2][IT][GE], ss = 0.f, dot = 0.f;
-#pragma unroll
-          for (int it = 0; it < IT; ++it)
-#pragma unroll
-            for (int side = 0; side < 2; ++side) {
-              const bool is = (side ? at.b[it] : at.a[it]) >= 0;
-#pragma unroll
-              for (int j = 0; j < GE; ++j) x[side][it][j] = y[side][it][j] = 0.f;
-              if (is) {
-                G::unpack(now.x[u][side][it], x[side][it]);
-                if (GRAD) G::unpack(now.y[GRAD ? u : 0][side][it], y[side][it]);
-              }
-            }
+          float x[2][IT][GE], y[2][IT][GE];
+          float2 ss2 = two(0.f, 0.f), dot2 = ss2;
 #pragma unroll
           for (int it = 0; it < IT; ++it) {
+#pragma unroll
+            for (int side = 0; side < 2; ++side) {
+              G::unpack(now.x[u][side][it], x[side][it]);
+              if (GRAD) G::unpack(now.y[GRAD ? u : 0][side][it], y[side][it]);
+            }
             if (GRAD) turned<GE, ACROSS>(y[0][it], y[1][it], cs[it], -1.f);
+            if constexpr (GE == 1) {
+              const float2 v = two(x[0][it][0], x[1][it][0]);
+              ss2 = __ffma2_rn(v, v, ss2);
+              if (GRAD)
+                dot2 = __ffma2_rn(__fmul2_rn(v, two(w[0][it][0], w[1][it][0])), two(y[0][it][0], y[1][it][0]), dot2);
+            } else {
 #pragma unroll
-            for (int j = 0; j < GE; ++j)
-#pragma unroll
-              for (int side = 0; side < 2; ++side) {
-                ss = fmaf(x[side][it][j], x[side][it][j], ss);
-                if (GRAD) dot = fmaf(x[side][it][j] * w[side][it][j], y[side][it][j], dot);
-              }
+              for (int side = 0; side < 2; ++side)
+                each2<GE>([&](int j) {
+                  const float2 v = two(x[side][it][j], x[side][it][j + 1]);
+                  ss2 = __ffma2_rn(v, v, ss2);
+                  if (GRAD)
+                    dot2 = __ffma2_rn(__fmul2_rn(v, two(w[side][it][j], w[side][it][j + 1])),
+                                      two(y[side][it][j], y[side][it][j + 1]), dot2);
+                });
+            }
           }
-          const bool none = pos < 0, live = h < H;
+          const bool live = h < H;
           float r = 1.f, mean = 0.f;
           if (p.norm) {
-            ss = lanes_sum(ss, lanes);
-            r = rsqrtf(ss / (float)p.d + p.eps);
-            if (GRAD) mean = lanes_sum(dot, lanes) * r / (float)p.d;  // mean of x^ w u
+            const float ss = lanes_sum(ss2.x + ss2.y, lanes), dot = GRAD ? lanes_sum(dot2.x + dot2.y, lanes) : 0.f;
+            r = rsqrtf(ss * inv_d + p.eps);
+            if (GRAD) mean = dot * r * inv_d;  // mean of x^ w u
           }
+          // (a lane past the last head adds nothing to dw)
+          const float ra = GRAD && !live ? 0.f : r;
           TI* dst = out + base + (long long)min(h, H - 1) * sH;
 #pragma unroll
           for (int it = 0; it < IT; ++it) {
 #pragma unroll
-            for (int side = 0; side < 2; ++side)
-#pragma unroll
-              for (int j = 0; j < GE; ++j) {
-                float& v = x[side][it][j];
-                if (GRAD) {
-                  const float xh = v * r, u_ = y[side][it][j];
-                  if (live && !none) acc[side][it][j] = fmaf(u_, xh, acc[side][it][j]);
-                  v = r * (w[side][it][j] * u_ - xh * mean);
-                } else {
-                  v *= r * w[side][it][j];
-                }
+            for (int side = 0; side < 2; ++side) {
+              auto one = [&](float2 v, float2 wt, float2 u_, float2& sum) {
+                const float2 xh = __fmul2_rn(v, two(ra, ra));
+                if (!GRAD) return __fmul2_rn(xh, wt);
+                sum = __ffma2_rn(u_, xh, sum);
+                return __fmul2_rn(__ffma2_rn(xh, two(-mean, -mean), __fmul2_rn(wt, u_)), two(ra, ra));
+              };
+              if constexpr (GE == 1) {
+                float2 sum = two(acc[side][it][0], 0.f);
+                x[side][it][0] = one(two(x[side][it][0], 0.f), two(w[side][it][0], 0.f), two(y[side][it][0], 0.f), sum).x;
+                acc[side][it][0] = sum.x;
+              } else {
+                each2<GE>([&](int j) {
+                  float2 sum = two(acc[side][it][j], acc[side][it][j + 1]);
+                  const float2 v = one(two(x[side][it][j], x[side][it][j + 1]), two(w[side][it][j], w[side][it][j + 1]),
+                                       two(y[side][it][j], y[side][it][j + 1]), sum);
+                  x[side][it][j] = v.x; x[side][it][j + 1] = v.y;
+                  acc[side][it][j] = sum.x; acc[side][it][j + 1] = sum.y;
+                });
               }
+            }
             if (!GRAD) turned<GE, ACROSS>(x[0][it], x[1][it], cs[it], 1.f);
 #pragma unroll
             for (int side = 0; side < 2; ++side) {
               const int c = side ? at.b[it] : at.a[it];
-#pragma unroll
-              for (int j = 0; j < GE; ++j) x[side][it][j] = none ? 0.f : x[side][it][j];
               if (live && c >= 0) G::store(dst + c, x[side][it]);
             }
           }
