@@ -354,7 +354,7 @@ struct NormRopeProblem {
   long long sB[2], sT[2], sH[2];
   relation_dtype dtype;
 };
-size_t norm_rope_grad_workspace_bytes(int tokens, int d);
+size_t norm_rope_grad_workspace_bytes(int d);
 cudaError_t launch_norm_rope(const NormRopeProblem& p, bool grad, cudaStream_t s);
 
 // Log probabilities of given tokens, and the logits' gradient (relation_logprobs.cu):

@@ -741,7 +741,7 @@ relation_status relation_norm_rope(const void* p1, const void* p2, const float* 
 size_t relation_norm_rope_grad_workspace_size(relation_shape shp, relation_dtype dt) {
   if (dt != RELATION_F32 && dt != RELATION_BF16) return 0;
   if (shp.B < 1 || shp.T < 1 || shp.d_h < 1 || shp.d_h > 256 || (long long)shp.B * shp.T > (1 << 30)) return 0;
-  return rel::norm_rope_grad_workspace_bytes(shp.B * shp.T, shp.d_h);
+  return rel::norm_rope_grad_workspace_bytes(shp.d_h);
 }
 
 relation_status relation_norm_rope_grad(const void* dq, const void* dk, const void* p1,
@@ -762,7 +762,7 @@ relation_status relation_norm_rope_grad(const void* dq, const void* dk, const vo
   for (const void* x : {(const void*)dw1, (const void*)dw2})
     if (reinterpret_cast<uintptr_t>(x) & 3u) return RELATION_ERR_ALIGNMENT;
   if (dw1 || dw2) {
-    if (!workspace || ws_bytes < rel::norm_rope_grad_workspace_bytes(p.B * p.T, p.d))
+    if (!workspace || ws_bytes < rel::norm_rope_grad_workspace_bytes(p.d))
       return RELATION_ERR_WORKSPACE;
     if (!aligned16(workspace)) return RELATION_ERR_ALIGNMENT;
     p.part = static_cast<float*>(workspace);

@@ -25,7 +25,7 @@ namespace normrope {
 
 constexpr int kThreads = 128, kWarps = kThreads / 32;
 constexpr int kMaxD = 256;
-constexpr int kMaxParts = 1216;  // CTAs at most, each of which leaves a partial sum of dw backward
+constexpr int kMaxParts = 608;  // CTAs at most (four an SM), each of which leaves a partial sum of dw backward
 
 // GE consecutive elements: 16 bytes of an aligned row, or one element
 template <typename TI, int GE>
@@ -176,10 +176,11 @@ __device__ __forceinline__ void fill_turns(float2* turn, int pos, const Steps& s
 
 // Forward, and with GRAD backward.  A warp takes whole tokens, 32 / lanes of a token's heads at a time, first
 // all its tokens' queries, then the keys: a lane's weights stay in registers, its turns for a token's heads,
-// and backward its columns' dw.
+// and backward its columns' dw.  With few tokens (gridDim.y > 1) a CTA takes one part of its tokens' heads:
+// `pq` parts of the queries, then the keys', U 32 / lanes heads each.
 template <typename TI, int GE, bool ACROSS, int IT, bool GRAD>
 __global__ void __launch_bounds__(kThreads, 4)
-    norm_rope_kernel(const __grid_constant__ NormRopeProblem p, int lanes) {
+    norm_rope_kernel(const __grid_constant__ NormRopeProblem p, int lanes, int pq) {
   using G = Group<TI, GE>;
   constexpr int U = GRAD ? 1 : 2;  // rows of a lane at a time; the next ones are on their way
   __shared__ __align__(16) float2 turns[kWarps][kMaxD / 2];
@@ -196,7 +197,12 @@ __global__ void __launch_bounds__(kThreads, 4)
   };
 #pragma unroll 1
   for (int which = 0; which < 2; ++which) {
-    const int H = p.H[which];
+    int h_lo = 0, h_hi = which ? p.H[1] : p.H[0];  // this CTA's heads
+    if (gridDim.y > 1) {
+      const int part = (int)blockIdx.y - (which ? pq : 0);
+      h_lo = part * U * slots;
+      h_hi = part < 0 || (!which && part >= pq) ? h_lo : min(h_hi, h_lo + U * slots);
+    }
     const TI* in = static_cast<const TI*>(which ? p.in[1] : p.in[0]);
     const TI* din = static_cast<const TI*>(which ? p.dout[1] : p.dout[0]);
     TI* out = static_cast<TI*>(which ? p.out[1] : p.out[0]);
@@ -208,15 +214,45 @@ __global__ void __launch_bounds__(kThreads, 4)
     for (int it = 0; it < IT; ++it)
 #pragma unroll
       for (int j = 0; j < GE; ++j) {
-        w[0][it][j] = wp && H && at.a[it] >= 0 ? wp[at.a[it] + j] : 1.f;
-        w[1][it][j] = wp && H && at.b[it] >= 0 ? wp[at.b[it] + j] : 1.f;
+        w[0][it][j] = wp && h_lo < h_hi && at.a[it] >= 0 ? wp[at.a[it] + j] : 1.f;
+        w[1][it][j] = wp && h_lo < h_hi && at.b[it] >= 0 ? wp[at.b[it] + j] : 1.f;
         acc[0][it][j] = acc[1][it][j] = 0.f;
       }
-    for (int n = (int)blockIdx.x * kWarps + warp; n < N && H > 0; n += (int)gridDim.x * kWarps) {
-      const int b = n / p.T, t = n - b * p.T, pos = p.positions ? p.positions[n] : t;
-      const long long base = (long long)b * sB + (long long)t * sT;
+    auto fetch = [&](long long base, int h, Rows& r) {  // (clamped: lanes past the end take the last head)
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const long long off = base + (long long)min(h + u * slots, h_hi - 1) * sH;
+#pragma unroll
+        for (int it = 0; it < IT; ++it)
+#pragma unroll
+          for (int side = 0; side < 2; ++side) {
+            const int c = side ? at.b[it] : at.a[it];
+            r.x[u][side][it] = typename G::Raw{};
+            if (GRAD) r.y[u][side][it] = typename G::Raw{};
+            if (c < 0) continue;
+            r.x[u][side][it] = G::load(in + off + c);
+            if (GRAD) r.y[u][side][it] = G::load(din + off + c);
+          }
+      }
+    };
+    auto token = [&](int n, long long& base, int& pos) {
+      const int b = n / p.T, t = n - b * p.T;
+      base = (long long)b * sB + (long long)t * sT;
+      pos = p.positions ? p.positions[n] : t;
+    };
+    Rows now, next;
+    const int step = (int)gridDim.x * kWarps;
+    long long base = 0, base2 = 0;
+    int pos = 0, pos2 = 0, n = h_lo < h_hi ? (int)blockIdx.x * kWarps + warp : N;
+    if (n < N) {
+      token(n, base, pos);
+      fetch(base, h_lo + slot, now);
+    }
+    for (; n < N; n += step, base = base2, pos = pos2) {
+      const bool more = n + step < N;
+      if (more) token(n + step, base2, pos2);
       if (pos < 0) {  // padding
-        for (int h = slot; h < H; h += slots)
+        for (int h = h_lo + slot; h < h_hi; h += slots)
 #pragma unroll
           for (int it = 0; it < IT; ++it)
 #pragma unroll
@@ -225,27 +261,9 @@ __global__ void __launch_bounds__(kThreads, 4)
               const float zero[GE] = {};
               if (c >= 0) G::store(out + base + (long long)h * sH + c, zero);
             }
+        if (more) fetch(base2, h_lo + slot, now);
         continue;
       }
-      auto fetch = [&](int h, Rows& r) {  // (clamped: lanes past the end take the last head)
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const long long off = base + (long long)min(h + u * slots, H - 1) * sH;
-#pragma unroll
-          for (int it = 0; it < IT; ++it)
-#pragma unroll
-            for (int side = 0; side < 2; ++side) {
-              const int c = side ? at.b[it] : at.a[it];
-              r.x[u][side][it] = typename G::Raw{};
-              if (GRAD) r.y[u][side][it] = typename G::Raw{};
-              if (c < 0) continue;
-              r.x[u][side][it] = G::load(in + off + c);
-              if (GRAD) r.y[u][side][it] = G::load(din + off + c);
-            }
-        }
-      };
-      Rows now, next;
-      fetch(slot, now);
       fill_turns(turn, pos, steps, p, lane);
       float2 cs[IT][GE];  // ACROSS: of the pairs (a + j, b + j); else a's pairs, then b's
 #pragma unroll
@@ -257,8 +275,12 @@ __global__ void __launch_bounds__(kThreads, 4)
           cs[it][j] = is ? turn[first + j] : make_float2(1.f, 0.f);
         }
 #pragma unroll 1
-      for (int h0 = 0; h0 < H; h0 += U * slots) {
-        if (h0 + U * slots < H) fetch(h0 + U * slots + slot, next);
+      for (int h0 = h_lo; h0 < h_hi; h0 += U * slots) {
+        if (h0 + U * slots < h_hi) {
+          fetch(base, h0 + U * slots + slot, next);
+        } else if (more) {
+          fetch(base2, h_lo + slot, next);
+        }
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int h = h0 + u * slots + slot;
@@ -289,7 +311,7 @@ __global__ void __launch_bounds__(kThreads, 4)
                 });
             }
           }
-          const bool live = h < H;
+          const bool live = h < h_hi;
           float r = 1.f, mean = 0.f;
           if (p.norm) {
             const float ss = lanes_sum(ss2.x + ss2.y, lanes), dot = GRAD ? lanes_sum(dot2.x + dot2.y, lanes) : 0.f;
@@ -298,7 +320,7 @@ __global__ void __launch_bounds__(kThreads, 4)
           }
           // (a lane past the last head adds nothing to dw)
           const float ra = GRAD && !live ? 0.f : r;
-          TI* dst = out + base + (long long)min(h, H - 1) * sH;
+          TI* dst = out + base + (long long)min(h, h_hi - 1) * sH;
 #pragma unroll
           for (int it = 0; it < IT; ++it) {
 #pragma unroll
@@ -355,7 +377,7 @@ __global__ void __launch_bounds__(kThreads, 4)
         float x = sums[0][c];
 #pragma unroll
         for (int i = 1; i < kWarps; ++i) x += sums[i][c];
-        p.part[((long long)blockIdx.x * 2 + which) * p.d + c] = x;
+        p.part[((long long)(blockIdx.y * gridDim.x + blockIdx.x) * 2 + which) * p.d + c] = x;
       }
     }
   }
@@ -367,8 +389,14 @@ __global__ void __launch_bounds__(256) dw_kernel(const float* part, int n, int d
   pdl_wait_and_launch();
   const int e = blockIdx.x * 8 + (threadIdx.x & 7), lot = threadIdx.x >> 3;
   double s = 0.0;
-  if (e < 2 * d)
-    for (int i = lot; i < n; i += 32) s += (double)part[(long long)i * 2 * d + e];
+  if (e < 2 * d) {
+    constexpr int K = kMaxParts / 32;  // (all loads at once)
+    float x[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) x[i] = lot + 32 * i < n ? part[(long long)(lot + 32 * i) * 2 * d + e] : 0.f;
+#pragma unroll
+    for (int i = 0; i < K; ++i) s += (double)x[i];
+  }
   red[lot][threadIdx.x & 7] = s;
   __syncthreads();
   if (lot == 0 && e < 2 * d) {
@@ -385,15 +413,19 @@ cudaError_t launch_t(const NormRopeProblem& p, bool grad, cudaStream_t s) {
   const int need = ACROSS ? half + (rest + 1) / 2 : (rest + 1) / 2;
   int lanes = 1;
   while (lanes < need && lanes < 32) lanes *= 2;
-  const int tiles = (p.B * p.T + kWarps - 1) / kWarps, grid = tiles < kMaxParts ? tiles : kMaxParts;
+  const int tiles = (p.B * p.T + kWarps - 1) / kWarps, per = (grad ? 1 : 2) * (32 / lanes);
+  // few tokens: every pass over the heads by a CTA of its own
+  const int pq = (p.H[0] + per - 1) / per, parts = pq + (p.H[1] + per - 1) / per;
+  const dim3 grid = (long long)tiles * parts <= kMaxParts ? dim3(tiles, parts)
+                                                          : dim3(tiles < kMaxParts ? tiles : kMaxParts);
   cudaError_t e;
   if (grad) {
-    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, true>, dim3(grid), kThreads, 0, s, 1, p, lanes);
+    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, true>, grid, kThreads, 0, s, 1, p, lanes, pq);
     if (e == cudaSuccess && p.part)
-      e = launch_pdl(dw_kernel, dim3((2 * p.d + 7) / 8), 256, 0, s, 1, (const float*)p.part, grid, p.d,
-                     p.dw[0], p.dw[1]);
+      e = launch_pdl(dw_kernel, dim3((2 * p.d + 7) / 8), 256, 0, s, 1, (const float*)p.part,
+                     (int)(grid.x * grid.y), p.d, p.dw[0], p.dw[1]);
   } else {
-    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, false>, dim3(grid), kThreads, 0, s, 1, p, lanes);
+    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, false>, grid, kThreads, 0, s, 1, p, lanes, pq);
   }
   if (e != cudaSuccess) note_failure("norm with rotation: launch");
   return e;
@@ -417,9 +449,8 @@ cudaError_t launch_g(const NormRopeProblem& p, bool grad, cudaStream_t s) {
 
 }  // namespace normrope
 
-size_t norm_rope_grad_workspace_bytes(int tokens, int d) {
-  const int tiles = (tokens + normrope::kWarps - 1) / normrope::kWarps;
-  return (size_t)(tiles < normrope::kMaxParts ? tiles : normrope::kMaxParts) * 2 * d * sizeof(float);
+size_t norm_rope_grad_workspace_bytes(int d) {
+  return (size_t)normrope::kMaxParts * 2 * d * sizeof(float);
 }
 
 cudaError_t launch_norm_rope(const NormRopeProblem& p, bool grad, cudaStream_t s) {
