@@ -176,11 +176,11 @@ __device__ __forceinline__ void fill_turns(float2* turn, int pos, const Steps& s
 
 // Forward, and with GRAD backward.  A warp takes whole tokens, 32 / lanes of a token's heads at a time, first
 // all its tokens' queries, then the keys: a lane's weights stay in registers, its turns for a token's heads,
-// and backward its columns' dw.  With few tokens (gridDim.y > 1) a CTA takes one part of its tokens' heads:
-// `pq` parts of the queries, then the keys', U 32 / lanes heads each.
+// and backward its columns' dw.  With few tokens (gridDim.y > 1) a CTA takes one part of its tokens' heads,
+// `per` of them: `pq` parts of the queries, then the keys'.
 template <typename TI, int GE, bool ACROSS, int IT, bool GRAD>
 __global__ void __launch_bounds__(kThreads, 4)
-    norm_rope_kernel(const __grid_constant__ NormRopeProblem p, int lanes, int pq) {
+    norm_rope_kernel(const __grid_constant__ NormRopeProblem p, int lanes, int pq, int per) {
   using G = Group<TI, GE>;
   constexpr int U = GRAD ? 1 : 2;  // rows of a lane at a time; the next ones are on their way
   __shared__ __align__(16) float2 turns[kWarps][kMaxD / 2];
@@ -200,8 +200,8 @@ __global__ void __launch_bounds__(kThreads, 4)
     int h_lo = 0, h_hi = which ? p.H[1] : p.H[0];  // this CTA's heads
     if (gridDim.y > 1) {
       const int part = (int)blockIdx.y - (which ? pq : 0);
-      h_lo = part * U * slots;
-      h_hi = part < 0 || (!which && part >= pq) ? h_lo : min(h_hi, h_lo + U * slots);
+      h_lo = part * per;
+      h_hi = part < 0 || (!which && part >= pq) ? h_lo : min(h_hi, h_lo + per);
     }
     const TI* in = static_cast<const TI*>(which ? p.in[1] : p.in[0]);
     const TI* din = static_cast<const TI*>(which ? p.dout[1] : p.dout[0]);
@@ -383,26 +383,28 @@ __global__ void __launch_bounds__(kThreads, 4)
   }
 }
 
-// dw from the CTAs' partial sums, in fp64: 8 columns a CTA, 32 lots of the partial sums
+// dw from the CTAs' partial sums: 8 columns a CTA, 32 lots of the sums, in a fixed order (fp32: at most 19
+// additions and 5 of pairs; in fp64 this kernel took twice as long)
 __global__ void __launch_bounds__(256) dw_kernel(const float* part, int n, int d, float* dw1, float* dw2) {
-  __shared__ double red[32][8];
+  constexpr int K = kMaxParts / 32;
+  __shared__ float red[8][33];
   pdl_wait_and_launch();
   const int e = blockIdx.x * 8 + (threadIdx.x & 7), lot = threadIdx.x >> 3;
-  double s = 0.0;
-  if (e < 2 * d) {
-    constexpr int K = kMaxParts / 32;  // (all loads at once)
-    float x[K];
+  float x[K], s = 0.f;
 #pragma unroll
-    for (int i = 0; i < K; ++i) x[i] = lot + 32 * i < n ? part[(long long)(lot + 32 * i) * 2 * d + e] : 0.f;
+  for (int i = 0; i < K; ++i)  // (all loads at once)
+    x[i] = e < 2 * d && lot + 32 * i < n ? part[(long long)(lot + 32 * i) * 2 * d + e] : 0.f;
 #pragma unroll
-    for (int i = 0; i < K; ++i) s += (double)x[i];
-  }
-  red[lot][threadIdx.x & 7] = s;
+  for (int i = 0; i < K; ++i) s += x[i];
+  red[threadIdx.x & 7][lot] = s;
   __syncthreads();
-  if (lot == 0 && e < 2 * d) {
-    for (int i = 1; i < 32; ++i) s += red[i][threadIdx.x & 7];
-    float* dw = e < d ? dw1 : dw2;
-    if (dw) dw[e < d ? e : e - d] = (float)s;
+  const int c = threadIdx.x >> 5, to = blockIdx.x * 8 + c;
+  s = red[c][threadIdx.x & 31];
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if ((threadIdx.x & 31) == 0 && to < 2 * d) {
+    float* dw = to < d ? dw1 : dw2;
+    if (dw) dw[to < d ? to : to - d] = s;
   }
 }
 
@@ -413,19 +415,27 @@ cudaError_t launch_t(const NormRopeProblem& p, bool grad, cudaStream_t s) {
   const int need = ACROSS ? half + (rest + 1) / 2 : (rest + 1) / 2;
   int lanes = 1;
   while (lanes < need && lanes < 32) lanes *= 2;
-  const int tiles = (p.B * p.T + kWarps - 1) / kWarps, per = (grad ? 1 : 2) * (32 / lanes);
-  // few tokens: every pass over the heads by a CTA of its own
-  const int pq = (p.H[0] + per - 1) / per, parts = pq + (p.H[1] + per - 1) / per;
-  const dim3 grid = (long long)tiles * parts <= kMaxParts ? dim3(tiles, parts)
-                                                          : dim3(tiles < kMaxParts ? tiles : kMaxParts);
+  // Few tokens: as many CTAs share a token's heads, in whole passes of a warp, as run at once
+  const int tiles = (p.B * p.T + kWarps - 1) / kWarps, pass = (grad ? 1 : 2) * (32 / lanes);
+  dim3 grid(tiles < kMaxParts ? tiles : kMaxParts);
+  int per = 0, pq = 0;
+  if (2 * tiles <= kMaxParts)
+    for (per = pass;; per *= 2) {
+      pq = (p.H[0] + per - 1) / per;
+      const int parts = pq + (p.H[1] + per - 1) / per;
+      if (parts <= 2 || (long long)tiles * parts <= kMaxParts) {
+        grid = dim3(tiles, parts);
+        break;
+      }
+    }
   cudaError_t e;
   if (grad) {
-    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, true>, grid, kThreads, 0, s, 1, p, lanes, pq);
+    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, true>, grid, kThreads, 0, s, 1, p, lanes, pq, per);
     if (e == cudaSuccess && p.part)
       e = launch_pdl(dw_kernel, dim3((2 * p.d + 7) / 8), 256, 0, s, 1, (const float*)p.part,
                      (int)(grid.x * grid.y), p.d, p.dw[0], p.dw[1]);
   } else {
-    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, false>, grid, kThreads, 0, s, 1, p, lanes, pq);
+    e = launch_pdl(norm_rope_kernel<TI, GE, ACROSS, IT, false>, grid, kThreads, 0, s, 1, p, lanes, pq, per);
   }
   if (e != cudaSuccess) note_failure("norm with rotation: launch");
   return e;
