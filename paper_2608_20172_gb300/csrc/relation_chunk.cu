@@ -420,25 +420,34 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
         if (at.x >= 0)
           tma_load_4d(sb + stage + kb * (kUnit * 128) + mine * box * 128, map, full, kb * 64, at.y, k.head, at.x);
       };
-      int2 at = page_at(0);
+      // The keys go one unit ahead: their place is free as soon as the scores of two units before are done,
+      // the values' only after the products with the weights (keys behind the values: a third of the time
+      // of a long prompt's piece was spent waiting for them).
+      int2 at = page_at(0), last = at;
       int issued = 0, raw = 0;
-      for (int j = 0; j < units; ++j) {
+      for (int j = 0; j <= units; ++j) {
         const int s = j % C::STAGES, u = j / C::STAGES;
         const int2 next = page_at(j + 1);  // (the next unit's pages are looked up meanwhile)
-        if (u > 0 && !mbar_wait_warp(bar(B_KE + s), (u - 1) & 1, ab)) break;
-        fetch(&tmK, C::OFF_K + s * C::UT, bar(B_KF + s), at);
-        issued = j + 1;
-        if (u > 0 && !mbar_wait_warp(bar(B_VE + s), (u - 1) & 1, ab)) break;
-        const uint32_t vs = C::OFF_V + s * C::UT;
-        if (!masked(j)) {
-          fetch(&tmV, vs, bar(B_VF + s), at);
-        } else {
-          fetch(&tmV, vs, bar(B_VR), at);
-          if (!mbar_wait_warp(bar(B_VR), raw & 1, ab)) break;
-          ++raw;
-          clean(vs, j);
-          if (lane == 0) mbar_arrive(bar(B_VF + s));
+        if (j < units) {
+          if (u > 0 && !mbar_wait_warp(bar(B_KE + s), (u - 1) & 1, ab)) break;
+          fetch(&tmK, C::OFF_K + s * C::UT, bar(B_KF + s), at);
+          issued = j + 1;
         }
+        if (j > 0) {
+          const int v = j - 1, sv = v % C::STAGES, uv = v / C::STAGES;
+          if (uv > 0 && !mbar_wait_warp(bar(B_VE + sv), (uv - 1) & 1, ab)) break;
+          const uint32_t vs = C::OFF_V + sv * C::UT;
+          if (!masked(v)) {
+            fetch(&tmV, vs, bar(B_VF + sv), last);
+          } else {
+            fetch(&tmV, vs, bar(B_VR), last);
+            if (!mbar_wait_warp(bar(B_VR), raw & 1, ab)) break;
+            ++raw;
+            clean(vs, v);
+            if (lane == 0) mbar_arrive(bar(B_VF + sv));
+          }
+        }
+        last = at;
         at = next;
       }
       if (ab.raised()) {  // copies in flight land before the CTA gives up its shared memory
@@ -471,30 +480,37 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
           }
         }
       };
-      long long o0, o1, n0, n1;
+      long long o0, o1, n0, n1, p0 = -1, p1 = -1;
       rows_of(0, o0, o1);
-      for (int j = 0; j < units; ++j) {
+      for (int j = 0; j <= units; ++j) {
         const int s = j % C::STAGES, u = j / C::STAGES;
         rows_of(j + 1, n0, n1);  // (the next unit's pages are looked up meanwhile)
-        if (u > 0 && !mbar_wait_warp(bar(B_KE + s), (u - 1) & 1, ab)) break;
-        fetch(K, C::OFF_K + s * C::UT, o0, o1);
-        if (VEC) {
-          cp_arrive(bar(B_KF + s));
-        } else {
-          fence_async_smem();
-          mbar_arrive(bar(B_KF + s));
+        if (j < units) {
+          if (u > 0 && !mbar_wait_warp(bar(B_KE + s), (u - 1) & 1, ab)) break;
+          fetch(K, C::OFF_K + s * C::UT, o0, o1);
+          if (VEC) {
+            cp_arrive(bar(B_KF + s));
+          } else {
+            fence_async_smem();
+            mbar_arrive(bar(B_KF + s));
+          }
         }
-        if (u > 0 && !mbar_wait_warp(bar(B_VE + s), (u - 1) & 1, ab)) break;
-        const uint32_t at = C::OFF_V + s * C::UT;
-        fetch(V, at, o0, o1);
-        if (VEC && !masked(j)) {
-          cp_arrive(bar(B_VF + s));
-        } else {
-          cp_wait_all();
-          __syncwarp();
-          if (masked(j)) clean(at, j); else fence_async_smem();
-          mbar_arrive(bar(B_VF + s));
+        if (j > 0) {
+          const int v = j - 1, sv = v % C::STAGES, uv = v / C::STAGES;
+          if (uv > 0 && !mbar_wait_warp(bar(B_VE + sv), (uv - 1) & 1, ab)) break;
+          const uint32_t at = C::OFF_V + sv * C::UT;
+          fetch(V, at, p0, p1);
+          if (VEC && !masked(v)) {
+            cp_arrive(bar(B_VF + sv));
+          } else {
+            cp_wait_all();
+            __syncwarp();
+            if (masked(v)) clean(at, v); else fence_async_smem();
+            mbar_arrive(bar(B_VF + sv));
+          }
         }
+        p0 = o0;
+        p1 = o1;
         o0 = n0;
         o1 = n1;
       }
