@@ -399,8 +399,7 @@ relation_status relation_paged_decode(const void* q, const void* k_pages, const 
  * them leaves the row as it is.  cols * page_size is at most 2^31 - 8192, N H at most 2^31 - 65536
  * (else RELATION_ERR_UNSUPPORTED).  A position of cols * page_size or more makes a token padding, a
  * page id outside [0, n_pages) reads page 0 (the row is then undefined); both are reported to
- * dev_status (if given) as RELATION_ERR_INVALID_ARG.  Asynchronous on `stream`; three launches; nothing
- * is allocated.
+ * dev_status (if given) as RELATION_ERR_INVALID_ARG.  Asynchronous on `stream`; nothing is allocated.
  */
 size_t relation_paged_chunk_workspace_size(int N, int B, int H, int cols, relation_pages cache,
                                            relation_dtype dt);

@@ -33,139 +33,188 @@ constexpr int kUnit = 64;  // keys that are loaded together; pieces are made of 
 constexpr int kPlanThreads = 1024;
 
 // The workspace: what the plan says, and the pieces' partial results.
-struct Item {
-  int tile, head, piece, slot;  // slot: of the partial result, -1: the tile's only piece
+struct Item {  // a CTA's work: a piece of a tile for one key head
+  int b, s0, row0, rows;          // request, its first token, the tile's first row within it, the tile's rows
+  int head, piece, pieces, slot;  // slot: of the partial result, -1: the tile's only piece
 };
-struct Tile {
-  int b, row0, pieces, n;  // request, first row within it, pieces, units of keys (as far as the plan knows)
+struct Split {  // a tile of several pieces
+  int b, s0, row0, rows, pieces, slot, pad0, pad1;  // slot: the first key head's first
 };
 struct Plan {
   int* head;     // {items, tiles of several pieces}
   int* first;    // [B + 1] first tile of a request
-  Tile* tiles;   // [max_tiles]
+  int4* tiles;   // [max_tiles] request, first row, pieces, units of keys and then the first slot
   int* upto;     // [max_tiles + 1] pieces before a tile
-  int2* split;   // [max_split] tiles of several pieces: {tile, first slot}
+  Split* split;  // [max_split]
   Item* items;   // [max_items]
   float4* stats; // [slots][rows] m, l, self evidence, whether the piece has it
   float* z;      // [slots][rows][width]
   int max_tiles, max_items, max_split, slots, rows, width;
+  int tile, target, least;  // rows of a tile; pieces aimed at; units that a piece has at least
+  int small;                // every CTA lays the work out by itself (few requests and tiles)
 };
-
-// What a block sums exclusively over its threads; `total` for all of them
-__device__ __forceinline__ int block_scan(int x, int* part, int* total) {
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  int s = x;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, s, o);
-    if (lane >= o) s += y;
-  }
-  if (lane == 31) part[warp] = s;
-  __syncthreads();
-  if (warp == 0) {
-    int t = lane < warps ? part[lane] : 0;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int y = __shfl_up_sync(0xffffffffu, t, o);
-      if (lane >= o) t += y;
-    }
-    part[lane] = t;
-  }
-  __syncthreads();
-  const int before = warp > 0 ? part[warp - 1] : 0;
-  *total = part[warps - 1];
-  __syncthreads();
-  return before + s - x;
-}
 
 // Request b's tokens, as far as the buffer holds them
 __device__ __forceinline__ int2 tokens_of(const ChunkProblem& p, int b) {
   const int s0 = min(max(p.starts[b], 0), p.N), s1 = min(max(p.starts[b + 1], s0), p.N);
   return make_int2(s0, s1);
 }
+__device__ __forceinline__ int tiles_of(int2 tokens, int G, int tile) {
+  return (int)(((long long)(tokens.y - tokens.x) * G + tile - 1) / tile);
+}
+// Units of keys that a tile's last row sees, which is the most where positions ascend
+__device__ __forceinline__ int units_of(const ChunkProblem& p, int2 tokens, int row0, int G, int tile) {
+  const int pos = p.positions[tokens.x + min((row0 + tile - 1) / G, tokens.y - tokens.x - 1)];
+  return pos < 0 || pos >= p.limit ? 1 : pos / kUnit + 1;
+}
+// Units of a piece: the mean of all pieces' if there were `target`, so that there are at most that many
+// more of them than tiles
+__device__ __forceinline__ int piece_of(const Plan& w, unsigned long long units) {
+  return (int)min(max((unsigned long long)w.least, (units + w.target - 1) / w.target), 1ull << 30);
+}
+
+// Three sums at once, exclusively over the threads of a block; their totals for all
+__device__ __forceinline__ int3 add3(int3 a, int3 b) { return make_int3(a.x + b.x, a.y + b.y, a.z + b.z); }
+__device__ __forceinline__ int3 warp_scan(int3 s, int lane) {  // inclusive
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    const int3 y = make_int3(__shfl_up_sync(0xffffffffu, s.x, o), __shfl_up_sync(0xffffffffu, s.y, o),
+                             __shfl_up_sync(0xffffffffu, s.z, o));
+    if (lane >= o) s = add3(s, y);
+  }
+  return s;
+}
+__device__ __forceinline__ int3 block_scan(int3 x, int3* part, int3* total) {
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int3 none = make_int3(0, 0, 0);
+  int3 s = warp_scan(x, lane);
+  __syncthreads();  // (the scan before has been read)
+  if (lane == 31) part[warp] = s;
+  __syncthreads();
+  const int3 t = warp_scan(lane < warps ? part[lane] : none, lane);
+  const int from = max(warp - 1, 0);
+  int3 before = make_int3(__shfl_sync(0xffffffffu, t.x, from), __shfl_sync(0xffffffffu, t.y, from),
+                          __shfl_sync(0xffffffffu, t.z, from));
+  if (warp == 0) before = none;
+  *total = make_int3(__shfl_sync(0xffffffffu, t.x, 31), __shfl_sync(0xffffffffu, t.y, 31),
+                     __shfl_sync(0xffffffffu, t.z, 31));
+  return make_int3(before.x + s.x - x.x, before.y + s.y - x.y, before.z + s.z - x.z);
+}
 
 __global__ void __launch_bounds__(kPlanThreads)
-    plan_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w, int rows, int target,
-                int least) {
-  __shared__ int part[32];
+    plan_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w) {
+  __shared__ int3 part[32];
   __shared__ unsigned long long work;
   pdl_wait_and_launch();
-  const int G = p.H / p.Hk;
-  int tiles = 0, total;
-  for (int b0 = 0; b0 < p.B; b0 += kPlanThreads) {
+  const int G = p.H / p.Hk, T = blockDim.x;
+  int tiles = 0;
+  int3 total;
+  if (threadIdx.x == 0) work = 0;
+  for (int b0 = 0; b0 < p.B; b0 += T) {
     const int b = b0 + (int)threadIdx.x;
-    int n = 0;
-    if (b < p.B) {
-      const int2 t = tokens_of(p, b);
-      n = (int)(((long long)(t.y - t.x) * G + rows - 1) / rows);
-    }
-    const int at = tiles + block_scan(n, part, &total);
+    const int n = b < p.B ? tiles_of(tokens_of(p, b), G, w.tile) : 0;
+    const int at = tiles + block_scan(make_int3(n, 0, 0), part, &total).x;
     if (b < p.B) w.first[b] = at;
-    tiles += total;
+    tiles += total.x;
   }
-  if (threadIdx.x == 0) {
-    w.first[p.B] = tiles;
-    work = 0;
-  }
+  if (threadIdx.x == 0) w.first[p.B] = tiles;
   __syncthreads();
   tiles = min(tiles, w.max_tiles);  // (requests whose tokens overlap: not laid out past the workspace)
   unsigned long long mine = 0;
-  for (int i = threadIdx.x; i < tiles; i += kPlanThreads) {
+  int4 t = make_int4(0, 0, 0, 0);
+  for (int i = threadIdx.x; i < tiles; i += T) {
     int lo = 0, hi = p.B;  // the last request whose first tile is not after this one
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
       if (w.first[mid] <= i) lo = mid; else hi = mid;
     }
-    const int2 t = tokens_of(p, lo);
-    const int row0 = (i - w.first[lo]) * rows;
-    const int last = t.x + min((row0 + rows - 1) / G, t.y - t.x - 1);
-    const int pos = p.positions[last], n = pos < 0 || pos >= p.limit ? 1 : pos / kUnit + 1;
-    w.tiles[i] = {lo, row0, 1, n};
-    mine += n;
+    const int row0 = (i - w.first[lo]) * w.tile;
+    t = make_int4(lo, row0, 1, units_of(p, tokens_of(p, lo), row0, G, w.tile));
+    if (tiles > T) w.tiles[i] = t;
+    mine += t.w;
   }
   for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
   if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&work, mine);
   __syncthreads();
-  const unsigned long long all = work * p.Hk;
-  const int cap = (int)min(max((unsigned long long)least, (all + target - 1) / target), 1ull << 30);
-  int pieces = 0, splits = 0, slots = 0;
-  for (int i0 = 0; i0 < tiles; i0 += kPlanThreads) {
+  const int per_piece = piece_of(w, work * p.Hk);
+  int3 sum = make_int3(0, 0, 0);  // pieces, tiles of several, their slots
+  for (int i0 = 0; i0 < tiles; i0 += T) {
     const int i = i0 + (int)threadIdx.x;
-    int n = 0;
+    if (i < tiles && tiles > T) t = w.tiles[i];
+    const int n = i < tiles ? (t.w + per_piece - 1) / per_piece : 0;
+    const int3 at = add3(sum, block_scan(make_int3(n, n > 1, n > 1 ? n * p.Hk : 0), part, &total));
+    sum = add3(sum, total);
     if (i < tiles) {
-      n = (w.tiles[i].n + cap - 1) / cap;
-      w.tiles[i].pieces = n;
+      const int2 tok = tokens_of(p, t.x);
+      t.z = n;
+      t.w = n > 1 ? at.z : -1;
+      w.tiles[i] = t;
+      w.upto[i] = at.x;
+      if (n > 1)
+        w.split[at.y] = {t.x, tok.x, t.y, min(w.tile, (tok.y - tok.x) * G - t.y), n, at.z, 0, 0};
     }
-    const bool is = n > 1;
-    const int at = pieces + block_scan(n, part, &total);
-    if (i < tiles) w.upto[i] = at;
-    pieces += total;
-    const int slot = slots + block_scan(is ? n * p.Hk : 0, part, &total);
-    slots += total;
-    const int s = splits + block_scan(is, part, &total);
-    splits += total;
-    if (is) w.split[s] = make_int2(i, slot);
-    if (i < tiles) w.tiles[i].n = is ? slot : -1;
   }
   if (threadIdx.x == 0) {
-    w.upto[tiles] = pieces;
-    w.head[0] = pieces * p.Hk;
-    w.head[1] = splits;
+    w.upto[tiles] = sum.x;
+    w.head[0] = sum.x * p.Hk;
+    w.head[1] = sum.y;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < tiles; i += kPlanThreads) {
-    const Tile t = w.tiles[i];
-    const int end = min(w.first[t.b + 1], tiles), from = w.upto[w.first[t.b]], per = w.upto[end] - from;
+  for (int i = threadIdx.x; i < tiles; i += T) {
+    t = w.tiles[i];
+    const int2 tok = tokens_of(p, t.x);
+    const int end = min(w.first[t.x + 1], tiles), from = w.upto[w.first[t.x]], per = w.upto[end] - from;
+    const int later = w.upto[end] - w.upto[i + 1], rows = min(w.tile, (tok.y - tok.x) * G - t.y);
     for (int h = 0; h < p.Hk; ++h)
-      for (int k = 0; k < t.pieces; ++k)
-        w.items[from * p.Hk + h * per + w.upto[end] - w.upto[i + 1] + k] = {
-            i, h, k, t.n < 0 ? -1 : t.n + h * t.pieces + k};
+      for (int k = 0; k < t.z; ++k)
+        w.items[from * p.Hk + h * per + later + k] = {t.x, tok.x, t.y, rows, h, k, t.z,
+                                                      t.w < 0 ? -1 : t.w + h * t.z + k};
   }
+}
+
+// The same for up to 32 requests and 32 tiles, by one warp and for one CTA, the tiles in their order: lane =
+// request, then lane = tile.  The first CTA writes down what the last kernel reads.
+__device__ __forceinline__ Item plan_small(const ChunkProblem& p, const Plan& w) {
+  const int lane = threadIdx.x & 31, G = p.H / p.Hk;
+  int2 tok = lane < p.B ? tokens_of(p, lane) : make_int2(0, 0);
+  const int n_tiles = lane < p.B ? tiles_of(tok, G, w.tile) : 0;
+  const int upto = warp_scan(make_int3(n_tiles, 0, 0), lane).x;
+  const int tiles = min(__shfl_sync(0xffffffffu, upto, 31), min(w.max_tiles, 32));
+  int b = 0, before = 0;  // this lane's tile: its request
+  for (int i = 0; i < p.B; ++i) {
+    const int u = __shfl_sync(0xffffffffu, upto, i);
+    if (lane >= u) { b = i + 1; before = u; }
+  }
+  b = min(b, p.B - 1);
+  tok = make_int2(__shfl_sync(0xffffffffu, tok.x, b), __shfl_sync(0xffffffffu, tok.y, b));
+  const bool is = lane < tiles;
+  const int row0 = (lane - before) * w.tile, units = is ? units_of(p, tok, row0, G, w.tile) : 0;
+  const int rows = is ? min(w.tile, (tok.y - tok.x) * G - row0) : 0;
+  const unsigned long long all = (unsigned long long)__reduce_add_sync(0xffffffffu, (unsigned)units) * p.Hk;
+  const int per_piece = piece_of(w, all), n = is ? (units + per_piece - 1) / per_piece : 0;
+  const int3 mine = make_int3(n * p.Hk, n > 1, n > 1 ? n * p.Hk : 0), end = warp_scan(mine, lane);
+  const int slot = n > 1 ? end.z - mine.z : -1;
+  if (blockIdx.x == 0) {
+    if (n > 1) w.split[end.y - 1] = {b, tok.x, row0, rows, n, slot, 0, 0};
+    if (lane == 31) w.head[1] = end.y;
+  }
+  // the tile that holds this CTA's item
+  const unsigned past = __ballot_sync(0xffffffffu, end.x > (int)blockIdx.x);
+  const int of = past ? __ffs(past) - 1 : 31, at = (int)blockIdx.x - __shfl_sync(0xffffffffu, end.x - mine.x, of);
+  const int pieces = __shfl_sync(0xffffffffu, n, of), first = __shfl_sync(0xffffffffu, slot, of);
+  Item it = {__shfl_sync(0xffffffffu, b, of), __shfl_sync(0xffffffffu, tok.x, of),
+             __shfl_sync(0xffffffffu, row0, of), __shfl_sync(0xffffffffu, rows, of),
+             0, 0, past ? pieces : 0, first < 0 ? -1 : first + at};
+  if (past) {
+    it.head = at / pieces;
+    it.piece = at - it.head * pieces;
+  }
+  return it;
 }
 
 // One item's rows and keys
 struct Work {
-  int tile, head, slot, b, s0, rows, row0, u0, u1, kmin, kmax;
+  int head, slot, b, s0, rows, row0, u0, u1, kmin, kmax;
 };
 
 // Row `key` of a request: element offset in the pages
@@ -184,24 +233,34 @@ __device__ __forceinline__ long long page_row(const ChunkProblem& p, const int* 
 template <int ROWS>
 __device__ __forceinline__ bool take_item(const ChunkProblem& p, const Plan& w, Work& k, int* pos,
                                           long long* off, int* lowest, int* highest) {
-  if ((int)blockIdx.x >= w.head[0]) return false;
-  const Item it = w.items[blockIdx.x];
-  const Tile t = w.tiles[it.tile];
-  const int2 tok = tokens_of(p, t.b);
-  const int G = p.H / p.Hk;
+  __shared__ Item shared_item;
+  Item it;
+  if (w.small) {
+    if (threadIdx.x < 32) {
+      it = plan_small(p, w);
+      if (threadIdx.x == 0) shared_item = it;
+    }
+  } else {
+    it = w.items[blockIdx.x];  // (read beside the number of them)
+    if ((int)blockIdx.x >= w.head[0]) return false;
+  }
   if (threadIdx.x == 0) {
     *lowest = 0x7fffffff;
     *highest = -1;
   }
   __syncthreads();
-  k.tile = it.tile; k.head = it.head; k.slot = it.slot; k.b = t.b; k.s0 = tok.x; k.row0 = t.row0;
-  k.rows = min(ROWS, (tok.y - tok.x) * G - t.row0);
+  if (w.small) {
+    it = shared_item;
+    if (it.pieces == 0) return false;
+  }
+  const int G = p.H / p.Hk;
+  k.head = it.head; k.slot = it.slot; k.b = it.b; k.s0 = it.s0; k.row0 = it.row0; k.rows = it.rows;
   if (threadIdx.x < ROWS) {
     const int r = threadIdx.x;
     int at = -1;
     off[r] = -1;
     if (r < k.rows) {
-      const int f = t.row0 + r, token = tok.x + f / G;
+      const int f = it.row0 + r, token = it.s0 + f / G;
       at = p.positions[token];
       if (at >= p.limit) {
         if (p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
@@ -221,8 +280,8 @@ __device__ __forceinline__ bool take_item(const ChunkProblem& p, const Plan& w, 
   __syncthreads();
   k.kmin = *lowest; k.kmax = *highest;
   const int n = k.kmax < 0 ? 0 : k.kmax / kUnit + 1;
-  k.u0 = (int)((long long)n * it.piece / t.pieces);
-  k.u1 = (int)((long long)n * (it.piece + 1) / t.pieces);
+  k.u0 = (int)((long long)n * it.piece / it.pieces);
+  k.u1 = (int)((long long)n * (it.piece + 1) / it.pieces);
   return true;
 }
 
@@ -301,11 +360,12 @@ __device__ __forceinline__ uint32_t unfinite_halves(uint32_t w) {  // 0xffff for
   return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
 
-// box: rows of a TMA box (a power of two, 8 to 64, that divides the page size)
+// TMA boxes have `big` rows of a page or 8; a unit's part of a page is cut into as many big ones as fit
 template <int D, int LOAD>
 __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
     chunk_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
-                    const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w, int box) {
+                    const __grid_constant__ CUtensorMap tmK8, const __grid_constant__ CUtensorMap tmV8,
+                    const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w, int big) {
   constexpr bool VEC = LOAD != kElements;
   using C = Cfg<D>;
   using BF = __nv_bfloat16;
@@ -401,36 +461,58 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
     };
     if constexpr (LOAD == kBoxes) {
       // A lane has one box of a unit, of one 64-column block of the keys or the values
-      const int boxes = kUnit / box, mine = lane % boxes, kb = lane / boxes;
-      auto page_at = [&](int j) {  // {page, row in it} of the lane's box of unit j; -1: none
-        const int key = (k.u0 + j) * kUnit + mine * box;
-        if (j >= units || key > k.kmax || kb >= C::KB) return make_int2(-1, 0);
-        const int col = page_of(key, p.page, p.page_mul, p.page_shift);
-        int id = table[col];
-        if ((unsigned)id >= (unsigned)p.n_pages) {
-          if (p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
-          id = 0;
-        }
-        return make_int2(id, key - col * p.page);
+      const int mine = lane % 8, kb = lane / 8;  // (at most 8 boxes)
+      struct Box {
+        int id, row, at, rows, all;  // page (-1: none), row in it, row in the unit, rows; all boxes' rows
       };
-      auto fetch = [&](const CUtensorMap* map, uint32_t stage, uint32_t full, int2 at) {
-        const unsigned who = __ballot_sync(0xffffffffu, at.x >= 0);
-        if (lane == 0) mbar_arrive_expect_tx(full, __popc(who) * box * 128);
+      auto box_of = [&](int j) {  // the lane's box of unit j; its page is looked up
+        Box x = {-1, 0, 0, 0, 0};
+        if (j >= units) return x;
+        int key = (k.u0 + j) * kUnit, col = page_of(key, p.page, p.page_mul, p.page_shift), row = key - col * p.page;
+        const int end = min(kUnit, k.kmax + 1 - key);
+        for (int i = 0, at = 0; at < end; ++i) {
+          const int rows = min(p.page - row, kUnit - at) >= big ? big : 8;
+          if (i == mine && kb < C::KB) {
+            x.id = col;
+            x.row = row;
+            x.at = at;
+            x.rows = rows;
+          }
+          x.all += rows;
+          at += rows;
+          row += rows;
+          if (row == p.page) {
+            row = 0;
+            ++col;
+          }
+        }
+        if (x.id >= 0) {
+          x.id = table[x.id];
+          if ((unsigned)x.id >= (unsigned)p.n_pages) {
+            if (p.dev_status) atomicExch(p.dev_status, (int)RELATION_ERR_INVALID_ARG);
+            x.id = 0;
+          }
+        }
+        return x;
+      };
+      auto fetch = [&](const CUtensorMap* map, const CUtensorMap* map8, uint32_t stage, uint32_t full, const Box& x) {
+        if (lane == 0) mbar_arrive_expect_tx(full, x.all * 128 * C::KB);
         __syncwarp();
-        if (at.x >= 0)
-          tma_load_4d(sb + stage + kb * (kUnit * 128) + mine * box * 128, map, full, kb * 64, at.y, k.head, at.x);
+        if (x.id >= 0)
+          tma_load_4d(sb + stage + kb * (kUnit * 128) + x.at * 128, x.rows == big ? map : map8, full, kb * 64, x.row,
+                      k.head, x.id);
       };
       // The keys go one unit ahead: their place is free as soon as the scores of two units before are done,
       // the values' only after the products with the weights (keys behind the values: a third of the time
       // of a long prompt's piece was spent waiting for them).
-      int2 at = page_at(0), last = at;
+      Box at = box_of(0), last = at;
       int issued = 0, raw = 0;
       for (int j = 0; j <= units; ++j) {
         const int s = j % C::STAGES, u = j / C::STAGES;
-        const int2 next = page_at(j + 1);  // (the next unit's pages are looked up meanwhile)
+        const Box next = box_of(j + 1);  // (the next unit's pages are looked up meanwhile)
         if (j < units) {
           if (u > 0 && !mbar_wait_warp(bar(B_KE + s), (u - 1) & 1, ab)) break;
-          fetch(&tmK, C::OFF_K + s * C::UT, bar(B_KF + s), at);
+          fetch(&tmK, &tmK8, C::OFF_K + s * C::UT, bar(B_KF + s), at);
           issued = j + 1;
         }
         if (j > 0) {
@@ -438,9 +520,9 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
           if (uv > 0 && !mbar_wait_warp(bar(B_VE + sv), (uv - 1) & 1, ab)) break;
           const uint32_t vs = C::OFF_V + sv * C::UT;
           if (!masked(v)) {
-            fetch(&tmV, vs, bar(B_VF + sv), last);
+            fetch(&tmV, &tmV8, vs, bar(B_VF + sv), last);
           } else {
-            fetch(&tmV, vs, bar(B_VR), last);
+            fetch(&tmV, &tmV8, vs, bar(B_VR), last);
             if (!mbar_wait_warp(bar(B_VR), raw & 1, ab)) break;
             ++raw;
             clean(vs, v);
@@ -956,14 +1038,11 @@ __global__ void __launch_bounds__(kJoinThreads)
   const long long rows = (long long)w.head[1] * p.Hk * w.rows;
   for (long long e = first; e < rows; e += step) {
     const int r = (int)(e % w.rows), h = (int)(e / w.rows % p.Hk);
-    const int2 s = w.split[e / w.rows / p.Hk];
-    const Tile t = w.tiles[s.x];
-    const int2 tok = tokens_of(p, t.b);
-    const int f = t.row0 + r;
-    if (f >= (tok.y - tok.x) * G) continue;
-    const int token = tok.x + f / G, head = h * G + f % G, at = p.positions[token];
+    const Split t = w.split[e / w.rows / p.Hk];
+    if (r >= t.rows) continue;
+    const int f = t.row0 + r, token = t.s0 + f / G, head = h * G + f % G, at = p.positions[token];
     if (at < 0 || at >= p.limit) continue;  // (zeros have been written)
-    const long long slot = s.y + h * t.pieces;
+    const long long slot = t.slot + h * t.pieces;
     float m = -INFINITY, l = 0.f, u_self = 0.f, z[4] = {0.f, 0.f, 0.f, 0.f};
     for (int k = lane; k < t.pieces; k += 32) m = fmaxf(m, w.stats[(slot + k) * w.rows + r].x);
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
@@ -1007,33 +1086,29 @@ __global__ void __launch_bounds__(kJoinThreads)
 // ---------------------------------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------------------------------
-struct Sizes {
-  int rows, target, least;  // rows of a tile, pieces aimed at, units that a piece has at least
-};
-Sizes sizes_of(int d, relation_dtype dt) {
-  if (dt == RELATION_F32) return {SM_ROWS, 304, 4};
-  return {BM, d <= 64 ? 608 : 304, 4};
-}
-
 // The plan's arrays in a workspace; the bytes of it
 size_t carve(Plan* w, uint8_t* base, int N, int B, int H, int Hk, int d, int limit, relation_dtype dt) {
-  const Sizes z = sizes_of(d, dt);
+  // (as many pieces as CTAs fit the GPU)
+  w->tile = dt == RELATION_F32 ? SM_ROWS : BM;
+  w->target = dt == RELATION_F32 || d > 64 ? 304 : 608;
+  w->least = 4;
   const long long G = H / Hk, rows = N * G;
   // a request of n rows has ceil(n / tile) tiles, and no more requests than tokens have any
-  const long long tiles = (rows + (long long)(B < N ? B : N) * (z.rows - 1)) / z.rows + 1;
+  const long long tiles = (rows + (long long)(B < N ? B : N) * (w->tile - 1)) / w->tile + 1;
   const long long units = ((long long)limit + kUnit - 1) / kUnit;
-  const long long most = (units + z.least - 1) / z.least;  // pieces of a tile
+  const long long most = (units + w->least - 1) / w->least;  // pieces of a tile
   // Pieces are as long as the mean of `target` pieces at least: all tiles have one and `target` more are
   // enough for the rest; a tile of several has them longer than half of that mean.
-  const long long items = tiles * Hk + (tiles * Hk * (most - 1) < z.target ? tiles * Hk * (most - 1) : z.target);
-  long long slots = 2LL * z.target;
+  const long long items = tiles * Hk + (tiles * Hk * (most - 1) < w->target ? tiles * Hk * (most - 1) : w->target);
+  long long slots = 2LL * w->target;
   if (tiles * Hk * most < slots) slots = tiles * Hk * most;
   const long long split = tiles < slots ? tiles : slots;
   w->max_tiles = (int)tiles;
   w->max_items = (int)items;
   w->max_split = (int)split;
+  w->small = tiles <= 32 && B <= 32;
   w->slots = most > 1 ? (int)slots : 0;
-  w->rows = rows < z.rows ? (int)rows : z.rows;
+  w->rows = rows < w->tile ? (int)rows : w->tile;
   w->width = (d + 3) & ~3;
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -1043,9 +1118,9 @@ size_t carve(Plan* w, uint8_t* base, int N, int B, int H, int Hk, int d, int lim
   };
   w->head = reinterpret_cast<int*>(take(16));
   w->first = reinterpret_cast<int*>(take((size_t)(B + 1) * 4));
-  w->tiles = reinterpret_cast<Tile*>(take((size_t)tiles * sizeof(Tile)));
+  w->tiles = reinterpret_cast<int4*>(take((size_t)tiles * 16));
   w->upto = reinterpret_cast<int*>(take((size_t)(tiles + 1) * 4));
-  w->split = reinterpret_cast<int2*>(take((size_t)split * 8));
+  w->split = reinterpret_cast<Split*>(take((size_t)split * sizeof(Split)));
   w->items = reinterpret_cast<Item*>(take((size_t)items * sizeof(Item)));
   w->stats = reinterpret_cast<float4*>(take((size_t)w->slots * w->rows * 16));
   w->z = reinterpret_cast<float*>(take((size_t)w->slots * w->rows * w->width * 4));
@@ -1084,13 +1159,22 @@ bool make_map(CUtensorMap* m, const void* base, const ChunkProblem& p, int rows)
 
 template <int D>
 cudaError_t launch_tc(const ChunkProblem& p, const Plan& w, bool groups, cudaStream_t s) {
-  int box = kUnit;
-  while (p.page % box) box /= 2;
-  CUtensorMap mk{}, mv{};
-  if (groups && box >= 8 && make_map(&mk, p.k, p, box) && make_map(&mv, p.v, p, box))
-    return launch_main(chunk_tc_kernel<D, kBoxes>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, mk, mv, p, w, box);
-  if (groups) return launch_main(chunk_tc_kernel<D, kGroups>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, mk, mv, p, w, 0);
-  return launch_main(chunk_tc_kernel<D, kElements>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, mk, mv, p, w, 0);
+  // Boxes as large as pages and units allow: a power of two that divides both, or where that is 8 (whose
+  // boxes alone would bound the kernel: pages of 24 rows of 80 bf16 455 us in eights) a page, or 32 rows of
+  // a large one, and eights for what is left.
+  int big = kUnit;
+  while (p.page % big) big /= 2;
+  if (big == 8) big = p.page < kUnit ? p.page : 32;
+  CUtensorMap m[4] = {};
+  if (groups && p.page % 8 == 0 && make_map(&m[0], p.k, p, big) && make_map(&m[1], p.v, p, big) &&
+      make_map(&m[2], p.k, p, 8) && make_map(&m[3], p.v, p, 8))
+    return launch_main(chunk_tc_kernel<D, kBoxes>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, m[0], m[1], m[2], m[3], p,
+                       w, big);
+  if (groups)
+    return launch_main(chunk_tc_kernel<D, kGroups>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, m[0], m[1], m[2], m[3], p,
+                       w, 0);
+  return launch_main(chunk_tc_kernel<D, kElements>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, m[0], m[1], m[2], m[3], p,
+                     w, 0);
 }
 
 template <int D>
@@ -1112,8 +1196,13 @@ cudaError_t launch_chunk(ChunkProblem p, void* workspace, cudaStream_t s) {
   page_division(p.page, &p.page_mul, &p.page_shift);
   Plan w;
   carve(&w, static_cast<uint8_t*>(workspace), p.N, p.B, p.H, p.Hk, p.d, p.limit, p.dtype);
-  const Sizes z = sizes_of(p.d, p.dtype);
-  cudaError_t e = launch_pdl(plan_kernel, dim3(1), kPlanThreads, 0, s, 1, p, w, z.rows, z.target, z.least);
+  cudaError_t e = cudaSuccess;
+  if (!w.small) {
+    // as many threads as requests or tiles want, in whole warps
+    int threads = 128;
+    while (threads < kPlanThreads && threads < w.max_tiles) threads *= 2;
+    e = launch_pdl(plan_kernel, dim3(1), (unsigned)threads, 0, s, 1, p, w);
+  }
   if (e != cudaSuccess) {
     note_failure("chunk: plan launch");
     return e;
