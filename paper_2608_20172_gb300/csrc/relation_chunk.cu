@@ -308,15 +308,15 @@ struct Mix {
 // ---------------------------------------------------------------------------------------------------
 constexpr int BM = 128;
 
-// Warps 0-3 scan (thread = row = TMEM lane), warp 4 loads, warp 5 issues the products; as the forward:
-// d <= 64 four CTAs per SM and steps of 32 keys, else two and steps of 64.
+// Warps 0-3 scan (thread = row = TMEM lane), warp 4 loads, warp 5 issues the products, as in the forward:
+// two CTAs per SM and steps of a unit.
 template <int D>
 struct Cfg {
-  static constexpr int SK = D == 64 ? 32 : 64;
-  static constexpr int CTAS = D == 64 ? 4 : 2;
-  static constexpr int TMEM_COLS = D == 64 ? 128 : 256;
+  static constexpr int SK = kUnit;
+  static constexpr int CTAS = 2;
+  static constexpr int TMEM_COLS = 256;
   static constexpr int OCOL = 2 * SK;
-  static constexpr int STAGES = 2;
+  static constexpr int STAGES = D == 64 ? 4 : 2;
   static constexpr int SPL = kUnit / SK;       // steps of a unit
   static constexpr int THREADS = 192;
   static constexpr int KB = D / 64;            // 128-byte blocks of a row
@@ -331,7 +331,7 @@ struct Cfg {
   static_assert(CTAS * (SMEM + 1024) <= 233472, "CTAs per SM");
   static_assert(OCOL + D <= TMEM_COLS, "TMEM");
 };
-enum : int { B_KF = 0, B_KE = 2, B_VF = 4, B_VE = 6, B_S = 8, B_P = 10, B_OD = 12, B_O = 14, B_VR = 15, N_BAR = 16 };
+enum : int { B_KF = 0, B_KE = 4, B_VF = 8, B_VE = 12, B_S = 16, B_P = 18, B_OD = 20, B_O = 22, B_VR = 23, N_BAR = 24 };
 // How a unit's rows are fetched: element by element, in 16-byte groups, by TMA in boxes of rows of a page
 enum : int { kElements = 0, kGroups = 1, kBoxes = 2 };
 
@@ -840,8 +840,8 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
 }
 
 // ---------------------------------------------------------------------------------------------------
-// fp32: 64 rows by 64 keys on 256 threads.  A thread has 4 rows by 4 keys of the scores, then 4 rows by
-// D / 16 columns of the products with the values; the weights pass through the keys' shared memory.
+// fp32: 64 rows by 64 keys on 256 threads.  A thread has 4 rows by 4 keys of the scores, then 4 rows by two
+// columns of every 32 of the products with the values; the weights pass through the keys' shared memory.
 // ---------------------------------------------------------------------------------------------------
 constexpr int SM_ROWS = 64, kSimtThreads = 256;
 
@@ -894,14 +894,19 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
 #pragma unroll
     for (int c = 0; c < D / 16; ++c) o[i][c] = 0.f;
   }
+  auto row_of = [&](int u) {  // a key's row, by its thread; the next unit's are looked up meanwhile
+    const int key = u * kUnit + (int)threadIdx.x;
+    return threadIdx.x < kUnit && u < k.u1 && key <= k.kmax ? page_row(p, table, key, k.head) : -1LL;
+  };
+  long long next = row_of(k.u0);
   for (int u = k.u0; u < k.u1; ++u) {
     const int key0 = u * kUnit;
     __syncthreads();  // the unit before has been used
-    if (threadIdx.x < kUnit)
-      sm.row[threadIdx.x] = key0 + (int)threadIdx.x <= k.kmax ? page_row(p, table, key0 + threadIdx.x, k.head) : -1;
+    if (threadIdx.x < kUnit) sm.row[threadIdx.x] = next;
     __syncthreads();
     fetch(static_cast<const float*>(p.k), sm.row, &sm.k[0][0], D + 4, kUnit);
     fetch(static_cast<const float*>(p.v), sm.row, &sm.v[0][0], D, kUnit);
+    next = row_of(u + 1);
     cp_wait_all();
     __syncthreads();
     float s[4][4];
@@ -968,17 +973,15 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
 #pragma unroll
         for (int jj = 0; jj < 4; ++jj)
 #pragma unroll
-          for (int e = 0; e < D / 64; ++e) {
-            const float4 v = *reinterpret_cast<const float4*>(&sm.v[j + jj][64 * e + 4 * tx]);
+          for (int e = 0; e < D / 32; ++e) {
+            const float2 v = *reinterpret_cast<const float2*>(&sm.v[j + jj][32 * e + 2 * tx]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
               const float x = jj == 0 ? a[i].x : jj == 1 ? a[i].y : jj == 2 ? a[i].z : a[i].w;
               // (a weight of 0 for a key that the row does not see would turn its infinity into NaN)
               if (decltype(mask)::value && key0 + j + jj >= at[i]) continue;
-              o[i][4 * e] = fmaf(x, v.x, o[i][4 * e]);
-              o[i][4 * e + 1] = fmaf(x, v.y, o[i][4 * e + 1]);
-              o[i][4 * e + 2] = fmaf(x, v.z, o[i][4 * e + 2]);
-              o[i][4 * e + 3] = fmaf(x, v.w, o[i][4 * e + 3]);
+              o[i][2 * e] = fmaf(x, v.x, o[i][2 * e]);
+              o[i][2 * e + 1] = fmaf(x, v.y, o[i][2 * e + 1]);
             }
           }
       }
@@ -997,10 +1000,9 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
     if (k.slot >= 0 && live) {
       float* dst = w.z + ((long long)k.slot * w.rows + r) * w.width;
 #pragma unroll
-      for (int e = 0; e < D / 64; ++e)
-        if (64 * e + 4 * tx < w.width)
-          *reinterpret_cast<float4*>(dst + 64 * e + 4 * tx) =
-              make_float4(o[i][4 * e], o[i][4 * e + 1], o[i][4 * e + 2], o[i][4 * e + 3]);
+      for (int e = 0; e < D / 32; ++e)
+        if (32 * e + 2 * tx < w.width)
+          *reinterpret_cast<float2*>(dst + 32 * e + 2 * tx) = make_float2(o[i][2 * e], o[i][2 * e + 1]);
       if (tx == 0)
         w.stats[(long long)k.slot * w.rows + r] = make_float4(m[i], l[i], u_self, has ? 1.f : 0.f);
       continue;
@@ -1010,11 +1012,11 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
     const float* V = static_cast<const float*>(p.v) + (live ? page_row(p, table, at[i], k.head) : 0);
     float* y = static_cast<float*>(p.out) + sm.off[r];
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e)
+    for (int e = 0; e < D / 32; ++e)
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int col = 64 * e + 4 * tx + c;
-        if (col < p.d) y[col] = live ? mix.y(o[i][4 * e + c], V[col]) : 0.f;
+      for (int c = 0; c < 2; ++c) {
+        const int col = 32 * e + 2 * tx + c;
+        if (col < p.d) y[col] = live ? mix.y(o[i][2 * e + c], V[col]) : 0.f;
       }
     if (tx == 0) {
       const int f = k.row0 + r, G = p.H / p.Hk;
@@ -1088,10 +1090,10 @@ __global__ void __launch_bounds__(kJoinThreads)
 // ---------------------------------------------------------------------------------------------------
 // The plan's arrays in a workspace; the bytes of it
 size_t carve(Plan* w, uint8_t* base, int N, int B, int H, int Hk, int d, int limit, relation_dtype dt) {
-  // (as many pieces as CTAs fit the GPU)
+  // (as many pieces as CTAs fit the GPU; fp32, whose units take long, twice as many and shorter ones)
   w->tile = dt == RELATION_F32 ? SM_ROWS : BM;
-  w->target = dt == RELATION_F32 || d > 64 ? 304 : 608;
-  w->least = 4;
+  w->target = dt == RELATION_F32 ? 608 : 304;
+  w->least = dt == RELATION_F32 ? 2 : 4;
   const long long G = H / Hk, rows = N * G;
   // a request of n rows has ceil(n / tile) tiles, and no more requests than tokens have any
   const long long tiles = (rows + (long long)(B < N ? B : N) * (w->tile - 1)) / w->tile + 1;
@@ -1215,7 +1217,10 @@ cudaError_t launch_chunk(ChunkProblem p, void* workspace, cudaStream_t s) {
     low |= (uintptr_t)(x * es);
   const bool groups = low % 16 == 0;
   e = p.dtype == RELATION_BF16 ? (p.d <= 64 ? launch_tc<64>(p, w, groups, s) : launch_tc<128>(p, w, groups, s))
-                               : (p.d <= 64 ? launch_simt<64>(p, w, groups, s) : launch_simt<128>(p, w, groups, s));
+                               : (p.d <= 32   ? launch_simt<32>(p, w, groups, s)
+                                  : p.d <= 64 ? launch_simt<64>(p, w, groups, s)
+                                  : p.d <= 96 ? launch_simt<96>(p, w, groups, s)
+                                              : launch_simt<128>(p, w, groups, s));
   if (e != cudaSuccess) return e;
   e = p.dtype == RELATION_F32 ? launch_pdl(join_kernel<float>, dim3(304), kJoinThreads, 0, s, 1, p, w)
                               : launch_pdl(join_kernel<__nv_bfloat16>, dim3(304), kJoinThreads, 0, s, 1, p, w);

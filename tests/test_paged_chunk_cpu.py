@@ -61,8 +61,8 @@ def test_workspace_size(lib):
     long = size(1, 1, 2, 10000, pages(), binding.BF16)
     assert small < long < 1 << 20  # rows of one token
     prompt = size(1 << 15, 64, 32, 10000, pages(H=32), binding.BF16)
-    # partial results of at most 1216 pieces of 128 rows, and the plan
-    assert prompt < 1216 * 128 * 68 * 4 + (1 << 22)
+    # partial results of at most 608 pieces of 128 rows, and the plan
+    assert prompt < 608 * 128 * 68 * 4 + (1 << 22)
     assert size(1 << 15, 64, 32, 20000, pages(H=32), binding.BF16) == prompt
     for bad in ((0, 1, 2, 8, pages()), (1, 0, 2, 8, pages()), (1, 1, 3, 8, pages()), (1, 1, 2, 0, pages()),
                 (1, 1, 2, 8, pages(d=129))):
