@@ -621,12 +621,22 @@ def _norm_rope_args(p1, p2, rot, positions, w1, w2, others):
                                      float(rot.scale))
 
 
+def _rotary_args(rot):
+    """freqs, layout (-1: unknown) and scale for the native calls."""
+    return (None, 0, 1.0) if rot is None else (rot.freqs, LAYOUTS.get(rot.layout, -1), float(rot.scale))
+
+
 def norm_rope(p1, p2, rotary: Rotary | None, positions=None, w1=None, w2=None, *, norm: bool = True,
               eps: float = 1.0e-6, out=None, stream=None):
     """Queries and keys normed per head (RMS, weights w1 and w2 fp32 [d] or None) and rotated by their
     positions: returns (q, k) for p1 [B, T, H, d] or [N, H, d] and p2 likewise with heads of its own
     (None: k is None).  positions int32, one a token (None: 0 .. T - 1 in every sequence); negative:
     padding, zeros.  ``norm=False``: the rotation (and the weights) alone.  See relation_norm_rope."""
+    if out is None and stream is None:
+        r = (_calls or _native()).norm_rope(p1, p2, *_rotary_args(rotary), positions, w1, w2, int(norm),
+                                            float(eps))
+        if r is not None:
+            return r
     if out is None:
         q, k = _like(p1, stream), None if p2 is None else _like(p2, stream)
     else:
@@ -653,6 +663,11 @@ def norm_rope_grad(dq, dk, p1, p2, rotary: Rotary | None, positions=None, w1=Non
                    stream=None):
     """Gradient of norm_rope: returns (dp1, dp2, dw1, dw2) from dq and dk (laid out like p1 and p2);
     dp2 and dw2 are None where p2 is, dw1 and dw2 with ``weights=False``."""
+    if workspace is None and stream is None:
+        r = (_calls or _native()).norm_rope_grad(dq, dk, p1, p2, *_rotary_args(rotary), positions, w1, w2,
+                                                 int(norm), float(eps), int(weights))
+        if r is not None:
+            return r
     if (dk is None) != (p2 is None):
         raise ValueError("dk and p2 belong together")
     dp1, dp2 = _like(p1, stream), None if p2 is None else _like(p2, stream)
@@ -710,7 +725,7 @@ def decode(q, k_cache, v_cache, lengths, lam: float, tau_s: float = 2.0, *, out=
 
 
 # The calls of a serving step are short, so that the host's time counts.  The common call (outputs to be
-# allocated, the current stream) goes through csrc/torch_calls.cpp, which checks, allocates and calls
+# allocated, the current stream), and that of the operators around a prompt, goes through csrc/torch_calls.cpp, which checks, allocates and calls
 # the library in native code (host time of page_plan, cache_append, paged_decode and sample: 8, 5, 9 and
 # 6 us a call, 19, 16, 21 and 14 in Python) and answers None to whatever it does not take; then, and
 # where there is none to use, the code here does the same and says what is wrong.
@@ -725,7 +740,8 @@ class _NoCalls:
     def page_plan(*_):
         return None
 
-    cache_append = paged_decode = sample = page_plan
+    cache_append = paged_decode = sample = norm_rope = norm_rope_grad = paged_chunk = logprobs = \
+        logprobs_grad = page_plan
 
 
 def _load_calls(lib):
@@ -746,7 +762,10 @@ def _load_calls(lib):
         return _NoCalls
     m.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
         lib.relation_page_plan, lib.relation_cache_append, lib.relation_paged_decode,
-        lib.relation_paged_decode_workspace_size, lib.relation_sample)))
+        lib.relation_paged_decode_workspace_size, lib.relation_sample, lib.relation_norm_rope,
+        lib.relation_norm_rope_grad, lib.relation_norm_rope_grad_workspace_size,
+        lib.relation_paged_chunk, lib.relation_paged_chunk_workspace_size, lib.relation_logprobs,
+        lib.relation_logprobs_grad)))
     return m
 
 
@@ -943,6 +962,11 @@ def paged_chunk(q, k_pages, v_pages, block_table, starts, positions, lam: float,
     q [N, H, d] with H a multiple of Hk, block_table int32 [B, cols] (rows may be strided), starts int32
     [B + 1] and positions int32 [N] as in a PagePlan (negative: padding).  Returns (Y [N, H, d], logZ
     [N, H]); see relation_paged_chunk."""
+    if out is None and logz is None and workspace is None and stream is None:
+        r = (_calls or _native()).paged_chunk(q, k_pages, v_pages, block_table, starts, positions, lam, tau_s,
+                                              dev_status)
+        if r is not None:
+            return r
     pages = pages_of(k_pages, v_pages)
     dev, shape, st = k_pages.get_device(), q.shape, q.stride()
     if len(shape) != 3 or shape[2] != pages.d_h or st[2] != 1 or \
@@ -1039,6 +1063,10 @@ def logprobs(logits, targets, *, temperature=None, top: int = 0, out: Logprobs |
     """Log probabilities of given tokens, the rows' entropies and their ``top`` most likely tokens:
     logits [R, V] (fp32 or bf16, rows may be strided), targets int32 [R] (negative: none), temperature
     fp32 [R] or None.  See relation_logprobs."""
+    if out is None and stream is None:
+        r = (_calls or _native()).logprobs(logits, targets, temperature, top, dev_status)
+        if r is not None:
+            return Logprobs._make(r)
     dev, dt, (R, V, st), top = logits.get_device(), _dtype_code(logits), _logit_rows(logits), int(top)
     _need("targets", targets, dev, _I32, R)
     if temperature is not None:
@@ -1069,6 +1097,11 @@ def logprobs_grad(logits, targets, logz, entropy, dlogprob=None, dentropy=None, 
     """Gradient of logprobs's logprob, entropy and logz with respect to the logits: dlogits [R, V] in
     their dtype, from the forward's logz and entropy and the gradients fp32 [R] (None: 0).  ``out`` may be
     the logits."""
+    if out is None and stream is None:
+        r = (_calls or _native()).logprobs_grad(logits, targets, logz, entropy, dlogprob, dentropy, dlogz,
+                                                temperature)
+        if r is not None:
+            return r
     dev, dt, (R, V, st) = logits.get_device(), _dtype_code(logits), _logit_rows(logits)
     _need("targets", targets, dev, _I32, R)
     for name, t in (("logz", logz), ("entropy", entropy)):
