@@ -266,8 +266,10 @@ relation_status relation_decode(const void* q, const void* k_cache, const void* 
  * block_table[b][r / page_size].  A step is
  *   relation_page_plan     the pages, slots and positions of the step's new tokens,
  *   relation_cache_append  their rows, rotated and mixed, into those slots,
- *   relation_paged_decode  the Relation row of every request's last token over its pages,
- *   relation_sample        the next tokens from their logits;
+ *   relation_paged_decode  the Relation row of every request's last token over its pages
+ *                          (relation_paged_chunk: the rows of several new tokens of each),
+ *   relation_sample        the next tokens from their logits (relation_logprobs: the log
+ *                          probabilities of given ones);
  * none of them needs a length on the host, so that a step can be captured in a CUDA graph.
  *
  * relation_page_plan: from the requests' lengths and counts,

@@ -11,7 +11,8 @@
 // short chunks fill it together.  The host knows neither counts nor positions, so a first small kernel lays
 // out the work: the tiles of all requests, each cut along its keys into so many pieces that about as many
 // pieces as CTAs fit the GPU have equal length, in an order that keeps the tiles of a request's head side by
-// side (they read the same keys) with the longest first.  A tile of one piece is finished by its CTA; of
+// side (they read the same keys) with the longest first, the requests with the longest history before the
+// others.  A tile of one piece is finished by its CTA; of
 // others every piece leaves its rows' (m, l, z), which a last kernel joins.
 //
 // bf16: the tensor-core forward's scan (relation_tc_fwd.cu, scan.cuh) with keys and values fetched from
@@ -31,6 +32,7 @@ namespace chunk {
 
 constexpr int kUnit = 64;  // keys that are loaded together; pieces are made of them
 constexpr int kPlanThreads = 1024;
+constexpr int kSorted = 512;  // requests that the plan brings into an order of its own
 
 // The workspace: what the plan says, and the pieces' partial results.
 struct Item {  // a CTA's work: a piece of a tile for one key head
@@ -42,8 +44,8 @@ struct Split {  // a tile of several pieces
 };
 struct Plan {
   int* head;     // {items, tiles of several pieces}
-  int* first;    // [B + 1] first tile of a request
-  int4* tiles;   // [max_tiles] request, first row, pieces, units of keys and then the first slot
+  int* first;    // [B + 1] first tile of a request, in the plan's order
+  int4* tiles;   // [max_tiles] request in that order, first row, pieces, units of keys and then the first slot
   int* upto;     // [max_tiles + 1] pieces before a tile
   Split* split;  // [max_split]
   Item* items;   // [max_items]
@@ -106,13 +108,28 @@ __global__ void __launch_bounds__(kPlanThreads)
   __shared__ int3 part[32];
   __shared__ unsigned long long work;
   pdl_wait_and_launch();
+  __shared__ int length[kSorted], order[kSorted];
   const int G = p.H / p.Hk, T = blockDim.x;
   int tiles = 0;
   int3 total;
   if (threadIdx.x == 0) work = 0;
+  // the longest requests first (their tiles would end last otherwise)
+  const bool sorted = p.B <= kSorted && p.B <= T;
+  if (sorted) {
+    const int b = threadIdx.x;
+    const int2 t = b < p.B ? tokens_of(p, b) : make_int2(0, 0);
+    const int mine = t.y > t.x ? units_of(p, t, (t.y - t.x) * G - 1, G, 1) : 0;
+    if (b < p.B) length[b] = mine;
+    __syncthreads();
+    int rank = 0;
+    for (int i = 0; i < p.B && b < p.B; ++i) rank += length[i] > mine || (length[i] == mine && i < b);
+    if (b < p.B) order[rank] = b;
+    __syncthreads();
+  }
+  auto request = [&](int i) { return sorted ? order[i] : i; };
   for (int b0 = 0; b0 < p.B; b0 += T) {
     const int b = b0 + (int)threadIdx.x;
-    const int n = b < p.B ? tiles_of(tokens_of(p, b), G, w.tile) : 0;
+    const int n = b < p.B ? tiles_of(tokens_of(p, request(b)), G, w.tile) : 0;
     const int at = tiles + block_scan(make_int3(n, 0, 0), part, &total).x;
     if (b < p.B) w.first[b] = at;
     tiles += total.x;
@@ -129,7 +146,7 @@ __global__ void __launch_bounds__(kPlanThreads)
       if (w.first[mid] <= i) lo = mid; else hi = mid;
     }
     const int row0 = (i - w.first[lo]) * w.tile;
-    t = make_int4(lo, row0, 1, units_of(p, tokens_of(p, lo), row0, G, w.tile));
+    t = make_int4(lo, row0, 1, units_of(p, tokens_of(p, request(lo)), row0, G, w.tile));
     if (tiles > T) w.tiles[i] = t;
     mine += t.w;
   }
@@ -145,13 +162,14 @@ __global__ void __launch_bounds__(kPlanThreads)
     const int3 at = add3(sum, block_scan(make_int3(n, n > 1, n > 1 ? n * p.Hk : 0), part, &total));
     sum = add3(sum, total);
     if (i < tiles) {
-      const int2 tok = tokens_of(p, t.x);
+      const int b = request(t.x);
+      const int2 tok = tokens_of(p, b);
       t.z = n;
       t.w = n > 1 ? at.z : -1;
       w.tiles[i] = t;
       w.upto[i] = at.x;
       if (n > 1)
-        w.split[at.y] = {t.x, tok.x, t.y, min(w.tile, (tok.y - tok.x) * G - t.y), n, at.z, 0, 0};
+        w.split[at.y] = {b, tok.x, t.y, min(w.tile, (tok.y - tok.x) * G - t.y), n, at.z, 0, 0};
     }
   }
   if (threadIdx.x == 0) {
@@ -162,12 +180,13 @@ __global__ void __launch_bounds__(kPlanThreads)
   __syncthreads();
   for (int i = threadIdx.x; i < tiles; i += T) {
     t = w.tiles[i];
-    const int2 tok = tokens_of(p, t.x);
+    const int b = request(t.x);
+    const int2 tok = tokens_of(p, b);
     const int end = min(w.first[t.x + 1], tiles), from = w.upto[w.first[t.x]], per = w.upto[end] - from;
     const int later = w.upto[end] - w.upto[i + 1], rows = min(w.tile, (tok.y - tok.x) * G - t.y);
     for (int h = 0; h < p.Hk; ++h)
       for (int k = 0; k < t.z; ++k)
-        w.items[from * p.Hk + h * per + later + k] = {t.x, tok.x, t.y, rows, h, k, t.z,
+        w.items[from * p.Hk + h * per + later + k] = {b, tok.x, t.y, rows, h, k, t.z,
                                                       t.w < 0 ? -1 : t.w + h * t.z + k};
   }
 }
@@ -1202,7 +1221,7 @@ cudaError_t launch_chunk(ChunkProblem p, void* workspace, cudaStream_t s) {
   if (!w.small) {
     // as many threads as requests or tiles want, in whole warps
     int threads = 128;
-    while (threads < kPlanThreads && threads < w.max_tiles) threads *= 2;
+    while (threads < kPlanThreads && (threads < w.max_tiles || threads < p.B)) threads *= 2;
     e = launch_pdl(plan_kernel, dim3(1), (unsigned)threads, 0, s, 1, p, w);
   }
   if (e != cudaSuccess) {
