@@ -36,17 +36,19 @@ constexpr int kSorted = 512;  // requests that the plan brings into an order of 
 
 // The workspace: what the plan says, and the pieces' partial results.
 struct Item {  // a CTA's work: a piece of a tile for one key head
-  int b, s0, row0, rows;          // request, its first token, the tile's first row within it, the tile's rows
-  int head, piece, pieces, slot;  // slot: of the partial result, -1: the tile's only piece
+  int b, s0, row0, rows;   // request, its first token, the tile's first row within it, the tile's rows
+  int head, u0, u1, slot;  // units u0 .. u1 - 1; slot: of the partial result, -1: the tile's only piece
 };
+constexpr int kToTheEnd = 0x7fffffff;  // u1 of a tile's last piece
 struct Split {  // a tile of several pieces
   int b, s0, row0, rows, pieces, slot, pad0, pad1;  // slot: the first key head's first
 };
 struct Plan {
   int* head;     // {items, tiles of several pieces}
   int* first;    // [B + 1] first tile of a request, in the plan's order
-  int4* tiles;   // [max_tiles] request in that order, first row, pieces, units of keys and then the first slot
-  int* upto;     // [max_tiles + 1] pieces before a tile
+  int4* tiles;   // [max_tiles] request in that order, first row, pieces (twice, and whether the last is a
+                 // rest), units of keys and then the first slot
+  int2* upto;    // [max_tiles + 1] pieces before a tile: all but the rests, the rests
   Split* split;  // [max_split]
   Item* items;   // [max_items]
   float4* stats; // [slots][rows] m, l, self evidence, whether the piece has it
@@ -70,48 +72,62 @@ __device__ __forceinline__ int units_of(const ChunkProblem& p, int2 tokens, int 
   return pos < 0 || pos >= p.limit ? 1 : pos / kUnit + 1;
 }
 // Units of a piece: the mean of all pieces' if there were `target`, so that there are at most that many
-// more of them than tiles
+// more of them than tiles.  A tile is cut into pieces of exactly that and what is left, which is started
+// after all others: it fills the time between the ends of these (equal pieces of a tile would end in a
+// second round).  Less than `least` is no piece of its own.
 __device__ __forceinline__ int piece_of(const Plan& w, unsigned long long units) {
   return (int)min(max((unsigned long long)w.least, (units + w.target - 1) / w.target), 1ull << 30);
 }
 
-// Three sums at once, exclusively over the threads of a block; their totals for all
-__device__ __forceinline__ int3 add3(int3 a, int3 b) { return make_int3(a.x + b.x, a.y + b.y, a.z + b.z); }
-__device__ __forceinline__ int3 warp_scan(int3 s, int lane) {  // inclusive
+struct Cut {
+  int pieces, rest;  // pieces, whether the last is shorter than the others
+};
+__device__ __forceinline__ Cut cut_of(int units, int per, int least) {
+  int n = (units + per - 1) / per;
+  if (n > 1 && units - (n - 1) * per < least) --n;
+  return {n, n > 1 && units - (n - 1) * per < per};
+}
+
+// Four sums at once, exclusively over the threads of a block; their totals for all
+__device__ __forceinline__ int4 add4(int4 a, int4 b) {
+  return make_int4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+}
+__device__ __forceinline__ int4 shfl4(int4 a, int from) {
+  return make_int4(__shfl_sync(0xffffffffu, a.x, from), __shfl_sync(0xffffffffu, a.y, from),
+                   __shfl_sync(0xffffffffu, a.z, from), __shfl_sync(0xffffffffu, a.w, from));
+}
+__device__ __forceinline__ int4 warp_scan(int4 s, int lane) {  // inclusive
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const int3 y = make_int3(__shfl_up_sync(0xffffffffu, s.x, o), __shfl_up_sync(0xffffffffu, s.y, o),
-                             __shfl_up_sync(0xffffffffu, s.z, o));
-    if (lane >= o) s = add3(s, y);
+    const int4 y = make_int4(__shfl_up_sync(0xffffffffu, s.x, o), __shfl_up_sync(0xffffffffu, s.y, o),
+                             __shfl_up_sync(0xffffffffu, s.z, o), __shfl_up_sync(0xffffffffu, s.w, o));
+    if (lane >= o) s = add4(s, y);
   }
   return s;
 }
-__device__ __forceinline__ int3 block_scan(int3 x, int3* part, int3* total) {
+__device__ __forceinline__ int4 block_scan(int4 x, int4* part, int4* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int3 none = make_int3(0, 0, 0);
-  int3 s = warp_scan(x, lane);
+  const int4 none = make_int4(0, 0, 0, 0);
+  const int4 s = warp_scan(x, lane);
   __syncthreads();  // (the scan before has been read)
   if (lane == 31) part[warp] = s;
   __syncthreads();
-  const int3 t = warp_scan(lane < warps ? part[lane] : none, lane);
-  const int from = max(warp - 1, 0);
-  int3 before = make_int3(__shfl_sync(0xffffffffu, t.x, from), __shfl_sync(0xffffffffu, t.y, from),
-                          __shfl_sync(0xffffffffu, t.z, from));
+  const int4 t = warp_scan(lane < warps ? part[lane] : none, lane);
+  int4 before = shfl4(t, max(warp - 1, 0));
   if (warp == 0) before = none;
-  *total = make_int3(__shfl_sync(0xffffffffu, t.x, 31), __shfl_sync(0xffffffffu, t.y, 31),
-                     __shfl_sync(0xffffffffu, t.z, 31));
-  return make_int3(before.x + s.x - x.x, before.y + s.y - x.y, before.z + s.z - x.z);
+  *total = shfl4(t, 31);
+  return make_int4(before.x + s.x - x.x, before.y + s.y - x.y, before.z + s.z - x.z, before.w + s.w - x.w);
 }
 
 __global__ void __launch_bounds__(kPlanThreads)
     plan_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w) {
-  __shared__ int3 part[32];
+  __shared__ int4 part[32];
   __shared__ unsigned long long work;
   pdl_wait_and_launch();
   __shared__ int length[kSorted], order[kSorted];
   const int G = p.H / p.Hk, T = blockDim.x;
   int tiles = 0;
-  int3 total;
+  int4 total;
   if (threadIdx.x == 0) work = 0;
   // the longest requests first (their tiles would end last otherwise)
   const bool sorted = p.B <= kSorted && p.B <= T;
@@ -130,7 +146,7 @@ __global__ void __launch_bounds__(kPlanThreads)
   for (int b0 = 0; b0 < p.B; b0 += T) {
     const int b = b0 + (int)threadIdx.x;
     const int n = b < p.B ? tiles_of(tokens_of(p, request(b)), G, w.tile) : 0;
-    const int at = tiles + block_scan(make_int3(n, 0, 0), part, &total).x;
+    const int at = tiles + block_scan(make_int4(n, 0, 0, 0), part, &total).x;
     if (b < p.B) w.first[b] = at;
     tiles += total.x;
   }
@@ -154,27 +170,29 @@ __global__ void __launch_bounds__(kPlanThreads)
   if ((threadIdx.x & 31) == 0 && mine) atomicAdd(&work, mine);
   __syncthreads();
   const int per_piece = piece_of(w, work * p.Hk);
-  int3 sum = make_int3(0, 0, 0);  // pieces, tiles of several, their slots
+  int4 sum = make_int4(0, 0, 0, 0);  // pieces but the rests, tiles of several, their slots, rests
   for (int i0 = 0; i0 < tiles; i0 += T) {
     const int i = i0 + (int)threadIdx.x;
     if (i < tiles && tiles > T) t = w.tiles[i];
-    const int n = i < tiles ? (t.w + per_piece - 1) / per_piece : 0;
-    const int3 at = add3(sum, block_scan(make_int3(n, n > 1, n > 1 ? n * p.Hk : 0), part, &total));
-    sum = add3(sum, total);
+    const Cut c = i < tiles ? cut_of(t.w, per_piece, w.least) : Cut{0, 0};
+    const bool several = c.pieces > 1;
+    const int4 at = add4(sum, block_scan(make_int4(c.pieces - c.rest, several, several ? c.pieces * p.Hk : 0, c.rest),
+                                         part, &total));
+    sum = add4(sum, total);
     if (i < tiles) {
       const int b = request(t.x);
       const int2 tok = tokens_of(p, b);
-      t.z = n;
-      t.w = n > 1 ? at.z : -1;
+      t.z = 2 * c.pieces + c.rest;
+      t.w = several ? at.z : -1;
       w.tiles[i] = t;
-      w.upto[i] = at.x;
-      if (n > 1)
-        w.split[at.y] = {b, tok.x, t.y, min(w.tile, (tok.y - tok.x) * G - t.y), n, at.z, 0, 0};
+      w.upto[i] = make_int2(at.x, at.w);
+      if (several)
+        w.split[at.y] = {b, tok.x, t.y, min(w.tile, (tok.y - tok.x) * G - t.y), c.pieces, at.z, 0, 0};
     }
   }
   if (threadIdx.x == 0) {
-    w.upto[tiles] = sum.x;
-    w.head[0] = sum.x * p.Hk;
+    w.upto[tiles] = make_int2(sum.x, sum.w);
+    w.head[0] = (sum.x + sum.w) * p.Hk;
     w.head[1] = sum.y;
   }
   __syncthreads();
@@ -182,12 +200,14 @@ __global__ void __launch_bounds__(kPlanThreads)
     t = w.tiles[i];
     const int b = request(t.x);
     const int2 tok = tokens_of(p, b);
-    const int end = min(w.first[t.x + 1], tiles), from = w.upto[w.first[t.x]], per = w.upto[end] - from;
-    const int later = w.upto[end] - w.upto[i + 1], rows = min(w.tile, (tok.y - tok.x) * G - t.y);
+    const int end = min(w.first[t.x + 1], tiles), from = w.upto[w.first[t.x]].x, per = w.upto[end].x - from;
+    const int later = w.upto[end].x - w.upto[i + 1].x, rows = min(w.tile, (tok.y - tok.x) * G - t.y);
+    const int pieces = t.z >> 1, rest = t.z & 1, rests = sum.x * p.Hk + w.upto[i].y * p.Hk;
     for (int h = 0; h < p.Hk; ++h)
-      for (int k = 0; k < t.z; ++k)
-        w.items[from * p.Hk + h * per + later + k] = {b, tok.x, t.y, rows, h, k, t.z,
-                                                      t.w < 0 ? -1 : t.w + h * t.z + k};
+      for (int k = 0; k < pieces; ++k)
+        w.items[rest && k == pieces - 1 ? rests + h : from * p.Hk + h * per + later + k] = {
+            b, tok.x, t.y, rows, h, k * per_piece, k == pieces - 1 ? kToTheEnd : (k + 1) * per_piece,
+            t.w < 0 ? -1 : t.w + h * pieces + k};
   }
 }
 
@@ -197,7 +217,7 @@ __device__ __forceinline__ Item plan_small(const ChunkProblem& p, const Plan& w)
   const int lane = threadIdx.x & 31, G = p.H / p.Hk;
   int2 tok = lane < p.B ? tokens_of(p, lane) : make_int2(0, 0);
   const int n_tiles = lane < p.B ? tiles_of(tok, G, w.tile) : 0;
-  const int upto = warp_scan(make_int3(n_tiles, 0, 0), lane).x;
+  const int upto = warp_scan(make_int4(n_tiles, 0, 0, 0), lane).x;
   const int tiles = min(__shfl_sync(0xffffffffu, upto, 31), min(w.max_tiles, 32));
   int b = 0, before = 0;  // this lane's tile: its request
   for (int i = 0; i < p.B; ++i) {
@@ -210,23 +230,33 @@ __device__ __forceinline__ Item plan_small(const ChunkProblem& p, const Plan& w)
   const int row0 = (lane - before) * w.tile, units = is ? units_of(p, tok, row0, G, w.tile) : 0;
   const int rows = is ? min(w.tile, (tok.y - tok.x) * G - row0) : 0;
   const unsigned long long all = (unsigned long long)__reduce_add_sync(0xffffffffu, (unsigned)units) * p.Hk;
-  const int per_piece = piece_of(w, all), n = is ? (units + per_piece - 1) / per_piece : 0;
-  const int3 mine = make_int3(n * p.Hk, n > 1, n > 1 ? n * p.Hk : 0), end = warp_scan(mine, lane);
-  const int slot = n > 1 ? end.z - mine.z : -1;
+  const int per_piece = piece_of(w, all);
+  const Cut c = is ? cut_of(units, per_piece, w.least) : Cut{0, 0};
+  const bool several = c.pieces > 1;
+  const int4 mine = make_int4((c.pieces - c.rest) * p.Hk, several, several ? c.pieces * p.Hk : 0, c.rest * p.Hk);
+  const int4 end = warp_scan(mine, lane);
+  const int slot = several ? end.z - mine.z : -1;
   if (blockIdx.x == 0) {
-    if (n > 1) w.split[end.y - 1] = {b, tok.x, row0, rows, n, slot, 0, 0};
+    if (several) w.split[end.y - 1] = {b, tok.x, row0, rows, c.pieces, slot, 0, 0};
     if (lane == 31) w.head[1] = end.y;
   }
-  // the tile that holds this CTA's item
-  const unsigned past = __ballot_sync(0xffffffffu, end.x > (int)blockIdx.x);
-  const int of = past ? __ffs(past) - 1 : 31, at = (int)blockIdx.x - __shfl_sync(0xffffffffu, end.x - mine.x, of);
-  const int pieces = __shfl_sync(0xffffffffu, n, of), first = __shfl_sync(0xffffffffu, slot, of);
+  // the tile that holds this CTA's item: among the pieces but the rests, or the rests after them
+  const int firsts = __shfl_sync(0xffffffffu, end.x, 31);
+  const bool rest = (int)blockIdx.x >= firsts;
+  const int upto_mine = rest ? firsts + end.w : end.x, own = rest ? mine.w : mine.x;
+  const unsigned past = __ballot_sync(0xffffffffu, upto_mine > (int)blockIdx.x);
+  const int of = past ? __ffs(past) - 1 : 31;
+  const int at = (int)blockIdx.x - __shfl_sync(0xffffffffu, upto_mine - own, of);
+  const int pieces = __shfl_sync(0xffffffffu, c.pieces, of), whole = pieces - __shfl_sync(0xffffffffu, c.rest, of);
+  const int first = __shfl_sync(0xffffffffu, slot, of);
   Item it = {__shfl_sync(0xffffffffu, b, of), __shfl_sync(0xffffffffu, tok.x, of),
-             __shfl_sync(0xffffffffu, row0, of), __shfl_sync(0xffffffffu, rows, of),
-             0, 0, past ? pieces : 0, first < 0 ? -1 : first + at};
+             __shfl_sync(0xffffffffu, row0, of), __shfl_sync(0xffffffffu, rows, of), 0, 0, 0, -1};
   if (past) {
-    it.head = at / pieces;
-    it.piece = at - it.head * pieces;
+    it.head = rest ? at : at / whole;
+    const int k = rest ? pieces - 1 : at - it.head * whole;
+    it.u0 = k * per_piece;
+    it.u1 = k == pieces - 1 ? kToTheEnd : it.u0 + per_piece;
+    it.slot = first < 0 ? -1 : first + it.head * pieces + k;
   }
   return it;
 }
@@ -270,7 +300,7 @@ __device__ __forceinline__ bool take_item(const ChunkProblem& p, const Plan& w, 
   __syncthreads();
   if (w.small) {
     it = shared_item;
-    if (it.pieces == 0) return false;
+    if (it.u1 == 0) return false;
   }
   const int G = p.H / p.Hk;
   k.head = it.head; k.slot = it.slot; k.b = it.b; k.s0 = it.s0; k.row0 = it.row0; k.rows = it.rows;
@@ -299,8 +329,8 @@ __device__ __forceinline__ bool take_item(const ChunkProblem& p, const Plan& w, 
   __syncthreads();
   k.kmin = *lowest; k.kmax = *highest;
   const int n = k.kmax < 0 ? 0 : k.kmax / kUnit + 1;
-  k.u0 = (int)((long long)n * it.piece / it.pieces);
-  k.u1 = (int)((long long)n * (it.piece + 1) / it.pieces);
+  k.u0 = min(it.u0, n);
+  k.u1 = min(it.u1, n);
   return true;
 }
 
@@ -1140,7 +1170,7 @@ size_t carve(Plan* w, uint8_t* base, int N, int B, int H, int Hk, int d, int lim
   w->head = reinterpret_cast<int*>(take(16));
   w->first = reinterpret_cast<int*>(take((size_t)(B + 1) * 4));
   w->tiles = reinterpret_cast<int4*>(take((size_t)tiles * 16));
-  w->upto = reinterpret_cast<int*>(take((size_t)(tiles + 1) * 4));
+  w->upto = reinterpret_cast<int2*>(take((size_t)(tiles + 1) * 8));
   w->split = reinterpret_cast<Split*>(take((size_t)split * sizeof(Split)));
   w->items = reinterpret_cast<Item*>(take((size_t)items * sizeof(Item)));
   w->stats = reinterpret_cast<float4*>(take((size_t)w->slots * w->rows * 16));
