@@ -380,7 +380,7 @@ struct Cfg {
   static_assert(CTAS * (SMEM + 1024) <= 233472, "CTAs per SM");
   static_assert(OCOL + D <= TMEM_COLS, "TMEM");
 };
-enum : int { B_KF = 0, B_KE = 4, B_VF = 8, B_VE = 12, B_S = 16, B_P = 18, B_OD = 20, B_O = 22, B_VR = 23, N_BAR = 24 };
+enum : int { B_KF = 0, B_KE = 4, B_VF = 8, B_VE = 12, B_S = 16, B_P = 18, B_OD = 20, B_O = 22, B_VR = 23, B_Q = 24, N_BAR = 25 };
 // How a unit's rows are fetched: element by element, in 16-byte groups, by TMA in boxes of rows of a page
 enum : int { kElements = 0, kGroups = 1, kBoxes = 2 };
 
@@ -423,11 +423,11 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
       (reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~static_cast<uintptr_t>(1023));
   const uint32_t sb = smem_u32(smem);
   auto bar = [&](int i) -> uint32_t { return sb + C::OFF_BAR + 8u * (uint32_t)i; };
-  static_assert(N_BAR * 8 <= 192, "barrier slots");
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_BAR + 192);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 200);
-  volatile int* special = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 204);
-  int* bounds = reinterpret_cast<int*>(smem + C::OFF_BAR + 208);
+  static_assert(N_BAR * 8 <= 200, "barrier slots");
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(smem + C::OFF_BAR + 200);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 204);
+  volatile int* special = reinterpret_cast<volatile int*>(smem + C::OFF_BAR + 208);
+  int* bounds = reinterpret_cast<int*>(smem + C::OFF_BAR + 212);
   int* pos = reinterpret_cast<int*>(smem + C::OFF_POS);
   long long* row_off = reinterpret_cast<long long*>(smem + C::OFF_ROW);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -449,6 +449,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
       mbar_init(bar(B_VE + s), 1);
     }
     mbar_init(bar(B_VR), 1);
+    mbar_init(bar(B_Q), 128);
     for (int b = 0; b < 2; ++b) {
       mbar_init(bar(B_S + b), 1);
       mbar_init(bar(B_P + b), 128);
@@ -460,20 +461,6 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
     fence_mbar_init();
   }
   if (warp == 5) tmem_alloc(smem_u32(tmem_slot), C::TMEM_COLS);
-  // the queries, 16-byte groups swizzled within 128 bytes; zeros for rows and columns that there are not
-  for (int e = threadIdx.x; e < BM * (D / 8); e += C::THREADS) {
-    const int r = e / (D / 8), c = e % (D / 8);
-    const long long off = row_off[r];
-    const bool real = off >= 0 && 8 * c < p.d;
-    const uint32_t dst = C::OFF_Q + (c >> 3) * (BM * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-    if (VEC) {
-      cp16(sb + dst, real ? Q + off + 8 * c : Q, real);
-    } else {
-      *reinterpret_cast<uint4*>(smem + dst) = real ? load8(Q + off, 8 * c, p.d) : make_uint4(0, 0, 0, 0);
-    }
-  }
-  cp_wait_all();
-  fence_async_smem();
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
@@ -673,7 +660,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
       if (hh == C::SPL - 1) mma_commit_w(bar(B_KE + st));
       return true;
     };
-    bool ok = true;
+    bool ok = mbar_wait_warp(bar(B_Q), 0, ab);
     for (int s = 0; ok && s < 2 && s < total; ++s) ok = issue_u(s);
     for (int s = 0; ok && s < total; ++s) {
       const int j = s / C::SPL, hh = s % C::SPL, st = j % C::STAGES, bf = s & 1;
@@ -698,6 +685,23 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
   } else {
     // ---------------------------------------------------------------- scan and epilogue
     const int t = threadIdx.x, at = pos[t];
+    // the queries, 16-byte groups swizzled within 128 bytes, while the first keys are on their way; zeros for
+    // rows and columns that there are not
+#pragma unroll 4
+    for (int e = t; e < BM * (D / 8); e += 128) {
+      const int r = e / (D / 8), c = e % (D / 8);
+      const long long off = row_off[r];
+      const bool real = off >= 0 && 8 * c < p.d;
+      const uint32_t dst = C::OFF_Q + (c >> 3) * (BM * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+      if (VEC) {
+        cp16(sb + dst, real ? Q + off + 8 * c : Q, real);
+      } else {
+        *reinterpret_cast<uint4*>(smem + dst) = real ? load8(Q + off, 8 * c, p.d) : make_uint4(0, 0, 0, 0);
+      }
+    }
+    cp_wait_all();
+    fence_async_smem();
+    mbar_arrive(bar(B_Q));
     const bool any = __any_sync(0xffffffffu, at >= 0);
     // the first key that some row of the warp does not take as history
     const int first = __reduce_min_sync(0xffffffffu, at < 0 ? 0x7fffffff : at);
@@ -706,9 +710,8 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
     // (the scale's rules are those of the forward)
     float m = -INFINITY, m_next = -INFINITY, l = 0.f, u_self = 0.f;
     bool ok = true;
-    auto rescale = [&](bool go, float mn, int s_done, float* scp) -> bool {
+    auto rescale = [&](bool go, float mn, int s_done) -> bool {
       const float sc = go ? ex2_approx(m - mn) : 1.0f;
-      if (scp) *scp = sc;
       if (!__any_sync(0xffffffffu, go)) return true;
       if (s_done >= 0) {
         if (!mbar_wait_warp(bar(B_OD + (s_done & 1)), (s_done / 2) & 1, ab)) return false;
@@ -735,50 +738,30 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
       if (!(ok = mbar_wait_warp(bar(B_S + bf), (s / 2) & 1, ab))) break;
       if (any) {
         tc_fence_after();
-        if (!(ok = rescale(m_next > m, m_next, s - 1, nullptr))) break;
+        if (!(ok = rescale(m_next > m, m_next, s - 1))) break;
         const uint32_t ucol = trow + bf * C::SK;
         const int tl = at - key0;  // keys before tl are the row's history, tl its own
         const bool diag = key0 + C::SK > first;
         float umax;
         float2 rs;
-        if constexpr (C::SK == 32) {
-          uint32_t U[32], pk[16];
-          tmem_ld32(ucol, U);
-          tmem_ld_wait();
-          if (__any_sync(0xffffffffu, m == -INFINITY)) {
-            const float um = diag ? tc::row_max32<true>(U, tl, u_self) : tc::row_max32<false>(U, tl, u_self);
-            if (m == -INFINITY && um != -INFINITY) m = fmaxf(um, 0.f) * bk;
-          }
-          rs = diag ? tc::scan_p32<true>(U, tl, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self, pk)
-                    : tc::scan_p32<false>(U, tl, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self, pk);
-          const float mt = umax == -INFINITY ? -INFINITY : fmaxf(umax, 0.f) * bk;
-          const bool jump = mt > m + tc::kStaleLog2;
-          if (__any_sync(0xffffffffu, jump)) {
-            if (!(ok = rescale(jump, fmaxf(mt, m_next), s - 1, nullptr))) break;
-            rs = diag ? tc::scan_p32<true>(U, tl, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self, pk)
-                      : tc::scan_p32<false>(U, tl, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self, pk);
-          }
-          tmem_st16(ucol, pk);
-        } else {
-          uint32_t U[tc::HN];
-          tmem_ld32(ucol, U);
-          tmem_ld32(ucol + 32, U + 32);
-          tmem_ld_wait();
-          if (__any_sync(0xffffffffu, m == -INFINITY)) {
-            const float um = diag ? tc::row_max<true>(U, tl, u_self) : tc::row_max<false>(U, tl, u_self);
-            if (m == -INFINITY && um != -INFINITY) m = fmaxf(um, 0.f) * bk;
-          }
+        uint32_t U[tc::HN];
+        tmem_ld32(ucol, U);
+        tmem_ld32(ucol + 32, U + 32);
+        tmem_ld_wait();
+        if (__any_sync(0xffffffffu, m == -INFINITY)) {
+          const float um = diag ? tc::row_max<true>(U, tl, u_self) : tc::row_max<false>(U, tl, u_self);
+          if (m == -INFINITY && um != -INFINITY) m = fmaxf(um, 0.f) * bk;
+        }
+        rs = diag ? tc::scan_p<true>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self)
+                  : tc::scan_p<false>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self);
+        float mt = umax == -INFINITY ? -INFINITY : fmaxf(umax, 0.f) * bk;
+        const bool jump = mt > m + tc::kStaleLog2;
+        if (__any_sync(0xffffffffu, jump)) {
+          if (!(ok = rescale(jump, fmaxf(mt, m_next), s - 1))) break;
           rs = diag ? tc::scan_p<true>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self)
                     : tc::scan_p<false>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self);
-          const float mt = umax == -INFINITY ? -INFINITY : fmaxf(umax, 0.f) * bk;
-          const bool jump = mt > m + tc::kStaleLog2;
-          if (__any_sync(0xffffffffu, jump)) {
-            if (!(ok = rescale(jump, fmaxf(mt, m_next), s - 1, nullptr))) break;
-            rs = diag ? tc::scan_p<true>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self)
-                      : tc::scan_p<false>(U, tl, ucol, ch, c2k, m == -INFINITY ? 0.f : -m, umax, u_self);
-          }
         }
-        const float mt = umax == -INFINITY ? -INFINITY : fmaxf(umax, 0.f) * bk;
+        mt = umax == -INFINITY ? -INFINITY : fmaxf(umax, 0.f) * bk;
         if (mt > m + tc::kRescaleLog2) m_next = fmaxf(m_next, mt);
         l += rs.x + rs.y;
         tmem_st_wait();
@@ -786,31 +769,41 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
       }
       mbar_arrive(bar(B_P + bf));
     }
+    // the row's own value, 16 columns ahead of their use
+    const bool part = k.slot >= 0, live = at >= 0;
+    const BF* own = V + (live && !part ? page_row(p, table, at, k.head) : 0);
+    auto own_at = [&](int c) {  // columns c .. c + 7
+      if (!live || part || c >= p.d) return make_uint4(0, 0, 0, 0);
+      return VEC ? *reinterpret_cast<const uint4*>(own + c) : load8(own, c, p.d);
+    };
+    uint4 v0 = own_at(0), v1 = own_at(8);
     if (ok) ok = mbar_wait_warp(bar(B_O), 0, ab);
     tc_fence_after();
     if (ok && __any_sync(0xffffffffu, row_off[t] >= 0)) {
-      const bool part = k.slot >= 0, live = at >= 0;
-      const long long own = live && !part ? page_row(p, table, at, k.head) : 0;
       const bool fix = *special != 0;
       // the first unit in which some row does not see every key, in this piece
       const int j0 = max(k.kmin / kUnit, k.u0) * kUnit, j1 = min(at, k.u1 * kUnit);
       const Mix mix(p, m, l, u_self, max(at, 0));
       uint8_t* stage = smem + C::OFF_Q + warp * (32 * D * 2) + lane * 128;
 #pragma unroll 1
-      for (int c0 = 0; c0 < p.d; c0 += 32) {
-        uint32_t zr[32];
+      for (int c0 = 0; c0 < p.d; c0 += 16) {
+        const uint32_t vw[8] = {v0.x, v0.y, v0.z, v0.w, v1.x, v1.y, v1.z, v1.w};
+        v0 = own_at(c0 + 16);
+        v1 = own_at(c0 + 24);
+        uint32_t zr[16];
         if (units > 0) {
-          tmem_ld32(trow + C::OCOL + c0, zr);
+          tmem_ld16(trow + C::OCOL + c0, zr);
           tmem_ld_wait();
         }
-        float z[32];
+        float z[16];
 #pragma unroll
-        for (int c = 0; c < 32; ++c) z[c] = units > 0 ? __uint_as_float(zr[c]) : 0.f;
+        for (int c = 0; c < 16; ++c) z[c] = units > 0 ? __uint_as_float(zr[c]) : 0.f;
         if (fix && live) {  // rare: the values that were taken out
+#pragma unroll 1
           for (int j = j0; j < j1; ++j) {
             const BF* v = V + page_row(p, table, j, k.head);
 #pragma unroll
-            for (int c = 0; c < 32; ++c) {
+            for (int c = 0; c < 16; ++c) {
               const float x = c0 + c < p.d ? (float)v[c0 + c] : 0.f;
               if (!isfinite(x)) z[c] += x;
             }
@@ -820,20 +813,17 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
           float* dst = w.z + ((long long)k.slot * w.rows + t) * w.width + c0;
           if (live)
 #pragma unroll
-            for (int c = 0; c < 32; c += 4)
+            for (int c = 0; c < 16; c += 4)
               if (c0 + c < w.width)
                 *reinterpret_cast<float4*>(dst + c) = make_float4(z[c], z[c + 1], z[c + 2], z[c + 3]);
         } else {
 #pragma unroll
-          for (int c = 0; c < 32; c += 8) {
-            uint4 vv = make_uint4(0, 0, 0, 0);
-            if (live && c0 + c < p.d)
-              vv = VEC ? *reinterpret_cast<const uint4*>(V + own + c0 + c) : load8(V + own, c0 + c, p.d);
-            const uint32_t vw[4] = {vv.x, vv.y, vv.z, vv.w};
+          for (int c = 0; c < 16; c += 8) {
             uint32_t yw[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              const float2 vf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&vw[e]));
+              const uint32_t w2 = vw[c / 2 + e];
+              const float2 vf = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&w2));
               yw[e] = live ? pack_bf16x2(mix.y(z[c + 2 * e], vf.x), mix.y(z[c + 2 * e + 1], vf.y)) : 0u;
             }
             const int g = ((c0 & 63) + c) >> 3;
