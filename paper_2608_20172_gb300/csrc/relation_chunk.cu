@@ -32,19 +32,20 @@ namespace chunk {
 
 constexpr int kUnit = 64;  // keys that are loaded together; pieces are made of them
 constexpr int kPlanThreads = 1024;
+constexpr int kJoinRows = 8;  // rows of a tile that the last kernel joins together
 constexpr int kSorted = 512;  // requests that the plan brings into an order of its own
 
 // The workspace: what the plan says, and the pieces' partial results.
-struct Item {  // a CTA's work: a piece of a tile for one key head
+struct alignas(16) Item {  // a CTA's work: a piece of a tile for one key head
   int b, s0, row0, rows;   // request, its first token, the tile's first row within it, the tile's rows
   int head, u0, u1, slot;  // units u0 .. u1 - 1; slot: of the partial result, -1: the tile's only piece
 };
 constexpr int kToTheEnd = 0x7fffffff;  // u1 of a tile's last piece
-struct Split {  // a tile of several pieces
+struct alignas(16) Split {  // a tile of several pieces
   int b, s0, row0, rows, pieces, slot, pad0, pad1;  // slot: the first key head's first
 };
 struct Plan {
-  int* head;     // {items, tiles of several pieces}
+  int* head;     // {items, tiles of several pieces, the most row groups (kJoinRows) that one of these has}
   int* first;    // [B + 1] first tile of a request, in the plan's order
   int4* tiles;   // [max_tiles] request in that order, first row, pieces (twice, and whether the last is a
                  // rest), units of keys and then the first slot
@@ -63,8 +64,8 @@ __device__ __forceinline__ int2 tokens_of(const ChunkProblem& p, int b) {
   const int s0 = min(max(p.starts[b], 0), p.N), s1 = min(max(p.starts[b + 1], s0), p.N);
   return make_int2(s0, s1);
 }
-__device__ __forceinline__ int tiles_of(int2 tokens, int G, int tile) {
-  return (int)(((long long)(tokens.y - tokens.x) * G + tile - 1) / tile);
+__device__ __forceinline__ int tiles_of(int2 tokens, int G, int tile) {  // (a power of two)
+  return (int)(((long long)(tokens.y - tokens.x) * G + tile - 1) >> (31 - __clz(tile)));
 }
 // Units of keys that a tile's last row sees, which is the most where positions ascend
 __device__ __forceinline__ int units_of(const ChunkProblem& p, int2 tokens, int row0, int G, int tile) {
@@ -76,7 +77,9 @@ __device__ __forceinline__ int units_of(const ChunkProblem& p, int2 tokens, int 
 // after all others: it fills the time between the ends of these (equal pieces of a tile would end in a
 // second round).  Less than `least` is no piece of its own.
 __device__ __forceinline__ int piece_of(const Plan& w, unsigned long long units) {
-  return (int)min(max((unsigned long long)w.least, (units + w.target - 1) / w.target), 1ull << 30);
+  const unsigned long long up = units + w.target - 1;  // (a division in 64 bits takes long)
+  const unsigned long long mean = up >> 32 ? up / w.target : (unsigned)up / (unsigned)w.target;
+  return (int)min(max((unsigned long long)w.least, mean), 1ull << 30);
 }
 
 struct Cut {
@@ -121,49 +124,65 @@ __device__ __forceinline__ int4 block_scan(int4 x, int4* part, int4* total) {
 
 __global__ void __launch_bounds__(kPlanThreads)
     plan_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w) {
+  // (what fits is kept in shared memory: a trip to global memory takes a tenth of a small plan)
   __shared__ int4 part[32];
   __shared__ unsigned long long work;
+  __shared__ int most, length[kSorted], order[kSorted], first_s[kSorted + 1];
+  __shared__ int2 tokens_s[kSorted], upto_s[kPlanThreads + 1];
   pdl_wait_and_launch();
-  __shared__ int length[kSorted], order[kSorted];
   const int G = p.H / p.Hk, T = blockDim.x;
+  const bool sorted = p.B <= kSorted && p.B <= T;
+  int* first = sorted ? first_s : w.first;
   int tiles = 0;
   int4 total;
-  if (threadIdx.x == 0) work = 0;
+  if (threadIdx.x == 0) {
+    work = 0;
+    most = 0;
+  }
   // the longest requests first (their tiles would end last otherwise)
-  const bool sorted = p.B <= kSorted && p.B <= T;
   if (sorted) {
     const int b = threadIdx.x;
-    const int2 t = b < p.B ? tokens_of(p, b) : make_int2(0, 0);
-    const int mine = t.y > t.x ? units_of(p, t, (t.y - t.x) * G - 1, G, 1) : 0;
-    if (b < p.B) length[b] = mine;
+    int2 t = make_int2(0, 0);
+    int mine = 0;
+    if (b < p.B) {
+      t = tokens_of(p, b);
+      tokens_s[b] = t;
+      if (t.y > t.x) mine = units_of(p, t, (t.y - t.x) * G - 1, G, 1);
+      length[b] = mine;
+    }
     __syncthreads();
     int rank = 0;
-    for (int i = 0; i < p.B && b < p.B; ++i) rank += length[i] > mine || (length[i] == mine && i < b);
-    if (b < p.B) order[rank] = b;
+    if (b < p.B) {
+      for (int i = 0; i < p.B; ++i) rank += length[i] > mine || (length[i] == mine && i < b);
+      order[rank] = b;
+    }
     __syncthreads();
   }
   auto request = [&](int i) { return sorted ? order[i] : i; };
+  auto tokens = [&](int b) { return sorted ? tokens_s[b] : tokens_of(p, b); };
   for (int b0 = 0; b0 < p.B; b0 += T) {
     const int b = b0 + (int)threadIdx.x;
-    const int n = b < p.B ? tiles_of(tokens_of(p, request(b)), G, w.tile) : 0;
+    const int n = b < p.B ? tiles_of(tokens(request(b)), G, w.tile) : 0;
     const int at = tiles + block_scan(make_int4(n, 0, 0, 0), part, &total).x;
-    if (b < p.B) w.first[b] = at;
+    if (b < p.B) first[b] = at;
     tiles += total.x;
   }
-  if (threadIdx.x == 0) w.first[p.B] = tiles;
+  if (threadIdx.x == 0) first[p.B] = tiles;
   __syncthreads();
   tiles = min(tiles, w.max_tiles);  // (requests whose tokens overlap: not laid out past the workspace)
+  const bool once = tiles <= T;     // a thread has a tile at most
+  int2* upto = once ? upto_s : w.upto;
   unsigned long long mine = 0;
   int4 t = make_int4(0, 0, 0, 0);
   for (int i = threadIdx.x; i < tiles; i += T) {
     int lo = 0, hi = p.B;  // the last request whose first tile is not after this one
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (w.first[mid] <= i) lo = mid; else hi = mid;
+      if (first[mid] <= i) lo = mid; else hi = mid;
     }
-    const int row0 = (i - w.first[lo]) * w.tile;
-    t = make_int4(lo, row0, 1, units_of(p, tokens_of(p, request(lo)), row0, G, w.tile));
-    if (tiles > T) w.tiles[i] = t;
+    const int row0 = (i - first[lo]) * w.tile;
+    t = make_int4(lo, row0, 1, units_of(p, tokens(request(lo)), row0, G, w.tile));
+    if (!once) w.tiles[i] = t;
     mine += t.w;
   }
   for (int o = 16; o > 0; o >>= 1) mine += __shfl_xor_sync(0xffffffffu, mine, o);
@@ -173,7 +192,7 @@ __global__ void __launch_bounds__(kPlanThreads)
   int4 sum = make_int4(0, 0, 0, 0);  // pieces but the rests, tiles of several, their slots, rests
   for (int i0 = 0; i0 < tiles; i0 += T) {
     const int i = i0 + (int)threadIdx.x;
-    if (i < tiles && tiles > T) t = w.tiles[i];
+    if (i < tiles && !once) t = w.tiles[i];
     const Cut c = i < tiles ? cut_of(t.w, per_piece, w.least) : Cut{0, 0};
     const bool several = c.pieces > 1;
     const int4 at = add4(sum, block_scan(make_int4(c.pieces - c.rest, several, several ? c.pieces * p.Hk : 0, c.rest),
@@ -181,28 +200,32 @@ __global__ void __launch_bounds__(kPlanThreads)
     sum = add4(sum, total);
     if (i < tiles) {
       const int b = request(t.x);
-      const int2 tok = tokens_of(p, b);
+      const int2 tok = tokens(b);
       t.z = 2 * c.pieces + c.rest;
       t.w = several ? at.z : -1;
-      w.tiles[i] = t;
-      w.upto[i] = make_int2(at.x, at.w);
-      if (several)
-        w.split[at.y] = {b, tok.x, t.y, min(w.tile, (tok.y - tok.x) * G - t.y), c.pieces, at.z, 0, 0};
+      if (!once) w.tiles[i] = t;
+      upto[i] = make_int2(at.x, at.w);
+      if (several) {
+        const int rows = min(w.tile, (tok.y - tok.x) * G - t.y);
+        w.split[at.y] = {b, tok.x, t.y, rows, c.pieces, at.z, 0, 0};
+        atomicMax(&most, (rows + kJoinRows - 1) / kJoinRows);
+      }
     }
   }
   if (threadIdx.x == 0) {
-    w.upto[tiles] = make_int2(sum.x, sum.w);
+    upto[tiles] = make_int2(sum.x, sum.w);
     w.head[0] = (sum.x + sum.w) * p.Hk;
     w.head[1] = sum.y;
   }
   __syncthreads();
+  if (threadIdx.x == 0) w.head[2] = most;
   for (int i = threadIdx.x; i < tiles; i += T) {
-    t = w.tiles[i];
+    if (!once) t = w.tiles[i];
     const int b = request(t.x);
-    const int2 tok = tokens_of(p, b);
-    const int end = min(w.first[t.x + 1], tiles), from = w.upto[w.first[t.x]].x, per = w.upto[end].x - from;
-    const int later = w.upto[end].x - w.upto[i + 1].x, rows = min(w.tile, (tok.y - tok.x) * G - t.y);
-    const int pieces = t.z >> 1, rest = t.z & 1, rests = sum.x * p.Hk + w.upto[i].y * p.Hk;
+    const int2 tok = tokens(b);
+    const int end = min(first[t.x + 1], tiles), from = upto[first[t.x]].x, per = upto[end].x - from;
+    const int later = upto[end].x - upto[i + 1].x, rows = min(w.tile, (tok.y - tok.x) * G - t.y);
+    const int pieces = t.z >> 1, rest = t.z & 1, rests = sum.x * p.Hk + upto[i].y * p.Hk;
     for (int h = 0; h < p.Hk; ++h)
       for (int k = 0; k < pieces; ++k)
         w.items[rest && k == pieces - 1 ? rests + h : from * p.Hk + h * per + later + k] = {
@@ -238,7 +261,11 @@ __device__ __forceinline__ Item plan_small(const ChunkProblem& p, const Plan& w)
   const int slot = several ? end.z - mine.z : -1;
   if (blockIdx.x == 0) {
     if (several) w.split[end.y - 1] = {b, tok.x, row0, rows, c.pieces, slot, 0, 0};
-    if (lane == 31) w.head[1] = end.y;
+    const int most = __reduce_max_sync(0xffffffffu, several ? (rows + kJoinRows - 1) / kJoinRows : 0);
+    if (lane == 31) {
+      w.head[1] = end.y;
+      w.head[2] = most;
+    }
   }
   // the tile that holds this CTA's item: among the pieces but the rests, or the rests after them
   const int firsts = __shfl_sync(0xffffffffu, end.x, 31);
@@ -1065,7 +1092,8 @@ __global__ void __launch_bounds__(kSimtThreads, 2)
 }
 
 // ---------------------------------------------------------------------------------------------------
-// The rows of tiles of several pieces, a warp each; zeros for the tokens of no request.
+// The rows of tiles of several pieces, a warp each, eight rows of a tile and head to a CTA (the first eight of
+// all, then the next: tiles of few rows leave nothing behind them); zeros for the tokens of no request.
 // ---------------------------------------------------------------------------------------------------
 constexpr int kJoinThreads = 256;
 
@@ -1073,23 +1101,30 @@ template <typename TI>
 __global__ void __launch_bounds__(kJoinThreads)
     join_kernel(const __grid_constant__ ChunkProblem p, const __grid_constant__ Plan w) {
   pdl_wait_and_launch();
-  const int lane = threadIdx.x & 31, G = p.H / p.Hk;
-  const long long first = ((long long)blockIdx.x * kJoinThreads + threadIdx.x) >> 5,
-                  step = (long long)gridDim.x * (kJoinThreads / 32);
-  const long long rows = (long long)w.head[1] * p.Hk * w.rows;
-  for (long long e = first; e < rows; e += step) {
-    const int r = (int)(e % w.rows), h = (int)(e / w.rows % p.Hk);
-    const Split t = w.split[e / w.rows / p.Hk];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = p.H / p.Hk;
+  const int heads = w.head[1] * p.Hk;  // tiles of several pieces, and heads
+  const long long groups = (long long)heads * w.head[2];
+  for (long long e = blockIdx.x; e < groups; e += gridDim.x) {
+    const int at_head = (int)(e % heads), h = at_head % p.Hk, r = (int)(e / heads) * kJoinRows + warp;
+    const Split t = w.split[at_head / p.Hk];
     if (r >= t.rows) continue;
     const int f = t.row0 + r, token = t.s0 + f / G, head = h * G + f % G, at = p.positions[token];
-    if (at < 0 || at >= p.limit) continue;  // (zeros have been written)
     const long long slot = t.slot + h * t.pieces;
-    float m = -INFINITY, l = 0.f, u_self = 0.f, z[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int k = lane; k < t.pieces; k += 32) m = fmaxf(m, w.stats[(slot + k) * w.rows + r].x);
+    float4 st = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+    if (lane < t.pieces) st = w.stats[(slot + lane) * w.rows + r];
+    if (at < 0 || at >= p.limit) continue;  // (zeros have been written)
+    const TI* V = static_cast<const TI*>(p.v) + page_row(p, p.table + (long long)t.b * p.t_stride, at, h);
+    float v[4], z[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) v[c] = lane + 32 * c < p.d ? (float)V[lane + 32 * c] : 0.f;
+    float m = st.x, l = 0.f, u_self = 0.f;
+    for (int k = lane + 32; k < t.pieces; k += 32) m = fmaxf(m, w.stats[(slot + k) * w.rows + r].x);
     for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
     for (int k0 = 0; k0 < t.pieces; k0 += 32) {
-      float4 st = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-      if (k0 + lane < t.pieces) st = w.stats[(slot + k0 + lane) * w.rows + r];
+      if (k0 > 0) {
+        st = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+        if (k0 + lane < t.pieces) st = w.stats[(slot + k0 + lane) * w.rows + r];
+      }
       // no key seen: 0; m is -inf too where every score is NaN (l NaN): NaN
       const float wt = st.x == -INFINITY ? 0.f * st.y : ex2_approx(st.x - m);
       const unsigned who = __ballot_sync(0xffffffffu, st.w != 0.f);
@@ -1107,13 +1142,14 @@ __global__ void __launch_bounds__(kJoinThreads)
       }
     }
     const Mix mix(p, m, l, u_self, at);
-    const TI* V = static_cast<const TI*>(p.v) + page_row(p, p.table + (long long)t.b * p.t_stride, at, h);
     TI* y = static_cast<TI*>(p.out) + (long long)token * p.qsT + (long long)head * p.qsH;
 #pragma unroll
     for (int c = 0; c < 4; ++c)
-      if (lane + 32 * c < p.d) y[lane + 32 * c] = (TI)mix.y(z[c], (float)V[lane + 32 * c]);
+      if (lane + 32 * c < p.d) y[lane + 32 * c] = (TI)mix.y(z[c], v[c]);
     if (lane == 0) p.logz[(long long)token * p.H + head] = mix.logz;
   }
+  const long long first = ((long long)blockIdx.x * kJoinThreads + threadIdx.x) >> 5,
+                  step = (long long)gridDim.x * (kJoinThreads / 32);
   const int before = min(max(p.starts[0], 0), p.N), after = min(max(p.starts[p.B], before), p.N);
   const long long none = (long long)(before + p.N - after) * p.H;
   for (long long e = first; e < none; e += step) {
