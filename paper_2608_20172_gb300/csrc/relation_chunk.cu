@@ -1165,10 +1165,11 @@ __global__ void __launch_bounds__(kJoinThreads)
 // ---------------------------------------------------------------------------------------------------
 // The plan's arrays in a workspace; the bytes of it
 size_t carve(Plan* w, uint8_t* base, int N, int B, int H, int Hk, int d, int limit, relation_dtype dt) {
-  // (as many pieces as CTAs fit the GPU; fp32, whose units take long, twice as many and shorter ones)
+  // (as many pieces as CTAs fit the GPU; fp32, whose units take long, twice as many and shorter ones,
+  // of one unit at least: 451 tokens of 8 x 72 take 42 us, with two units at least 47)
   w->tile = dt == RELATION_F32 ? SM_ROWS : BM;
   w->target = dt == RELATION_F32 ? 608 : 304;
-  w->least = dt == RELATION_F32 ? 2 : 4;
+  w->least = dt == RELATION_F32 ? 1 : 4;
   const long long G = H / Hk, rows = N * G;
   // a request of n rows has ceil(n / tile) tiles, and no more requests than tokens have any
   const long long tiles = (rows + (long long)(B < N ? B : N) * (w->tile - 1)) / w->tile + 1;
