@@ -7,17 +7,22 @@
 //   Y = (1 - g) v_p + g sum_j e^{E_j} v_j / sum_j e^{E_j},  logZ = logaddexp(S, A).
 // G = H / H_kv query heads share a key/value head.
 //
-// A tile is kRows (token, query head of one key head) pairs of a request, token-major: shared heads and
+// A tile is 128 (fp32: 64) (token, query head of one key head) pairs of a request, token-major: shared heads and
 // short chunks fill it together.  The host knows neither counts nor positions, so a first small kernel lays
-// out the work: the tiles of all requests, each cut along its keys into so many pieces that about as many
-// pieces as CTAs fit the GPU have equal length, in an order that keeps the tiles of a request's head side by
+// out the work: the tiles of all requests, each cut along its keys into pieces of the mean length of as many
+// pieces as CTAs fit the GPU and a rest, which is started last, in an order that keeps the tiles of a request's head side by
 // side (they read the same keys) with the longest first, the requests with the longest history before the
-// others.  A tile of one piece is finished by its CTA; of
-// others every piece leaves its rows' (m, l, z), which a last kernel joins.
+// others.  A tile of one piece is finished by its CTA; of others every piece leaves its rows' (m, l, z), which a last kernel joins.
 //
 // bf16: the tensor-core forward's scan (relation_tc_fwd.cu, scan.cuh) with keys and values fetched from
 // their pages by TMA, a box of rows that lie in one page at a time (cp.async, row by row, for pages whose
 // size is no multiple of 8).  fp32: register tiles on the CUDA cores.
+//
+// Bound by the hand-off between scan and products (tensor cores 33 %, special functions 49 % busy).
+// Measured: 4 pieces of 2048 tokens behind 16384 rows of 16 x 128 bf16 620 us, 1.08 PFLOP/s; 48 requests,
+// half of them decoding, of 32 query heads over 8 x 80 in pages of 24 rows 390 us (of 64 rows 355); 5 tokens
+// behind 2048 rows of 12 x 64 16 us, dependent trips; fp32, 451 tokens of 8 query heads over 4 x 72 42 us,
+// long pieces 42 TFLOP/s.
 #include <cudaTypedefs.h>
 #include <math.h>
 
@@ -1238,8 +1243,8 @@ bool make_map(CUtensorMap* m, const void* base, const ChunkProblem& p, int rows)
 template <int D>
 cudaError_t launch_tc(const ChunkProblem& p, const Plan& w, bool groups, cudaStream_t s) {
   // Boxes as large as pages and units allow: a power of two that divides both, or where that is 8 (whose
-  // boxes alone would bound the kernel: pages of 24 rows of 80 bf16 455 us in eights) a page, or 32 rows of
-  // a large one, and eights for what is left.
+  // boxes alone would bound the kernel: 48 requests in pages of 24 rows of 80 bf16 518 us in eights, 390 so) a
+  // page, or 32 rows of a large one, and eights for what is left.
   int big = kUnit;
   while (p.page % big) big /= 2;
   if (big == 8) big = p.page < kUnit ? p.page : 32;

@@ -15,8 +15,10 @@
 // Gradient, of g log p_y + h H + k logZ:
 //   dx_j = (1 / T) (g (delta_jy - p_j) - h p_j (log p_j + H) + k p_j).
 //
-// Bound by memory: the logits are read once (gradient: and written).  Few rows are shared by clusters
-// of CTAs that join through distributed shared memory.
+// Memory is the floor: the logits are read once (gradient: and written).  Few rows are shared by clusters
+// of CTAs that join through distributed shared memory.  Measured: 2048 rows of 50257 bf16 42 us, 4.9 TB/s,
+// with 20 alternatives 60 us, bound by issue (2.9 instructions per clock); one row of 32000 fp32 with 5
+// alternatives 7 us, a chain of barriers; the gradient of 4096 rows of 50257 bf16 139 us, 5.9 TB/s.
 #include <float.h>
 #include <math.h>
 
