@@ -455,8 +455,9 @@ relation_status relation_sample(const void* logits, int R, int V, long long s_ro
  *               descending order, equal ones by index, and their log p; -1 and -inf where fewer
  *               tokens are unmasked.
  * A row without an unmasked token has logz = -inf, entropy 0 and logprob -inf (0 without a given
- * token); one with a NaN, or with a temperature that is not positive and finite (reported to
- * dev_status, if given, as RELATION_ERR_INVALID_ARG), NaN in all of them and tokens -1.  A given
+ * token); one with a NaN, or with a temperature that is not positive and finite or whose
+ * reciprocal overflows fp32 (reported to dev_status, if given, as RELATION_ERR_INVALID_ARG), NaN
+ * in all of them and tokens -1.  A given
  * token >= V has logprob NaN and is reported likewise.  Logits of +inf share the probability among
  * them.  Sums in fp32.  Asynchronous on `stream`; one launch; nothing is allocated.
  */
@@ -473,7 +474,9 @@ relation_status relation_logprobs(const void* logits, int R, int V, long long s_
  * 0; g counts as 0 in a row without a given token).
  *   logz, entropy : the forward's for the same logits, targets and temperature.
  *   dlogits     [R][V] in dt, row stride s_out; it may be the logits (s_out = s_row).
- * A row whose logz is -inf gets zeros, one whose logz is NaN or whose given token is >= V NaN.
+ * Rows with |logz| above 64 (low temperatures, logits with a large common part) take their maximum
+ * and sum from the logits again, since logz is too coarse there; they take longer.  A row without an
+ * unmasked token gets zeros, one whose logz is NaN or whose given token is >= V NaN.
  * Asynchronous on `stream`; one launch; nothing is allocated.
  */
 relation_status relation_logprobs_grad(const void* logits, int R, int V, long long s_row,

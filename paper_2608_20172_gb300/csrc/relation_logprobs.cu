@@ -14,11 +14,12 @@
 // per lane.  The lists' elements are ranked against each other.
 // Gradient, of g log p_y + h H + k logZ:
 //   dx_j = (1 / T) (g (delta_jy - p_j) - h p_j (log p_j + H) + k p_j).
+// log p_j is x_j / T - logZ where logZ is small; other rows' CTA takes M and l again.
 //
 // Memory is the floor: the logits are read once (gradient: and written).  Few rows are shared by clusters
 // of CTAs that join through distributed shared memory.  Measured: 2048 rows of 50257 bf16 42 us, 4.9 TB/s,
 // with 20 alternatives 60 us, bound by issue (2.9 instructions per clock); one row of 32000 fp32 with 5
-// alternatives 7 us, a chain of barriers; the gradient of 4096 rows of 50257 bf16 139 us, 5.9 TB/s.
+// alternatives 7 us, a chain of barriers; the gradient of 4096 rows of 50257 bf16 134 us, 6.1 TB/s.
 #include <float.h>
 #include <math.h>
 
@@ -189,7 +190,8 @@ __device__ __forceinline__ int rank_of(u64 key, const u64* list, int n) {
 }
 
 template <typename TI, int kThreads>
-__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 8 : 2) logprobs_kernel(const __grid_constant__ LogprobsProblem p, int n_cl) {
+__global__ void __launch_bounds__(kThreads, kThreads == 256 ? 8 : 2)
+    logprobs_kernel(const __grid_constant__ LogprobsProblem p, int n_cl) {
   constexpr int N = Vec<TI>::N;
   constexpr int kWarps = kThreads / 32;
   __shared__ Smem<kWarps> sm;
@@ -416,6 +418,58 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 8 : 2) logprobs_ke
 
 // Gradient: a CTA takes kChunk groups of a row.
 constexpr int kGradThreads = 256, kGradU = 4, kChunk = kGradThreads * kGradU;
+constexpr float kNear = 64.f;  // |logz| of the rows whose log p is x / T - logz
+
+// One of the CTA's threads' values: the largest (NaN: any), or the sum in a fixed order
+template <bool MAX>
+__device__ __forceinline__ float block_join(float v, float* part) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    const float y = __shfl_xor_sync(0xffffffffu, v, o);
+    v = MAX ? max_nan(v, y) : v + y;
+  }
+  __syncthreads();  // (what was joined before has been read)
+  if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+  __syncthreads();
+  v = part[0];
+#pragma unroll
+  for (int i = 1; i < kGradThreads / 32; ++i) v = MAX ? max_nan(v, part[i]) : v + part[i];
+  return v;
+}
+
+// A whole row by one CTA with its own maximum and sum: large |logz|, infinite logits, no token, NaN.  The row
+// is read before any of it is written, each element of the last pass by the thread that writes it: the output
+// may be the logits.  4096 rows of 50257 bf16 that all come here take 475 us, ordinary ones 135.
+template <typename TI>
+__device__ __noinline__ void grad_far(const Row<TI> x, TI* out, int target, float scale, float logz, float H,
+                                      float g, float h, float k, int V) {
+  __shared__ float part[kGradThreads / 32];
+  const bool bad = logz != logz || target >= V;  // (uniform, as all that follows is but the elements)
+  float m = -INFINITY, l = 0.f;
+  if (!bad) {
+    for (int c = (int)threadIdx.x; c < V; c += kGradThreads) m = max_nan(m, (float)x.x[c]);
+    m = block_join<true>(m, part);
+  }
+  // t = (x - m) / T; the largest ones' is 0, infinite ones' too
+  auto t_of = [&](float v) { return v == m ? 0.f : (v - m) * scale; };
+  if (!bad && m != -INFINITY) {
+    for (int c = (int)threadIdx.x; c < V; c += kGradThreads) l += ex2_approx(t_of((float)x.x[c]) * kLog2e);
+    l = block_join<false>(l, part);
+  }
+  const float logl = logf(l), inv = 1.f / l;
+  for (int c = (int)threadIdx.x; c < V; c += kGradThreads) {
+    float d = NAN;
+    if (!bad && m == -INFINITY) {
+      d = 0.f;
+    } else if (!bad) {
+      const float t = t_of((float)x.x[c]), q = ex2_approx(t * kLog2e) * inv;
+      d = q == 0.f ? 0.f : q * (k - g - h * (t - logl + H));
+      if (c == target) d += g;
+      d *= scale;
+    }
+    out[c] = (TI)d;
+  }
+}
 
 template <typename TI, bool VEC>
 __global__ void __launch_bounds__(kGradThreads)
@@ -437,18 +491,17 @@ __global__ void __launch_bounds__(kGradThreads)
   const float h = p.dentropy ? p.dentropy[row] : 0.f, k = p.dlogz ? p.dlogz[row] : 0.f;
   // a = log2 p_j:  dx_j = 2^a (c0 + c1 a), and g / T more for the given token
   const float s2 = scale * kLog2e, z2 = -logz * kLog2e;
-  const float c0 = target >= p.V ? NAN : (k - g - h * H) * scale;  // (a token outside the row has no log p)
+  const float c0 = target >= p.V ? NAN : (k - g - h * H) * scale;  // (no log p: the NaN leads to grad_far)
   const float c1 = -h * kLn2 * scale;
-  // Rows that take care: without a token (-inf), with NaN, and those whose logz does not hold the logarithm
-  // of the equal largest ones' number, +inf or nothing but the type's lowest value
-  const bool odd = !(fabsf(logz) <= 1e30f) || !isfinite(c0) || !isfinite(c1) || !isfinite(s2);
+  // log p_j = x_j / T - logz is a difference of two rounded numbers: up to kNear its roundings are below 3e-5
+  // of p; beyond, and where a coefficient leaves the type, a row's maximum is taken from its logits first.
+  if (!(fabsf(logz) <= kNear) || !isfinite(c0) || !isfinite(c1) || !isfinite(s2)) {
+    if (chunk == 0) grad_far(x, out, target, scale, logz, H, g, h, k, p.V);
+    return;
+  }
   auto grad = [&](float v, int c) {
-    if (logz == -INFINITY) return 0.f;
-    float a = fmaf(v, s2, z2);
-    if (fabsf(logz) > 1e30f)
-      a = (logz == INFINITY ? v == INFINITY : a >= -1e-6f * fabsf(z2)) ? -H * kLog2e : -INFINITY;
-    const float q = ex2_approx(a);
-    const float d = c0 != c0 ? c0 : q == 0.f ? 0.f : q * fmaf(a, c1, c0);
+    const float a = fmaf(v, s2, z2), q = ex2_approx(a);
+    const float d = q == 0.f ? 0.f : q * fmaf(a, c1, c0);
     return c == target ? fmaf(g, scale, d) : d;
   };
 #pragma unroll
@@ -459,26 +512,21 @@ __global__ void __launch_bounds__(kGradThreads)
     if (x.whole(gr)) {
       float v[N];
       Vec<TI>::unpack(w[i], v);
-      if (odd) {
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[j] = grad(v[j], at + j);
-      } else {
+      for (int j = 0; j < N; j += 2) {
+        float2 a = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(s2, s2), make_float2(z2, z2));
+        // (2^a is 0 long before -inf would make 2^a a NaN)
+        a.x = max_nan(a.x, -300.f);
+        a.y = max_nan(a.y, -300.f);
+        const float2 d = __fmul2_rn(make_float2(ex2_approx(a.x), ex2_approx(a.y)),
+                                    __ffma2_rn(a, make_float2(c1, c1), make_float2(c0, c0)));
+        v[j] = d.x;
+        v[j + 1] = d.y;
+      }
+      if ((unsigned)(target - at) < (unsigned)N) {
 #pragma unroll
-        for (int j = 0; j < N; j += 2) {
-          float2 a = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(s2, s2), make_float2(z2, z2));
-          // (2^a is 0 long before -inf would make 2^a a NaN)
-          a.x = max_nan(a.x, -300.f);
-          a.y = max_nan(a.y, -300.f);
-          const float2 d = __fmul2_rn(make_float2(ex2_approx(a.x), ex2_approx(a.y)),
-                                      __ffma2_rn(a, make_float2(c1, c1), make_float2(c0, c0)));
-          v[j] = d.x;
-          v[j + 1] = d.y;
-        }
-        if ((unsigned)(target - at) < (unsigned)N) {
-#pragma unroll
-          for (int j = 0; j < N; ++j)
-            if (at + j == target) v[j] = fmaf(g, scale, v[j]);
-        }
+        for (int j = 0; j < N; ++j)
+          if (at + j == target) v[j] = fmaf(g, scale, v[j]);
       }
       if (VEC) {
         *reinterpret_cast<uint4*>(out + at) = Vec<TI>::pack(v);
