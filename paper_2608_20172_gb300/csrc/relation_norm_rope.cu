@@ -15,7 +15,7 @@
 // Bound by memory: a row is read and written once (backward: two reads).  A few lanes share a row, 16
 // bytes of two parts of it each, so that both channels of a pair are in one lane in either layout and
 // the sums are a few shuffles; a token's turns are taken once for all heads.  Four CTAs of 128 threads an SM
-// (three: 134 us in the first case below, five, with one part a lane: 141).  Measured: 32768 tokens of 32 + 8
+// (three: 134 us in the first case below, five, which leave registers for one row in flight a lane: 141).  Measured: 32768 tokens of 32 + 8
 // heads of 128 bf16 118 us, 5.7 TB/s; the gradient of 16384 tokens of 16 + 16 heads 86 us, 4.7 TB/s; 32
 // tokens of 12 + 12 heads of 64 3.5 us, one chain of position, turn and row.
 #include <math.h>
