@@ -19,7 +19,7 @@
 // Memory is the floor: the logits are read once (gradient: and written).  Few rows are shared by clusters
 // of CTAs that join through distributed shared memory.  Measured: 2048 rows of 50257 bf16 42 us, 4.9 TB/s,
 // with 20 alternatives 60 us, bound by issue (2.9 instructions per clock); one row of 32000 fp32 with 5
-// alternatives 7 us, a chain of barriers; the gradient of 4096 rows of 50257 bf16 134 us, 6.1 TB/s.
+// alternatives 7 us, a chain of barriers; the gradient of 4096 rows of 50257 bf16 129 us, 6.4 TB/s.
 #include <float.h>
 #include <math.h>
 
@@ -439,35 +439,60 @@ __device__ __forceinline__ float block_join(float v, float* part) {
 
 // A whole row by one CTA with its own maximum and sum: large |logz|, infinite logits, no token, NaN.  The row
 // is read before any of it is written, each element of the last pass by the thread that writes it: the output
-// may be the logits.  4096 rows of 50257 bf16 that all come here take 475 us, ordinary ones 135.
-template <typename TI>
+// may be the logits.  4096 rows of 50257 bf16 that all come here take 302 us (an
+// element at a time 475), ordinary ones 129.
+template <typename TI, bool VEC>
 __device__ __noinline__ void grad_far(const Row<TI> x, TI* out, int target, float scale, float logz, float H,
                                       float g, float h, float k, int V) {
+  constexpr int N = Vec<TI>::N;
   __shared__ float part[kGradThreads / 32];
   const bool bad = logz != logz || target >= V;  // (uniform, as all that follows is but the elements)
   float m = -INFINITY, l = 0.f;
   if (!bad) {
-    for (int c = (int)threadIdx.x; c < V; c += kGradThreads) m = max_nan(m, (float)x.x[c]);
+    for (int gr = (int)threadIdx.x; gr < x.groups; gr += kGradThreads) {
+      float v[N];
+      x.load(gr, v);
+#pragma unroll
+      for (int j = 0; j < N; ++j) m = max_nan(m, v[j]);
+    }
     m = block_join<true>(m, part);
   }
   // t = (x - m) / T; the largest ones' is 0, infinite ones' too
   auto t_of = [&](float v) { return v == m ? 0.f : (v - m) * scale; };
   if (!bad && m != -INFINITY) {
-    for (int c = (int)threadIdx.x; c < V; c += kGradThreads) l += ex2_approx(t_of((float)x.x[c]) * kLog2e);
+    for (int gr = (int)threadIdx.x; gr < x.groups; gr += kGradThreads) {
+      float v[N];
+      x.load(gr, v);  // (-inf outside the row: a weight of 0)
+#pragma unroll
+      for (int j = 0; j < N; ++j) l += ex2_approx(t_of(v[j]) * kLog2e);
+    }
     l = block_join<false>(l, part);
   }
   const float logl = logf(l), inv = 1.f / l;
-  for (int c = (int)threadIdx.x; c < V; c += kGradThreads) {
-    float d = NAN;
-    if (!bad && m == -INFINITY) {
-      d = 0.f;
-    } else if (!bad) {
-      const float t = t_of((float)x.x[c]), q = ex2_approx(t * kLog2e) * inv;
-      d = q == 0.f ? 0.f : q * (k - g - h * (t - logl + H));
-      if (c == target) d += g;
-      d *= scale;
+  for (int gr = (int)threadIdx.x; gr < x.groups; gr += kGradThreads) {
+    const int at = gr * N - x.off;
+    float v[N];
+    x.load(gr, v);
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      float d = NAN;
+      if (!bad && m == -INFINITY) {
+        d = 0.f;
+      } else if (!bad) {
+        const float t = t_of(v[j]), q = ex2_approx(t * kLog2e) * inv;
+        d = q == 0.f ? 0.f : q * (k - g - h * (t - logl + H));
+        if (at + j == target) d += g;
+        d *= scale;
+      }
+      v[j] = d;
     }
-    out[c] = (TI)d;
+    if (VEC && x.whole(gr)) {
+      *reinterpret_cast<uint4*>(out + at) = Vec<TI>::pack(v);
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+        if (at + j >= 0 && at + j < V) out[at + j] = (TI)v[j];
+    }
   }
 }
 
@@ -496,7 +521,7 @@ __global__ void __launch_bounds__(kGradThreads)
   // log p_j = x_j / T - logz is a difference of two rounded numbers: up to kNear its roundings are below 3e-5
   // of p; beyond, and where a coefficient leaves the type, a row's maximum is taken from its logits first.
   if (!(fabsf(logz) <= kNear) || !isfinite(c0) || !isfinite(c1) || !isfinite(s2)) {
-    if (chunk == 0) grad_far(x, out, target, scale, logz, H, g, h, k, p.V);
+    if (chunk == 0) grad_far<TI, VEC>(x, out, target, scale, logz, H, g, h, k, p.V);
     return;
   }
   auto grad = [&](float v, int c) {
