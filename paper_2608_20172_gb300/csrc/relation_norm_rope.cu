@@ -113,27 +113,31 @@ __device__ __forceinline__ void each2(F f) {  // f(j) for channels j, j + 1
   for (int j = 0; j < GE; j += 2) f(j);
 }
 
-// A lane's two groups turned (sign 1) or turned back (-1) by their pairs' (cos, sin)
+// A lane's two groups, at channels a and b, turned (sign 1) or turned back (-1) by their pairs' (cos, sin).
+// Channels from d_rot on are left alone: a turn by 0 would multiply an infinite or NaN neighbour by 0.
 template <int GE, bool ACROSS>
-__device__ __forceinline__ void turned(float (&x)[GE], float (&y)[GE], const float2 (&cs)[GE], float sign) {
+__device__ __forceinline__ void turned(float (&x)[GE], float (&y)[GE], const float2 (&cs)[GE], float sign, int at,
+                                       int bt, int d_rot) {
+  const bool is = at < d_rot;
   if constexpr (GE == 1) {
     const float s = cs[0].y * sign, a = x[0], b = y[0];
-    x[0] = a * cs[0].x - b * s;
-    y[0] = a * s + b * cs[0].x;
+    x[0] = is ? a * cs[0].x - b * s : a;
+    y[0] = is ? a * s + b * cs[0].x : b;
   } else if constexpr (ACROSS) {
     each2<GE>([&](int j) {
       const float2 c = two(cs[j].x, cs[j + 1].x), s = two(cs[j].y * sign, cs[j + 1].y * sign);
       const float2 a = two(x[j], x[j + 1]), b = two(y[j], y[j + 1]);
       const float2 u = __ffma2_rn(two(-b.x, -b.y), s, __fmul2_rn(a, c));
       const float2 v = __ffma2_rn(a, s, __fmul2_rn(b, c));
-      x[j] = u.x; x[j + 1] = u.y;
-      y[j] = v.x; y[j + 1] = v.y;
+      x[j] = is ? u.x : a.x; x[j + 1] = is ? u.y : a.y;  // (selected: a branch took 94 us for 89)
+      y[j] = is ? v.x : b.x; y[j + 1] = is ? v.y : b.y;
     });
   } else {
 #pragma unroll
     for (int j = 0; j < GE; ++j) {
       float(&v)[GE] = j < GE / 2 ? x : y;
       const int e = 2 * (j < GE / 2 ? j : j - GE / 2);
+      if ((j < GE / 2 ? at : bt) + e >= d_rot) continue;
       const float s = cs[j].y * sign;
       const float2 u = __ffma2_rn(two(v[e + 1], v[e]), two(-s, s), __fmul2_rn(two(v[e], v[e + 1]), two(cs[j].x, cs[j].x)));
       v[e] = u.x;
@@ -296,7 +300,7 @@ __global__ void __launch_bounds__(kThreads, 4)
               G::unpack(now.x[u][side][it], x[side][it]);
               if (GRAD) G::unpack(now.y[GRAD ? u : 0][side][it], y[side][it]);
             }
-            if (GRAD) turned<GE, ACROSS>(y[0][it], y[1][it], cs[it], -1.f);
+            if (GRAD) turned<GE, ACROSS>(y[0][it], y[1][it], cs[it], -1.f, at.a[it], at.b[it], p.d_rot);
             if constexpr (GE == 1) {
               const float2 v = two(x[0][it][0], x[1][it][0]);
               ss2 = __ffma2_rn(v, v, ss2);
@@ -348,7 +352,7 @@ __global__ void __launch_bounds__(kThreads, 4)
                 });
               }
             }
-            if (!GRAD) turned<GE, ACROSS>(x[0][it], x[1][it], cs[it], 1.f);
+            if (!GRAD) turned<GE, ACROSS>(x[0][it], x[1][it], cs[it], 1.f, at.a[it], at.b[it], p.d_rot);
 #pragma unroll
             for (int side = 0; side < 2; ++side) {
               const int c = side ? at.b[it] : at.a[it];

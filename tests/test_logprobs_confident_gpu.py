@@ -1,0 +1,65 @@
+"""The gradient of a token that is almost certain, 1 - p, where the rows' log-normaliser is some tens: a
+difference of two numbers of that size, which is to be as exact as the normaliser that it is given."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2608_20172_gb300 import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF16, F32 = torch.bfloat16, torch.float32
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _lib():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    binding.load()
+
+
+def rows(R, V, low, high, temperature, gap, dtype, seed):
+    """Logits whose largest, at a random place, is low to high temperatures above 0 and about `gap` of them
+    above all others."""
+    rng = np.random.default_rng(seed)
+    top = rng.uniform(low, high, R)
+    x = (top[:, None] - gap + rng.standard_normal((R, V))) * temperature
+    at = rng.integers(0, V, R)
+    x[np.arange(R), at] = top * temperature
+    return torch.from_numpy(x).to(dtype).to(DEV), at
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("sign", [1.0, -1.0])
+@pytest.mark.parametrize("T", [1.0, 0.7, 0.3, 3.3])
+def test_almost_certain_tokens(T, sign, dtype):
+    """1 - p of the given token.  Its logarithm is x / T - logz.  logz is a number between 32 and 64 in size,
+    rounded once: off by 2^-19 = 32 u, and by the error of log l; l is a sum of 1 and small weights, a thread
+    adds up at most V / 128 of them and 24 additions join the threads, each with a rounding of a number of about
+    1; log l adds 2 of itself, at most 0.1.  The difference is taken to a few u of itself, 2^x has 2 ulp (4 u);
+    g / T, its product and the sum add 4 u of g p / T.  Weights far below 1 carry errors of theirs: 30 u each."""
+    R, V = 256, 300
+    x, at = rows(R, V, *((34.0, 62.0) if sign > 0 else (-62.0, -34.0)), T, 14.0, dtype, seed=int(10 * T))
+    rng = np.random.default_rng(1)
+    g = torch.tensor(rng.choice([-1.0, 1.0], R) * rng.uniform(0.5, 2.0, R), dtype=F32, device=DEV)
+    temperature = torch.full((R,), T, dtype=F32, device=DEV)
+    targets = torch.from_numpy(at.astype(np.int32)).to(DEV)
+    r = binding.logprobs(x, targets, temperature=temperature)
+    assert float(r.logz.abs().min()) > 32 and float(r.logz.abs().max()) < 64
+    got = binding.logprobs_grad(x, targets, r.logz, r.entropy, g, temperature=temperature)
+    got = got.double().cpu().numpy()[np.arange(R), at]
+    v = x.double().cpu().numpy()
+    T = float(temperature[0])
+    t = (v - v[np.arange(R), at][:, None]) / T
+    w = np.exp(t)
+    w[np.arange(R), at] = 0.0
+    rest = w.sum(1)
+    want = g.double().cpu().numpy() / T * (rest / (1 + rest))
+    assert rest.max() < 0.1
+    tol = np.abs(g.double().cpu().numpy()) / T * U * (32 + V / 128 + 24 + 1 + 4 + 4 + 30 * rest)
+    tol += (torch.finfo(dtype).eps / 2 * 1.01 + 4 * U) * np.abs(want)
+    err = np.abs(got - want)
+    assert (err <= tol).all(), (float((err / tol).max()), float((err * T / U).max()))
