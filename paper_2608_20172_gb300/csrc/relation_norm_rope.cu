@@ -225,10 +225,11 @@ __global__ void __launch_bounds__(kThreads, 4)
         w[1][it][j] = wp && h_lo < h_hi && at.b[it] >= 0 ? wp[at.b[it] + j] : 1.f;
         acc[0][it][j] = acc[1][it][j] = 0.f;
       }
-    auto fetch = [&](long long base, int h, Rows& r) {  // (clamped: lanes past the end take the last head)
+    auto fetch = [&](long long base, int h, Rows& r) {  // (zeros for lanes past the last head)
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const long long off = base + (long long)min(h + u * slots, h_hi - 1) * sH;
+        const bool live = h + u * slots < h_hi;
+        const long long off = base + (long long)(h + u * slots) * sH;
 #pragma unroll
         for (int it = 0; it < IT; ++it)
 #pragma unroll
@@ -236,7 +237,7 @@ __global__ void __launch_bounds__(kThreads, 4)
             const int c = side ? at.b[it] : at.a[it];
             r.x[u][side][it] = typename G::Raw{};
             if (GRAD) r.y[u][side][it] = typename G::Raw{};
-            if (c < 0) continue;
+            if (c < 0 || !live) continue;
             r.x[u][side][it] = G::load(in + off + c);
             if (GRAD) r.y[u][side][it] = G::load(din + off + c);
           }
@@ -325,9 +326,9 @@ __global__ void __launch_bounds__(kThreads, 4)
             r = rsqrtf(ss * inv_d + p.eps);
             if (GRAD) mean = dot * r * inv_d;  // mean of x^ w u
           }
-          // (a lane past the last head adds nothing to dw)
+          // (a lane past the last head adds 0 to dw; r may be infinite there)
           const float ra = GRAD && !live ? 0.f : r;
-          TI* dst = out + base + (long long)min(h, h_hi - 1) * sH;
+          TI* dst = out + base + (long long)h * sH;
 #pragma unroll
           for (int it = 0; it < IT; ++it) {
 #pragma unroll

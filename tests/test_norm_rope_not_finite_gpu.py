@@ -58,7 +58,7 @@ def test_channels_that_are_not_turned_stay_by_themselves(value):
             assert same(got, want), (c.rotary, at)
 
 
-@pytest.mark.parametrize("head", [0])
+@pytest.mark.parametrize("head", [0, 1])
 @pytest.mark.parametrize("value", [INF, -INF, NAN])
 def test_gradients_of_channels_that_are_not_turned_stay_by_themselves(value, head):
     """dy of such a channel goes to its own dw, and without the norm to its own dx."""
@@ -78,3 +78,21 @@ def test_gradients_of_channels_that_are_not_turned_stay_by_themselves(value, hea
                 else:
                     want[4, head, at] = value * c.tw[i][at]
                 assert same(got[i], want), (norm, c.rotary, at)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("H,d,pad", [(1, 64, 0), (3, 64, 0), (9, 64, 0), (5, 32, 0), (3, 33, 0), (3, 64, 1)])
+def test_last_head_counts_once(H, d, pad, dtype):
+    """Numbers of heads that do not fill a warp's passes: an infinity in the last one's x or dy makes its
+    column of dw infinite."""
+    for which, norm in (("x", False), ("dy", False), ("dy", True)):
+        c = Case(6, H, H, d, 0, "half", dtype, seed=4, pad=pad, norm=norm)
+        plain = c.backward()
+        for i in range(2):
+            (c.tx if which == "x" else c.tdy)[i][3, H - 1, 5] = INF
+        got = c.backward()
+        for i in range(2):
+            other = (c.tdy if which == "x" else c.tx)[i][3, H - 1, 5]
+            want = plain[2 + i].clone()
+            want[5] = INF * float(torch.sign(other))
+            assert float(other) != 0 and same(got[2 + i], want), (which, norm)
