@@ -337,7 +337,9 @@ __global__ void __launch_bounds__(kThreads, 4)
                 const float2 xh = __fmul2_rn(v, two(ra, ra));
                 if (!GRAD) return __fmul2_rn(xh, wt);
                 sum = __ffma2_rn(u_, xh, sum);
-                return __fmul2_rn(__ffma2_rn(xh, two(-mean, -mean), __fmul2_rn(wt, u_)), two(ra, ra));
+                const float2 wu = __fmul2_rn(wt, u_);
+                // (without the norm x has no part in dx, not even by 0)
+                return p.norm ? __fmul2_rn(__ffma2_rn(xh, two(-mean, -mean), wu), two(ra, ra)) : wu;
               };
               if constexpr (GE == 1) {
                 float2 sum = two(acc[side][it][0], 0.f);

@@ -80,6 +80,21 @@ def test_gradients_of_channels_that_are_not_turned_stay_by_themselves(value, hea
                 assert same(got[i], want), (norm, c.rotary, at)
 
 
+@pytest.mark.parametrize("value", [INF, -INF, NAN])
+def test_without_the_norm_dx_does_not_depend_on_x(value):
+    """dx = w u; x goes to its channel's dw alone."""
+    for c, at in cases(norm=False):
+        plain = c.backward()
+        for t in c.tx:
+            t[4, 1, at] = value
+        got = c.backward()
+        for i in range(2):
+            assert torch.equal(got[i], plain[i]), (c.rotary, at)
+            want = plain[2 + i].clone()
+            want[at] = value * c.tdy[i][4, 1, at]
+            assert same(got[2 + i], want), (c.rotary, at)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("H,d,pad", [(1, 64, 0), (3, 64, 0), (9, 64, 0), (5, 32, 0), (3, 33, 0), (3, 64, 1)])
 def test_last_head_counts_once(H, d, pad, dtype):
