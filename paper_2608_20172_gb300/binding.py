@@ -11,6 +11,7 @@ there is no CPU fallback.
 from __future__ import annotations
 
 import ctypes
+import functools
 import importlib.machinery
 import importlib.util
 import math
@@ -1184,6 +1185,32 @@ def selftest_wait_timeout(dev_status: torch.Tensor, timeout_us: int = 1000, stre
         _status(dev_status, torch.cuda.current_device()), int(timeout_us), _stream(stream)))
 
 
+class _FirstGradients(torch.autograd.Function):
+    """Gradients as they are, in a graph that cannot be gone through: ``tensors`` are what they depend on."""
+
+    @staticmethod
+    def forward(ctx, grads, *tensors):
+        return grads
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the gradients of the library's operators have no gradients of their own: "
+                           "no second derivatives")
+
+
+def _first_only(backward):
+    """A backward that can be asked for with create_graph: its gradients are no constants, and a second
+    derivative that goes through them is an error."""
+    @functools.wraps(backward)
+    def first(ctx, *grads):
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return out
+        return _FirstGradients.apply(out, *grads, *(t for t in ctx.saved_tensors if t is not None))
+    return first
+
+
 class RelationFunction(torch.autograd.Function):
     """Autograd wrapper: Y = Relation(q, k, v; lambda).  lambda is a 1-element tensor
     (its gradient is returned); tau_S is a constant."""
@@ -1196,6 +1223,7 @@ class RelationFunction(torch.autograd.Function):
         return y
 
     @staticmethod
+    @_first_only
     def backward(ctx, dy):
         q, k, v, y, logz = ctx.saved_tensors
         if dy.stride() != q.stride() or dy.dtype != q.dtype:
@@ -1216,6 +1244,7 @@ class NormRopeFunction(torch.autograd.Function):
         return q, k
 
     @staticmethod
+    @_first_only
     def backward(ctx, dq, dk):
         p1, p2, w1, w2, freqs, positions = ctx.saved_tensors
         rot = None if ctx.rotary is None else Rotary(freqs, *ctx.rotary)
@@ -1236,6 +1265,7 @@ class LogprobsFunction(torch.autograd.Function):
         return r.logprob, r.entropy, r.logz
 
     @staticmethod
+    @_first_only
     def backward(ctx, dlogprob, dentropy, dlogz):
         logits, targets, temperature, logz, entropy = ctx.saved_tensors
         g = (x.contiguous() for x in (dlogprob, dentropy, dlogz))
