@@ -1211,6 +1211,23 @@ def _first_only(backward):
     return first
 
 
+class _Constant(torch.autograd.Function):
+    """An input that an operator has no gradient of: a backward that wants it is refused."""
+
+    @staticmethod
+    def forward(ctx, t, name):
+        ctx.name = name
+        return t.view_as(t)
+
+    @staticmethod
+    def backward(ctx, _):
+        raise ValueError(f"there is no gradient of the {ctx.name}: detach it")
+
+
+def _constant(t, name):
+    return _Constant.apply(t, name) if t is not None and t.requires_grad and torch.is_grad_enabled() else t
+
+
 class RelationFunction(torch.autograd.Function):
     """Autograd wrapper: Y = Relation(q, k, v; lambda).  lambda is a 1-element tensor
     (its gradient is returned); tau_S is a constant."""
@@ -1233,10 +1250,16 @@ class RelationFunction(torch.autograd.Function):
 
 
 class NormRopeFunction(torch.autograd.Function):
-    """Autograd wrapper of norm_rope: (q, k) = f(p1, p2, w1, w2); w1 and w2 may be None."""
+    """Autograd wrapper of norm_rope: (q, k) = f(p1, p2, w1, w2); w1 and w2 may be None.  There is no gradient
+    of the rotation's frequencies: a backward that wants it is refused."""
+
+    @classmethod
+    def apply(cls, p1, p2, w1, w2, rotary, positions=None, norm=True, eps=1.0e-6):
+        freqs = None if rotary is None else _constant(rotary.freqs, "rotation's frequencies")
+        return super().apply(p1, p2, w1, w2, rotary, positions, norm, eps, freqs)
 
     @staticmethod
-    def forward(ctx, p1, p2, w1, w2, rotary, positions=None, norm=True, eps=1.0e-6):
+    def forward(ctx, p1, p2, w1, w2, rotary, positions, norm, eps, _):
         q, k = norm_rope(p1, p2, rotary, positions, w1, w2, norm=norm, eps=eps)
         freqs = None if rotary is None else rotary.freqs
         ctx.save_for_backward(p1, p2, w1, w2, freqs, positions)
@@ -1252,14 +1275,19 @@ class NormRopeFunction(torch.autograd.Function):
                   else _like(x).copy_(g) for g, x in ((dq, p1), (dk if p2 is not None else None, p2)))
         dp1, dp2, dw1, dw2 = norm_rope_grad(dq, dk, p1, p2, rot, positions, w1, w2, norm=ctx.norm,
                                             eps=ctx.eps, weights=w1 is not None or w2 is not None)
-        return dp1, dp2, None if w1 is None else dw1, None if w2 is None else dw2, None, None, None, None
+        return dp1, dp2, None if w1 is None else dw1, None if w2 is None else dw2, None, None, None, None, None
 
 
 class LogprobsFunction(torch.autograd.Function):
-    """Autograd wrapper of logprobs: (logprob, entropy, logz) = f(logits) for given targets."""
+    """Autograd wrapper of logprobs: (logprob, entropy, logz) = f(logits) for given targets.  There is no
+    gradient of the temperature: a backward that wants it is refused."""
+
+    @classmethod
+    def apply(cls, logits, targets, temperature=None):
+        return super().apply(logits, targets, _constant(temperature, "temperature"))
 
     @staticmethod
-    def forward(ctx, logits, targets, temperature=None):
+    def forward(ctx, logits, targets, temperature):
         r = logprobs(logits, targets, temperature=temperature)
         ctx.save_for_backward(logits, targets, temperature, r.logz, r.entropy)
         return r.logprob, r.entropy, r.logz
