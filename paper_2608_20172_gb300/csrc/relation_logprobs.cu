@@ -419,6 +419,7 @@ __global__ void __launch_bounds__(kThreads, kThreads == 256 ? 8 : 2)
 // Gradient: a CTA takes kChunk groups of a row.
 constexpr int kGradThreads = 256, kGradU = 4, kChunk = kGradThreads * kGradU;
 constexpr float kNear = 64.f;  // |logz| of the rows whose log p is x / T - logz
+constexpr float kLog2eRest = 1.92596303e-8f;  // log2 e less kLog2e
 
 // One of the CTA's threads' values: the largest (NaN: any), or the sum in a fixed order
 template <bool MAX>
@@ -514,19 +515,22 @@ __global__ void __launch_bounds__(kGradThreads)
   const int target = p.targets[row];
   const float g = p.dlogprob && target >= 0 ? p.dlogprob[row] : 0.f;
   const float h = p.dentropy ? p.dentropy[row] : 0.f, k = p.dlogz ? p.dlogz[row] : 0.f;
-  // a = log2 p_j:  dx_j = 2^a (c0 + c1 a), and g / T more for the given token
+  // a = log2 p_j:  dx_j = 2^a (c0 + c1 a), and g / T more for the given token.  The factors of x and logz are
+  // pairs of numbers: rounded to one each, a was off by 190 u where the two were near 60 (u = 2^-24), which is
+  // all of 1 - p of a token that is almost certain.
   const float s2 = scale * kLog2e, z2 = -logz * kLog2e;
+  const float s2l = fmaf(scale, kLog2e, -s2) + scale * kLog2eRest, z2l = fmaf(-logz, kLog2e, -z2) - logz * kLog2eRest;
   const float c0 = target >= p.V ? NAN : (k - g - h * H) * scale;  // (no log p: the NaN leads to grad_far)
   const float c1 = -h * kLn2 * scale;
-  // log p_j = x_j / T - logz is a difference of two rounded numbers: up to kNear its roundings are below 3e-5
-  // of p; beyond, and where a coefficient leaves the type, a row's maximum is taken from its logits first.
+  // log p_j = x_j / T - logz is off by logz's own rounding: up to kNear by 2^-19 at most, as much as by the sum's
+  // roundings; beyond, and where a coefficient leaves the type, a row's maximum is taken from its logits first.
   if (!(fabsf(logz) <= kNear) || !isfinite(c0) || !isfinite(c1) || !isfinite(s2)) {
     if (chunk == 0) grad_far<TI, VEC>(x, out, target, scale, logz, H, g, h, k, p.V);
     return;
   }
   auto grad = [&](float v, int c) {
-    const float a = fmaf(v, s2, z2), q = ex2_approx(a);
-    const float d = q == 0.f ? 0.f : q * fmaf(a, c1, c0);
+    const float a = fmaxf(fmaf(v, s2, z2) + fmaf(v, s2l, z2l), -300.f);
+    const float d = ex2_approx(a) * fmaf(a, c1, c0);
     return c == target ? fmaf(g, scale, d) : d;
   };
 #pragma unroll
@@ -539,10 +543,13 @@ __global__ void __launch_bounds__(kGradThreads)
       Vec<TI>::unpack(w[i], v);
 #pragma unroll
       for (int j = 0; j < N; j += 2) {
-        float2 a = __ffma2_rn(make_float2(v[j], v[j + 1]), make_float2(s2, s2), make_float2(z2, z2));
-        // (2^a is 0 long before -inf would make 2^a a NaN)
-        a.x = max_nan(a.x, -300.f);
-        a.y = max_nan(a.y, -300.f);
+        const float2 x2 = make_float2(v[j], v[j + 1]);
+        float2 a = __fadd2_rn(__ffma2_rn(x2, make_float2(s2, s2), make_float2(z2, z2)),
+                              __ffma2_rn(x2, make_float2(s2l, s2l), make_float2(z2l, z2l)));
+        // (2^a is 0 long before -inf would make 2^a times a a NaN; a masked token's parts may be infinities of either
+        // sign, whose sum is one already: no logit of a row that comes here is)
+        a.x = fmaxf(a.x, -300.f);
+        a.y = fmaxf(a.y, -300.f);
         const float2 d = __fmul2_rn(make_float2(ex2_approx(a.x), ex2_approx(a.y)),
                                     __ffma2_rn(a, make_float2(c1, c1), make_float2(c0, c0)));
         v[j] = d.x;

@@ -63,3 +63,28 @@ def test_almost_certain_tokens(T, sign, dtype):
     tol += (torch.finfo(dtype).eps / 2 * 1.01 + 4 * U) * np.abs(want)
     err = np.abs(got - want)
     assert (err <= tol).all(), (float((err / tol).max()), float((err * T / U).max()))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("mask", [-math.inf, "lowest"])
+@pytest.mark.parametrize("V", [7, 300, 1001])
+def test_masked_tokens_at_any_temperature(V, mask, dtype):
+    """Masked tokens get exactly 0, the others what they get without them: zeros for any of many temperatures,
+    whose parts of log2 e / T have either sign."""
+    R = 64
+    rng = np.random.default_rng(V)
+    T = rng.uniform(0.5, 3.0, R).astype(np.float32)
+    x = torch.from_numpy(rng.standard_normal((R, V)) + 8).to(dtype).to(DEV)
+    x[:, 1::3] = torch.finfo(dtype).min if mask == "lowest" else mask
+    targets = torch.zeros(R, dtype=torch.int32, device=DEV)
+    targets[1] = 1  # (a masked one: g / T alone)
+    temperature = torch.from_numpy(T).to(DEV)
+    g, h, k = (torch.tensor(rng.standard_normal(R), dtype=F32, device=DEV) for _ in range(3))
+    r = binding.logprobs(x, targets, temperature=temperature)
+    assert float(r.logz.abs().max()) < 64
+    got = binding.logprobs_grad(x, targets, r.logz, r.entropy, g, h, k, temperature=temperature)
+    assert torch.isfinite(got).all()
+    masked = got[:, 1::3].clone()
+    assert abs(float(masked[1, 0]) - float(g[1]) / float(T[1])) <= 2.0 ** -7 * abs(float(g[1]) / float(T[1]))
+    masked[1, 0] = 0
+    assert (masked == 0).all()
