@@ -398,8 +398,8 @@ relation_status relation_paged_decode(const void* q, const void* k_pages, const 
  * fp32 or bf16 with any 1 <= d_h <= 128; rows as in relation_paged_decode.  bf16 runs on the tensor
  * cores (P rounded to bf16 for the product with the values, sums and states in fp32).  Keys and values
  * behind a token's own row are not its business, whatever they hold: an infinite or NaN value among
- * them leaves the row as it is.  cols * page_size is at most 2^31 - 8192, N H at most 2^31 - 65536
- * (else RELATION_ERR_UNSUPPORTED).  A position of cols * page_size or more makes a token padding, a
+ * them leaves the row as it is.  cols * page_size is at most 2^31 - 8192, (N + B) H at most 2^31 - 65536
+ * (else RELATION_ERR_UNSUPPORTED, and a workspace size of 0).  A position of cols * page_size or more makes a token padding, a
  * page id outside [0, n_pages) reads page 0 (the row is then undefined); both are reported to
  * dev_status (if given) as RELATION_ERR_INVALID_ARG.  Asynchronous on `stream`; nothing is allocated.
  */
@@ -444,7 +444,8 @@ relation_status relation_sample(const void* logits, int R, int V, long long s_ro
 /*
  * relation_logprobs: the log probabilities of given tokens, with every row's entropy and its most
  * likely tokens.  For a row x of logits at temperature T, p_j = exp(x_j / T) / sum_i exp(x_i / T).
- *   logits      [R][V] in dt, row stride s_row (element alignment), V <= 2^30.  -inf masks a token.
+ *   logits      [R][V] in dt, row stride s_row (element alignment), V <= 2^30, R <= 2^27 (else
+ *               RELATION_ERR_UNSUPPORTED).  -inf masks a token.
  *   targets     device int[R]: the given token of every row; negative: none.
  *   temperature device float[R], > 0, or null (1).
  *   logprob     device float[R]: log p of the given token (0 where there is none).
@@ -474,6 +475,7 @@ relation_status relation_logprobs(const void* logits, int R, int V, long long s_
  * 0; g counts as 0 in a row without a given token).
  *   logz, entropy : the forward's for the same logits, targets and temperature.
  *   dlogits     [R][V] in dt, row stride s_out; it may be the logits (s_out = s_row).
+ * V <= 2^30 and R (V / 4096 + 2) < 2^31, the quotient rounded down (else RELATION_ERR_UNSUPPORTED).
  * Rows with |logz| above 64 (low temperatures, logits with a large common part) take their maximum
  * and sum from the logits again, since logz is too coarse there; they take longer.  A row without an
  * unmasked token gets zeros, one whose logz is NaN or whose given token is >= V NaN.
@@ -589,7 +591,7 @@ typedef struct relation_rotary {
  *   w1, w2 : device float[d_h], the norms' weights of the queries and the keys; null: 1.
  *   positions : device int[B T]; null: t in every sequence.  A negative one is padding: zeros.
  * fp32 or bf16 (arithmetic in fp32, angles as 64-bit parts of a turn at every position), any d_h up to
- * 256, B T up to 2^30 (else RELATION_ERR_UNSUPPORTED).  Rows whose pointers and strides are multiples
+ * 256, B T up to 2^30, heads of queries and keys together up to 2^24 (else RELATION_ERR_UNSUPPORTED).  Rows whose pointers and strides are multiples
  * of 16 bytes, with d_h (and, for layout 1, d_rot / 2) made of 16-byte groups, move in such groups,
  * any others element by element.  With rope_base 0, relation_cache_append takes the result.
  * Asynchronous on `stream`; one launch; nothing is allocated.
