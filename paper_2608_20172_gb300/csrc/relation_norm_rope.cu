@@ -9,8 +9,9 @@
 //   dw_c = sum over the rows of u_c x^_c,  dx = r (w u - x^ mean(x^ w u)).
 //
 // The angle is kept as a part of a whole turn in 64-bit integers: f / (2 pi) modulo 1 times 2^64, times
-// the position, modulo 2^64 -- exact at every position, no reduction by 2 pi, and no fp64 but one
-// product a frequency.
+// the position, modulo 2^64: no reduction by 2 pi and no fp64.  The step of a position is off by less than 2^-64 of
+// a turn, the angle at the last one by 2^-33 of a turn, far below fp32's rounding (from a product in fp64 it was
+// off by 2^-53 f times the position; two products in fp64 took as much and 1 us a call).
 //
 // Bound by memory: a row is read and written once (backward: two reads).  A few lanes share a row, 16
 // bytes of two parts of it each, so that both channels of a pair are in one lane in either layout and
@@ -150,14 +151,25 @@ __device__ __forceinline__ void turned(float (&x)[GE], float (&y)[GE], const flo
 // lane, lane + 32, ...
 struct Steps {
   unsigned long long s[kMaxD / 64];
+  // f / (2 pi) modulo 1: f's 53 bits times 1 / (2 pi) in 128 (after Payne and Hanek), the 64 bits behind the point;
+  // off by 2^-64 + f 2^-128 of a turn, frequencies of 2^117 and more count as 0
+  static __device__ __forceinline__ unsigned long long part(double f) {
+    constexpr unsigned long long C1 = 0x28be60db9391054aull, C0 = 0x7f09d5f47d4d3770ull;
+    const unsigned long long bits = (unsigned long long)__double_as_longlong(f);
+    const int e = (int)(bits >> 52) & 0x7ff, shift = 1139 - max(e, 1), word = shift >> 6, k = shift & 63;
+    const unsigned long long m = (bits & 0xfffffffffffffull) | (e ? 1ull << 52 : 0ull);  // f = m 2^(64 - shift)
+    const unsigned long long l1 = m * C1, w0 = m * C0, w1 = __umul64hi(m, C0) + l1,
+                             w2 = __umul64hi(m, C1) + (w1 < l1);
+    const unsigned long long lo = word == 0 ? w0 : word == 1 ? w1 : word == 2 ? w2 : 0ull;
+    const unsigned long long hi = word == 0 ? w1 : word == 1 ? w2 : 0ull;
+    const unsigned long long r = k ? lo >> k | hi << (64 - k) : lo;
+    return bits >> 63 ? 0ull - r : r;
+  }
   __device__ __forceinline__ Steps(const NormRopeProblem& p, int lane) {
 #pragma unroll
     for (int i = 0; i < kMaxD / 64; ++i) {
       s[i] = 0;
-      if (lane + 32 * i < p.d_rot / 2) {
-        const double t = p.freqs[lane + 32 * i] * 0.15915494309189533576888376337251;
-        s[i] = (unsigned long long)__double2ll_rn((t - rint(t)) * 9223372036854775808.0) << 1;
-      }
+      if (lane + 32 * i < p.d_rot / 2) s[i] = part(p.freqs[lane + 32 * i]);
     }
   }
 };
