@@ -398,7 +398,6 @@ struct Cfg {
   static constexpr int TMEM_COLS = 256;
   static constexpr int OCOL = 2 * SK;
   static constexpr int STAGES = D == 64 ? 4 : 2;
-  static constexpr int SPL = kUnit / SK;       // steps of a unit
   static constexpr int THREADS = 192;
   static constexpr int KB = D / 64;            // 128-byte blocks of a row
   static constexpr int UT = kUnit * D * 2;     // bytes of a unit's keys or values
@@ -441,7 +440,8 @@ __device__ __forceinline__ uint32_t unfinite_halves(uint32_t w) {  // 0xffff for
   return ((w & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((w & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
 }
 
-// TMA boxes have `big` rows of a page or 8; a unit's part of a page is cut into as many big ones as fit
+// TMA boxes have `big` rows of a page or 8; a unit's part of a page is cut into as many big ones as fit (tmK8 and
+// tmV8 are empty where these are all)
 template <int D, int LOAD>
 __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
     chunk_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -671,46 +671,40 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
     constexpr uint32_t idesc_qk = idesc_bf16_f32(BM, C::SK, false, false);
     const int dk = (p.d + 15) / 16;  // 16-column steps; z has as many columns
     const uint32_t idesc_pv = idesc_bf16_f32(BM, 16 * dk, false, true);
-    const int total = units * C::SPL;
     auto issue_u = [&](int s) -> bool {
-      const int j = s / C::SPL, hh = s % C::SPL, st = j % C::STAGES, bf = s & 1;
-      if (hh == 0) {
-        if (!mbar_wait_warp(bar(B_KF + st), (j / C::STAGES) & 1, ab)) return false;
-        if (LOAD != kBoxes) fence_async_smem();  // (cp.async wrote the unit through the generic proxy)
-        tc_fence_after();
-      }
+      const int st = s % C::STAGES, bf = s & 1;
+      if (!mbar_wait_warp(bar(B_KF + st), (s / C::STAGES) & 1, ab)) return false;
+      if (LOAD != kBoxes) fence_async_smem();  // (cp.async wrote the unit through the generic proxy)
+      tc_fence_after();
 #pragma unroll
       for (int kk = 0; kk < D / 16; ++kk) {
         if (kk >= dk) break;
         const uint32_t koff = (kk >> 2) * (BM * 128) + (kk & 3) * 32;
         const uint32_t kkoff = (kk >> 2) * (kUnit * 128) + (kk & 3) * 32;
         const uint64_t a = smem_desc_sw128(sb + C::OFF_Q + koff, 16, 1024);
-        const uint64_t bd = smem_desc_sw128(sb + C::OFF_K + st * C::UT + hh * C::SK * 128 + kkoff, 16, 1024);
+        const uint64_t bd = smem_desc_sw128(sb + C::OFF_K + st * C::UT + kkoff, 16, 1024);
         mma_ss_w(tmem + bf * C::SK, a, bd, idesc_qk, kk > 0 ? 1u : 0u);
       }
       mma_commit_w(bar(B_S + bf));
-      if (hh == C::SPL - 1) mma_commit_w(bar(B_KE + st));
+      mma_commit_w(bar(B_KE + st));
       return true;
     };
     bool ok = mbar_wait_warp(bar(B_Q), 0, ab);
-    for (int s = 0; ok && s < 2 && s < total; ++s) ok = issue_u(s);
-    for (int s = 0; ok && s < total; ++s) {
-      const int j = s / C::SPL, hh = s % C::SPL, st = j % C::STAGES, bf = s & 1;
-      if (hh == 0) {
-        if (!(ok = mbar_wait_warp(bar(B_VF + st), (j / C::STAGES) & 1, ab))) break;
-        if (LOAD != kBoxes) fence_async_smem();
-      }
+    for (int s = 0; ok && s < 2 && s < units; ++s) ok = issue_u(s);
+    for (int s = 0; ok && s < units; ++s) {
+      const int st = s % C::STAGES, bf = s & 1;
+      if (!(ok = mbar_wait_warp(bar(B_VF + st), (s / C::STAGES) & 1, ab))) break;
+      if (LOAD != kBoxes) fence_async_smem();
       if (!(ok = mbar_wait_warp(bar(B_P + bf), (s / 2) & 1, ab))) break;
       tc_fence_after();
 #pragma unroll
       for (int kk = 0; kk < C::SK / 16; ++kk) {
-        const uint64_t bd = smem_desc_sw128(sb + C::OFF_V + st * C::UT + (hh * C::SK + kk * 16) * 128,
-                                            kUnit * 128, 1024);
+        const uint64_t bd = smem_desc_sw128(sb + C::OFF_V + st * C::UT + kk * 16 * 128, kUnit * 128, 1024);
         mma_ts_w(tmem + C::OCOL, tmem + bf * C::SK + kk * 8, bd, idesc_pv, (s > 0 || kk > 0) ? 1u : 0u);
       }
       mma_commit_w(bar(B_OD + bf));
-      if (hh == C::SPL - 1) mma_commit_w(bar(B_VE + st));
-      if (s + 2 < total && !(ok = issue_u(s + 2))) break;
+      mma_commit_w(bar(B_VE + st));
+      if (s + 2 < units && !(ok = issue_u(s + 2))) break;
     }
     mma_commit_w(bar(B_O));
     __syncwarp();
@@ -764,8 +758,7 @@ __global__ void __launch_bounds__(Cfg<D>::THREADS, Cfg<D>::CTAS)
       if (go) m = mn;
       return true;
     };
-    const int total = units * C::SPL;
-    for (int s = 0; s < total; ++s) {
+    for (int s = 0; s < units; ++s) {
       const int bf = s & 1, key0 = k.u0 * kUnit + s * C::SK;
       if (!(ok = mbar_wait_warp(bar(B_S + bf), (s / 2) & 1, ab))) break;
       if (any) {
@@ -1248,9 +1241,10 @@ cudaError_t launch_tc(const ChunkProblem& p, const Plan& w, bool groups, cudaStr
   int big = kUnit;
   while (p.page % big) big /= 2;
   if (big == 8) big = p.page < kUnit ? p.page : 32;
+  const bool eights = p.page % big != 0 || kUnit % big != 0;  // (boxes of 8 are used beside the big ones)
   CUtensorMap m[4] = {};
   if (groups && p.page % 8 == 0 && make_map(&m[0], p.k, p, big) && make_map(&m[1], p.v, p, big) &&
-      make_map(&m[2], p.k, p, 8) && make_map(&m[3], p.v, p, 8))
+      (!eights || (make_map(&m[2], p.k, p, 8) && make_map(&m[3], p.v, p, 8))))
     return launch_main(chunk_tc_kernel<D, kBoxes>, Cfg<D>::THREADS, Cfg<D>::SMEM, w, s, m[0], m[1], m[2], m[3], p,
                        w, big);
   if (groups)
