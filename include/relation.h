@@ -477,7 +477,9 @@ relation_status relation_logprobs(const void* logits, int R, int V, long long s_
  *   dlogits     [R][V] in dt, row stride s_out; it may be the logits (s_out = s_row).
  * V <= 2^30 and R (V / 4096 + 2) < 2^31, the quotient rounded down (else RELATION_ERR_UNSUPPORTED).
  * Rows with |logz| above 64 (low temperatures, logits with a large common part) take their maximum
- * and sum from the logits again, since logz is too coarse there; they take longer.  A row without an
+ * and sum from the logits again, since logz is too coarse there, each by one thread block: many such
+ * rows take 2.3 times as long, a single one of 131072 fp32 84 us in place of 3.  In other rows p is off
+ * by logz's own rounding.  A row without an
  * unmasked token gets zeros, one whose logz is NaN or whose given token is >= V NaN.
  * Asynchronous on `stream`; one launch; nothing is allocated.
  */

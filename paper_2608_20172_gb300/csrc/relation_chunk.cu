@@ -19,10 +19,10 @@
 // size is no multiple of 8).  fp32: register tiles on the CUDA cores.
 //
 // Bound by the hand-off between scan and products (tensor cores 33 %, special functions 49 % busy).
-// Measured: 4 pieces of 2048 tokens behind 16384 rows of 16 x 128 bf16 620 us, 1.08 PFLOP/s; 48 requests,
-// half of them decoding, of 32 query heads over 8 x 80 in pages of 24 rows 390 us (of 64 rows 355); 5 tokens
-// behind 2048 rows of 12 x 64 16 us, dependent trips; fp32, 451 tokens of 8 query heads over 4 x 72 42 us,
-// long pieces 42 TFLOP/s.
+// Measured: 4 pieces of prompts, 6933 tokens of 16 x 128 bf16 that see 8970 rows on average, 620 us, 0.82
+// PFLOP/s; 48 requests, half of them decoding, 6174 tokens of 32 query heads over 8 x 80 that see 2094 rows in
+// pages of 24, 390 us (of 64 354); 5 tokens behind 2048 rows of 12 x 64 16 us, dependent trips; fp32, 451
+// tokens of 8 query heads over 4 x 72 43 us, 3646 tokens of 8 x 128 that see 4764 rows 2.12 ms, 33 TFLOP/s.
 #include <cudaTypedefs.h>
 #include <math.h>
 

@@ -19,7 +19,7 @@
 // Memory is the floor: the logits are read once (gradient: and written).  Few rows are shared by clusters
 // of CTAs that join through distributed shared memory.  Measured: 2048 rows of 50257 bf16 42 us, 4.9 TB/s,
 // with 20 alternatives 60 us, bound by issue (2.9 instructions per clock); one row of 32000 fp32 with 5
-// alternatives 7 us, a chain of barriers; the gradient of 4096 rows of 50257 bf16 129 us, 6.4 TB/s.
+// alternatives 7 us, a chain of barriers; the gradient of 4096 rows of 50257 bf16 130 us, 6.3 TB/s.
 #include <float.h>
 #include <math.h>
 
@@ -440,8 +440,8 @@ __device__ __forceinline__ float block_join(float v, float* part) {
 
 // A whole row by one CTA with its own maximum and sum: large |logz|, infinite logits, no token, NaN.  The row
 // is read before any of it is written, each element of the last pass by the thread that writes it: the output
-// may be the logits.  4096 rows of 50257 bf16 that all come here take 302 us (an
-// element at a time 475), ordinary ones 129.
+// may be the logits.  4096 rows of 50257 bf16 that all come here take 302 us (an element at a time 475),
+// ordinary ones 130; few rows wait for one CTA's three passes, one of 131072 fp32 84 us against 3.
 template <typename TI, bool VEC>
 __device__ __noinline__ void grad_far(const Row<TI> x, TI* out, int target, float scale, float logz, float H,
                                       float g, float h, float k, int V) {

@@ -10,15 +10,16 @@
 //
 // The angle is kept as a part of a whole turn in 64-bit integers: f / (2 pi) modulo 1 times 2^64, times
 // the position, modulo 2^64: no reduction by 2 pi and no fp64.  The step of a position is off by less than 2^-64 of
-// a turn, the angle at the last one by 2^-33 of a turn, far below fp32's rounding (from a product in fp64 it was
-// off by 2^-53 f times the position; two products in fp64 took as much and 1 us a call).
+// a turn, the angle at the last one by 2^-33 of a turn, far below fp32's rounding (a product in fp64 is off by 2^-53
+// of f, times the position; its rounding carried along in fp64 too took 1 us more a call).
 //
 // Bound by memory: a row is read and written once (backward: two reads).  A few lanes share a row, 16
 // bytes of two parts of it each, so that both channels of a pair are in one lane in either layout and
 // the sums are a few shuffles; a token's turns are taken once for all heads.  Four CTAs of 128 threads an SM
-// (three: 134 us in the first case below, five, which leave registers for one row in flight a lane: 141).  Measured: 32768 tokens of 32 + 8
-// heads of 128 bf16 118 us, 5.7 TB/s; the gradient of 16384 tokens of 16 + 16 heads 86 us, 4.7 TB/s; 32
-// tokens of 12 + 12 heads of 64 3.5 us, one chain of position, turn and row.
+// (three: 134 us in the first case below, five, which leave registers for one row in flight a lane: 141); the
+// bf16 gradient spills 40 to 72 bytes for it.  Measured: 32768 tokens of 32 + 8 heads of 128 bf16 118 us, 5.7
+// TB/s (16384 fp32 109); the gradient of 16384 tokens of 16 + 16 heads 84 us, 4.8 TB/s (fp32 139); 32 tokens of
+// 12 + 12 heads of 64 3.3 us, one chain of position, turn and row.
 #include <math.h>
 
 #include "common.cuh"
