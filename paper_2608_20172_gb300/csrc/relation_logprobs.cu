@@ -524,7 +524,8 @@ __global__ void __launch_bounds__(kGradThreads)
   const float c1 = -h * kLn2 * scale;
   // log p_j = x_j / T - logz is off by logz's own rounding: up to kNear by 2^-19 at most, as much as by the sum's
   // roundings; beyond, and where a coefficient leaves the type, a row's maximum is taken from its logits first.
-  if (!(fabsf(logz) <= kNear) || !isfinite(c0) || !isfinite(c1) || !isfinite(s2)) {
+  // (a masked token's 2^a, 0, is multiplied by c0 - 300 c1, which has to be finite)
+  if (!(fabsf(logz) <= kNear) || !(fabsf(c0) <= 1e38f) || !(fabsf(c1) <= 5e35f) || !isfinite(s2)) {
     if (chunk == 0) grad_far<TI, VEC>(x, out, target, scale, logz, H, g, h, k, p.V);
     return;
   }

@@ -88,3 +88,27 @@ def test_masked_tokens_at_any_temperature(V, mask, dtype):
     assert abs(float(masked[1, 0]) - float(g[1]) / float(T[1])) <= 2.0 ** -7 * abs(float(g[1]) / float(T[1]))
     masked[1, 0] = 0
     assert (masked == 0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V", [8, 301])
+def test_masked_tokens_of_large_coefficients(V, dtype):
+    """A gradient of the entropy near the type's end: masked tokens get 0, whatever 0 would be multiplied by."""
+    rng = np.random.default_rng(V)
+    x = torch.from_numpy(rng.standard_normal((4, V))).to(dtype).to(DEV)
+    x[:, 2::3] = -math.inf
+    targets = torch.full((4,), -1, dtype=torch.int32, device=DEV)
+    h = torch.tensor([3e36, -3e36, 1e35, 2e37], dtype=F32, device=DEV)
+    r = binding.logprobs(x, targets)
+    got = binding.logprobs_grad(x, targets, r.logz, r.entropy, None, h).double().cpu().numpy()
+    assert (got[:, 2::3] == 0).all()
+    v, hh = x.double().cpu().numpy(), h.double().cpu().numpy()[:, None]
+    logp = v - np.log(np.exp(v).sum(1, keepdims=True))
+    p = np.exp(logp)
+    with np.errstate(invalid="ignore"):
+        plogp = np.where(p > 0, p * logp, 0.0)
+    H = -plogp.sum(1, keepdims=True)
+    want = -hh * (plogp + p * H)
+    # log p and H are off by 60 u of 1 and of themselves (at most 64 additions of each, and logz's rounding)
+    tol = 60 * U * np.abs(hh) * p * (2 + np.abs(np.where(p > 0, logp, 0)) + 2 * H) + 1.01 * torch.finfo(dtype).eps / 2 * np.abs(want)
+    assert (np.abs(got - want) <= tol).all()
