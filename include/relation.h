@@ -398,10 +398,11 @@ relation_status relation_paged_decode(const void* q, const void* k_pages, const 
  * fp32 or bf16 with any 1 <= d_h <= 128; rows as in relation_paged_decode.  bf16 runs on the tensor
  * cores (P rounded to bf16 for the product with the values, sums and states in fp32).  Keys and values
  * behind a token's own row are not its business, whatever they hold: an infinite or NaN value among
- * them leaves the row as it is.  cols * page_size is at most 2^31 - 8192, (N + B) H at most 2^31 - 65536
- * (else RELATION_ERR_UNSUPPORTED, and a workspace size of 0).  A position of cols * page_size or more makes a token padding, a
- * page id outside [0, n_pages) reads page 0 (the row is then undefined); both are reported to
- * dev_status (if given) as RELATION_ERR_INVALID_ARG.  Asynchronous on `stream`; nothing is allocated.
+ * them leaves the row as it is.  cols * page_size is at most 2^31 - 8192, (N + B) H at most
+ * 2^31 - 65536 (else RELATION_ERR_UNSUPPORTED, and a workspace size of 0).  A position of
+ * cols * page_size or more makes a token padding, a page id outside [0, n_pages) reads page 0 (the
+ * row is then undefined); both are reported to dev_status (if given) as RELATION_ERR_INVALID_ARG.
+ * Asynchronous on `stream`; nothing is allocated.
  */
 size_t relation_paged_chunk_workspace_size(int N, int B, int H, int cols, relation_pages cache,
                                            relation_dtype dt);
@@ -593,9 +594,10 @@ typedef struct relation_rotary {
  *   w1, w2 : device float[d_h], the norms' weights of the queries and the keys; null: 1.
  *   positions : device int[B T]; null: t in every sequence.  A negative one is padding: zeros.
  * fp32 or bf16 (arithmetic in fp32, angles as 64-bit parts of a turn at every position), any d_h up to
- * 256, B T up to 2^30, heads of queries and keys together up to 2^24 (else RELATION_ERR_UNSUPPORTED).  Rows whose pointers and strides are multiples
- * of 16 bytes, with d_h (and, for layout 1, d_rot / 2) made of 16-byte groups, move in such groups,
- * any others element by element.  With rope_base 0, relation_cache_append takes the result.
+ * 256, B T up to 2^30, heads of queries and keys together up to 2^24 (else
+ * RELATION_ERR_UNSUPPORTED).  Rows whose pointers and strides are multiples of 16 bytes, with d_h
+ * (and, for layout 1, d_rot / 2) made of 16-byte groups, move in such groups, any others element by
+ * element.  With rope_base 0, relation_cache_append takes the result.
  * Asynchronous on `stream`; one launch; nothing is allocated.
  */
 relation_status relation_norm_rope(const void* p1, const void* p2, const float* w1, const float* w2,
